@@ -419,6 +419,101 @@ salr_status_t salr_concat_adapters(const uint16_t* const* a_list, const uint16_t
                                    uint16_t* b_cat, void* stream);
 
 /*
+ * What a fine-tuning step needs on either side of the layers: the loss of a language-model head with the gradient that
+ * salr_sparse_lowrank_linear_backward starts from, the norm of the gradients it ends with, and the optimiser step that uses them.
+ *
+ * salr_linear_cross_entropy -- softmax cross entropy of the logits l = h * w^T [T, V], which are never stored:
+ *
+ *     lse[t] = log sum_v exp(l[t][v]),   loss[t] = lse[t] - l[t][targets[t]],
+ *     G[t][v] = grad_loss[t] * (exp(l[t][v] - lse[t]) - [v == targets[t]]),   dh = G * w,   dw = G^T * h
+ *
+ *   h          in   [T, K] bf16 hidden states; K % 8 == 0, K <= 2^22 (else SHAPE)
+ *   w          in   [V, K] bf16, the head (rows along K, as the weight of a PyTorch linear); 1 <= V < 2^31 where T > 0 (else SHAPE)
+ *   targets    in   [T] int64.  A negative target masks its token: loss, lse, and the gradient are 0 there, whatever the hidden
+ *                   state holds (NaN and infinities too).  A target >= V gives NaN in the token's loss, lse and gradients.
+ *   grad_loss  in   [T] fp32, the gradient of what is minimised with respect to loss[t] (1 / tokens for the mean); NULL: ones
+ *   loss, lse  out  [T] fp32
+ *   dh         out  [T, K] bf16; NULL = not computed
+ *   dw         out  [V, K] bf16; NULL = not computed (a frozen head)
+ *   workspace  --   salr_linear_cross_entropy_workspace_bytes(T, K, V, want_dh, want_dw) bytes, 256-byte aligned; contents
+ *                   unspecified.  It holds the products of a piece of the vocabulary at a time (about 128 MiB), never T x V.
+ *
+ * Precision: fp32 sums, maxima and logits; the probabilities are rounded to bf16 once, as operands of the matrix cores, and dh
+ * and dw at the end.  The probability of the target stays out of that: 1 - p is summed, not subtracted.  A logit that is NaN or
+ * +infinite makes the token's results NaN.  Results are the same bit for bit from call to call.
+ * Errors: INVALID_ARG (null where data is required, negative size, a pointer that is not 16-byte aligned (targets, grad_loss, loss and lse:
+ * not aligned to their type)), SHAPE, CAPACITY, HIP.  The workspace query returns 0 for sizes the call would refuse.
+ */
+size_t salr_linear_cross_entropy_workspace_bytes(int64_t T, int64_t K, int64_t V, int want_dh, int want_dw);
+salr_status_t salr_linear_cross_entropy(const uint16_t* h, int64_t T, int64_t K, const uint16_t* w, int64_t V, const int64_t* targets,
+                                        const float* grad_loss, float* loss, float* lse, uint16_t* dh, uint16_t* dw, void* workspace,
+                                        size_t workspace_bytes, void* stream);
+
+/*
+ * The list of tensors that salr_adamw_step and salr_grad_norm go through in one launch, whatever their number and sizes.
+ * salr_step_plan writes it to HOST memory (salr_step_plan_bytes(counts, n) bytes) and copies nothing to the device: the caller does,
+ * once, and hands the device copy (16-byte aligned) to the calls below for as long as the tensors stay where they are.
+ */
+typedef enum { SALR_F32 = 0, SALR_BF16 = 1 } salr_type_t;
+
+typedef struct {
+    void* param;        /* [count] fp32 or bf16; may be NULL in a list for salr_grad_norm only                          */
+    uint16_t* copy;     /* [count] bf16, written as the rounded param by every step (fp32 params), or NULL              */
+    const void* grad;   /* [count] fp32 or bf16                                                                        */
+    void* exp_avg;      /* [count] fp32, or 8-bit values (4 exponent, 3 mantissa bits, no infinities: OCP E4M3)        */
+    void* exp_avg_sq;   /* the same; in 8 bits it holds the square root                                                */
+    float* scales;      /* 8 bits: [ceil(count / 128)][2] fp32, what the values of exp_avg and exp_avg_sq are times;
+                           else NULL                                                                                   */
+    int64_t count;      /* elements; 0 is legal (the pointers are not looked at then)                                  */
+} salr_step_tensor_t;
+
+/*
+ * salr_step_plan_bytes: 0 for no elements at all, (size_t)-1 for counts out of range (negative, above 2^42, or 2^31 - 1 records).
+ * salr_step_plan: state_bits 32 or 8, or 0 for a list that only salr_grad_norm is to read.  *chunks gets the number of records, which
+ * the calls want to know.
+ * Errors: INVALID_ARG (null where data is required, negative size, a tensor that is not 16-byte aligned (scales: 8), a type or
+ * state_bits that is none, scales missing for 8 bits, a copy of a bf16 param), SHAPE (count above 2^42, too many records), CAPACITY (plan_bytes).
+ */
+size_t salr_step_plan_bytes(const int64_t* counts, int64_t n);
+salr_status_t salr_step_plan(const salr_step_tensor_t* tensors, int64_t n, salr_type_t param_type, salr_type_t grad_type, int state_bits,
+                             void* plan, size_t plan_bytes, int64_t* chunks);
+
+/*
+ * salr_adamw_step -- for every element of every tensor of the list, with c = *grad_scale (1 where grad_scale is NULL):
+ *
+ *     g = c grad;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2;
+ *     param = param (1 - lr weight_decay) - lr / (1 - beta1^step) m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ *
+ * each operation rounded to fp32 on its own; bf16 params are rounded to nearest at the end.  Where c is not finite nothing changes
+ * (salr_grad_norm gives NaN for gradients whose norm is not finite).  States in 8 bits: a block of 128 elements keeps, in fp32, the
+ * largest |m| and sqrt(v) over 448; m is rounded to the nearest of the 8-bit values, sqrt(v) up or down at random so that its mean is
+ * right (from the element's place in the list and `seed`: a run with the same seeds gives the same results), and to the
+ * smallest of them rather than to zero.  A block whose largest magnitude is below 2^-100 is stored as zeros.
+ *
+ *   plan, chunks          the list, on the device; of the types and state_bits that it was made for
+ *   step                  number of this step, from 1 on
+ *   grad_scale            in  one fp32 on the device, or NULL
+ * Errors: INVALID_ARG (null plan with chunks > 0, a type or state_bits that is none, negative chunks, step < 1, a beta outside [0, 1),
+ * a hyperparameter that is negative or not finite), SHAPE, HIP.
+ */
+salr_status_t salr_adamw_step(const void* plan, int64_t chunks, salr_type_t param_type, salr_type_t grad_type, int state_bits, double lr,
+                              double beta1, double beta2, double eps, double weight_decay, int64_t step, int64_t seed,
+                              const float* grad_scale, void* stream);
+
+/*
+ * salr_grad_norm -- out[0] = sqrt(sum of the squares of all gradients of the list), out[1] = min(1, max_norm / (out[0] + 1e-6)), the
+ * factor that brings the norm to max_norm (INFINITY: no clipping); NaN where the norm is not finite.  Squares are summed in fp64, in
+ * the same order every time.
+ *
+ *   out        out  [2] fp32 on the device; out + 1 serves as grad_scale of salr_adamw_step
+ *   workspace  --   SALR_GRAD_NORM_WORKSPACE_BYTES, 8-byte aligned; contents unspecified
+ * Errors: INVALID_ARG (also max_norm negative or NaN), SHAPE, CAPACITY, HIP.
+ */
+#define SALR_GRAD_NORM_WORKSPACE_BYTES 8192
+salr_status_t salr_grad_norm(const void* plan, int64_t chunks, salr_type_t grad_type, float max_norm, float* out, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/*
  * Measurement hook (not part of the method): when both events are non-NULL, the next calls of
  * salr_sparse_lowrank_linear on this host thread attach the two events to the launch of the fused
  * decode+GEMM kernel: `start_event` takes the time the kernel begins executing and `stop_event` the

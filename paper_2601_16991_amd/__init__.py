@@ -28,6 +28,11 @@ _vp = ctypes.c_void_p
 _i64 = ctypes.c_int64
 
 
+class StepTensor(ctypes.Structure):
+    """salr_step_tensor_t of include/salr.h."""
+    _fields_ = [("param", _vp), ("copy", _vp), ("grad", _vp), ("exp_avg", _vp), ("exp_avg_sq", _vp), ("scales", _vp), ("count", _i64)]
+
+
 class SalrError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = int(status)
@@ -106,6 +111,19 @@ def lib() -> ctypes.CDLL:
         L.salr_sparse_lowrank_linear_backward.restype = ctypes.c_int
         L.salr_sparse_lowrank_linear_backward.argtypes = [_vp, _vp, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _vp,
                                                           _vp, _vp, ctypes.c_size_t, _vp]
+        L.salr_linear_cross_entropy_workspace_bytes.restype = ctypes.c_size_t
+        L.salr_linear_cross_entropy_workspace_bytes.argtypes = [_i64, _i64, _i64, ctypes.c_int, ctypes.c_int]
+        L.salr_linear_cross_entropy.restype = ctypes.c_int
+        L.salr_linear_cross_entropy.argtypes = [_vp, _i64, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
+        L.salr_step_plan_bytes.restype = ctypes.c_size_t
+        L.salr_step_plan_bytes.argtypes = [ctypes.POINTER(_i64), _i64]
+        L.salr_step_plan.restype = ctypes.c_int
+        L.salr_step_plan.argtypes = [ctypes.POINTER(StepTensor), _i64, ctypes.c_int, ctypes.c_int, ctypes.c_int, _vp, ctypes.c_size_t,
+                                     ctypes.POINTER(_i64)]
+        L.salr_adamw_step.restype = ctypes.c_int
+        L.salr_adamw_step.argtypes = [_vp, _i64, ctypes.c_int, ctypes.c_int, ctypes.c_int, *[ctypes.c_double] * 5, _i64, _i64, _vp, _vp]
+        L.salr_grad_norm.restype = ctypes.c_int
+        L.salr_grad_norm.argtypes = [_vp, _i64, ctypes.c_int, ctypes.c_float, _vp, _vp, ctypes.c_size_t, _vp]
         L.salr_set_kernel_timing_events.restype = None
         L.salr_set_kernel_timing_events.argtypes = [_vp, _vp]
         _lib = L
@@ -584,3 +602,162 @@ def linear(x, bitmap, values, row_offsets, a_cat, b_cat, workspace: Optional[tor
     room for partial outputs); where the allocator has no room for it the call runs on what it was given.  With the fastest size nothing but the result is
     allocated; salr_sparse_lowrank_linear, which takes y, never allocates.  linear_prepared and linear_2of4 alike."""
     return _native().linear(0, x, bitmap, values, row_offsets, None, a_cat, b_cat, None, workspace, None)
+
+
+# ---- a fine-tuning step around the layers: the head's loss, the gradients' norm, the optimiser
+
+def salr_linear_cross_entropy_workspace_bytes(T: int, K: int, V: int, want_dh: bool, want_dw: bool) -> int:
+    return int(lib().salr_linear_cross_entropy_workspace_bytes(T, K, V, int(want_dh), int(want_dw)))
+
+
+def salr_linear_cross_entropy(h: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, grad_loss: Optional[torch.Tensor],
+                              loss: torch.Tensor, lse: torch.Tensor, dh: Optional[torch.Tensor], dw: Optional[torch.Tensor],
+                              workspace: Optional[torch.Tensor], stream=None) -> None:
+    """Enqueue softmax cross entropy of the logits h w^T: loss, lse fp32 [T], dh bf16 [T, K], dw bf16 [V, K]; None = not computed."""
+    T, K = h.shape
+    V = w.shape[0]
+    for name, t, shape in (("w", w, (V, K)), ("targets", targets, (T,)), ("grad_loss", grad_loss, (T,)), ("loss", loss, (T,)),
+                           ("lse", lse, (T,)), ("dh", dh, (T, K)), ("dw", dw, (V, K))):
+        if t is not None and tuple(t.shape) != shape:
+            raise ValueError(f"{name} must be {shape}")
+    ws_ptr = None if workspace is None else workspace.data_ptr()
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    st = lib().salr_linear_cross_entropy(
+        _ptr(h, _BF16_TYPES, "h"), T, K, _ptr(w, _BF16_TYPES, "w"), V, _ptr(targets, (torch.int64,), "targets"),
+        _ptr(grad_loss, (torch.float32,), "grad_loss"), _ptr(loss, (torch.float32,), "loss"), _ptr(lse, (torch.float32,), "lse"),
+        _ptr(dh, _BF16_TYPES, "dh"), _ptr(dw, _BF16_TYPES, "dw"), ws_ptr, ws_bytes, _stream(stream))
+    _check(st, "salr_linear_cross_entropy")
+
+
+def linear_cross_entropy(h, w, targets, grad_loss=None, need_dh=True, need_dw=False, workspace=None):
+    """(loss, lse, dh, dw) of softmax cross entropy on the logits h w^T, which are never stored; entries not asked for are None.
+
+    h [T, K] and w [V, K] bf16, targets [T] int64 (negative: the token is masked), grad_loss [T] fp32 (None: ones) the gradient of
+    what is minimised with respect to each token's loss."""
+    return _native().linear_cross_entropy(h, w, targets, grad_loss, need_dh, need_dw, workspace)
+
+
+_TYPE_CODES = {torch.float32: 0, torch.bfloat16: 1}   # salr_type_t
+_STATE_BITS = {torch.float32: 32, torch.float8_e4m3fn: 8}
+STEP_BLOCK = 128                                      # elements that share two scales of 8-bit states
+GRAD_NORM_WORKSPACE_BYTES = 8192                      # SALR_GRAD_NORM_WORKSPACE_BYTES of include/salr.h
+
+
+def _same_type(tensors, name: str, kinds):
+    types = {t.dtype for t in tensors}
+    if len(types) > 1 or not types <= set(kinds):
+        raise TypeError(f"{name}: dtypes {sorted(map(str, types))}, expected one of {sorted(map(str, kinds))}")
+    return types.pop() if types else next(iter(kinds))
+
+
+class _StepList:
+    """The tensors of a step as salr_step_plan lays them out: written once, copied to the device, read by every call."""
+
+    def __init__(self, grads, params=None, copies=None, exp_avg=None, exp_avg_sq=None, scales=None):
+        grads = list(grads)
+        lists = [None if x is None else list(x) for x in (params, copies, exp_avg, exp_avg_sq, scales)]
+        params, copies, exp_avg, exp_avg_sq, scales = lists
+        if not grads:
+            raise ValueError("no tensors")
+        if any(x is not None and len(x) != len(grads) for x in lists):
+            raise ValueError("lists of different lengths")
+        self._keep = (grads, *lists)
+        self.grad_type = _TYPE_CODES[_same_type(grads, "grads", _TYPE_CODES)]
+        self.param_type, self.state_bits = 0, 0
+        if params is not None:
+            self.param_type = _TYPE_CODES[_same_type(params, "params", _TYPE_CODES)]
+            state = _same_type(exp_avg, "exp_avg", _STATE_BITS)
+            _same_type(exp_avg_sq, "exp_avg_sq", {state: 0})
+            self.state_bits = _STATE_BITS[state]
+            if (scales is not None) != (self.state_bits == 8):
+                raise ValueError("scales go with states in 8 bits")
+        table = (StepTensor * len(grads))()
+        device = grads[0].device
+        for i, g in enumerate(grads):
+            n = g.numel()
+            entry = {"grad": (g, tuple(_TYPE_CODES), n)}
+            if params is not None:
+                entry.update(param=(params[i], tuple(_TYPE_CODES), n), exp_avg=(exp_avg[i], tuple(_STATE_BITS), n),
+                             exp_avg_sq=(exp_avg_sq[i], tuple(_STATE_BITS), n))
+                if copies is not None and copies[i] is not None:
+                    entry["copy"] = (copies[i], (torch.bfloat16,), n)
+                if scales is not None:
+                    entry["scales"] = (scales[i], (torch.float32,), 2 * ((n + STEP_BLOCK - 1) // STEP_BLOCK))
+            for name, (t, kinds, size) in entry.items():
+                if t.numel() != size:
+                    raise ValueError(f"{name} {i}: {t.numel()} elements, expected {size}")
+                setattr(table[i], name, _ptr(t, kinds, name))
+                if t.device != device:
+                    raise ValueError("tensors on different devices")
+            table[i].count = n
+        counts = (_i64 * len(grads))(*[t.count for t in table])
+        need = int(lib().salr_step_plan_bytes(counts, len(grads)))
+        host = torch.empty(max(need, 64), dtype=torch.uint8)
+        chunks = _i64()
+        _check(lib().salr_step_plan(table, len(grads), self.param_type, self.grad_type, self.state_bits, host.data_ptr(), host.numel(),
+                                    ctypes.byref(chunks)), "salr_step_plan")
+        self.chunks = chunks.value
+        self.plan = host.to(device)
+
+
+class GradNorm:
+    """The norm of many gradients at once: ``GradNorm(grads)(max_norm)`` is a tensor [norm, min(1, max_norm / (norm + 1e-6))], the second
+    value NaN where the norm is not finite.  The tensors are read where they are at every call, on the stream that is current then;
+    calls that overlap on different streams need a ``GradNorm`` each."""
+
+    def __init__(self, grads, _list=None):
+        self._list = _list or _StepList(grads)
+        self._workspace = torch.empty(GRAD_NORM_WORKSPACE_BYTES, dtype=torch.uint8, device=self._list.plan.device)
+        self._call = _native().grad_norm
+
+    def __call__(self, max_norm: float = float("inf"), out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        l = self._list
+        got = self._call(l.plan, l.chunks, l.grad_type, max_norm, self._workspace, out, _handle(stream))
+        return got if out is None else out
+
+
+def adamw_states(params, bits: int = 32):
+    """(exp_avg, exp_avg_sq, scales) for ``AdamW``, all zero: lists with one tensor a param, scales None for 32 bits."""
+    if bits not in (8, 32):
+        raise ValueError("bits must be 8 or 32")
+    kind = torch.float32 if bits == 32 else torch.float8_e4m3fn
+    m, v = ([torch.zeros(p.numel(), dtype=torch.uint8 if bits == 8 else kind, device=p.device).view(kind) for p in params] for _ in range(2))
+    if bits == 32:
+        return m, v, None
+    return m, v, [torch.zeros((p.numel() + STEP_BLOCK - 1) // STEP_BLOCK, 2, device=p.device) for p in params]
+
+
+class AdamW:
+    """AdamW over many tensors in one launch a step.
+
+    params        fp32 or bf16 tensors, updated in place
+    grads         their gradients (fp32 or bf16), read where they are at every step: a backward pass writes into them
+    exp_avg, exp_avg_sq   states: fp32, or ``torch.float8_e4m3fn`` with ``scales`` [ceil(n / 128), 2] fp32 each; None: zeros in
+                  ``bits`` (``adamw_states``).  In 8 bits exp_avg_sq holds the square root.
+    copies        bf16 tensors (or None) that receive the rounded params of fp32 params: what the layers read
+    """
+
+    def __init__(self, params, grads, exp_avg=None, exp_avg_sq=None, scales=None, copies=None, bits: int = 32):
+        params = list(params)
+        if (exp_avg is None) != (exp_avg_sq is None):
+            raise ValueError("exp_avg and exp_avg_sq go together")
+        if exp_avg is None:
+            exp_avg, exp_avg_sq, scales = adamw_states(params, bits)
+        self.params, self.grads, self.exp_avg, self.exp_avg_sq, self.scales, self.copies = params, grads, exp_avg, exp_avg_sq, scales, copies
+        self._list = _StepList(grads, params, copies, exp_avg, exp_avg_sq, scales)
+        self._norm = None
+        self._call = _native().adamw_step
+
+    def grad_norm(self, max_norm: float = float("inf"), stream=None) -> torch.Tensor:
+        """[norm, factor] of the gradients (see ``GradNorm``); ``grad_norm(c)[1:]`` is a ``grad_scale`` for ``step``."""
+        if self._norm is None:
+            self._norm = GradNorm(None, self._list)
+        return self._norm(max_norm, None, stream)
+
+    def step(self, lr: float, step: int, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.0,
+             grad_scale: Optional[torch.Tensor] = None, seed: int = 0, stream=None) -> None:
+        """Step number ``step`` (from 1 on).  ``grad_scale``: one fp32 on the device that the gradients are multiplied by; where it is
+        not finite nothing changes.  ``seed``: of the random rounding of 8-bit states, another one every step."""
+        l = self._list
+        self._call(l.plan, l.chunks, l.param_type, l.grad_type, l.state_bits, lr, beta1, beta2, eps, weight_decay, step, seed, grad_scale,
+                   _handle(stream))

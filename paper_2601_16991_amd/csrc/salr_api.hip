@@ -4,6 +4,7 @@
 #include "salr_internal.hpp"
 
 #include <atomic>
+#include <limits>
 
 namespace {
 
@@ -41,6 +42,17 @@ constexpr int64_t kMaxSvdDim = 65535LL * 32;      // gridDim.y of the transposin
 // codes (large batches, K % 64 == 0, rows of at most 524288 columns); the workspace is then the plain layer's.
 bool qsalr_decodes_codes(int64_t M, int64_t K, int64_t N, int64_t nnz) {
     return nnz > 0 && K > 0 && salr::linear_takes_twostage(M, K, N) && (K / 32 + 15) / 16 <= 1024;
+}
+
+bool misaligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
+bool is_type(salr_type_t t) { return t == SALR_F32 || t == SALR_BF16; }
+
+// Sizes that salr_linear_cross_entropy takes: whole vectors along K, offsets within a tile of 256 rows and all grids in 31 bits.
+bool cross_entropy_sizes_ok(int64_t T, int64_t K, int64_t V) {
+    constexpr int64_t most = 2147483647LL, tile = 256;
+    if (K % 8 != 0 || K > ((int64_t)1 << 22) || T > most || V > most || (T > 0 && V < 1)) return false;
+    const int64_t m = (T + 15) / 16, n = (V + tile - 1) / tile, k = (K + tile - 1) / tile;
+    return (m == 0 || n <= most / m) && (k == 0 || n <= most / k) && (k == 0 || m <= most / k / 256) && T * (K / 8 + 1) / 256 <= most;
 }
 
 }  // namespace
@@ -452,6 +464,85 @@ salr_status_t salr_sparse_lowrank_linear_backward(const uint16_t* x, const uint1
     if (need > 0 && (!workspace || workspace_bytes < need)) return SALR_ERR_CAPACITY;
     hipError_t e = salr::launch_linear_backward(x, dy, M, K, N, bitmap, values, row_offsets, a_cat, b_cat, R, dx,
                                                 want_dadb ? da : nullptr, want_dadb ? db : nullptr, workspace,
+                                                static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SALR_OK : SALR_ERR_HIP;
+}
+
+size_t salr_linear_cross_entropy_workspace_bytes(int64_t T, int64_t K, int64_t V, int want_dh, int want_dw) {
+    if (T < 0 || K < 0 || V < 0 || !cross_entropy_sizes_ok(T, K, V)) return 0;
+    return salr::ce_plan(T, K, V, want_dh != 0, want_dw != 0).bytes;
+}
+
+salr_status_t salr_linear_cross_entropy(const uint16_t* h, int64_t T, int64_t K, const uint16_t* w, int64_t V, const int64_t* targets,
+                                        const float* grad_loss, float* loss, float* lse, uint16_t* dh, uint16_t* dw, void* workspace,
+                                        size_t workspace_bytes, void* stream) {
+    if (T < 0 || K < 0 || V < 0) return SALR_ERR_INVALID_ARG;
+    if (T > 0 && (!targets || !loss || !lse || (K > 0 && V > 0 && (!h || !w)))) return SALR_ERR_INVALID_ARG;
+    if (misaligned(h, 16) || misaligned(w, 16) || misaligned(dh, 16) || misaligned(dw, 16) || misaligned(workspace, 256) || misaligned(targets, 8) ||
+        misaligned(grad_loss, 4) || misaligned(loss, 4) || misaligned(lse, 4))
+        return SALR_ERR_INVALID_ARG;
+    if (!cross_entropy_sizes_ok(T, K, V)) return SALR_ERR_SHAPE;
+    const salr::CePlan plan = salr::ce_plan(T, K, V, dh != nullptr, dw != nullptr);
+    if (workspace_bytes < plan.bytes) return SALR_ERR_CAPACITY;
+    if (plan.bytes > 0 && !workspace) return SALR_ERR_INVALID_ARG;
+    if (T == 0 && (!dw || V == 0)) return SALR_OK;
+    const salr::CeArgs args{h, T, K, w, V, targets, grad_loss, loss, lse, dh, dw, static_cast<hipStream_t>(stream)};
+    const hipError_t e = salr::launch_cross_entropy(args, workspace);
+    return e == hipSuccess ? SALR_OK : SALR_ERR_HIP;
+}
+
+size_t salr_step_plan_bytes(const int64_t* counts, int64_t n) {
+    if (n < 0 || (n > 0 && !counts)) return (size_t)-1;
+    const int64_t chunks = salr::step_chunks(counts, n);
+    return chunks < 0 ? (size_t)-1 : (size_t)chunks * sizeof(salr::StepChunk);
+}
+
+salr_status_t salr_step_plan(const salr_step_tensor_t* tensors, int64_t n, salr_type_t param_type, salr_type_t grad_type, int state_bits, void* plan,
+                             size_t plan_bytes, int64_t* chunks) {
+    if (n < 0 || (n > 0 && !tensors) || !chunks || !is_type(param_type) || !is_type(grad_type) || (state_bits != 0 && state_bits != 8 && state_bits != 32)) return SALR_ERR_INVALID_ARG;
+    int64_t need = 0;
+    for (int64_t i = 0; i < n; ++i) {
+        const salr_step_tensor_t& t = tensors[i];
+        if (t.count < 0) return SALR_ERR_INVALID_ARG;
+        if (t.count == 0) continue;
+        const int64_t here = salr::step_chunks(&t.count, 1);
+        if (here < 0 || (need += here) > salr::kStepMaxChunks) return SALR_ERR_SHAPE;
+        if (!t.grad || misaligned(t.grad, 16)) return SALR_ERR_INVALID_ARG;
+        if (state_bits == 0) continue;
+        if (!t.param || !t.exp_avg || !t.exp_avg_sq || (state_bits == 8 && !t.scales)) return SALR_ERR_INVALID_ARG;
+        if (param_type == SALR_BF16 && t.copy) return SALR_ERR_INVALID_ARG;
+        if (misaligned(t.param, 16) || misaligned(t.copy, 16) || misaligned(t.exp_avg, 16) || misaligned(t.exp_avg_sq, 16) || misaligned(t.scales, 8))
+            return SALR_ERR_INVALID_ARG;
+    }
+    if (plan_bytes < (size_t)need * sizeof(salr::StepChunk)) return SALR_ERR_CAPACITY;
+    if (need > 0 && !plan) return SALR_ERR_INVALID_ARG;
+    salr::write_step_plan(tensors, n, param_type == SALR_F32, grad_type == SALR_F32, state_bits, static_cast<salr::StepChunk*>(plan));
+    *chunks = need;
+    return SALR_OK;
+}
+
+salr_status_t salr_adamw_step(const void* plan, int64_t chunks, salr_type_t param_type, salr_type_t grad_type, int state_bits, double lr,
+                              double beta1, double beta2, double eps, double weight_decay, int64_t step, int64_t seed,
+                              const float* grad_scale, void* stream) {
+    if (chunks < 0 || (chunks > 0 && !plan) || !is_type(param_type) || !is_type(grad_type) || (state_bits != 8 && state_bits != 32)) return SALR_ERR_INVALID_ARG;
+    const double most = std::numeric_limits<float>::max();
+    const auto fine = [&](double x) { return x >= 0.0 && x <= most; };   // (false for NaN)
+    if (!fine(lr) || !fine(eps) || !fine(weight_decay) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || step < 1) return SALR_ERR_INVALID_ARG;
+    if (misaligned(plan, 16) || misaligned(grad_scale, 4)) return SALR_ERR_INVALID_ARG;
+    if (chunks > salr::kStepMaxChunks) return SALR_ERR_SHAPE;
+    const salr::AdamwArgs args{lr, beta1, beta2, eps, weight_decay, step, seed, grad_scale};
+    const hipError_t e = salr::launch_adamw(static_cast<const salr::StepChunk*>(plan), chunks, param_type == SALR_F32, grad_type == SALR_F32, state_bits == 8,
+                                            args, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SALR_OK : SALR_ERR_HIP;
+}
+
+salr_status_t salr_grad_norm(const void* plan, int64_t chunks, salr_type_t grad_type, float max_norm, float* out, void* workspace,
+                             size_t workspace_bytes, void* stream) {
+    if (chunks < 0 || (chunks > 0 && !plan) || !is_type(grad_type) || !(max_norm >= 0.f) || !out || !workspace) return SALR_ERR_INVALID_ARG;
+    if (misaligned(plan, 16) || misaligned(out, 4) || misaligned(workspace, 8)) return SALR_ERR_INVALID_ARG;
+    if (chunks > salr::kStepMaxChunks) return SALR_ERR_SHAPE;
+    if (workspace_bytes < SALR_GRAD_NORM_WORKSPACE_BYTES) return SALR_ERR_CAPACITY;
+    const hipError_t e = salr::launch_grad_norm(static_cast<const salr::StepChunk*>(plan), chunks, grad_type == SALR_F32, max_norm, out, workspace,
                                                 static_cast<hipStream_t>(stream));
     return e == hipSuccess ? SALR_OK : SALR_ERR_HIP;
 }

@@ -18,7 +18,7 @@ namespace {
 
 PyObject* g_salr_error = nullptr;   // class SalrError(status, where), handed over by the package
 
-enum Kind { kBf16, kU32, kU8 };
+enum Kind { kBf16, kU32, kU8, kF32, kI64 };
 
 // Thrown once a Python error is set.
 struct PyFailure {};
@@ -32,6 +32,8 @@ bool dtype_ok(at::ScalarType t, Kind kind) {
     switch (kind) {
         case kBf16: return t == at::kBFloat16 || t == at::kShort || t == at::kUInt16;
         case kU32: return t == at::kInt || t == at::kUInt32;
+        case kF32: return t == at::kFloat;
+        case kI64: return t == at::kLong;
         default: return t == at::kByte;
     }
 }
@@ -386,6 +388,104 @@ PyObject* py_decode(PyObject*, PyObject* const* v, Py_ssize_t n) {
     SALR_CATCH
 }
 
+// linear_cross_entropy(h, w, targets, grad_loss, need_dh, need_dw, workspace) -> (loss, lse, dh, dw)
+PyObject* py_linear_cross_entropy(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    SALR_TRY
+    need_args(n, 7, "linear_cross_entropy");
+    const at::Tensor &h = tensor_of(v[0], "h"), &w = tensor_of(v[1], "w"), &targets = tensor_of(v[2], "targets"), &grad = tensor_of(v[3], "grad_loss");
+    need_matrix(h, "h");
+    need_matrix(w, "w");
+    const int64_t T = h.size(0), K = h.size(1), V = w.size(0);
+    if (w.size(1) != K) fail(PyExc_ValueError, "%s must be [V, K]", "w");
+    if (!targets.defined() || targets.dim() != 1 || targets.size(0) != T) fail(PyExc_ValueError, "%s must be [T]", "targets");
+    if (grad.defined() && (grad.dim() != 1 || grad.size(0) != T)) fail(PyExc_ValueError, "%s must be [T]", "grad_loss");
+    const uint16_t *hp = device_ptr<uint16_t>(h, kBf16, "h"), *wp = device_ptr<uint16_t>(w, kBf16, "w");
+    const int64_t* tp = device_ptr<int64_t>(targets, kI64, "targets");
+    const float* gp = device_ptr<float>(grad, kF32, "grad_loss");
+    if (!h.is_cuda()) fail(PyExc_TypeError, "%s must be a CUDA tensor", "h");
+    const bool need_dh = PyObject_IsTrue(v[4]) == 1, need_dw = PyObject_IsTrue(v[5]) == 1;
+    at::Tensor loss = empty_on({T}, at::kFloat, h), lse = empty_on({T}, at::kFloat, h), dh, dw;
+    if (need_dh) dh = empty_on({T, K}, h.scalar_type(), h);
+    if (need_dw) dw = empty_on({V, K}, w.scalar_type(), h);
+    Workspace ws;
+    ws.given(v[6]);
+    if (v[6] == Py_None) ws.allocate(salr_linear_cross_entropy_workspace_bytes(T, K, V, need_dh, need_dw), h);
+    float *lp = device_ptr<float>(loss, kF32, "loss"), *sp = device_ptr<float>(lse, kF32, "lse");
+    // (an output without elements has no memory, and is asked for all the same: the workspace was sized with it)
+    uint16_t* dhp = need_dh ? static_cast<uint16_t*>(dh.data_ptr()) : nullptr;
+    uint16_t* dwp = need_dw ? static_cast<uint16_t*>(dw.data_ptr()) : nullptr;
+    void* stream = stream_of(Py_None);
+    salr_status_t st;
+    {
+        Gil release;
+        st = salr_linear_cross_entropy(hp, T, K, wp, V, tp, gp, lp, sp, dhp, dwp, ws.ptr, ws.bytes, stream);
+    }
+    check(st, "salr_linear_cross_entropy");
+    PyObject* out = PyTuple_New(4);
+    at::Tensor* results[4] = {&loss, &lse, &dh, &dw};
+    for (int i = 0; i < 4; ++i) {
+        if (!results[i]->defined()) Py_INCREF(Py_None);
+        PyTuple_SET_ITEM(out, i, results[i]->defined() ? THPVariable_Wrap(*results[i]) : Py_None);
+    }
+    return out;
+    SALR_CATCH
+}
+
+double double_of(PyObject* o) {
+    const double x = PyFloat_AsDouble(o);
+    if (x == -1.0 && PyErr_Occurred()) throw PyFailure{};
+    return x;
+}
+
+// adamw_step(plan, chunks, param_type, grad_type, state_bits, lr, beta1, beta2, eps, weight_decay, step, seed, grad_scale, stream)
+PyObject* py_adamw_step(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    SALR_TRY
+    need_args(n, 14, "adamw_step");
+    const uint8_t* plan = device_ptr<uint8_t>(tensor_of(v[0], "plan"), kU8, "plan");
+    const int64_t chunks = int_of(v[1]);
+    const salr_type_t pt = static_cast<salr_type_t>(int_of(v[2])), gt = static_cast<salr_type_t>(int_of(v[3]));
+    const at::Tensor& scale = tensor_of(v[12], "grad_scale");
+    if (scale.defined() && scale.numel() != 1) fail(PyExc_ValueError, "%s must be one value", "grad_scale");
+    const float* sp = device_ptr<float>(scale, kF32, "grad_scale");
+    const int bits = (int)int_of(v[4]);
+    const double lr = double_of(v[5]), b1 = double_of(v[6]), b2 = double_of(v[7]), eps = double_of(v[8]), decay = double_of(v[9]);
+    const int64_t step = int_of(v[10]), seed = int_of(v[11]);
+    void* stream = stream_of(v[13]);
+    salr_status_t st;
+    {
+        Gil release;
+        st = salr_adamw_step(plan, chunks, pt, gt, bits, lr, b1, b2, eps, decay, step, seed, sp, stream);
+    }
+    check(st, "salr_adamw_step");
+    Py_RETURN_NONE;
+    SALR_CATCH
+}
+
+// grad_norm(plan, chunks, grad_type, max_norm, workspace, out, stream) -> out, allocated like the workspace where it is None
+PyObject* py_grad_norm(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    SALR_TRY
+    need_args(n, 7, "grad_norm");
+    const uint8_t* plan = device_ptr<uint8_t>(tensor_of(v[0], "plan"), kU8, "plan");
+    const int64_t chunks = int_of(v[1]);
+    const salr_type_t gt = static_cast<salr_type_t>(int_of(v[2]));
+    const float max_norm = (float)double_of(v[3]);
+    const at::Tensor& ws = tensor_of(v[4], "workspace");
+    uint8_t* wp = device_ptr<uint8_t>(ws, kU8, "workspace");
+    if (!ws.defined()) fail(PyExc_TypeError, "%s must be a tensor", "workspace");
+    at::Tensor out = v[5] == Py_None ? empty_on({2}, at::kFloat, ws) : tensor_of(v[5], "out");
+    if (out.numel() != 2) fail(PyExc_ValueError, "%s must hold two values", "out");
+    float* op = device_ptr<float>(out, kF32, "out");
+    void* stream = stream_of(v[6]);
+    salr_status_t st;
+    {
+        Gil release;
+        st = salr_grad_norm(plan, chunks, gt, max_norm, op, wp, (size_t)ws.numel(), stream);
+    }
+    check(st, "salr_grad_norm");
+    return result(v[5], std::move(out));
+    SALR_CATCH
+}
+
 PyObject* py_set_error(PyObject*, PyObject* cls) {
     Py_XINCREF(cls);
     Py_XSETREF(g_salr_error, cls);
@@ -399,6 +499,9 @@ PyMethodDef kMethods[] = {
     SALR_FAST("linear_backward", py_linear_backward),
     SALR_FAST("mask", py_mask),
     SALR_FAST("decode", py_decode),
+    SALR_FAST("linear_cross_entropy", py_linear_cross_entropy),
+    SALR_FAST("adamw_step", py_adamw_step),
+    SALR_FAST("grad_norm", py_grad_norm),
     {"encode", py_encode, METH_O, nullptr},
     {"set_error", py_set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},

@@ -8,6 +8,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "../../include/salr.h"
+
 namespace salr {
 
 hipError_t launch_encode(const uint16_t* w, int64_t rows, int64_t cols, uint32_t* bitmap, uint16_t* values,
@@ -800,5 +802,60 @@ void launch_dense_stage(const uint16_t* x, int64_t M, int64_t K, int64_t N, cons
 // out[i] = bf16(sum over z < ksplit of partial[z * splitk_slice(count) + i]); with valid < cols the columns from `valid` on of out's
 // rows of `cols` are zeros instead
 void launch_splitk_reduce(const float* partial, int64_t count, int ksplit, uint16_t* out, hipStream_t stream, int cols = 0, int valid = 0);
+
+// ---- The optimiser's side of a fine-tuning step (salr_step.hip)
+// One record of a plan: up to kStepChunk elements of one tensor, from a multiple of that on.  `position`: where they are among all
+// elements of the plan, tensors counted in whole blocks (low 32 bits; see random20).
+struct StepChunk {
+    void* param;
+    uint16_t* copy;
+    const void* grad;
+    void* exp_avg;
+    void* exp_avg_sq;
+    float* scales;
+    int32_t count;
+    uint32_t position;
+    uint64_t pad;
+};
+static_assert(sizeof(StepChunk) == 64, "a plan's size is told in these");
+constexpr int64_t kStepBlock = 128;     // elements that share two scales
+constexpr int64_t kStepChunk = 8192;    // a workgroup's share of a tensor
+constexpr int64_t kStepMaxCount = (int64_t)1 << 42;
+constexpr int64_t kStepMaxChunks = 2147483647LL;   // gridDim.x
+constexpr int kGradNormBlocks = 1024;   // workgroups of the norm, one partial sum each
+struct AdamwArgs {
+    double lr, beta1, beta2, eps, weight_decay;
+    int64_t step, seed;
+    const float* grad_scale;
+};
+// Records that tensors of these sizes take; -1 where a size is out of range.
+int64_t step_chunks(const int64_t* counts, int64_t n);
+void write_step_plan(const salr_step_tensor_t* tensors, int64_t n, bool param32, bool grad32, int state_bits, StepChunk* out);
+hipError_t launch_adamw(const StepChunk* plan, int64_t chunks, bool param32, bool grad32, bool eight, const AdamwArgs& a, hipStream_t stream);
+hipError_t launch_grad_norm(const StepChunk* plan, int64_t chunks, bool grad32, float max_norm, float* out, void* workspace, hipStream_t stream);
+
+// ---- Softmax cross entropy of a head without its logits (salr_cross_entropy.hip)
+constexpr int64_t kCePieceBytes = (int64_t)128 << 20;   // E of a piece of the vocabulary, see ce_plan
+struct CeArgs {
+    const uint16_t* h;
+    int64_t T, K;
+    const uint16_t* w;
+    int64_t V;
+    const int64_t* targets;
+    const float* grad_loss;
+    float* loss;
+    float* lse;
+    uint16_t* dh;
+    uint16_t* dw;
+    hipStream_t stream;
+};
+struct CePlan {
+    int64_t rows, m_tiles;   // tokens of a tile, tiles of tokens
+    int64_t tiles, piece_tiles, slices;   // of 256 columns: all, of a piece; slices of a piece that dh is summed over
+    size_t stats, running, rescale, target_logit, of_rows, e, lower, sums, h_live;   // offsets in the workspace
+    size_t bytes;
+};
+CePlan ce_plan(int64_t T, int64_t K, int64_t V, bool want_dh, bool want_dw);
+hipError_t launch_cross_entropy(const CeArgs& a, void* workspace);
 
 }  // namespace salr

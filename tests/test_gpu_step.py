@@ -1,0 +1,325 @@
+"""GPU tests of salr_adamw_step and salr_grad_norm against a plain 64-bit implementation.
+
+Tolerances (u = 2^-24): m and v take three roundings of terms of one sign each or less than their sum of magnitudes; the step takes about
+ten on top; a bf16 result one of 2^-9 more.  8-bit states: m is within half a spacing of its value (and a rounding's worth of it), sqrt(v)
+is one of the two values around it and the one that the position's random bits say, unless the rounding of x moves it past them.
+"""
+import pytest
+import torch
+
+import finetune_ref as ref
+from gpu_util import dev
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+HYPER = dict(lr=1e-3, beta1=0.9, beta2=0.99, eps=1e-8, weight_decay=0.1, step=7)
+SIZES = [1, 7, 8, 127, 128, 129, 1000, 8191, 8192, 8193, 20001, 0, 3 * 8192 + 5]
+
+
+def _tensors(sizes, bits, param, grad, seed):
+    gen = torch.Generator().manual_seed(seed)
+    made = []
+    for n in sizes:
+        size = torch.exp2(-16 * torch.rand(n, generator=gen) ** 4)
+        t = {"param": (torch.randn(n, generator=gen) * 0.05).to(param), "grad": (torch.randn(n, generator=gen) * 1e-2 * size).to(grad)}
+        if bits == 32:
+            t["exp_avg"] = torch.randn(n, generator=gen) * 1e-2 * size
+            t["exp_avg_sq"] = (torch.rand(n, generator=gen) * 1e-2 * size) ** 2
+        else:
+            t["exp_avg"] = (torch.randn(n, generator=gen) * 100 * size).clamp(-448, 448).to(torch.float8_e4m3fn)
+            t["exp_avg_sq"] = (torch.rand(n, generator=gen) * 440 * size).to(torch.float8_e4m3fn)
+            t["scales"] = torch.rand((n + 127) // 128, 2, generator=gen) * 1e-4
+        made.append(t)
+    return made
+
+
+def _state(t):
+    """m, v in float64 as they were before the step."""
+    n = t["param"].numel()
+    if "scales" not in t:
+        return t["exp_avg"].double(), t["exp_avg_sq"].double()
+    s = t["scales"].double()
+    m = t["exp_avg"].float().double() * ref.per_element(s[:, 0], n)
+    r = t["exp_avg_sq"].float().double() * ref.per_element(s[:, 1], n)
+    return m, r * r
+
+
+def _guarded(x):
+    """On the device, with 256 bytes of a pattern on either side; the view and the whole."""
+    raw = torch.full((512 + (x.numel() * x.element_size() + 15) // 16 * 16,), 0xA5, dtype=torch.uint8, device=dev())
+    view = raw[256:256 + x.numel() * x.element_size()]
+    view.copy_(x.reshape(-1).view(torch.uint8).to(dev()) if x.numel() else view)
+    return view.view(x.dtype).view(x.shape), raw
+
+
+def _untouched(raw, x):
+    used = x.numel() * x.element_size()
+    outside = torch.cat([raw[:256], raw[256 + used:]])
+    return bool((outside == 0xA5).all())
+
+
+def _optimizer(made, copies):
+    import paper_2601_16991_amd as salr
+    on, raws = [], []
+    for t in made:
+        d = {}
+        for k, x in t.items():
+            d[k], raw = _guarded(x)
+            raws.append((raw, x))
+        if copies:
+            x = torch.zeros(t["param"].numel(), dtype=torch.bfloat16)
+            d["copy"], raw = _guarded(x)
+            raws.append((raw, x))
+        on.append(d)
+    opt = salr.AdamW([d["param"] for d in on], [d["grad"] for d in on], [d["exp_avg"] for d in on], [d["exp_avg_sq"] for d in on],
+                     scales=[d["scales"] for d in on] if "scales" in on[0] else None, copies=[d["copy"] for d in on] if copies else None)
+    return opt, on, raws
+
+
+@pytest.mark.parametrize("clip", [None, 0.37])
+@pytest.mark.parametrize("param,grad", [(torch.float32, torch.bfloat16), (torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16),
+                                        (torch.bfloat16, torch.float32)])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_step_against_64_bits(bits, param, grad, clip):
+    made = _tensors(SIZES, bits, param, grad, 100 + bits)
+    opt, on, raws = _optimizer(made, param == torch.float32)
+    scale = None if clip is None else torch.tensor([clip], device=dev())
+    opt.step(grad_scale=scale, seed=5, **HYPER)
+    torch.cuda.synchronize()
+    c = 1.0 if clip is None else float(torch.tensor(clip, dtype=torch.float32))
+    position = 0
+    for t, d in zip(made, on):
+        n = t["param"].numel()
+        m0, v0 = _state(t)
+        p, m, v = ref.adamw(t["param"], t["grad"], m0, v0, c=c, **HYPER)
+        update = (p - t["param"].double() * (1 - HYPER["lr"] * HYPER["weight_decay"])).abs()
+        size_m = HYPER["beta1"] * m0.abs() + (1 - HYPER["beta1"]) * (t["grad"].double() * c).abs()
+        # the update's error: that of m, relative to m's terms, and twelve roundings
+        swing = update * (16 * U) + (size_m * 8 * U) / (m.abs() + 1e-300) * update
+        tol = swing + 4 * U * (t["param"].double().abs() + update)
+        if param == torch.bfloat16:
+            tol = tol + 2.0 ** -8 * p.abs()
+        assert ((d["param"].cpu().double() - p).abs() <= tol + 1e-30).all()
+        if "copy" in d:
+            assert torch.equal(d["copy"].cpu(), d["param"].cpu().bfloat16())
+        if bits == 32:
+            assert ((d["exp_avg"].cpu().double() - m).abs() <= 8 * U * size_m + 1e-37).all()
+            assert ((d["exp_avg_sq"].cpu().double() - v).abs() <= 12 * U * v + 1e-37).all()
+        elif n:
+            s = d["scales"].cpu().double()
+            r = v.sqrt()
+            for k, x in ((0, m), (1, r)):
+                most = ref.blocks_max(x)
+                assert ((s[:, k] - most / 448).abs() <= 16 * U * most / 448 + (8 * U * ref.blocks_max(size_m) / 448 if k == 0 else 0)).all()
+            x = m / ref.per_element(s[:, 0], n)
+            off = 16 * U * (size_m / ref.per_element(s[:, 0], n) + x.abs())
+            code = d["exp_avg"].cpu().float().double()
+            assert ((code - x).abs() <= 0.5 * ref.fp8_spacing(x) * (1 + 2 * U) + off).all()
+            x = r / ref.per_element(s[:, 1], n)
+            code = d["exp_avg_sq"].cpu().float().double()
+            spacing, bits20 = ref.fp8_spacing(x), ref.random20(torch.arange(n) + position, 5).double()
+            away = x / spacing + bits20 / 2 ** 20
+            want = (torch.floor(away) * spacing).clamp(2.0 ** -9, 448)
+            sure = (away - away.round()).abs() > 64 * U * (x / spacing) + 2.0 ** -20
+            at_top = (x - 448).abs() < 1e-3   # (a rounding below 448 is another code there)
+            inside = (x.log2() - x.log2().round()).abs() > 1e-5   # (and across a power of two another spacing)
+            assert (code == want)[sure & ~at_top & inside].all()
+            assert sure.double().mean() > 0.99 or n < 200
+            assert ((code - x).abs() <= spacing * (1 + 1e-5) + 2.0 ** -9).all()
+        position += (n + 127) // 128 * 128
+    assert all(_untouched(raw, x) for raw, x in raws)
+    for t, d in zip(made, on):
+        assert torch.equal(d["grad"].cpu().view(torch.uint8), t["grad"].view(torch.uint8)) if t["grad"].numel() else True
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_many_steps_minimise(bits):
+    """A quadratic: both forms of the states bring it down, to within the steps' size."""
+    import paper_2601_16991_amd as salr
+    gen = torch.Generator().manual_seed(3)
+    target = [torch.randn(n, generator=gen).to(dev()) for n in (1000, 333)]
+    p = [torch.zeros_like(t) for t in target]
+    g = [torch.empty_like(t) for t in target]
+    opt = salr.AdamW(p, g, bits=bits)
+    for k in range(1, 401):
+        for a, b, c in zip(g, p, target):
+            torch.sub(b, c, out=a)
+        opt.step(lr=0.02, step=k, seed=k)
+    assert max(float((a - b).abs().max()) for a, b in zip(p, target)) < 0.1
+
+
+def test_eight_bit_averages_follow_slow_changes():
+    """sqrt(v) falls by 0.05 % a step where the gradients end: rounded to nearest it would stay for ever.  One large element keeps the
+    block's scale, the others have to decay.  After k steps their mean is 0.999^(k/2) of what it was.  A value of about 100 moves by whole
+    spacings of 8, k * 0.05 / 8 times or 2.5, with a standard deviation of sqrt(2.5) spacings; the mean of 127 x 64 of them has one of
+    0.14 %.  1 % is allowed."""
+    import paper_2601_16991_amd as salr
+    blocks = 64
+    n = 128 * blocks
+    p, g = torch.zeros(n, device=dev()), torch.zeros(n, device=dev())
+    m, v, s = salr.adamw_states([p], 8)
+    start = torch.full((n,), 100.0)
+    start[::128] = 448.0
+    v[0].copy_(start.to(torch.float8_e4m3fn))
+    s[0][:, 1] = 1e-3
+    opt = salr.AdamW([p], [g], m, v, scales=s)
+    k = 400
+    for i in range(1, k + 1):
+        g[::128] = 0.448   # keeps the large one where it is
+        opt.step(lr=0.0, step=i, beta2=0.999, seed=i)
+    got = (v[0].float().view(-1, 128) * s[0][:, 1:])[:, 1:]
+    want = float(start.to(torch.float8_e4m3fn).float()[1]) * 1e-3 * 0.999 ** (k / 2)
+    assert abs(float(got.mean()) / want - 1) < 0.01
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_zero_and_tiny_blocks(bits):
+    """No gradient and no state: nothing but the decay.  Magnitudes below 2^-100 are stored as zeros in 8 bits."""
+    import paper_2601_16991_amd as salr
+    p = [torch.ones(300, device=dev()), torch.ones(300, device=dev())]
+    g = [torch.zeros(300, device=dev()), torch.full((300,), 1e-37, device=dev())]
+    opt = salr.AdamW(p, g, bits=bits)
+    opt.step(lr=0.1, step=1, weight_decay=0.5)
+    assert torch.allclose(p[0], torch.full_like(p[0], 0.95)) and torch.isfinite(p[1]).all()
+    if bits == 8:
+        assert all((x.float() == 0).all() for x in opt.exp_avg + opt.exp_avg_sq) and all((x == 0).all() for x in opt.scales)
+    before = [x.clone() for x in p]
+    opt.step(lr=0.1, step=2, weight_decay=0.0)
+    assert torch.equal(p[0], before[0])
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_gradient_that_is_not_finite_changes_nothing_when_clipped(bits):
+    made = _tensors([500, 9000], bits, torch.float32, torch.bfloat16, 9)
+    made[1]["grad"][77] = float("inf")
+    opt, on, _ = _optimizer(made, True)
+    before = [{k: x.clone() for k, x in d.items()} for d in on]
+    norm = opt.grad_norm(1.0)
+    opt.step(grad_scale=norm[1:], **HYPER)
+    torch.cuda.synchronize()
+    assert torch.isinf(norm[0]) and torch.isnan(norm[1])
+    for a, b in zip(on, before):
+        for k in a:
+            assert torch.equal(a[k].view(torch.uint8), b[k].view(torch.uint8)), k
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_not_finite_values_stay_in_their_block(bits):
+    made = _tensors([1000], bits, torch.float32, torch.float32, 10)
+    opt, on, _ = _optimizer(made, False)
+    opt.step(seed=1, **HYPER)
+    good = on[0]["param"].cpu()
+    made[0]["grad"][300] = float("nan")
+    opt, on, _ = _optimizer(made, False)
+    opt.step(seed=1, **HYPER)
+    got = on[0]["param"].cpu()
+    assert torch.isnan(got[300]) and torch.equal(got[torch.arange(1000) != 300], good[torch.arange(1000) != 300])
+    assert torch.isnan(on[0]["exp_avg"].cpu().float()[300])
+
+
+def test_same_seed_same_bits_and_another_seed_others():
+    def go(seed):
+        opt, on, _ = _optimizer(_tensors([5000], 8, torch.float32, torch.float32, 11), False)
+        opt.step(seed=seed, **HYPER)
+        return on[0]["exp_avg_sq"].cpu().view(torch.uint8)
+    assert torch.equal(go(1), go(1)) and not torch.equal(go(1), go(2))
+
+
+@pytest.mark.parametrize("grad", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("sizes", [[1], [7, 0, 129], SIZES, [8192 * 40 + 3] * 30])
+def test_norm(sizes, grad):
+    import paper_2601_16991_amd as salr
+    gen = torch.Generator().manual_seed(len(sizes))
+    g = [torch.randn(n, generator=gen).to(grad) for n in sizes]
+    want = float(torch.sqrt(sum(x.double().square().sum() for x in g)))
+    norm = salr.GradNorm([x.to(dev()) for x in g])
+    for most in (float("inf"), 0.5 * want, 2 * want, 0.0):
+        got = norm(most).cpu().double()
+        assert abs(got[0] - want) <= 2 * U * want
+        assert abs(got[1] - min(1.0, most / (want + 1e-6))) <= 8 * U
+    assert torch.equal(norm(1.0), norm(1.0))
+
+
+def test_norm_of_large_small_and_no_gradients():
+    import paper_2601_16991_amd as salr
+    big = salr.GradNorm([torch.full((100,), 1e30, device=dev())])(1.0).cpu()
+    assert ref.close(float(big[0]), 1e31) and ref.close(float(big[1]), 1e-31)
+    small = salr.GradNorm([torch.full((100,), 1e-30, device=dev())])(1.0).cpu()
+    assert ref.close(float(small[0]), 1e-29) and float(small[1]) == 1.0
+    none = salr.GradNorm([torch.zeros(100, device=dev()), torch.empty(0, device=dev())])(1.0).cpu()
+    assert none.tolist() == [0.0, 1.0]
+    empty = salr.GradNorm([torch.empty(0, device=dev())])(1.0).cpu()
+    assert empty.tolist() == [0.0, 1.0]
+
+
+def test_on_another_stream_and_in_a_graph():
+    made = _tensors([3000, 20000], 8, torch.float32, torch.bfloat16, 12)
+    opt, on, _ = _optimizer(made, True)
+    opt.step(grad_scale=opt.grad_norm(0.1)[1:], seed=2, **HYPER)
+    torch.cuda.synchronize()
+    want = [{k: x.cpu() for k, x in d.items()} for d in on]
+
+    def reset():
+        for t, d in zip(made, on):
+            for k, x in t.items():
+                d[k].view(torch.uint8).copy_(x.view(torch.uint8))
+
+    def same():
+        torch.cuda.synchronize()
+        return all(torch.equal(d[k].cpu().view(torch.uint8), w[k].view(torch.uint8)) for d, w in zip(on, want) for k in d)
+
+    reset()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        opt.step(grad_scale=opt.grad_norm(0.1)[1:], seed=2, **HYPER)
+    assert same()
+    out = torch.empty(2, device=dev())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt._norm(0.1, out)
+        opt.step(grad_scale=out[1:], seed=2, **HYPER)
+    for _ in range(3):
+        reset()
+        out.zero_()
+        graph.replay()
+        assert same()
+
+
+def test_refusals():
+    import paper_2601_16991_amd as salr
+    p, g = torch.zeros(64, device=dev()), torch.zeros(64, device=dev())
+    with pytest.raises(ValueError):
+        salr.AdamW([p], [g[:32]])
+    with pytest.raises(ValueError):
+        salr.AdamW([p, p], [g])
+    with pytest.raises(ValueError):
+        salr.AdamW([], [])
+    with pytest.raises(ValueError):
+        salr.AdamW([p], [g], bits=16)
+    with pytest.raises(TypeError):
+        salr.AdamW([p.half()], [g])
+    with pytest.raises(TypeError):
+        salr.AdamW([p, p.bfloat16()], [g, g])
+    with pytest.raises(TypeError):
+        salr.AdamW([p.cpu()], [g.cpu()])
+    with pytest.raises(TypeError):
+        salr.GradNorm([torch.zeros(8, 8, device=dev())[:, ::2]])
+    with pytest.raises(ValueError):
+        salr.AdamW([p], [g], torch.zeros(1, 64, device=dev()), torch.zeros(1, 64, device=dev()), scales=[torch.zeros(1, 2, device=dev())])
+    with pytest.raises(salr.SalrError):
+        salr.GradNorm([torch.zeros(9, device=dev())[1:]])   # not on 16 bytes
+    with pytest.raises(salr.SalrError):
+        salr.AdamW([p.bfloat16()], [g], copies=[torch.zeros(64, dtype=torch.bfloat16, device=dev())])
+    opt = salr.AdamW([p], [g])
+    for bad in (dict(lr=-1.0, step=1), dict(lr=1e-3, step=0), dict(lr=1e-3, step=1, beta1=1.0), dict(lr=float("nan"), step=1),
+                dict(lr=1e-3, step=1, eps=-1.0)):
+        with pytest.raises(salr.SalrError):
+            opt.step(**bad)
+    with pytest.raises(ValueError):
+        opt.step(lr=1e-3, step=1, grad_scale=torch.ones(2, device=dev()))
+    with pytest.raises(TypeError):
+        opt.step(lr=1e-3, step=1, grad_scale=torch.ones(1, device=dev(), dtype=torch.float64))
+    with pytest.raises(salr.SalrError):
+        opt.grad_norm(-1.0)
