@@ -4,11 +4,11 @@
 //
 // Without dw one pass over the vocabulary makes loss and dh (two products, what the result needs).  It goes in pieces of the
 // vocabulary; in each
-//   logits  a tile of 256 tokens x 256 columns at a time: E = 2^(l log2 e - M_tile) in bf16, M_tile the whole number at or above
-//           the tile's largest exponent of the row, and the row's sum of E in fp32;
-//   rows    M_row = the running maximum of the M_tile, the running sum;
-//   dh      accumulators += E w.  What E lacks, 2^(M_tile - M_row), is a power of two: it is taken from the exponents of the
-//           operand on its way to the matrix cores, one 16-bit subtraction for two values, exact.
+//   logits  a tile of 256 tokens x 256 columns at a time: E = 2^(l log2 e - M_tile) in bf16, M_tile a multiple of 128 near the
+//           tile's largest exponent of the row, and the row's sum of E in fp32;
+//   rows    M_row = the running maximum of the M_tile, the running sum; E of tiles with another M is brought to M_row, a subtraction
+//           from its exponents;
+//   dh      sums = 2^(M_row before - M_row) sums + E w.
 // The column of the target is left out of E and of the sum S' and joins at the end, dh = grad (E w - S' w_target) / (S' + e_target):
 // a token that is predicted well has 1 - p_target = S' / S to full precision, not the difference of rounded numbers.
 //
@@ -24,7 +24,6 @@
 namespace salr {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-constexpr int kMaxTilesInLds = 128;   // tiles of 256 columns whose exponents a workgroup of the dh product keeps (kM bytes each)
 
 enum CeMode { kStatistics, kExponentials, kGradients };
 
@@ -39,9 +38,14 @@ __device__ __forceinline__ uint32_t pack_two_bf16(float a, float b) {
     return __builtin_bit_cast(uint32_t, v);
 }
 
+// The reference of a tile's row: the multiple of 128 next to its largest exponent, so that its E lie below 2^65.  bf16 and fp32 hold those
+// as well as numbers below 1, and hardly any row has tiles of two references: with logits within 44 of zero it is 0.
+constexpr float kReferenceStep = 128.f;
+__device__ __forceinline__ float tile_exponent(float most) { return kReferenceStep * rintf(most * (kLog2e / kReferenceStep)); }
+
 // l = h w^T of one tile and what becomes of it.  `w`: the piece's first row, `columns` of it exist; `pitch`: of `out` [T][pitch].
 template <class Shape, int kMode>
-__global__ __launch_bounds__(512) void ce_logits_kernel(const uint16_t* __restrict__ h, int64_t T, int64_t K, const uint16_t* __restrict__ w,
+__global__ __launch_bounds__(Shape::kThreads) void ce_logits_kernel(const uint16_t* __restrict__ h, int64_t T, int64_t K, const uint16_t* __restrict__ w,
                                                         int64_t columns, int64_t first, const int64_t* __restrict__ targets, int m_tiles, int n_tiles,
                                                         float2* __restrict__ stats, float* __restrict__ target_logit, const CeRow* __restrict__ rows,
                                                         uint16_t* __restrict__ out, int64_t pitch) {
@@ -61,20 +65,43 @@ __global__ __launch_bounds__(512) void ce_logits_kernel(const uint16_t* __restri
     for (int i = 0; i < kMI; ++i)
 #pragma unroll
         for (int j = 0; j < kNI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const TileSource<false, kM, 8> hs(h + m0 * K, K, T - m0, K, wave, lane);
-    const TileSource<false, 256, 8> ws(w + n0 * K, K, columns - n0, K, wave, lane);
-    tile_product<Shape, false, false>(hs, ws, 0, (int)((K + 63) / 64), lds, acc, [](const bf16x8& p, int, int) { return p; });
+    const TileSource<false, kM, Shape::kWaves> hs(h + m0 * K, K, T - m0, K, wave, lane);
+    const TileSource<false, 256, Shape::kWaves> ws(w + n0 * K, K, columns - n0, K, wave, lane);
+    tile_product<Shape, false, false>(hs, ws, 0, (int)((K + kProductStep - 1) / kProductStep), lds, acc);
 
-    // A lane holds columns 16 (wn kNI + j) + 4 g + r of row 16 (wm kMI + i) + i16.
+    // A lane holds columns 16 (wn kNI + j) + 4 g + r of row 16 (wm kMI + i) + i16.  What few lanes have to do (columns past the end, the
+    // target's) is tested once for a wave: over a tile the exponentials alone are 2 us, every other instruction an element 0.5.
     float* largest = reinterpret_cast<float*>(lds + kTile);   // [kWN][kM]
     float* sums = largest + kWN * kM;
     const int here = (int)(columns - n0 < 256 ? columns - n0 : 256);   // columns that exist
-    int target[kMI];
+    const int first_n = 16 * wn * kNI + 4 * g;
+    if (here < 256) {
+#pragma unroll
+        for (int i = 0; i < kMI; ++i)
+#pragma unroll
+            for (int j = 0; j < kNI; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (first_n + 16 * j + r >= here) acc[i][j][r] = -__builtin_inff();
+    }
+    int target[kMI];   // column in this wave's part of the tile, from the lane's first one on; others: none of its columns
 #pragma unroll
     for (int i = 0; i < kMI; ++i) {
         const int64_t m = m0 + 16 * (wm * kMI + i) + i16;
         const int64_t t = m < T ? targets[m] - first - n0 : -1;
-        target[i] = t >= 0 && t < here ? (int)t : -1;
+        target[i] = t >= 0 && t < here ? (int)t - first_n : -1;
+        if constexpr (kMode != kGradients) {
+            if (__any(target[i] >= 0 && target[i] < 16 * kNI)) {
+#pragma unroll
+                for (int j = 0; j < kNI; ++j)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (16 * j + r == target[i]) {
+                            target_logit[m] = acc[i][j][r];
+                            acc[i][j][r] = -__builtin_inff();
+                        }
+            }
+        }
     }
     if constexpr (kMode != kGradients) {
 #pragma unroll
@@ -83,12 +110,7 @@ __global__ __launch_bounds__(512) void ce_logits_kernel(const uint16_t* __restri
 #pragma unroll
             for (int j = 0; j < kNI; ++j)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int n = 16 * (wn * kNI + j) + 4 * g + r;
-                    if (n == target[i]) target_logit[m0 + 16 * (wm * kMI + i) + i16] = acc[i][j][r];
-                    if (n == target[i] || n >= here) acc[i][j][r] = -__builtin_inff();
-                    most = fmaxf(most, acc[i][j][r]);
-                }
+                for (int r = 0; r < 4; ++r) most = fmaxf(most, acc[i][j][r]);
             most = fmaxf(most, __shfl_xor(most, 16));
             most = fmaxf(most, __shfl_xor(most, 32));
             if (g == 0) largest[wn * kM + 16 * (wm * kMI + i) + i16] = most;
@@ -98,16 +120,23 @@ __global__ __launch_bounds__(512) void ce_logits_kernel(const uint16_t* __restri
 #pragma unroll
     for (int i = 0; i < kMI; ++i) {
         const int row = 16 * (wm * kMI + i) + i16;
+        float M, alpha = 1.f;
         CeRow of{};
-        float M;
         if constexpr (kMode == kGradients) {
             if (m0 + row < T) of = rows[m0 + row];
-            M = of.M;
+            M = of.M, alpha = of.alpha;
+            if (__any(!of.live)) {   // a masked token: alpha and M are 0
+#pragma unroll
+                for (int j = 0; j < kNI; ++j)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[i][j][r] = of.live ? acc[i][j][r] : 0.f;
+            }
         } else {
             float most = largest[row];
 #pragma unroll
             for (int q = 1; q < kWN; ++q) most = fmaxf(most, largest[q * kM + row]);
-            M = most == -__builtin_inff() ? 0.f : ceilf(most * kLog2e);   // (nothing in the row: every E is 2^-inf)
+            M = tile_exponent(most);
+            M = M == -__builtin_inff() ? 0.f : M;   // (nothing in the row: every E is 2^-inf)
         }
         float sum = 0.f;
 #pragma unroll
@@ -116,12 +145,15 @@ __global__ __launch_bounds__(512) void ce_logits_kernel(const uint16_t* __restri
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 e[r] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], kLog2e, -M));
-                if constexpr (kMode == kGradients) {
-                    const int n = 16 * (wn * kNI + j) + 4 * g + r;
-                    e[r] = n >= here || !of.live ? 0.f : n == target[i] ? -of.beta : of.alpha * e[r];
-                }
-                sum += e[r];
+                if constexpr (kMode == kGradients) e[r] *= alpha;
             }
+            if constexpr (kMode == kGradients) {
+                if (__any(target[i] >= 16 * j && target[i] < 16 * j + 4)) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) e[r] = 16 * j + r == target[i] ? -of.beta : e[r];
+                }
+            }
+            sum += (e[0] + e[1]) + (e[2] + e[3]);
             if constexpr (kMode != kStatistics)
                 *reinterpret_cast<uint2*>(lds + row * kOutPitch + 32 * (wn * kNI + j) + 8 * g) = make_uint2(pack_two_bf16(e[0], e[1]), pack_two_bf16(e[2], e[3]));
         }
@@ -133,7 +165,7 @@ __global__ __launch_bounds__(512) void ce_logits_kernel(const uint16_t* __restri
     }
     __syncthreads();
     if constexpr (kMode != kGradients) {
-        for (int row = threadIdx.x; row < kM; row += 512) {
+        for (int row = threadIdx.x; row < kM; row += Shape::kThreads) {
             if (m0 + row >= T) break;
             float most = largest[row], sum = sums[row];
 #pragma unroll
@@ -141,11 +173,11 @@ __global__ __launch_bounds__(512) void ce_logits_kernel(const uint16_t* __restri
                 most = fmaxf(most, largest[q * kM + row]);
                 sum += sums[q * kM + row];
             }
-            stats[(int64_t)at.nt * T + m0 + row] = make_float2(most == -__builtin_inff() ? most : ceilf(most * kLog2e), sum);
+            stats[(int64_t)at.nt * T + m0 + row] = make_float2(tile_exponent(most), sum);
         }
     }
     if constexpr (kMode != kStatistics) {
-        for (int row = wave * 2 + (lane >> 5); row < kM; row += 16) {
+        for (int row = wave * 2 + (lane >> 5); row < kM; row += 2 * Shape::kWaves) {
             if (m0 + row >= T) break;
             *reinterpret_cast<uint4*>(out + (m0 + row) * pitch + n0 + 8 * (lane & 31)) = *reinterpret_cast<const uint4*>(lds + row * kOutPitch + 16 * (lane & 31));
         }
@@ -158,7 +190,8 @@ struct CeRowArgs {
     bool first, last;          // piece of the vocabulary
     float2* running;           // [T]: M and sum so far
     float* rescale;            // [T]: 2^(M before - M now)
-    uint8_t* lower;            // [n_tiles][T]: M now - M_tile; null: not wanted
+    uint16_t* e;               // E of the piece, brought to M now where a tile's M is another; null: there is none
+    int64_t pitch;
     const float* target_logit;
     const int64_t* targets;
     const float* grad_loss;    // null: ones
@@ -191,10 +224,28 @@ __global__ __launch_bounds__(1024) void ce_rows_kernel(CeRowArgs a) {
         for (int n = wave; n < a.n_tiles; n += 16) {
             const float2 s = a.stats[(int64_t)n * a.T + t];
             sum += s.y * __builtin_amdgcn_exp2f(s.x - M);
-            if (a.lower != nullptr) a.lower[(int64_t)n * a.T + t] = (uint8_t)fminf(M - s.x, 255.f);
         }
     }
     part[1][wave][lane] = sum;
+    if (a.e != nullptr) {
+        // The exponents of E in tiles with a reference below the row's, lowered by the difference: exact.  The wave goes through such
+        // rows one by one, its lanes through the tile's columns.
+        for (int n = wave; n < a.n_tiles; n += 16) {
+            const float behind = here ? M - a.stats[(int64_t)n * a.T + t].x : 0.f;
+            uint64_t rows = __ballot(behind > 0.f && behind < inf);
+            while (rows != 0) {
+                const int of = __ffsll((unsigned long long)rows) - 1;
+                rows &= rows - 1;
+                uint2* at = reinterpret_cast<uint2*>(a.e + ((int64_t)blockIdx.x * 64 + of) * a.pitch + (int64_t)n * 256) + lane;
+                const bool gone = __shfl(behind, of) > kReferenceStep;
+                const u16x2 by = gone ? u16x2{0xFFFF, 0xFFFF} : u16x2{(uint16_t)kReferenceStep << 7, (uint16_t)kReferenceStep << 7};
+                uint2 q = *at;
+                q.x = __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, q.x), by));
+                q.y = __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, q.y), by));
+                *at = q;
+            }
+        }
+    }
     __syncthreads();
     if (wave != 0 || !here) return;
     const float scale = __builtin_amdgcn_exp2f(before.x - M);
@@ -224,13 +275,13 @@ __global__ __launch_bounds__(1024) void ce_rows_kernel(CeRowArgs a) {
     if (a.rows != nullptr) a.rows[t] = CeRow{M, alpha, beta, target >= 0};
 }
 
-// acc += E w over the columns of a piece (contracted), slice kz of them.  `lower` null: E as it is (G).
-template <class Shape, bool kLower>
-__global__ __launch_bounds__(512) void ce_dh_kernel(const uint16_t* __restrict__ e, int64_t T, int64_t pitch, const uint16_t* __restrict__ w,
-                                                    int64_t columns, int64_t K, int m_tiles, int n_tiles, int slices, const uint8_t* __restrict__ lower,
-                                                    const float* __restrict__ rescale, bool first, float* __restrict__ sums) {
+// sums = rescale sums + E w over the columns of a piece (contracted), slice kz of them.  `rescale` null: ones.
+template <class Shape>
+__global__ __launch_bounds__(Shape::kThreads) void ce_dh_kernel(const uint16_t* __restrict__ e, int64_t T, int64_t pitch, const uint16_t* __restrict__ w,
+                                                    int64_t columns, int64_t K, int m_tiles, int n_tiles, int slices, const float* __restrict__ rescale,
+                                                    bool first, float* __restrict__ sums) {
     constexpr int kMI = Shape::kMI, kNI = Shape::kNI, kWN = Shape::kWN, kM = Shape::kM;
-    __shared__ __attribute__((aligned(16))) char lds[Shape::kLdsBytes + (kLower ? kMaxTilesInLds * kM : 0)];
+    __shared__ __attribute__((aligned(16))) char lds[Shape::kLdsBytes];
     const TilePlace at(m_tiles, n_tiles, slices);
     if (!at.any) return;
     const int64_t m0 = (int64_t)at.mt * kM, n0 = (int64_t)at.nt * 256;
@@ -238,19 +289,11 @@ __global__ __launch_bounds__(512) void ce_dh_kernel(const uint16_t* __restrict__
     const int wm = wave / kWN, wn = wave % kWN, i16 = lane & 15, g = lane >> 4;
     // slices start at whole tiles of 256 columns: four steps
     const int tiles = (int)((columns + 255) / 256), t_begin = (int)((int64_t)tiles * at.kz / slices), t_end = (int)((int64_t)tiles * (at.kz + 1) / slices);
-    if constexpr (kLower) {
-        uint8_t* mine = reinterpret_cast<uint8_t*>(lds + Shape::kLdsBytes);
-        for (int n = threadIdx.x; n < (t_end - t_begin) * kM; n += 512) {
-            const int64_t m = m0 + n % kM;
-            mine[n] = m < T ? lower[(int64_t)(t_begin + n / kM) * T + m] : 0;
-        }
-        __syncthreads();
-    }
     f32x4 acc[kMI][kNI];
 #pragma unroll
     for (int i = 0; i < kMI; ++i) {
         const int64_t m = m0 + 16 * (wm * kMI + i) + i16;
-        const float scale = !first && m < T ? (kLower ? rescale[m] : 1.f) : 0.f;
+        const float scale = !first && m < T && rescale != nullptr ? rescale[m] : 1.f;
 #pragma unroll
         for (int j = 0; j < kNI; ++j) {
             const int64_t n = n0 + 16 * (wn * kNI + j) + 4 * g;
@@ -259,21 +302,9 @@ __global__ __launch_bounds__(512) void ce_dh_kernel(const uint16_t* __restrict__
             acc[i][j] = v;
         }
     }
-    const TileSource<false, kM, 8> es(e + m0 * pitch, pitch, T - m0, pitch, wave, lane);
-    const TileSource<true, 256, 8> ws(w + n0, K, K - n0, columns, wave, lane);
-    const uint8_t* mine = reinterpret_cast<const uint8_t*>(lds + Shape::kLdsBytes) + 16 * wm * kMI + i16;
-    tile_product<Shape, false, true>(es, ws, 4 * t_begin, 4 * t_end, lds, acc, [&](const bf16x8& p, int s, int i) {
-        if constexpr (kLower) {
-            const uint32_t d = mine[((s >> 2) - t_begin) * kM + 16 * i];
-            const u16x2 by = __builtin_bit_cast(u16x2, d * 0x00800080u);
-            u32x4 q = __builtin_bit_cast(u32x4, p);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) q[c] = __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, (uint32_t)q[c]), by));
-            return __builtin_bit_cast(bf16x8, q);
-        } else {
-            return p;
-        }
-    });
+    const TileSource<false, kM, Shape::kWaves> es(e + m0 * pitch, pitch, T - m0, pitch, wave, lane);
+    const TileSource<true, 256, Shape::kWaves> ws(w + n0, K, K - n0, columns, wave, lane);
+    tile_product<Shape, false, true>(es, ws, 4 * t_begin, 4 * t_end, lds, acc);
 #pragma unroll
     for (int i = 0; i < kMI; ++i) {
         const int64_t m = m0 + 16 * (wm * kMI + i) + i16;
@@ -313,7 +344,7 @@ __global__ __launch_bounds__(256) void ce_dh_finish_kernel(const float* __restri
 
 // dw of a piece: G^T h, both operands across the contraction.
 template <class Shape>
-__global__ __launch_bounds__(512) void ce_dw_kernel(const uint16_t* __restrict__ gr, int64_t T, int64_t pitch, const uint16_t* __restrict__ h, int64_t K,
+__global__ __launch_bounds__(Shape::kThreads) void ce_dw_kernel(const uint16_t* __restrict__ gr, int64_t T, int64_t pitch, const uint16_t* __restrict__ h, int64_t K,
                                                     int64_t columns, int m_tiles, int n_tiles, uint16_t* __restrict__ dw) {
     constexpr int kMI = Shape::kMI, kNI = Shape::kNI, kWN = Shape::kWN;
     __shared__ __attribute__((aligned(16))) char lds[Shape::kLdsBytes];
@@ -327,9 +358,9 @@ __global__ __launch_bounds__(512) void ce_dw_kernel(const uint16_t* __restrict__
     for (int i = 0; i < kMI; ++i)
 #pragma unroll
         for (int j = 0; j < kNI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const TileSource<true, 256, 8> gs(gr + m0, pitch, pitch - m0, T, wave, lane);
-    const TileSource<true, 256, 8> hs(h + n0, K, K - n0, T, wave, lane);
-    tile_product<Shape, true, true>(gs, hs, 0, (int)((T + 63) / 64), lds, acc, [](const bf16x8& p, int, int) { return p; });
+    const TileSource<true, 256, Shape::kWaves> gs(gr + m0, pitch, pitch - m0, T, wave, lane);
+    const TileSource<true, 256, Shape::kWaves> hs(h + n0, K, K - n0, T, wave, lane);
+    tile_product<Shape, true, true>(gs, hs, 0, (int)((T + kProductStep - 1) / kProductStep), lds, acc);
 #pragma unroll
     for (int i = 0; i < kMI; ++i) {
         const int64_t m = m0 + 16 * (wm * kMI + i) + i16;
@@ -351,12 +382,11 @@ __global__ __launch_bounds__(256) void ce_live_rows_kernel(const uint16_t* __res
     reinterpret_cast<uint4*>(out)[id] = targets[id / per_row] >= 0 ? q : make_uint4(0, 0, 0, 0);
 }
 
-typedef TileShape<8, 2, 2> Shape256;
-typedef TileShape<4, 2, 3> Shape128;
-typedef TileShape<4, 1, 2> Shape64;
-typedef TileShape<2, 1, 2> Shape32;
-typedef TileShape<1, 1, 2> Shape16;
-
+typedef TileShape<8, 4, 2, 4, 2, 3> Shape256;
+typedef TileShape<4, 4, 2, 4, 3, 3> Shape128;
+typedef TileShape<4, 2, 1, 8, 2, 2> Shape64;
+typedef TileShape<2, 2, 1, 8, 2, 2> Shape32;
+typedef TileShape<1, 2, 1, 8, 2, 2> Shape16;
 static int64_t rows_of_tile(int64_t T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : T <= 128 ? 128 : 256; }
 
 CePlan ce_plan(int64_t T, int64_t K, int64_t V, bool want_dh, bool want_dw) {
@@ -368,10 +398,7 @@ CePlan ce_plan(int64_t T, int64_t K, int64_t V, bool want_dh, bool want_dw) {
     const bool pieces = want_dh || want_dw;
     int64_t per = p.tiles;
     if (pieces) {
-        // a piece of E stays within half of the cache in front of memory (256 MB), and its tiles' exponents within LDS
-        const int64_t most = kCePieceBytes / (512 * (T > 0 ? T : 1));
-        const int64_t cap = want_dw ? (most > 1 ? most : 1) : (most < 1 ? 1 : most > kMaxTilesInLds ? kMaxTilesInLds : most);
-        const int64_t n = (p.tiles + cap - 1) / (cap > 0 ? cap : 1);
+        const int64_t most = kCePieceBytes / (512 * (T > 0 ? T : 1)), cap = most > 1 ? most : 1, n = (p.tiles + cap - 1) / cap;
         per = n > 0 ? (p.tiles + n - 1) / n : 0;
     }
     p.piece_tiles = per;
@@ -393,7 +420,6 @@ CePlan ce_plan(int64_t T, int64_t K, int64_t V, bool want_dh, bool want_dw) {
     p.target_logit = take((size_t)T * 4);
     p.of_rows = take((size_t)T * sizeof(CeRow));
     if (pieces) p.e = take((size_t)T * per * 512);
-    if (want_dh && !want_dw) p.lower = take((size_t)T * per);
     if (want_dh) p.sums = take((size_t)p.slices * T * K * 4);
     if (want_dw) p.h_live = take((size_t)T * K * 2);
     p.bytes = at;
@@ -403,7 +429,7 @@ CePlan ce_plan(int64_t T, int64_t K, int64_t V, bool want_dh, bool want_dw) {
 template <class Shape, int kMode>
 static void launch_logits(const CeArgs& a, const CePlan& p, char* ws, int64_t tile0, int64_t tiles, const uint16_t* h) {
     const int64_t first = tile0 * 256, columns = a.V - first < tiles * 256 ? a.V - first : tiles * 256;
-    hipLaunchKernelGGL((ce_logits_kernel<Shape, kMode>), dim3(product_grid(p.m_tiles * tiles)), dim3(512), 0, a.stream, h, a.T, a.K, a.w + first * a.K,
+    hipLaunchKernelGGL((ce_logits_kernel<Shape, kMode>), dim3(product_grid(p.m_tiles * tiles)), dim3(Shape::kThreads), 0, a.stream, h, a.T, a.K, a.w + first * a.K,
                        columns, first, a.targets, (int)p.m_tiles, (int)tiles, reinterpret_cast<float2*>(ws + p.stats), reinterpret_cast<float*>(ws + p.target_logit),
                        reinterpret_cast<const CeRow*>(ws + p.of_rows), reinterpret_cast<uint16_t*>(ws + p.e), p.piece_tiles * 256);
 }
@@ -445,21 +471,17 @@ static hipError_t launch_shape(const CeArgs& a, const CePlan& p, char* ws) {
             } else {
                 launch_logits<Shape, kExponentials>(a, p, ws, tile0, tiles, a.h);
                 r.n_tiles = (int)tiles, r.first = tile0 == 0, r.last = tile0 + tiles == p.tiles;
-                r.lower = reinterpret_cast<uint8_t*>(ws + p.lower);
+                r.e = e, r.pitch = pitch;
                 hipLaunchKernelGGL(ce_rows_kernel, row_grid, dim3(1024), 0, a.stream, r);
             }
             if (a.dh != nullptr && n_tiles > 0) {
                 const dim3 grid(product_grid(p.m_tiles * n_tiles * p.slices));
-                if (statistics_first)
-                    hipLaunchKernelGGL((ce_dh_kernel<Shape, false>), grid, dim3(512), 0, a.stream, e, a.T, pitch, a.w + first * a.K, columns, a.K, (int)p.m_tiles,
-                                       n_tiles, (int)p.slices, nullptr, nullptr, tile0 == 0, sums);
-                else
-                    hipLaunchKernelGGL((ce_dh_kernel<Shape, true>), grid, dim3(512), 0, a.stream, e, a.T, pitch, a.w + first * a.K, columns, a.K, (int)p.m_tiles,
-                                       n_tiles, (int)p.slices, r.lower, r.rescale, tile0 == 0, sums);
+                hipLaunchKernelGGL(ce_dh_kernel<Shape>, grid, dim3(Shape::kThreads), 0, a.stream, e, a.T, pitch, a.w + first * a.K, columns, a.K, (int)p.m_tiles,
+                                   n_tiles, (int)p.slices, statistics_first ? nullptr : r.rescale, tile0 == 0, sums);
             }
         }
         if (a.dw != nullptr && n_tiles > 0)
-            hipLaunchKernelGGL(ce_dw_kernel<Shape256>, dim3(product_grid(tiles * n_tiles)), dim3(512), 0, a.stream, e, a.T, pitch, h_live, a.K, columns, (int)tiles,
+            hipLaunchKernelGGL(ce_dw_kernel<Shape256>, dim3(product_grid(tiles * n_tiles)), dim3(Shape256::kThreads), 0, a.stream, e, a.T, pitch, h_live, a.K, columns, (int)tiles,
                                n_tiles, a.dw + first * a.K);
     }
     if (a.dh != nullptr && units > 0) {

@@ -835,7 +835,7 @@ hipError_t launch_adamw(const StepChunk* plan, int64_t chunks, bool param32, boo
 hipError_t launch_grad_norm(const StepChunk* plan, int64_t chunks, bool grad32, float max_norm, float* out, void* workspace, hipStream_t stream);
 
 // ---- Softmax cross entropy of a head without its logits (salr_cross_entropy.hip)
-constexpr int64_t kCePieceBytes = (int64_t)128 << 20;   // E of a piece of the vocabulary, see ce_plan
+constexpr int64_t kCePieceBytes = (int64_t)256 << 20;   // E of a piece of the vocabulary, see ce_plan
 struct CeArgs {
     const uint16_t* h;
     int64_t T, K;
@@ -852,7 +852,7 @@ struct CeArgs {
 struct CePlan {
     int64_t rows, m_tiles;   // tokens of a tile, tiles of tokens
     int64_t tiles, piece_tiles, slices;   // of 256 columns: all, of a piece; slices of a piece that dh is summed over
-    size_t stats, running, rescale, target_logit, of_rows, e, lower, sums, h_live;   // offsets in the workspace
+    size_t stats, running, rescale, target_logit, of_rows, e, sums, h_live;   // offsets in the workspace
     size_t bytes;
 };
 CePlan ce_plan(int64_t T, int64_t K, int64_t V, bool want_dh, bool want_dw);

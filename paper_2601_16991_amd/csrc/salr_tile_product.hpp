@@ -4,13 +4,15 @@
 //
 // An operand lies in memory along k (P[m][k]: "rows" layout) or across it (P[k][m]: "columns" layout, transposed on its way from
 // LDS to registers by ds_read_b64_tr_b16).  Workgroup: kWM x kWN waves, wave tile 16 kMI (m) x 16 kNI (n), tile of n always 256
-// wide, steps of 64 along k.  Loads go straight to LDS (16 bytes a lane) into a ring of kStages steps; nothing is read past an
+// wide, steps of 64 along k.  Loads go straight to LDS (16 bytes a lane), each operand into a ring of its own; nothing is read past an
 // operand's end: rows, columns and steps that are not there come out of the buffer load as zeros.
 //
-// LDS of one step.  Rows layout: [rows][64] with rows of 128 bytes, 16-byte piece c of row r at c ^ ((r >> 1) & 7).  Columns layout:
-// [64][256] with rows of 512 bytes, 32-byte piece c of row k at c ^ ((k & 3) | ((k >> 3) & 3) << 2): the sixteen rows that one
-// transposing read touches lie on different banks.
+// LDS of one step.  Rows layout: [rows][64] with rows of 128 bytes, 16-byte piece c of row r at c ^ rows_swizzle(r).  Columns layout:
+// [64][256] with rows of 512 bytes, 32-byte piece c of row k at c ^ columns_swizzle(k): the sixteen rows that one transposing read
+// touches lie on different banks.
 #pragma once
+
+#include <type_traits>
 
 #include "salr_device.hpp"
 
@@ -22,64 +24,69 @@ typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kProductXcds = 8;
 
-// c += a b, a: sixteen n, b: sixteen m; lane 16 g + i then holds n = 4 g .. 4 g + 3 of m = i.
+// c += a b, a: sixteen n, b: sixteen m; lane 16 g + i then holds n = 4 g .. 4 g + 3 of m = i.  kInPlace: in the accumulation registers
+// that c is in (where accumulators take half of the 512, the builtin moves them about); the compiler does not know the
+// instruction's latency then: the k loop waits for the last ones itself.
+template <bool kInPlace>
 __device__ __forceinline__ void product_mfma(f32x4& c, const bf16x8& a, const bf16x8& b) {
-    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    if constexpr (kInPlace) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+    else c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-// One operand's tile: kRows wide (m or n), k-steps [.., ..) of `steps` from `k0` on.  All members but the lane's are uniform.
+constexpr int kProductStep = 64;   // of k
+
+__device__ __forceinline__ int rows_swizzle(int r) { return (r >> 1) & 7; }
+__device__ __forceinline__ int columns_swizzle(int k) { return (k & 3) | ((k >> 3) & 3) << 2; }
+
+// One operand's tile: kRows wide (m or n), steps of k counted from its start.  All members but the lane's are uniform.
 template <bool kColumns, int kRows, int kWaves>
 struct TileSource {
     static_assert(!kColumns || kRows == 256, "columns layout: tiles of 256");
-    static constexpr int kLoads = kRows / 8 / kWaves > 0 ? kRows / 8 / kWaves : 1;   // 1 KB each, per wave and step
-    static constexpr int kBytes = kRows * 128;
+    static constexpr int kInstructions = kRows / 8;   // loads of 1 KB in a step, of all waves
+    static constexpr int kLoads = kInstructions >= kWaves ? kInstructions / kWaves : 1;
+    static constexpr bool kAllWaves = kInstructions >= kWaves;
     static constexpr uint32_t kOut = 0xFFFFFFF0u;   // past every buffer: zeros
 
     uint64_t base;      // of step 0
     int64_t bytes;      // from there to the end of the last row of the tile
     uint32_t advance;   // bytes a step
-    uint32_t pitch;     // bytes a row
     uint32_t offset;    // this lane's place in load 0
     uint32_t stride;    // from load to load
-    uint32_t loads_here;   // loads of this wave (rows layout with fewer rows than waves * 8: 0 or 1)
-    int32_t k_left;     // rows layout: columns from this lane's first one of step 0 to the end
+    int32_t k_left;     // rows layout: columns from this lane's first one of step 0 to the end; columns layout: columns of the tile that exist
 
     // rows layout: `rows_left` rows from p on, each `k_end` long; columns layout: k_end rows, `rows_left` columns from p on
     __device__ __forceinline__ TileSource(const uint16_t* p, int64_t pitch_elems, int64_t rows_left, int64_t k_end, int wave, int lane) {
         base = reinterpret_cast<uint64_t>(p);
-        pitch = (uint32_t)(pitch_elems * 2);
-        loads_here = kRows / 8 >= kWaves ? kLoads : (wave < kRows / 8 ? 1 : 0);
-        if constexpr (!kColumns) {
-            const int row = 8 * wave + (lane >> 3), piece = (lane & 7) ^ ((row >> 1) & 7);
+        const uint32_t pitch = (uint32_t)(pitch_elems * 2);
+        const int64_t here = rows_left < kRows ? rows_left : kRows;
+        if constexpr (!kColumns) {   // load j: rows 8 (wave + kWaves j) .. + 7, eight lanes each
+            const int row = 8 * wave + (lane >> 3), piece = (lane & 7) ^ rows_swizzle(row);
             offset = row * pitch + piece * 16;
             stride = 8 * kWaves * pitch;
-            advance = 128;
-            bytes = (rows_left < kRows ? rows_left : kRows) * (int64_t)pitch - (pitch - (int64_t)k_end * 2);
+            advance = kProductStep * 2;
+            bytes = here * (int64_t)pitch - (pitch - (int64_t)k_end * 2);
             k_left = (int32_t)(k_end - 8 * piece);
-        } else {
-            // load j: step rows 2 (wave + kWaves j) and the next one; with 8 waves the swizzle of row + 16 j differs, so the piece
-            // is worked out per load
-            const int row = 2 * wave + (lane >> 5);
-            offset = row * pitch;
+        } else {   // load j: k rows 2 (wave + kWaves j) and the next one, 32 lanes each
+            offset = (2 * wave + (lane >> 5)) * pitch;
             stride = 2 * kWaves * pitch;
-            advance = 64 * pitch;
-            bytes = k_end * (int64_t)pitch - (pitch - (rows_left < kRows ? rows_left : kRows) * 2);
-            k_left = (int32_t)(rows_left < kRows ? rows_left : kRows);   // columns of the tile that are there
+            advance = kProductStep * pitch;
+            bytes = k_end * (int64_t)pitch - (pitch - here * 2);
+            k_left = (int32_t)here;
         }
     }
 
     // Load j of step `s` to LDS at `lds` (uniform): all of it in assembly, so that the waits stay with the caller.  `live`: the step exists.
     __device__ __forceinline__ void fetch(int s, int j, uint32_t lds, bool live, int wave, int lane) const {
-        if (kRows / 8 < kWaves && loads_here == 0) return;
+        if (!kAllWaves && wave >= kInstructions) return;
         const uint64_t at = base + (uint64_t)s * advance;
         const int64_t left = live ? bytes - (int64_t)s * advance : 0;
         const uint32_t room = left <= 0 ? 0u : left < 0x7FFFFFFF ? (uint32_t)left : 0x7FFFFFFFu;
         uint32_t v;
         if constexpr (!kColumns) {
-            v = 64 * s < k_left ? offset + j * stride : kOut;
+            v = kProductStep * s < k_left ? offset + j * stride : kOut;
         } else {
             const int row = 2 * (wave + kWaves * j) + (lane >> 5), slot = lane & 31;
-            const int piece = (((slot >> 1) ^ ((row & 3) | ((row >> 3) & 3) << 2)) << 1) | (slot & 1);
+            const int piece = (((slot >> 1) ^ columns_swizzle(row)) << 1) | (slot & 1);
             v = 8 * piece < k_left ? offset + j * stride + piece * 16 : kOut;
         }
         const u32x4 buffer = {(uint32_t)at, (uint32_t)(at >> 32) & 0xFFFFu, room, 0x00020000u};
@@ -88,24 +95,23 @@ struct TileSource {
     }
 };
 
-// Sixteen rows (from `row0` on) by 32 k (half `s` of the step) of a tile, as an operand of the instruction.
+// Sixteen rows (from `row0` on) by 32 of k (half of a step) of a tile, as an operand of the instruction.
 template <bool kColumns>
-__device__ __forceinline__ bf16x8 tile_operand(const char* tile, int row0, int s, int lane) {
+__device__ __forceinline__ bf16x8 tile_operand(const char* tile, int row0, int half, int lane) {
     const int i = lane & 15, g = lane >> 4;
     if constexpr (!kColumns) {
         const int row = row0 + i;
-        return *reinterpret_cast<const bf16x8*>(tile + row * 128 + (((4 * s + g) ^ ((row >> 1) & 7)) * 16));
+        return *reinterpret_cast<const bf16x8*>(tile + row * 128 + (((4 * half + g) ^ rows_swizzle(row)) * 16));
     } else {
         // lane i of a group of sixteen names 8 bytes: k row (i / 4), columns 4 (i % 4) ..; it receives column i of the four rows
         typedef __attribute__((address_space(3))) bf16x4* LdsPtr;
-        bf16x4 half[2];
+        bf16x4 four[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int k = 32 * s + 8 * g + 4 * h + (i >> 2);
-            const int piece = (row0 >> 4) ^ ((k & 3) | ((k >> 3) & 3) << 2);
-            half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsPtr)(tile + k * 512 + piece * 32 + (i & 3) * 8));
+            const int k = 32 * half + 8 * g + 4 * h + (i >> 2);
+            four[h] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsPtr)(tile + k * 512 + ((row0 >> 4) ^ columns_swizzle(k)) * 32 + (i & 3) * 8));
         }
-        return __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7);
+        return __builtin_shufflevector(four[0], four[1], 0, 1, 2, 3, 4, 5, 6, 7);
     }
 }
 
@@ -127,59 +133,99 @@ struct TilePlace {
 };
 inline unsigned product_grid(int64_t workgroups) { return (unsigned)((workgroups + kProductXcds - 1) / kProductXcds * kProductXcds); }
 
-// Shape of a workgroup's tile: 16 kMI kWM x 256.
-template <int kMI_, int kWM_, int kStages_>
+// Shape of a workgroup's tile: 16 kMI kWM x 16 kNI kWN (256); steps of either operand that LDS holds.
+template <int kMI_, int kNI_, int kWM_, int kWN_, int kPSlots_, int kQSlots_>
 struct TileShape {
-    static constexpr int kMI = kMI_, kWM = kWM_, kStages = kStages_;
-    static constexpr int kWN = 8 / kWM, kNI = 16 / kWN, kWaves = 8, kThreads = 512;
-    static constexpr int kM = 16 * kMI * kWM, kN = 256;
-    static constexpr int kStageBytes = (kM + kN) * 128;
-    static constexpr int kLdsBytes = kStages * kStageBytes;
+    static constexpr int kMI = kMI_, kNI = kNI_, kWM = kWM_, kWN = kWN_, kPSlots = kPSlots_, kQSlots = kQSlots_;
+    static constexpr int kWaves = kWM * kWN, kThreads = 64 * kWaves;
+    static constexpr int kM = 16 * kMI * kWM, kN = 16 * kNI * kWN;
+    static constexpr int kPBytes = kM * 2 * kProductStep, kQBytes = kN * 2 * kProductStep;
+    static constexpr int kLdsBytes = kPSlots * kPBytes + kQSlots * kQBytes;
+    static constexpr bool kInPlace = kMI * kNI * 4 > 128;
+    static_assert(kN == 256, "tile of n");
+    static_assert(kPSlots >= 2 && (kQSlots == kPSlots || kQSlots == 3), "see tile_product");
 };
 
-// The k loop over steps [begin, end) of both sources; acc[i][j] += ... .  `adjust(p, s, half, i)` may change the operand of P (m).
-// On return every wave has read its last operands and no load is under way.
-template <class Shape, bool kPColumns, bool kQColumns, class Adjust>
-__device__ __forceinline__ void tile_product(const TileSource<kPColumns, Shape::kM, 8>& ps, const TileSource<kQColumns, 256, 8>& qs, int begin, int end,
-                                             char* lds, f32x4 (&acc)[Shape::kMI][Shape::kNI], Adjust&& adjust) {
-    constexpr int S = Shape::kStages, kMI = Shape::kMI, kNI = Shape::kNI;
+// The k loop over steps [begin, end) of both sources; acc[i][j] += ... .  On return every wave has read its last operands and no load is
+// under way.
+//
+// A step is two halves of 32 along k.  The operands of a half are read from LDS during the products of the half before.  The barrier
+// between the halves says that the next step has landed, and that every wave holds the rest of this one in registers: its slots are free.
+// Requests are spread over the products, because a burst of them holds the waves up (4 to 6 % of a call): P's into the slot just left, in
+// the second half; Q's, where it has a slot more, in the first half of the next step.
+template <class Shape, bool kPColumns, bool kQColumns>
+__device__ __forceinline__ void tile_product(const TileSource<kPColumns, Shape::kM, Shape::kWaves>& ps, const TileSource<kQColumns, 256, Shape::kWaves>& qs,
+                                             int begin, int end, char* lds, f32x4 (&acc)[Shape::kMI][Shape::kNI]) {
+    typedef TileSource<kPColumns, Shape::kM, Shape::kWaves> PSource;
+    typedef TileSource<kQColumns, 256, Shape::kWaves> QSource;
+    constexpr int SP = Shape::kPSlots, SQ = Shape::kQSlots, kMI = Shape::kMI, kNI = Shape::kNI, kLoads = PSource::kLoads + QSource::kLoads;
+    // loads that every wave makes in a step (a wave that has one more waits for it earlier than it has to)
+    constexpr int kSure = QSource::kLoads + (PSource::kAllWaves ? PSource::kLoads : 0);
+    constexpr bool kApart = SQ > 2;
+    constexpr int kSureP = PSource::kAllWaves ? PSource::kLoads : 0;
+    // what may be under way when step s + 1 has to be there, by what was requested behind its two parts.  Apart: Q of step s + SQ - 1
+    // during the half before, P of s + SP - 1 before that; else both of s + SP - 1 then.
+    constexpr int kUnderWay = !kApart ? (SP - 2) * kSure : SP == 2 ? QSource::kLoads : (SQ - 3) * kSure + kSureP + QSource::kLoads;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / Shape::kWN, wn = wave % Shape::kWN;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
-    constexpr int kPLoads = TileSource<kPColumns, Shape::kM, 8>::kLoads, kQLoads = TileSource<kQColumns, 256, 8>::kLoads;
-    auto fetch = [&](int s, int slot) {
-        const uint32_t to = lds0 + slot * Shape::kStageBytes;
-#pragma unroll
-        for (int j = 0; j < kQLoads; ++j) qs.fetch(s, j, to + Shape::kM * 128, s < end, wave, lane);
-#pragma unroll
-        for (int j = 0; j < kPLoads; ++j) ps.fetch(s, j, to, s < end, wave, lane);
+    constexpr int kQFirst = SP * Shape::kPBytes;   // Q's ring behind P's
+    auto fetch_p = [&](int s, int slot, int c) { ps.fetch(s, c, lds0 + slot * Shape::kPBytes, s < end, wave, lane); };
+    auto fetch_q = [&](int s, int slot, int c) { qs.fetch(s, c, lds0 + kQFirst + slot * Shape::kQBytes, s < end, wave, lane); };
+    auto read = [&](int p_slot, int q_slot, int half, int c, bf16x8 (&q)[kNI], bf16x8 (&p)[kMI]) {
+        if (c < kNI) q[c] = tile_operand<kQColumns>(lds + kQFirst + q_slot * Shape::kQBytes, 16 * (wn * kNI + c), half, lane);
+        else p[c - kNI] = tile_operand<kPColumns>(lds + p_slot * Shape::kPBytes, 16 * (wm * kMI + c - kNI), half, lane);
     };
+    constexpr int kQAhead = kApart ? SQ - 1 : SQ;   // steps of Q requested before the first
 #pragma unroll
-    for (int p = 0; p < S - 1; ++p) fetch(begin + p, p);
-    int slot = 0;
-    for (int s = begin; s < end; ++s) {
-        // step s has landed (at most the loads of the S - 2 steps after it are under way; a wave that has none of P's waits longer), and
-        // every wave is through with step s - 1, whose slot the next request fills
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((S - 2) * (kQLoads + (Shape::kM >= 64 ? kPLoads : 0))) : "memory");
-        const int last = slot == 0 ? S - 1 : slot - 1;
-        fetch(s + S - 1, last);
-        const char* pt = lds + slot * Shape::kStageBytes;
-        const char* qt = pt + Shape::kM * 128;
+    for (int t = 0; t < (SP > kQAhead ? SP : kQAhead); ++t) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            bf16x8 q[kNI], p[kMI];
+        for (int c = 0; c < PSource::kLoads; ++c)
+            if (t < SP) fetch_p(begin + t, t, c);
 #pragma unroll
-            for (int j = 0; j < kNI; ++j) q[j] = tile_operand<kQColumns>(qt, 16 * (wn * kNI + j), half, lane);
+        for (int c = 0; c < QSource::kLoads; ++c)
+            if (t < kQAhead) fetch_q(begin + t, t, c);
+    }
+    bf16x8 q0[kNI], p0[kMI], q1[kNI], p1[kMI];
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((SP - 1) * kSureP + (kQAhead - 1) * QSource::kLoads) : "memory");
 #pragma unroll
-            for (int i = 0; i < kMI; ++i) p[i] = adjust(tile_operand<kPColumns>(pt, 16 * (wm * kMI + i), half, lane), s, i);
+    for (int c = 0; c < kNI + kMI; ++c) read(0, 0, 0, c, q0, p0);
+    // Products of one half, with the reads of the next (operands in the order in which its products want them) and `requests` spread over them.
+    auto products = [&](const bf16x8 (&q)[kNI], const bf16x8 (&p)[kMI], auto&& read_next, auto requests, auto&& request) {
+        constexpr int kRequests = decltype(requests)::value;
 #pragma unroll
-            for (int i = 0; i < kMI; ++i)
+        for (int i = 0; i < kMI; ++i) {
 #pragma unroll
-                for (int j = 0; j < kNI; ++j) product_mfma(acc[i][j], q[j], p[i]);
+            for (int c = (kNI + kMI) * i / kMI; c < (kNI + kMI) * (i + 1) / kMI; ++c) read_next(c);
+#pragma unroll
+            for (int c = kRequests * i / kMI; c < kRequests * (i + 1) / kMI; ++c) request(c);
+#pragma unroll
+            for (int j = 0; j < kNI; ++j) product_mfma<Shape::kInPlace>(acc[i][j], q[j], p[i]);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        slot = slot + 1 == S ? 0 : slot + 1;
+    };
+    int p_slot = 0, q_slot = 0;
+    for (int s = begin; s < end; ++s) {
+        const int p_next = p_slot + 1 == SP ? 0 : p_slot + 1, q_next = q_slot + 1 == SQ ? 0 : q_slot + 1;
+        const int q_before = q_slot == 0 ? SQ - 1 : q_slot - 1;
+        products(q0, p0, [&](int c) { read(p_slot, q_slot, 1, c, q1, p1); }, std::integral_constant<int, kApart ? QSource::kLoads : 0>{},
+                 [&](int c) { fetch_q(s + SQ - 1, q_before, c); });
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kUnderWay) : "memory");
+        products(q1, p1, [&](int c) { read(p_next, q_next, 0, c, q0, p0); }, std::integral_constant<int, kApart ? PSource::kLoads : kLoads>{}, [&](int c) {
+            if (c < PSource::kLoads) fetch_p(s + SP, p_slot, c);
+            else fetch_q(s + SQ, q_slot, c - PSource::kLoads);
+        });
+        p_slot = p_next;
+        q_slot = q_next;
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if constexpr (Shape::kInPlace) {   // the last products have written their results, and no read of them moves up
+        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < kMI; ++i)
+#pragma unroll
+            for (int j = 0; j < kNI; ++j) asm volatile("" : "+a"(acc[i][j]));
+    }
 }
 
 }  // namespace salr
