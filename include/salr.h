@@ -468,7 +468,7 @@ typedef struct {
 } salr_step_tensor_t;
 
 /*
- * salr_step_plan_bytes: 0 for no elements at all, (size_t)-1 for counts out of range (negative, above 2^42, or 2^31 - 1 records).
+ * salr_step_plan_bytes: 0 for no elements at all, (size_t)-1 for counts out of range (negative, above 2^42, or more than 2^29 - 1 records).
  * salr_step_plan: state_bits 32 or 8, or 0 for a list that only salr_grad_norm is to read.  *chunks gets the number of records, which
  * the calls want to know.
  * Errors: INVALID_ARG (null where data is required, negative size, a tensor that is not 16-byte aligned (scales: 8), a type or
@@ -506,7 +506,8 @@ salr_status_t salr_adamw_step(const void* plan, int64_t chunks, salr_type_t para
  * the same order every time.
  *
  *   out        out  [2] fp32 on the device; out + 1 serves as grad_scale of salr_adamw_step
- *   workspace  --   SALR_GRAD_NORM_WORKSPACE_BYTES, 8-byte aligned; contents unspecified
+ *   workspace  --   SALR_GRAD_NORM_WORKSPACE_BYTES, 8-byte aligned.  Its first 4 bytes are zero before the first call (the caller clears them
+ *                   once), and every call leaves them zero; calls that may overlap need a workspace each
  * Errors: INVALID_ARG (also max_norm negative or NaN), SHAPE, CAPACITY, HIP.
  */
 #define SALR_GRAD_NORM_WORKSPACE_BYTES 8192

@@ -707,7 +707,7 @@ class GradNorm:
 
     def __init__(self, grads, _list=None):
         self._list = _list or _StepList(grads)
-        self._workspace = torch.empty(GRAD_NORM_WORKSPACE_BYTES, dtype=torch.uint8, device=self._list.plan.device)
+        self._workspace = torch.zeros(GRAD_NORM_WORKSPACE_BYTES, dtype=torch.uint8, device=self._list.plan.device)
         self._call = _native().grad_norm
 
     def __call__(self, max_norm: float = float("inf"), out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:

@@ -49,14 +49,14 @@ __global__ __launch_bounds__(Shape::kThreads) void ce_logits_kernel(const uint16
                                                         int64_t columns, int64_t first, const int64_t* __restrict__ targets, int m_tiles, int n_tiles,
                                                         float2* __restrict__ stats, float* __restrict__ target_logit, const CeRow* __restrict__ rows,
                                                         uint16_t* __restrict__ out, int64_t pitch) {
-    constexpr int kMI = Shape::kMI, kNI = Shape::kNI, kWN = Shape::kWN, kM = Shape::kM;
-    constexpr int kOutPitch = 512 + 16;   // bytes of a row of E in LDS
+    constexpr int kMI = Shape::kMI, kNI = Shape::kNI, kWN = Shape::kWN, kM = Shape::kM, kN = Shape::kN;
+    constexpr int kOutPitch = 2 * kN + 16;   // bytes of a row of E in LDS
     constexpr int kTile = kMode == kStatistics ? 0 : kM * kOutPitch;
     constexpr int kEnd = kTile + 2 * kWN * kM * 4;
     __shared__ __attribute__((aligned(16))) char lds[kEnd > Shape::kLdsBytes ? kEnd : Shape::kLdsBytes];
     const TilePlace at(m_tiles, n_tiles, 1);
     if (!at.any) return;   // uniform for the workgroup, before any barrier
-    const int64_t m0 = (int64_t)at.mt * kM, n0 = (int64_t)at.nt * 256;
+    const int64_t m0 = (int64_t)at.mt * kM, n0 = (int64_t)at.nt * kN;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / kWN, wn = wave % kWN, i16 = lane & 15, g = lane >> 4;
 
@@ -66,16 +66,16 @@ __global__ __launch_bounds__(Shape::kThreads) void ce_logits_kernel(const uint16
 #pragma unroll
         for (int j = 0; j < kNI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     const TileSource<false, kM, Shape::kWaves> hs(h + m0 * K, K, T - m0, K, wave, lane);
-    const TileSource<false, 256, Shape::kWaves> ws(w + n0 * K, K, columns - n0, K, wave, lane);
+    const TileSource<false, kN, Shape::kWaves> ws(w + n0 * K, K, columns - n0, K, wave, lane);
     tile_product<Shape, false, false>(hs, ws, 0, (int)((K + kProductStep - 1) / kProductStep), lds, acc);
 
     // A lane holds columns 16 (wn kNI + j) + 4 g + r of row 16 (wm kMI + i) + i16.  What few lanes have to do (columns past the end, the
     // target's) is tested once for a wave: over a tile the exponentials alone are 2 us, every other instruction an element 0.5.
     float* largest = reinterpret_cast<float*>(lds + kTile);   // [kWN][kM]
     float* sums = largest + kWN * kM;
-    const int here = (int)(columns - n0 < 256 ? columns - n0 : 256);   // columns that exist
+    const int here = (int)(columns - n0 < kN ? columns - n0 : kN);   // columns that exist
     const int first_n = 16 * wn * kNI + 4 * g;
-    if (here < 256) {
+    if (here < kN) {
 #pragma unroll
         for (int i = 0; i < kMI; ++i)
 #pragma unroll
@@ -177,9 +177,11 @@ __global__ __launch_bounds__(Shape::kThreads) void ce_logits_kernel(const uint16
         }
     }
     if constexpr (kMode != kStatistics) {
-        for (int row = wave * 2 + (lane >> 5); row < kM; row += 2 * Shape::kWaves) {
+        constexpr int kVecs = kN / 8, kRowsAtOnce = Shape::kThreads / kVecs;   // 16 bytes a lane
+        const int vec = threadIdx.x % kVecs;
+        for (int row = threadIdx.x / kVecs; row < kM; row += kRowsAtOnce) {
             if (m0 + row >= T) break;
-            *reinterpret_cast<uint4*>(out + (m0 + row) * pitch + n0 + 8 * (lane & 31)) = *reinterpret_cast<const uint4*>(lds + row * kOutPitch + 16 * (lane & 31));
+            *reinterpret_cast<uint4*>(out + (m0 + row) * pitch + n0 + 8 * vec) = *reinterpret_cast<const uint4*>(lds + row * kOutPitch + 16 * vec);
         }
     }
 }
@@ -192,6 +194,7 @@ struct CeRowArgs {
     float* rescale;            // [T]: 2^(M before - M now)
     uint16_t* e;               // E of the piece, brought to M now where a tile's M is another; null: there is none
     int64_t pitch;
+    int width;                 // columns of a tile: 64, 128 or 256
     const float* target_logit;
     const int64_t* targets;
     const float* grad_loss;    // null: ones
@@ -201,44 +204,61 @@ struct CeRowArgs {
     CeRow* rows;               // null: not wanted
 };
 
-// Sixteen waves on 64 rows, a lane a row; wave q takes every sixteenth tile.
+// Maximum of references and the sum with respect to it.  References are multiples of 128, -infinity (no column), +infinity or NaN.
+struct CeSum {
+    float M, sum, least;   // least: smallest reference of a tile that has one
+    __device__ __forceinline__ void add(float M2, float sum2, float least2) {
+        const float top = fmaxf(M, M2), M_ref = top == -__builtin_inff() ? 0.f : top;
+        sum = sum * __builtin_amdgcn_exp2f(M - M_ref) + sum2 * __builtin_amdgcn_exp2f(M2 - M_ref);
+        M = top;
+        least = fminf(least, least2);
+    }
+};
+
+// kRows rows a workgroup, 1024 / kRows threads a row; the tiles dealt out to them in turn.
+template <int kRows>
 __global__ __launch_bounds__(1024) void ce_rows_kernel(CeRowArgs a) {
-    __shared__ float part[2][16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t t = (int64_t)blockIdx.x * 64 + lane;
+    constexpr int kParts = 1024 / kRows;
+    __shared__ CeSum part[16][kRows];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = threadIdx.x % kRows, first_tile = threadIdx.x / kRows;
+    const int64_t t = (int64_t)blockIdx.x * kRows + row;
     const bool here = t < a.T;
     const float inf = __builtin_inff();
-    float most = -inf, sum = 0.f;
+    CeSum all{-inf, 0.f, inf};
     if (here) {
 #pragma unroll 8
-        for (int n = wave; n < a.n_tiles; n += 16) most = fmaxf(most, a.stats[(int64_t)n * a.T + t].x);
-    }
-    part[0][wave][lane] = most;
-    __syncthreads();
-    for (int q = 0; q < 16; ++q) most = fmaxf(most, part[0][q][lane]);
-    const float2 before = here && !a.first ? a.running[t] : make_float2(-inf, 0.f);
-    most = fmaxf(most, before.x);
-    const float M = most == -inf ? 0.f : most;
-    if (here) {
-#pragma unroll 8
-        for (int n = wave; n < a.n_tiles; n += 16) {
+        for (int n = first_tile; n < a.n_tiles; n += kParts) {
             const float2 s = a.stats[(int64_t)n * a.T + t];
-            sum += s.y * __builtin_amdgcn_exp2f(s.x - M);
+            all.add(s.x, s.y, s.x > -inf ? s.x : inf);
         }
     }
-    part[1][wave][lane] = sum;
-    if (a.e != nullptr) {
-        // The exponents of E in tiles with a reference below the row's, lowered by the difference: exact.  The wave goes through such
-        // rows one by one, its lanes through the tile's columns.
-        for (int n = wave; n < a.n_tiles; n += 16) {
-            const float behind = here ? M - a.stats[(int64_t)n * a.T + t].x : 0.f;
-            uint64_t rows = __ballot(behind > 0.f && behind < inf);
-            while (rows != 0) {
-                const int of = __ffsll((unsigned long long)rows) - 1;
-                rows &= rows - 1;
-                uint2* at = reinterpret_cast<uint2*>(a.e + ((int64_t)blockIdx.x * 64 + of) * a.pitch + (int64_t)n * 256) + lane;
+#pragma unroll
+    for (int o = kRows; o < 64; o <<= 1) {
+        const CeSum other{__shfl_xor(all.M, o), __shfl_xor(all.sum, o), __shfl_xor(all.least, o)};
+        all.add(other.M, other.sum, other.least);
+    }
+    if (lane < kRows) part[wave][row] = all;
+    __syncthreads();
+    const float2 before = here && !a.first ? a.running[t] : make_float2(-inf, 0.f);
+    all = CeSum{before.x, before.y, inf};
+    for (int q = 0; q < 16; ++q) all.add(part[q][row].M, part[q][row].sum, part[q][row].least);
+    const float M = all.M == -inf ? 0.f : all.M, sum = all.sum;
+    if (a.e != nullptr && __any(here && all.least < M)) {
+        // The exponents of E in tiles with a reference below the row's, lowered by the difference: exact.  The wave goes through such tiles
+        // one by one, its lanes through the columns.
+        for (int n0 = 0; n0 < a.n_tiles; n0 += kParts) {
+            const int n = n0 + first_tile;
+            const float behind = here && n < a.n_tiles ? M - a.stats[(int64_t)n * a.T + t].x : 0.f;
+            uint64_t todo = __ballot(behind > 0.f && behind < inf);
+            while (todo != 0) {
+                const int of = __ffsll((unsigned long long)todo) - 1;
+                todo &= todo - 1;
+                const int64_t at_row = (int64_t)blockIdx.x * kRows + (wave * 64 + of) % kRows, at_tile = n0 + (wave * 64 + of) / kRows;
                 const bool gone = __shfl(behind, of) > kReferenceStep;
-                const u16x2 by = gone ? u16x2{0xFFFF, 0xFFFF} : u16x2{(uint16_t)kReferenceStep << 7, (uint16_t)kReferenceStep << 7};
+                if (4 * lane >= a.width) continue;
+                uint2* at = reinterpret_cast<uint2*>(a.e + at_row * a.pitch + at_tile * a.width) + lane;
+                const uint16_t step = (uint16_t)((int)kReferenceStep << 7);
+                const u16x2 by = gone ? u16x2{0xFFFF, 0xFFFF} : u16x2{step, step};
                 uint2 q = *at;
                 q.x = __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, q.x), by));
                 q.y = __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, q.y), by));
@@ -246,13 +266,9 @@ __global__ __launch_bounds__(1024) void ce_rows_kernel(CeRowArgs a) {
             }
         }
     }
-    __syncthreads();
-    if (wave != 0 || !here) return;
-    const float scale = __builtin_amdgcn_exp2f(before.x - M);
-    sum = a.first ? 0.f : before.y * scale;
-    for (int q = 0; q < 16; ++q) sum += part[1][q][lane];
-    a.running[t] = make_float2(most, sum);
-    a.rescale[t] = scale;
+    if (threadIdx.x >= kRows || !here) return;
+    a.running[t] = make_float2(all.M, sum);
+    a.rescale[t] = __builtin_amdgcn_exp2f(before.x - M);
     if (!a.last) return;
     // S' = sum of 2^(l log2 e - M) over the other columns, e the target's (M may lie below the target's own exponent)
     const int64_t target = a.targets[t];
@@ -287,8 +303,7 @@ __global__ __launch_bounds__(Shape::kThreads) void ce_dh_kernel(const uint16_t* 
     const int64_t m0 = (int64_t)at.mt * kM, n0 = (int64_t)at.nt * 256;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / kWN, wn = wave % kWN, i16 = lane & 15, g = lane >> 4;
-    // slices start at whole tiles of 256 columns: four steps
-    const int tiles = (int)((columns + 255) / 256), t_begin = (int)((int64_t)tiles * at.kz / slices), t_end = (int)((int64_t)tiles * (at.kz + 1) / slices);
+    const int64_t steps = (columns + kProductStep - 1) / kProductStep;   // (E is written in whole steps)
     f32x4 acc[kMI][kNI];
 #pragma unroll
     for (int i = 0; i < kMI; ++i) {
@@ -304,7 +319,7 @@ __global__ __launch_bounds__(Shape::kThreads) void ce_dh_kernel(const uint16_t* 
     }
     const TileSource<false, kM, Shape::kWaves> es(e + m0 * pitch, pitch, T - m0, pitch, wave, lane);
     const TileSource<true, 256, Shape::kWaves> ws(w + n0, K, K - n0, columns, wave, lane);
-    tile_product<Shape, false, true>(es, ws, 4 * t_begin, 4 * t_end, lds, acc);
+    tile_product<Shape, false, true>(es, ws, (int)(steps * at.kz / slices), (int)(steps * (at.kz + 1) / slices), lds, acc);
 #pragma unroll
     for (int i = 0; i < kMI; ++i) {
         const int64_t m = m0 + 16 * (wm * kMI + i) + i16;
@@ -327,6 +342,7 @@ __global__ __launch_bounds__(256) void ce_dh_finish_kernel(const float* __restri
     const int64_t target = targets[t];
     const CeRow of = rows[t];
     float x[8] = {};
+#pragma unroll 4
     for (int z = 0; z < slices; ++z) {
         const float4* from = reinterpret_cast<const float4*>(sums + ((int64_t)z * T + t) * K + k);
         const float4 a = from[0], b = from[1];
@@ -361,16 +377,19 @@ __global__ __launch_bounds__(Shape::kThreads) void ce_dw_kernel(const uint16_t* 
     const TileSource<true, 256, Shape::kWaves> gs(gr + m0, pitch, pitch - m0, T, wave, lane);
     const TileSource<true, 256, Shape::kWaves> hs(h + n0, K, K - n0, T, wave, lane);
     tile_product<Shape, true, true>(gs, hs, 0, (int)((T + kProductStep - 1) / kProductStep), lds, acc);
+    // through LDS, so that rows leave as whole vectors, side by side
+    constexpr int kOutPitch = 512 + 16;
 #pragma unroll
-    for (int i = 0; i < kMI; ++i) {
-        const int64_t m = m0 + 16 * (wm * kMI + i) + i16;
+    for (int i = 0; i < kMI; ++i)
 #pragma unroll
-        for (int j = 0; j < kNI; ++j) {
-            const int64_t n = n0 + 16 * (wn * kNI + j) + 4 * g;
-            if (m < columns && n < K)
-                *reinterpret_cast<uint2*>(dw + m * K + n) = make_uint2(pack_two_bf16(acc[i][j][0], acc[i][j][1]), pack_two_bf16(acc[i][j][2], acc[i][j][3]));
-        }
-    }
+        for (int j = 0; j < kNI; ++j)
+            *reinterpret_cast<uint2*>(lds + (16 * (wm * kMI + i) + i16) * kOutPitch + 32 * (wn * kNI + j) + 8 * g) =
+                make_uint2(pack_two_bf16(acc[i][j][0], acc[i][j][1]), pack_two_bf16(acc[i][j][2], acc[i][j][3]));
+    __syncthreads();
+    const int vec = threadIdx.x % 32;
+    if (n0 + 8 * vec >= K) return;
+    for (int row = threadIdx.x / 32; row < 256 && m0 + row < columns; row += Shape::kThreads / 32)
+        *reinterpret_cast<uint4*>(dw + (m0 + row) * K + n0 + 8 * vec) = *reinterpret_cast<const uint4*>(lds + row * kOutPitch + 16 * vec);
 }
 
 // Hidden states with those of masked tokens as zeros: G is zero there, but not what it is multiplied by.
@@ -382,31 +401,61 @@ __global__ __launch_bounds__(256) void ce_live_rows_kernel(const uint16_t* __res
     reinterpret_cast<uint4*>(out)[id] = targets[id / per_row] >= 0 ? q : make_uint4(0, 0, 0, 0);
 }
 
+// Tiles: 256 columns wide, or 64 where few tokens on a small vocabulary would leave CUs without one.
 typedef TileShape<8, 4, 2, 4, 2, 3> Shape256;
 typedef TileShape<4, 4, 2, 4, 3, 3> Shape128;
 typedef TileShape<4, 2, 1, 8, 2, 2> Shape64;
 typedef TileShape<2, 2, 1, 8, 2, 2> Shape32;
 typedef TileShape<1, 2, 1, 8, 2, 2> Shape16;
-static int64_t rows_of_tile(int64_t T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : T <= 128 ? 128 : 256; }
+typedef TileShape<4, 1, 1, 4, 4, 4> Narrow64;
+typedef TileShape<2, 1, 1, 4, 4, 4> Narrow32;
+typedef TileShape<1, 1, 1, 4, 4, 4> Narrow16;
+
+constexpr int64_t kCus = 256;
+
+// What a launch of `tiles` workgroups, one to a CU, takes in rounds of all CUs: a round that is part full costs 55 to 95 % of a full one
+// (2048 to 32768 columns, 4096 deep: 640 tiles 2.7 rounds, 512 exactly 2, 128 tiles 0.85).
+static double tile_rounds(int64_t tiles) {
+    const double f = (double)(tiles % kCus) / kCus;
+    return (double)(tiles / kCus) + (f > 0.0 ? 0.55 + 0.4 * f : 0.0);
+}
+// A round of tiles of 128 tokens against one of 256: a step of them takes 0.9 us and 1.56.
+constexpr double kHalfTile = 0.6;
+
+static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 CePlan ce_plan(int64_t T, int64_t K, int64_t V, bool want_dh, bool want_dw) {
     CePlan p{};
-    const int64_t kM = rows_of_tile(T);
-    p.rows = kM;
-    p.m_tiles = (T + kM - 1) / kM;
-    p.tiles = (V + 255) / 256;
     const bool pieces = want_dh || want_dw;
-    int64_t per = p.tiles;
+    const int64_t all = ceil_div(V, 256) * 256;
+    p.piece = all;
     if (pieces) {
-        const int64_t most = kCePieceBytes / (512 * (T > 0 ? T : 1)), cap = most > 1 ? most : 1, n = (p.tiles + cap - 1) / cap;
-        per = n > 0 ? (p.tiles + n - 1) / n : 0;
+        const int64_t most = kCePieceBytes / (512 * (T > 0 ? T : 1)), cap = (most > 1 ? most : 1) * 256, n = ceil_div(all, cap);
+        if (n > 0) p.piece = ceil_div(ceil_div(all, n), 256) * 256;
     }
-    p.piece_tiles = per;
+    // tokens of a tile: the fewest that hold them all up to 64; from there the faster of 128 and 256
+    // (66 against 91 us for 256 x 4096 x 32768, 214 against 194 for 777)
+    const int64_t few = T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : 128, tiles = p.piece / 256;
+    p.rows = few;
+    if (T > 128 && tile_rounds(ceil_div(T, 256) * tiles) <= kHalfTile * tile_rounds(ceil_div(T, 128) * tiles)) p.rows = 256;
+    p.m_tiles = ceil_div(T, p.rows);
+    // columns of a tile: 64 where wide ones are too few to go round (24 x 8192 x 32000: 104 us against 165)
+    p.width = few <= 64 && tiles < 384 ? 64 : 256;
+    p.dh_rows = few, p.slices = 1;
     if (want_dh) {
-        const int64_t tiles = p.m_tiles * ((K + 255) / 256);
-        int64_t s = 1;
-        while (tiles * s < 192 && s * 2 <= per) s *= 2;
-        p.slices = s;
+        const int64_t n_tiles = ceil_div(K, 256), steps = p.piece / kProductStep;
+        if (few <= 64) {   // bound by memory: two workgroups to a CU
+            while (n_tiles * p.slices < 384 && p.slices * 4 <= steps && p.slices < 64) p.slices *= 2;
+        } else {
+            // a slice more costs a pass over [T, K] in fp32, there and back
+            double best = 0.0;
+            for (int64_t rows = 128; rows <= (T > 128 ? 256 : 128); rows *= 2)
+                for (int64_t s = 1; s <= 16 && s * 4 <= steps; ++s) {
+                    const double us = tile_rounds(ceil_div(T, rows) * n_tiles * s) * (rows == 128 ? kHalfTile : 1.0) * 1.56 * (double)steps / s +
+                                      (double)s * T * K * 8 / 5e6;
+                    if (best == 0.0 || us < best) best = us, p.dh_rows = rows, p.slices = s;
+                }
+        }
     }
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -414,95 +463,125 @@ CePlan ce_plan(int64_t T, int64_t K, int64_t V, bool want_dh, bool want_dw) {
         at += round_up_256(bytes);
         return here;
     };
-    p.stats = take((size_t)p.tiles * T * sizeof(float2));
+    p.stats = take((size_t)((want_dh && !want_dw ? p.piece : all) / p.width) * T * sizeof(float2));
     p.running = take((size_t)T * sizeof(float2));
     p.rescale = take((size_t)T * 4);
     p.target_logit = take((size_t)T * 4);
     p.of_rows = take((size_t)T * sizeof(CeRow));
-    if (pieces) p.e = take((size_t)T * per * 512);
+    if (pieces) p.e = take((size_t)T * p.piece * 2);
     if (want_dh) p.sums = take((size_t)p.slices * T * K * 4);
     if (want_dw) p.h_live = take((size_t)T * K * 2);
     p.bytes = at;
     return p;
 }
 
-template <class Shape, int kMode>
-static void launch_logits(const CeArgs& a, const CePlan& p, char* ws, int64_t tile0, int64_t tiles, const uint16_t* h) {
-    const int64_t first = tile0 * 256, columns = a.V - first < tiles * 256 ? a.V - first : tiles * 256;
-    hipLaunchKernelGGL((ce_logits_kernel<Shape, kMode>), dim3(product_grid(p.m_tiles * tiles)), dim3(Shape::kThreads), 0, a.stream, h, a.T, a.K, a.w + first * a.K,
-                       columns, first, a.targets, (int)p.m_tiles, (int)tiles, reinterpret_cast<float2*>(ws + p.stats), reinterpret_cast<float*>(ws + p.target_logit),
-                       reinterpret_cast<const CeRow*>(ws + p.of_rows), reinterpret_cast<uint16_t*>(ws + p.e), p.piece_tiles * 256);
-}
+namespace {
 
-template <class Shape>
-static hipError_t launch_shape(const CeArgs& a, const CePlan& p, char* ws) {
-    const int n_tiles = (int)((a.K + 255) / 256);
-    uint16_t* e = reinterpret_cast<uint16_t*>(ws + p.e);
-    const int64_t pitch = p.piece_tiles * 256;
-    CeRow* rows = reinterpret_cast<CeRow*>(ws + p.of_rows);
-    float* sums = reinterpret_cast<float*>(ws + p.sums);
-    CeRowArgs r{};
-    r.stats = reinterpret_cast<const float2*>(ws + p.stats);
-    r.running = reinterpret_cast<float2*>(ws + p.running);
-    r.rescale = reinterpret_cast<float*>(ws + p.rescale);
-    r.target_logit = reinterpret_cast<const float*>(ws + p.target_logit);
-    r.targets = a.targets, r.grad_loss = a.grad_loss, r.T = a.T, r.V = a.V, r.loss = a.loss, r.lse = a.lse, r.rows = rows;
-    const dim3 row_grid((unsigned)((a.T + 63) / 64));
-    const unsigned units = (unsigned)((a.T * (a.K / 8) + 255) / 256);
-    const bool statistics_first = a.dw != nullptr || a.dh == nullptr;
-    if (a.T > 0 && statistics_first) {
-        launch_logits<Shape, kStatistics>(a, p, ws, 0, p.tiles, a.h);
-        r.n_tiles = (int)p.tiles, r.first = r.last = true;
-        hipLaunchKernelGGL(ce_rows_kernel, row_grid, dim3(1024), 0, a.stream, r);
+struct CeRun {   // one call
+    const CeArgs& a;
+    const CePlan& p;
+    char* ws;
+    template <class T>
+    T* at(size_t offset) const { return reinterpret_cast<T*>(ws + offset); }
+
+    template <class Shape, int kMode>
+    void logits_on(int64_t first, int64_t columns) const {
+        const int64_t tiles = (columns + Shape::kN - 1) / Shape::kN;
+        hipLaunchKernelGGL((ce_logits_kernel<Shape, kMode>), dim3(product_grid(p.m_tiles * tiles)), dim3(Shape::kThreads), 0, a.stream, a.h, a.T, a.K,
+                           a.w + first * a.K, columns, first, a.targets, (int)p.m_tiles, (int)tiles, at<float2>(p.stats), at<float>(p.target_logit),
+                           at<const CeRow>(p.of_rows), at<uint16_t>(p.e), p.piece);
     }
-    if (a.dh == nullptr && a.dw == nullptr) return hipGetLastError();
-    const uint16_t* h_live = a.h;
-    if (a.dw != nullptr && units > 0) {
-        uint16_t* to = reinterpret_cast<uint16_t*>(ws + p.h_live);
-        hipLaunchKernelGGL(ce_live_rows_kernel, dim3(units), dim3(256), 0, a.stream, a.h, a.targets, a.T, a.K, to);
-        h_live = to;
-    }
-    for (int64_t tile0 = 0; tile0 < p.tiles; tile0 += p.piece_tiles) {
-        const int64_t tiles = p.tiles - tile0 < p.piece_tiles ? p.tiles - tile0 : p.piece_tiles, first = tile0 * 256;
-        const int64_t columns = a.V - first < tiles * 256 ? a.V - first : tiles * 256;
-        if (a.T > 0) {
-            if (statistics_first) {
-                launch_logits<Shape, kGradients>(a, p, ws, tile0, tiles, a.h);
-            } else {
-                launch_logits<Shape, kExponentials>(a, p, ws, tile0, tiles, a.h);
-                r.n_tiles = (int)tiles, r.first = tile0 == 0, r.last = tile0 + tiles == p.tiles;
-                r.e = e, r.pitch = pitch;
-                hipLaunchKernelGGL(ce_rows_kernel, row_grid, dim3(1024), 0, a.stream, r);
-            }
-            if (a.dh != nullptr && n_tiles > 0) {
-                const dim3 grid(product_grid(p.m_tiles * n_tiles * p.slices));
-                hipLaunchKernelGGL(ce_dh_kernel<Shape>, grid, dim3(Shape::kThreads), 0, a.stream, e, a.T, pitch, a.w + first * a.K, columns, a.K, (int)p.m_tiles,
-                                   n_tiles, (int)p.slices, statistics_first ? nullptr : r.rescale, tile0 == 0, sums);
-            }
+    template <int kMode>
+    void logits(int64_t first, int64_t columns) const {
+        const bool narrow = p.width == 64;
+        switch (p.rows) {
+            case 16: return narrow ? logits_on<Narrow16, kMode>(first, columns) : logits_on<Shape16, kMode>(first, columns);
+            case 32: return narrow ? logits_on<Narrow32, kMode>(first, columns) : logits_on<Shape32, kMode>(first, columns);
+            case 64: return narrow ? logits_on<Narrow64, kMode>(first, columns) : logits_on<Shape64, kMode>(first, columns);
+            case 128: return logits_on<Shape128, kMode>(first, columns);
+            default: return logits_on<Shape256, kMode>(first, columns);
         }
-        if (a.dw != nullptr && n_tiles > 0)
-            hipLaunchKernelGGL(ce_dw_kernel<Shape256>, dim3(product_grid(tiles * n_tiles)), dim3(Shape256::kThreads), 0, a.stream, e, a.T, pitch, h_live, a.K, columns, (int)tiles,
-                               n_tiles, a.dw + first * a.K);
     }
-    if (a.dh != nullptr && units > 0) {
-        if (statistics_first)
-            hipLaunchKernelGGL(ce_dh_finish_kernel<true>, dim3(units), dim3(256), 0, a.stream, sums, (int)p.slices, a.T, a.K, rows, a.targets, a.V, a.w, a.dh);
-        else
-            hipLaunchKernelGGL(ce_dh_finish_kernel<false>, dim3(units), dim3(256), 0, a.stream, sums, (int)p.slices, a.T, a.K, rows, a.targets, a.V, a.w, a.dh);
+    void rows(int64_t columns, bool first, bool last, bool with_e) const {
+        CeRowArgs r{};
+        r.stats = at<const float2>(p.stats);
+        r.n_tiles = (int)((columns + p.width - 1) / p.width);
+        r.first = first, r.last = last;
+        r.running = at<float2>(p.running), r.rescale = at<float>(p.rescale);
+        r.e = with_e ? at<uint16_t>(p.e) : nullptr, r.pitch = p.piece, r.width = (int)p.width;
+        r.target_logit = at<const float>(p.target_logit), r.targets = a.targets, r.grad_loss = a.grad_loss;
+        r.T = a.T, r.V = a.V, r.loss = a.loss, r.lse = a.lse, r.rows = at<CeRow>(p.of_rows);
+        if (a.T <= 4) hipLaunchKernelGGL(ce_rows_kernel<4>, dim3(1), dim3(1024), 0, a.stream, r);
+        else if (a.T <= 512) hipLaunchKernelGGL(ce_rows_kernel<16>, dim3((unsigned)((a.T + 15) / 16)), dim3(1024), 0, a.stream, r);
+        else hipLaunchKernelGGL(ce_rows_kernel<64>, dim3((unsigned)((a.T + 63) / 64)), dim3(1024), 0, a.stream, r);
     }
-    return hipGetLastError();
-}
+    int n_tiles() const { return (int)((a.K + 255) / 256); }
+    unsigned units() const { return (unsigned)((a.T * (a.K / 8) + 255) / 256); }   // workgroups with eight columns of a row a thread
+
+    template <class Shape>
+    void dh_on(int64_t first, int64_t columns, bool rescaled) const {
+        const int64_t m_tiles = ceil_div(a.T, Shape::kM);
+        hipLaunchKernelGGL(ce_dh_kernel<Shape>, dim3(product_grid(m_tiles * n_tiles() * p.slices)), dim3(Shape::kThreads), 0, a.stream, at<const uint16_t>(p.e),
+                           a.T, p.piece, a.w + first * a.K, columns, a.K, (int)m_tiles, n_tiles(), (int)p.slices, rescaled ? at<const float>(p.rescale) : nullptr,
+                           first == 0, at<float>(p.sums));
+    }
+    void dh(int64_t first, int64_t columns, bool rescaled) const {
+        if (n_tiles() == 0) return;
+        switch (p.dh_rows) {
+            case 16: return dh_on<Shape16>(first, columns, rescaled);
+            case 32: return dh_on<Shape32>(first, columns, rescaled);
+            case 64: return dh_on<Shape64>(first, columns, rescaled);
+            case 128: return dh_on<Shape128>(first, columns, rescaled);
+            default: return dh_on<Shape256>(first, columns, rescaled);
+        }
+    }
+    template <bool kPlain>
+    void dh_finish() const {
+        if (units() == 0) return;
+        hipLaunchKernelGGL(ce_dh_finish_kernel<kPlain>, dim3(units()), dim3(256), 0, a.stream, at<const float>(p.sums), (int)p.slices, a.T, a.K,
+                           at<const CeRow>(p.of_rows), a.targets, a.V, a.w, a.dh);
+    }
+    void live_rows() const {
+        if (units() == 0) return;
+        hipLaunchKernelGGL(ce_live_rows_kernel, dim3(units()), dim3(256), 0, a.stream, a.h, a.targets, a.T, a.K, at<uint16_t>(p.h_live));
+    }
+    void dw(int64_t first, int64_t columns) const {
+        if (n_tiles() == 0) return;
+        const int64_t tiles = (columns + 255) / 256;
+        hipLaunchKernelGGL(ce_dw_kernel<Shape256>, dim3(product_grid(tiles * n_tiles())), dim3(Shape256::kThreads), 0, a.stream, at<const uint16_t>(p.e), a.T, p.piece,
+                           at<const uint16_t>(p.h_live), a.K, columns, (int)tiles, n_tiles(), a.dw + first * a.K);
+    }
+};
+
+}  // namespace
 
 hipError_t launch_cross_entropy(const CeArgs& a, void* workspace) {
     const CePlan p = ce_plan(a.T, a.K, a.V, a.dh != nullptr, a.dw != nullptr);
-    char* ws = static_cast<char*>(workspace);
-    switch (p.rows) {
-        case 16: return launch_shape<Shape16>(a, p, ws);
-        case 32: return launch_shape<Shape32>(a, p, ws);
-        case 64: return launch_shape<Shape64>(a, p, ws);
-        case 128: return launch_shape<Shape128>(a, p, ws);
-        default: return launch_shape<Shape256>(a, p, ws);
+    const CeRun run{a, p, static_cast<char*>(workspace)};
+    if (a.T == 0) {   // no tokens: dw is zero
+        for (int64_t first = 0; first < a.V; first += p.piece) run.dw(first, a.V - first < p.piece ? a.V - first : p.piece);
+        return hipGetLastError();
     }
+    const bool one_pass = a.dh != nullptr && a.dw == nullptr;   // on E; else the statistics come first, and pieces of G where they are wanted
+    if (!one_pass) {
+        run.logits<kStatistics>(0, a.V);
+        run.rows(a.V, true, true, false);
+        if (a.dw == nullptr) return hipGetLastError();
+        run.live_rows();
+    }
+    for (int64_t first = 0; first < a.V; first += p.piece) {
+        const int64_t columns = a.V - first < p.piece ? a.V - first : p.piece;
+        if (one_pass) {
+            run.logits<kExponentials>(first, columns);
+            run.rows(columns, first == 0, first + columns == a.V, true);
+        } else {
+            run.logits<kGradients>(first, columns);
+        }
+        if (a.dh != nullptr) run.dh(first, columns, one_pass);
+        if (a.dw != nullptr) run.dw(first, columns);
+    }
+    if (a.dh != nullptr) one_pass ? run.dh_finish<false>() : run.dh_finish<true>();
+    return hipGetLastError();
 }
 
 }  // namespace salr

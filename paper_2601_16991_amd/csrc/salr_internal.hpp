@@ -819,10 +819,11 @@ struct StepChunk {
 };
 static_assert(sizeof(StepChunk) == 64, "a plan's size is told in these");
 constexpr int64_t kStepBlock = 128;     // elements that share two scales
-constexpr int64_t kStepChunk = 8192;    // a workgroup's share of a tensor
+constexpr int64_t kStepChunk = 8192;    // elements of a record
 constexpr int64_t kStepMaxCount = (int64_t)1 << 42;
-constexpr int64_t kStepMaxChunks = 2147483647LL;   // gridDim.x
-constexpr int kGradNormBlocks = 1024;   // workgroups of the norm, one partial sum each
+constexpr int64_t kStepMaxChunks = 536870911LL;   // gridDim.x, four workgroups each
+constexpr int kGradNormBlocks = 512;    // workgroups of the norm, one partial sum each (two to a CU)
+static_assert(256 + kGradNormBlocks * 8 <= SALR_GRAD_NORM_WORKSPACE_BYTES, "room for the partial sums");
 struct AdamwArgs {
     double lr, beta1, beta2, eps, weight_decay;
     int64_t step, seed;
@@ -851,7 +852,9 @@ struct CeArgs {
 };
 struct CePlan {
     int64_t rows, m_tiles;   // tokens of a tile, tiles of tokens
-    int64_t tiles, piece_tiles, slices;   // of 256 columns: all, of a piece; slices of a piece that dh is summed over
+    int64_t width;           // columns of a tile of logits
+    int64_t piece;           // columns of a piece
+    int64_t dh_rows, slices; // tokens of a tile of dh; slices of a piece that it is summed over
     size_t stats, running, rescale, target_logit, of_rows, e, sums, h_live;   // offsets in the workspace
     size_t bytes;
 };

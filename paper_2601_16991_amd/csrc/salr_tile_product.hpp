@@ -3,8 +3,8 @@
 //   C[m][n] = sum_k P(m, k) Q(n, k)
 //
 // An operand lies in memory along k (P[m][k]: "rows" layout) or across it (P[k][m]: "columns" layout, transposed on its way from
-// LDS to registers by ds_read_b64_tr_b16).  Workgroup: kWM x kWN waves, wave tile 16 kMI (m) x 16 kNI (n), tile of n always 256
-// wide, steps of 64 along k.  Loads go straight to LDS (16 bytes a lane), each operand into a ring of its own; nothing is read past an
+// LDS to registers by ds_read_b64_tr_b16).  Workgroup: kWM x kWN waves, wave tile 16 kMI (m) x 16 kNI (n), steps of
+// 64 along k.  Loads go straight to LDS (16 bytes a lane), each operand into a ring of its own; nothing is read past an
 // operand's end: rows, columns and steps that are not there come out of the buffer load as zeros.
 //
 // LDS of one step.  Rows layout: [rows][64] with rows of 128 bytes, 16-byte piece c of row r at c ^ rows_swizzle(r).  Columns layout:
@@ -133,7 +133,7 @@ struct TilePlace {
 };
 inline unsigned product_grid(int64_t workgroups) { return (unsigned)((workgroups + kProductXcds - 1) / kProductXcds * kProductXcds); }
 
-// Shape of a workgroup's tile: 16 kMI kWM x 16 kNI kWN (256); steps of either operand that LDS holds.
+// Shape of a workgroup's tile: 16 kMI kWM (m) x 16 kNI kWN (n); steps of either operand that LDS holds.
 template <int kMI_, int kNI_, int kWM_, int kWN_, int kPSlots_, int kQSlots_>
 struct TileShape {
     static constexpr int kMI = kMI_, kNI = kNI_, kWM = kWM_, kWN = kWN_, kPSlots = kPSlots_, kQSlots = kQSlots_;
@@ -142,8 +142,8 @@ struct TileShape {
     static constexpr int kPBytes = kM * 2 * kProductStep, kQBytes = kN * 2 * kProductStep;
     static constexpr int kLdsBytes = kPSlots * kPBytes + kQSlots * kQBytes;
     static constexpr bool kInPlace = kMI * kNI * 4 > 128;
-    static_assert(kN == 256, "tile of n");
     static_assert(kPSlots >= 2 && (kQSlots == kPSlots || kQSlots == 3), "see tile_product");
+    static_assert(kN / 8 >= kWaves, "every wave has loads of Q");
 };
 
 // The k loop over steps [begin, end) of both sources; acc[i][j] += ... .  On return every wave has read its last operands and no load is
@@ -154,10 +154,10 @@ struct TileShape {
 // Requests are spread over the products, because a burst of them holds the waves up (4 to 6 % of a call): P's into the slot just left, in
 // the second half; Q's, where it has a slot more, in the first half of the next step.
 template <class Shape, bool kPColumns, bool kQColumns>
-__device__ __forceinline__ void tile_product(const TileSource<kPColumns, Shape::kM, Shape::kWaves>& ps, const TileSource<kQColumns, 256, Shape::kWaves>& qs,
+__device__ __forceinline__ void tile_product(const TileSource<kPColumns, Shape::kM, Shape::kWaves>& ps, const TileSource<kQColumns, Shape::kN, Shape::kWaves>& qs,
                                              int begin, int end, char* lds, f32x4 (&acc)[Shape::kMI][Shape::kNI]) {
     typedef TileSource<kPColumns, Shape::kM, Shape::kWaves> PSource;
-    typedef TileSource<kQColumns, 256, Shape::kWaves> QSource;
+    typedef TileSource<kQColumns, Shape::kN, Shape::kWaves> QSource;
     constexpr int SP = Shape::kPSlots, SQ = Shape::kQSlots, kMI = Shape::kMI, kNI = Shape::kNI, kLoads = PSource::kLoads + QSource::kLoads;
     // loads that every wave makes in a step (a wave that has one more waits for it earlier than it has to)
     constexpr int kSure = QSource::kLoads + (PSource::kAllWaves ? PSource::kLoads : 0);
