@@ -12,7 +12,8 @@
 // The column of the target is left out of E and of the sum S' and joins at the end, dh = grad (E w - S' w_target) / (S' + e_target):
 // a token that is predicted well has 1 - p_target = S' / S to full precision, not the difference of rounded numbers.
 //
-// With dw G is needed itself, so the statistics come first (a third product, on the logits) and the pieces hold G.
+// With dw G is needed itself.  Where E of the whole vocabulary in fp32 is no more than a piece may take, G is made from that; else the statistics
+// come first (a product more, on the logits) and the pieces hold G.
 //
 // Sums and statistics are fp32; E and G are rounded once to bf16, as operands of the matrix cores.
 // A masked token (target < 0) has loss 0 and gradient 0 whatever its hidden state holds.
@@ -25,7 +26,7 @@ namespace salr {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
-enum CeMode { kStatistics, kExponentials, kGradients };
+enum CeMode { kStatistics, kExponentials, kExponentials32, kGradients };   // what a tile of logits becomes: nothing but its statistics, E in bf16 or fp32, G
 
 struct CeRow {   // of a token, once its statistics are complete
     float M, alpha, beta;   // G = alpha 2^(l log2 e - M), of the target's column -beta
@@ -48,10 +49,11 @@ template <class Shape, int kMode>
 __global__ __launch_bounds__(Shape::kThreads) void ce_logits_kernel(const uint16_t* __restrict__ h, int64_t T, int64_t K, const uint16_t* __restrict__ w,
                                                         int64_t columns, int64_t first, const int64_t* __restrict__ targets, int m_tiles, int n_tiles,
                                                         float2* __restrict__ stats, float* __restrict__ target_logit, const CeRow* __restrict__ rows,
-                                                        uint16_t* __restrict__ out, int64_t pitch) {
+                                                        void* __restrict__ out, int64_t pitch) {
     constexpr int kMI = Shape::kMI, kNI = Shape::kNI, kWN = Shape::kWN, kM = Shape::kM, kN = Shape::kN;
     constexpr int kOutPitch = 2 * kN + 16;   // bytes of a row of E in LDS
-    constexpr int kTile = kMode == kStatistics ? 0 : kM * kOutPitch;
+    constexpr bool kBf16 = kMode == kExponentials || kMode == kGradients;
+    constexpr int kTile = kBf16 ? kM * kOutPitch : 0;
     constexpr int kEnd = kTile + 2 * kWN * kM * 4;
     __shared__ __attribute__((aligned(16))) char lds[kEnd > Shape::kLdsBytes ? kEnd : Shape::kLdsBytes];
     const TilePlace at(m_tiles, n_tiles, 1);
@@ -154,7 +156,10 @@ __global__ __launch_bounds__(Shape::kThreads) void ce_logits_kernel(const uint16
                 }
             }
             sum += (e[0] + e[1]) + (e[2] + e[3]);
-            if constexpr (kMode != kStatistics)
+            if constexpr (kMode == kExponentials32) {
+                if (m0 + row < T) *reinterpret_cast<float4*>(static_cast<float*>(out) + (m0 + row) * pitch + n0 + first_n + 16 * j) = make_float4(e[0], e[1], e[2], e[3]);
+            }
+            if constexpr (kBf16)
                 *reinterpret_cast<uint2*>(lds + row * kOutPitch + 32 * (wn * kNI + j) + 8 * g) = make_uint2(pack_two_bf16(e[0], e[1]), pack_two_bf16(e[2], e[3]));
         }
         if constexpr (kMode != kGradients) {
@@ -176,12 +181,12 @@ __global__ __launch_bounds__(Shape::kThreads) void ce_logits_kernel(const uint16
             stats[(int64_t)at.nt * T + m0 + row] = make_float2(tile_exponent(most), sum);
         }
     }
-    if constexpr (kMode != kStatistics) {
+    if constexpr (kBf16) {
         constexpr int kVecs = kN / 8, kRowsAtOnce = Shape::kThreads / kVecs;   // 16 bytes a lane
         const int vec = threadIdx.x % kVecs;
         for (int row = threadIdx.x / kVecs; row < kM; row += kRowsAtOnce) {
             if (m0 + row >= T) break;
-            *reinterpret_cast<uint4*>(out + (m0 + row) * pitch + n0 + 8 * vec) = *reinterpret_cast<const uint4*>(lds + row * kOutPitch + 16 * vec);
+            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + (m0 + row) * pitch + n0 + 8 * vec) = *reinterpret_cast<const uint4*>(lds + row * kOutPitch + 16 * vec);
         }
     }
 }
@@ -289,6 +294,24 @@ __global__ __launch_bounds__(1024) void ce_rows_kernel(CeRowArgs a) {
     a.loss[t] = loss;
     a.lse[t] = lse;
     if (a.rows != nullptr) a.rows[t] = CeRow{M, alpha, beta, target >= 0};
+}
+
+// G from E in fp32 and the tiles' references, eight columns a thread, up to a whole step of columns.
+__global__ __launch_bounds__(256) void ce_gradients_kernel(const float* __restrict__ e, int64_t T, int64_t columns, int64_t pitch, const float2* __restrict__ stats,
+                                                           int width, const CeRow* __restrict__ rows, const int64_t* __restrict__ targets,
+                                                           uint16_t* __restrict__ out) {
+    const int64_t n = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 8, t = blockIdx.x;
+    if (n >= (columns + kProductStep - 1) / kProductStep * kProductStep) return;
+    const CeRow of = rows[t];
+    const int64_t target = targets[t];
+    const float4* from = reinterpret_cast<const float4*>(e + t * pitch + n);
+    const float4 a = from[0], b = from[1];
+    const float M = stats[n / width * T + t].x, factor = M == -__builtin_inff() ? 0.f : of.alpha * __builtin_amdgcn_exp2f(M - of.M);
+    float x[8] = {a.x * factor, a.y * factor, a.z * factor, a.w * factor, b.x * factor, b.y * factor, b.z * factor, b.w * factor};
+#pragma unroll
+    for (int c = 0; c < 8; ++c) x[c] = n + c == target ? -of.beta : x[c];
+    const uint4 q = make_uint4(pack_two_bf16(x[0], x[1]), pack_two_bf16(x[2], x[3]), pack_two_bf16(x[4], x[5]), pack_two_bf16(x[6], x[7]));
+    *reinterpret_cast<uint4*>(out + t * pitch + n) = of.live ? q : make_uint4(0, 0, 0, 0);
 }
 
 // sums = rescale sums + E w over the columns of a piece (contracted), slice kz of them.  `rescale` null: ones.
@@ -469,6 +492,9 @@ CePlan ce_plan(int64_t T, int64_t K, int64_t V, bool want_dh, bool want_dw) {
     p.target_logit = take((size_t)T * 4);
     p.of_rows = take((size_t)T * sizeof(CeRow));
     if (pieces) p.e = take((size_t)T * p.piece * 2);
+    // with dw: E in fp32 where that is no more than a piece may take
+    p.holds_e32 = want_dw && p.piece == all && T * all * 4 <= kCePieceBytes;
+    if (p.holds_e32) p.e32 = take((size_t)T * p.piece * 4);
     if (want_dh) p.sums = take((size_t)p.slices * T * K * 4);
     if (want_dw) p.h_live = take((size_t)T * K * 2);
     p.bytes = at;
@@ -489,7 +515,7 @@ struct CeRun {   // one call
         const int64_t tiles = (columns + Shape::kN - 1) / Shape::kN;
         hipLaunchKernelGGL((ce_logits_kernel<Shape, kMode>), dim3(product_grid(p.m_tiles * tiles)), dim3(Shape::kThreads), 0, a.stream, a.h, a.T, a.K,
                            a.w + first * a.K, columns, first, a.targets, (int)p.m_tiles, (int)tiles, at<float2>(p.stats), at<float>(p.target_logit),
-                           at<const CeRow>(p.of_rows), at<uint16_t>(p.e), p.piece);
+                           at<const CeRow>(p.of_rows), kMode == kExponentials32 ? at<void>(p.e32) : at<void>(p.e), p.piece);
     }
     template <int kMode>
     void logits(int64_t first, int64_t columns) const {
@@ -541,6 +567,11 @@ struct CeRun {   // one call
         hipLaunchKernelGGL(ce_dh_finish_kernel<kPlain>, dim3(units()), dim3(256), 0, a.stream, at<const float>(p.sums), (int)p.slices, a.T, a.K,
                            at<const CeRow>(p.of_rows), a.targets, a.V, a.w, a.dh);
     }
+    void gradients() const {
+        const unsigned across = (unsigned)ceil_div(a.V, 2048);
+        hipLaunchKernelGGL(ce_gradients_kernel, dim3((unsigned)a.T, across), dim3(256), 0, a.stream, at<const float>(p.e32), a.T, a.V, p.piece, at<const float2>(p.stats),
+                           (int)p.width, at<const CeRow>(p.of_rows), a.targets, at<uint16_t>(p.e));
+    }
     void live_rows() const {
         if (units() == 0) return;
         hipLaunchKernelGGL(ce_live_rows_kernel, dim3(units()), dim3(256), 0, a.stream, a.h, a.targets, a.T, a.K, at<uint16_t>(p.h_live));
@@ -564,7 +595,7 @@ hipError_t launch_cross_entropy(const CeArgs& a, void* workspace) {
     }
     const bool one_pass = a.dh != nullptr && a.dw == nullptr;   // on E; else the statistics come first, and pieces of G where they are wanted
     if (!one_pass) {
-        run.logits<kStatistics>(0, a.V);
+        p.holds_e32 ? run.logits<kExponentials32>(0, a.V) : run.logits<kStatistics>(0, a.V);
         run.rows(a.V, true, true, false);
         if (a.dw == nullptr) return hipGetLastError();
         run.live_rows();
@@ -574,6 +605,8 @@ hipError_t launch_cross_entropy(const CeArgs& a, void* workspace) {
         if (one_pass) {
             run.logits<kExponentials>(first, columns);
             run.rows(columns, first == 0, first + columns == a.V, true);
+        } else if (p.holds_e32) {
+            run.gradients();
         } else {
             run.logits<kGradients>(first, columns);
         }

@@ -855,7 +855,8 @@ struct CePlan {
     int64_t width;           // columns of a tile of logits
     int64_t piece;           // columns of a piece
     int64_t dh_rows, slices; // tokens of a tile of dh; slices of a piece that it is summed over
-    size_t stats, running, rescale, target_logit, of_rows, e, sums, h_live;   // offsets in the workspace
+    bool holds_e32;          // with dw: E of the whole vocabulary in fp32
+    size_t stats, running, rescale, target_logit, of_rows, e, e32, sums, h_live;   // offsets in the workspace
     size_t bytes;
 };
 CePlan ce_plan(int64_t T, int64_t K, int64_t V, bool want_dh, bool want_dw);
