@@ -44,6 +44,9 @@ __device__ __forceinline__ uint32_t pack_two_bf16(float a, float b) {
 constexpr float kReferenceStep = 128.f;
 __device__ __forceinline__ float tile_exponent(float most) { return kReferenceStep * rintf(most * (kLog2e / kReferenceStep)); }
 
+// x 2^by for a whole `by` that may be -infinity; 2^-128 is no normal number, so not by multiplying.
+__device__ __forceinline__ float times_power(float x, float by) { return __builtin_amdgcn_ldexpf(x, (int)fminf(fmaxf(by, -1000.f), 1000.f)); }
+
 // l = h w^T of one tile and what becomes of it.  `w`: the piece's first row, `columns` of it exist; `pitch`: of `out` [T][pitch].
 template <class Shape, int kMode>
 __global__ __launch_bounds__(Shape::kThreads) void ce_logits_kernel(const uint16_t* __restrict__ h, int64_t T, int64_t K, const uint16_t* __restrict__ w,
@@ -196,7 +199,7 @@ struct CeRowArgs {
     int n_tiles;
     bool first, last;          // piece of the vocabulary
     float2* running;           // [T]: M and sum so far
-    float* rescale;            // [T]: 2^(M before - M now)
+    float* rescale;            // [T]: M before - M now
     uint16_t* e;               // E of the piece, brought to M now where a tile's M is another; null: there is none
     int64_t pitch;
     int width;                 // columns of a tile: 64, 128 or 256
@@ -214,7 +217,7 @@ struct CeSum {
     float M, sum, least;   // least: smallest reference of a tile that has one
     __device__ __forceinline__ void add(float M2, float sum2, float least2) {
         const float top = fmaxf(M, M2), M_ref = top == -__builtin_inff() ? 0.f : top;
-        sum = sum * __builtin_amdgcn_exp2f(M - M_ref) + sum2 * __builtin_amdgcn_exp2f(M2 - M_ref);
+        sum = times_power(sum, M - M_ref) + times_power(sum2, M2 - M_ref);
         M = top;
         least = fminf(least, least2);
     }
@@ -250,30 +253,40 @@ __global__ __launch_bounds__(1024) void ce_rows_kernel(CeRowArgs a) {
     const float M = all.M == -inf ? 0.f : all.M, sum = all.sum;
     if (a.e != nullptr && __any(here && all.least < M)) {
         // The exponents of E in tiles with a reference below the row's, lowered by the difference: exact.  The wave goes through such tiles
-        // one by one, its lanes through the columns.
+        // four at a time, its lanes through the columns.
         for (int n0 = 0; n0 < a.n_tiles; n0 += kParts) {
             const int n = n0 + first_tile;
             const float behind = here && n < a.n_tiles ? M - a.stats[(int64_t)n * a.T + t].x : 0.f;
             uint64_t todo = __ballot(behind > 0.f && behind < inf);
             while (todo != 0) {
-                const int of = __ffsll((unsigned long long)todo) - 1;
-                todo &= todo - 1;
-                const int64_t at_row = (int64_t)blockIdx.x * kRows + (wave * 64 + of) % kRows, at_tile = n0 + (wave * 64 + of) / kRows;
-                const bool gone = __shfl(behind, of) > kReferenceStep;
-                if (4 * lane >= a.width) continue;
-                uint2* at = reinterpret_cast<uint2*>(a.e + at_row * a.pitch + at_tile * a.width) + lane;
-                const uint16_t step = (uint16_t)((int)kReferenceStep << 7);
-                const u16x2 by = gone ? u16x2{0xFFFF, 0xFFFF} : u16x2{step, step};
-                uint2 q = *at;
-                q.x = __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, q.x), by));
-                q.y = __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, q.y), by));
-                *at = q;
+                uint2* at[4] = {};
+                uint2 q[4];
+                uint32_t by[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int of = __ffsll((unsigned long long)todo) - 1;   // the same in all lanes; -1: no more
+                    if (of < 0) break;
+                    todo &= todo - 1;
+                    const int64_t at_row = (int64_t)blockIdx.x * kRows + (wave * 64 + of) % kRows, at_tile = n0 + (wave * 64 + of) / kRows;
+                    by[u] = __shfl(behind, of) > kReferenceStep ? 0xFFFFFFFFu : ((uint32_t)(int)kReferenceStep << 7) * 0x00010001u;
+                    if (4 * lane >= a.width) continue;
+                    at[u] = reinterpret_cast<uint2*>(a.e + at_row * a.pitch + at_tile * a.width) + lane;
+                    q[u] = *at[u];
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    if (at[u] == nullptr) continue;
+                    const u16x2 lower = __builtin_bit_cast(u16x2, by[u]);
+                    q[u].x = __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, q[u].x), lower));
+                    q[u].y = __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, q[u].y), lower));
+                    *at[u] = q[u];
+                }
             }
         }
     }
     if (threadIdx.x >= kRows || !here) return;
     a.running[t] = make_float2(all.M, sum);
-    a.rescale[t] = __builtin_amdgcn_exp2f(before.x - M);
+    a.rescale[t] = before.x - M;
     if (!a.last) return;
     // S' = sum of 2^(l log2 e - M) over the other columns, e the target's (M may lie below the target's own exponent)
     const int64_t target = a.targets[t];
@@ -282,14 +295,15 @@ __global__ __launch_bounds__(1024) void ce_rows_kernel(CeRowArgs a) {
     if (target >= a.V) {
         loss = lse = alpha = beta = nan;
     } else if (target >= 0) {
-        const float l = a.target_logit[t], up = fmaf(l, kLog2e, -M), top = up > 0.f ? ceilf(up) : 0.f;
-        const float e = __builtin_amdgcn_exp2f(up - top), lower = __builtin_amdgcn_exp2f(-top), rest = sum * lower, all = rest + e;
+        const float l = a.target_logit[t], up = fmaf(l, kLog2e, -M), top = up > 0.f || all.M == -inf ? ceilf(up) : 0.f;
+        const float e = __builtin_amdgcn_exp2f(up - top), rest = times_power(sum, -top), total = rest + e;
         const float gl = a.grad_loss != nullptr ? a.grad_loss[t] : 1.f;
-        lse = kLn2 * (M + top) + logf(all);
-        loss = e > 1e-30f ? log1pf(rest / e) : lse - l;
-        alpha = gl * lower / all;
-        beta = gl * (rest / all);
-        if (!(all > 0.f && all < inf)) loss = lse = alpha = beta = nan;
+        lse = kLn2 * (M + top) + logf(total);
+        const float ratio = rest / e;   // (where the target is far below the others it leaves fp32)
+        loss = ratio < 1e6f ? log1pf(ratio) : lse - l;
+        alpha = sum == 0.f ? 0.f : times_power(gl / total, -top);
+        beta = gl * (rest / total);
+        if (!(total > 0.f && total < inf)) loss = lse = alpha = beta = nan;
     }
     a.loss[t] = loss;
     a.lse[t] = lse;
@@ -306,15 +320,15 @@ __global__ __launch_bounds__(256) void ce_gradients_kernel(const float* __restri
     const int64_t target = targets[t];
     const float4* from = reinterpret_cast<const float4*>(e + t * pitch + n);
     const float4 a = from[0], b = from[1];
-    const float M = stats[n / width * T + t].x, factor = M == -__builtin_inff() ? 0.f : of.alpha * __builtin_amdgcn_exp2f(M - of.M);
-    float x[8] = {a.x * factor, a.y * factor, a.z * factor, a.w * factor, b.x * factor, b.y * factor, b.z * factor, b.w * factor};
+    const float by = stats[n / width * T + t].x - of.M;
+    float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-    for (int c = 0; c < 8; ++c) x[c] = n + c == target ? -of.beta : x[c];
+    for (int c = 0; c < 8; ++c) x[c] = n + c == target ? -of.beta : of.alpha * times_power(x[c], by);
     const uint4 q = make_uint4(pack_two_bf16(x[0], x[1]), pack_two_bf16(x[2], x[3]), pack_two_bf16(x[4], x[5]), pack_two_bf16(x[6], x[7]));
     *reinterpret_cast<uint4*>(out + t * pitch + n) = of.live ? q : make_uint4(0, 0, 0, 0);
 }
 
-// sums = rescale sums + E w over the columns of a piece (contracted), slice kz of them.  `rescale` null: ones.
+// sums = 2^rescale sums + E w over the columns of a piece (contracted), slice kz of them.  `rescale` null: zeros.
 template <class Shape>
 __global__ __launch_bounds__(Shape::kThreads) void ce_dh_kernel(const uint16_t* __restrict__ e, int64_t T, int64_t pitch, const uint16_t* __restrict__ w,
                                                     int64_t columns, int64_t K, int m_tiles, int n_tiles, int slices, const float* __restrict__ rescale,
@@ -331,12 +345,16 @@ __global__ __launch_bounds__(Shape::kThreads) void ce_dh_kernel(const uint16_t* 
 #pragma unroll
     for (int i = 0; i < kMI; ++i) {
         const int64_t m = m0 + 16 * (wm * kMI + i) + i16;
-        const float scale = !first && m < T && rescale != nullptr ? rescale[m] : 1.f;
+        const float by = !first && m < T && rescale != nullptr ? rescale[m] : 0.f;
 #pragma unroll
         for (int j = 0; j < kNI; ++j) {
             const int64_t n = n0 + 16 * (wn * kNI + j) + 4 * g;
             f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
-            if (!first && m < T && n < K) v = *reinterpret_cast<const f32x4*>(sums + ((int64_t)at.kz * T + m) * K + n) * scale;
+            if (!first && m < T && n < K) {
+                v = *reinterpret_cast<const f32x4*>(sums + ((int64_t)at.kz * T + m) * K + n);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[r] = times_power(v[r], by);
+            }
             acc[i][j] = v;
         }
     }
@@ -537,9 +555,10 @@ struct CeRun {   // one call
         r.e = with_e ? at<uint16_t>(p.e) : nullptr, r.pitch = p.piece, r.width = (int)p.width;
         r.target_logit = at<const float>(p.target_logit), r.targets = a.targets, r.grad_loss = a.grad_loss;
         r.T = a.T, r.V = a.V, r.loss = a.loss, r.lse = a.lse, r.rows = at<CeRow>(p.of_rows);
-        if (a.T <= 4) hipLaunchKernelGGL(ce_rows_kernel<4>, dim3(1), dim3(1024), 0, a.stream, r);
-        else if (a.T <= 512) hipLaunchKernelGGL(ce_rows_kernel<16>, dim3((unsigned)((a.T + 15) / 16)), dim3(1024), 0, a.stream, r);
-        else hipLaunchKernelGGL(ce_rows_kernel<64>, dim3((unsigned)((a.T + 63) / 64)), dim3(1024), 0, a.stream, r);
+        // fewer rows a workgroup where there are few: a thread's chain over the tiles stays short
+        if (a.T <= 256) hipLaunchKernelGGL(ce_rows_kernel<4>, dim3((unsigned)ceil_div(a.T, 4)), dim3(1024), 0, a.stream, r);
+        else if (a.T <= 4096) hipLaunchKernelGGL(ce_rows_kernel<16>, dim3((unsigned)ceil_div(a.T, 16)), dim3(1024), 0, a.stream, r);
+        else hipLaunchKernelGGL(ce_rows_kernel<64>, dim3((unsigned)ceil_div(a.T, 64)), dim3(1024), 0, a.stream, r);
     }
     int n_tiles() const { return (int)((a.K + 255) / 256); }
     unsigned units() const { return (unsigned)((a.T * (a.K / 8) + 255) / 256); }   // workgroups with eight columns of a row a thread

@@ -117,6 +117,40 @@ def test_logits_far_from_zero(shift):
     _check(h, w, t, g, _run(h, w, t, g, True, True), True, True)
 
 
+@pytest.mark.parametrize("logit", [-500.0, -90.0, 0.0, 90.0, 500.0, 2.0 ** 20])
+def test_a_vocabulary_of_one_word(logit):
+    T, K = 20, 8
+    h, w = torch.zeros(T, K).bfloat16(), torch.zeros(1, K).bfloat16()
+    h[:, 0], w[:, 0] = 1.0, logit
+    t, g = torch.zeros(T, dtype=torch.int64), torch.ones(T)
+    _check(h, w, t, g, _run(h, w, t, g, True, False), True, False)
+    _check(h, w, t, g, _run(h, w, t, g, True, True), True, True)
+
+
+@pytest.mark.parametrize("need_dw", [False, True])
+@pytest.mark.parametrize("low,high", [(-62.0, 44.0), (-300.0, 44.0), (-44.0, 100.0), (-1000.0, 1000.0), (-46.0, -43.0), (43.0, 46.0)])
+def test_logits_of_a_row_far_apart(low, high, need_dw):
+    """Every fifth word at `high`, the others at `low`, in whole tiles and within them; targets of both kinds."""
+    T, K, V = 40, 64, 1300
+    h, w, t, g = _inputs(T, K, V, 21, masked=False, std_w=0.01, sure=0.0)
+    v = torch.arange(V)
+    top = torch.where(v < 700, v // 64 % 5 == 1, v % 5 == 1)
+    h[:, 0] = 1.0
+    w[:, 0] = torch.where(top, high, low).bfloat16()
+    t[: T // 2] = torch.nonzero(top)[: T // 2, 0]
+    _check(h, w, t, g, _run(h, w, t, g, True, need_dw), True, need_dw)
+
+
+def test_many_rows_with_references_of_two_kinds():
+    """Tokens of which each has one tile far above the others: every E of the rest is brought in line."""
+    T, K, V = 300, 64, 5000
+    h, w, t, g = _inputs(T, K, V, 22, masked=False, std_w=0.05, sure=0.0)
+    w[2000:2100, 0] = 60.0
+    h[:, 0] = 1.0
+    h[::3, 0] = 0.25
+    _check(h, w, t, g, _run(h, w, t, g, True, False), True, False)
+
+
 def test_well_predicted_tokens_keep_their_gradient():
     """1 - p of 1e-9 and less: the gradient is that small and right to bf16, not the difference of rounded probabilities."""
     T, K, V = 64, 128, 2000
