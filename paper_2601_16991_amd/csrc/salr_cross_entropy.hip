@@ -448,6 +448,7 @@ typedef TileShape<4, 4, 2, 4, 3, 3> Shape128;
 typedef TileShape<4, 2, 1, 8, 2, 2> Shape64;
 typedef TileShape<2, 2, 1, 8, 2, 2> Shape32;
 typedef TileShape<1, 2, 1, 8, 2, 2> Shape16;
+typedef TileShape<4, 1, 2, 4, 3, 3> Narrow128;
 typedef TileShape<4, 1, 1, 4, 4, 4> Narrow64;
 typedef TileShape<2, 1, 1, 4, 4, 4> Narrow32;
 typedef TileShape<1, 1, 1, 4, 4, 4> Narrow16;
@@ -480,8 +481,9 @@ CePlan ce_plan(int64_t T, int64_t K, int64_t V, bool want_dh, bool want_dw) {
     p.rows = few;
     if (T > 128 && tile_rounds(ceil_div(T, 256) * tiles) <= kHalfTile * tile_rounds(ceil_div(T, 128) * tiles)) p.rows = 256;
     p.m_tiles = ceil_div(T, p.rows);
-    // columns of a tile: 64 where wide ones are too few to go round (24 x 8192 x 32000: 104 us against 165)
-    p.width = few <= 64 && tiles < 384 ? 64 : 256;
+    // columns of a tile: 64 where wide ones are too few to go round.  A CU draws about 45 GB/s from memory, so more of them count even where each
+    // reads the tokens again (24 x 8192 x 32000: 104 us against 165; 256 x 4096 x 8192 35 against 48, but 512 x 4096 x 8192 53 against 53)
+    p.width = few <= 64 ? (tiles < 384 ? 64 : 256) : p.rows == 128 && p.m_tiles * tiles <= 96 ? 64 : 256;
     p.dh_rows = few, p.slices = 1;
     if (want_dh) {
         const int64_t n_tiles = ceil_div(K, 256), steps = p.piece / kProductStep;
@@ -542,7 +544,7 @@ struct CeRun {   // one call
             case 16: return narrow ? logits_on<Narrow16, kMode>(first, columns) : logits_on<Shape16, kMode>(first, columns);
             case 32: return narrow ? logits_on<Narrow32, kMode>(first, columns) : logits_on<Shape32, kMode>(first, columns);
             case 64: return narrow ? logits_on<Narrow64, kMode>(first, columns) : logits_on<Shape64, kMode>(first, columns);
-            case 128: return logits_on<Shape128, kMode>(first, columns);
+            case 128: return narrow ? logits_on<Narrow128, kMode>(first, columns) : logits_on<Shape128, kMode>(first, columns);
             default: return logits_on<Shape256, kMode>(first, columns);
         }
     }
