@@ -487,8 +487,8 @@ CePlan ce_plan(int64_t T, int64_t K, int64_t V, bool want_dh, bool want_dw) {
     p.dh_rows = few, p.slices = 1;
     if (want_dh) {
         const int64_t n_tiles = ceil_div(K, 256), steps = p.piece / kProductStep;
-        if (few <= 64) {   // bound by memory: two workgroups to a CU
-            while (n_tiles * p.slices < 384 && p.slices * 4 <= steps && p.slices < 64) p.slices *= 2;
+        if (few <= 64) {   // bound by memory: two workgroups to a CU, four steps at least
+            while (n_tiles * p.slices < 384 && p.slices * 8 <= steps && p.slices < 64) p.slices *= 2;
         } else {
             // a slice more costs a pass over [T, K] in fp32, there and back
             double best = 0.0;
