@@ -637,67 +637,16 @@ def linear_cross_entropy(h, w, targets, grad_loss=None, need_dh=True, need_dw=Fa
     return _native().linear_cross_entropy(h, w, targets, grad_loss, need_dh, need_dw, workspace)
 
 
-_TYPE_CODES = {torch.float32: 0, torch.bfloat16: 1}   # salr_type_t
-_STATE_BITS = {torch.float32: 32, torch.float8_e4m3fn: 8}
 STEP_BLOCK = 128                                      # elements that share two scales of 8-bit states
 GRAD_NORM_WORKSPACE_BYTES = 8192                      # SALR_GRAD_NORM_WORKSPACE_BYTES of include/salr.h
 
 
-def _same_type(tensors, name: str, kinds):
-    types = {t.dtype for t in tensors}
-    if len(types) > 1 or not types <= set(kinds):
-        raise TypeError(f"{name}: dtypes {sorted(map(str, types))}, expected one of {sorted(map(str, kinds))}")
-    return types.pop() if types else next(iter(kinds))
-
-
 class _StepList:
-    """The tensors of a step as salr_step_plan lays them out: written once, copied to the device, read by every call."""
+    """The tensors of a step as salr_step_plan lays them out: checked and written once, copied to the device, read by every call."""
 
     def __init__(self, grads, params=None, copies=None, exp_avg=None, exp_avg_sq=None, scales=None):
-        grads = list(grads)
-        lists = [None if x is None else list(x) for x in (params, copies, exp_avg, exp_avg_sq, scales)]
-        params, copies, exp_avg, exp_avg_sq, scales = lists
-        if not grads:
-            raise ValueError("no tensors")
-        if any(x is not None and len(x) != len(grads) for x in lists):
-            raise ValueError("lists of different lengths")
-        self._keep = (grads, *lists)
-        self.grad_type = _TYPE_CODES[_same_type(grads, "grads", _TYPE_CODES)]
-        self.param_type, self.state_bits = 0, 0
-        if params is not None:
-            self.param_type = _TYPE_CODES[_same_type(params, "params", _TYPE_CODES)]
-            state = _same_type(exp_avg, "exp_avg", _STATE_BITS)
-            _same_type(exp_avg_sq, "exp_avg_sq", {state: 0})
-            self.state_bits = _STATE_BITS[state]
-            if (scales is not None) != (self.state_bits == 8):
-                raise ValueError("scales go with states in 8 bits")
-        table = (StepTensor * len(grads))()
-        device = grads[0].device
-        for i, g in enumerate(grads):
-            n = g.numel()
-            entry = {"grad": (g, tuple(_TYPE_CODES), n)}
-            if params is not None:
-                entry.update(param=(params[i], tuple(_TYPE_CODES), n), exp_avg=(exp_avg[i], tuple(_STATE_BITS), n),
-                             exp_avg_sq=(exp_avg_sq[i], tuple(_STATE_BITS), n))
-                if copies is not None and copies[i] is not None:
-                    entry["copy"] = (copies[i], (torch.bfloat16,), n)
-                if scales is not None:
-                    entry["scales"] = (scales[i], (torch.float32,), 2 * ((n + STEP_BLOCK - 1) // STEP_BLOCK))
-            for name, (t, kinds, size) in entry.items():
-                if t.numel() != size:
-                    raise ValueError(f"{name} {i}: {t.numel()} elements, expected {size}")
-                setattr(table[i], name, _ptr(t, kinds, name))
-                if t.device != device:
-                    raise ValueError("tensors on different devices")
-            table[i].count = n
-        counts = (_i64 * len(grads))(*[t.count for t in table])
-        need = int(lib().salr_step_plan_bytes(counts, len(grads)))
-        host = torch.empty(max(need, 64), dtype=torch.uint8)
-        chunks = _i64()
-        _check(lib().salr_step_plan(table, len(grads), self.param_type, self.grad_type, self.state_bits, host.data_ptr(), host.numel(),
-                                    ctypes.byref(chunks)), "salr_step_plan")
-        self.chunks = chunks.value
-        self.plan = host.to(device)
+        self._keep = (grads, params, copies, exp_avg, exp_avg_sq, scales)
+        self.plan, self.chunks, self.param_type, self.grad_type, self.state_bits = _native().step_list(*self._keep)
 
 
 class GradNorm:
@@ -706,7 +655,7 @@ class GradNorm:
     calls that overlap on different streams need a ``GradNorm`` each."""
 
     def __init__(self, grads, _list=None):
-        self._list = _list or _StepList(grads)
+        self._list = _list or _StepList(list(grads))
         self._workspace = torch.zeros(GRAD_NORM_WORKSPACE_BYTES, dtype=torch.uint8, device=self._list.plan.device)
         self._call = _native().grad_norm
 
@@ -738,7 +687,8 @@ class AdamW:
     """
 
     def __init__(self, params, grads, exp_avg=None, exp_avg_sq=None, scales=None, copies=None, bits: int = 32):
-        params = list(params)
+        params, grads = list(params), list(grads)
+        exp_avg, exp_avg_sq, scales, copies = (None if x is None else list(x) for x in (exp_avg, exp_avg_sq, scales, copies))
         if (exp_avg is None) != (exp_avg_sq is None):
             raise ValueError("exp_avg and exp_avg_sq go together")
         if exp_avg is None:

@@ -7,9 +7,12 @@
 // launches.  Nothing here computes: a status other than SALR_OK comes back as the binding's SalrError.
 #include <ATen/hip/EmptyTensor.h>
 #include <ATen/ops/empty.h>
+#include <ATen/core/Tensor.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
+
+#include <vector>
 
 #include "salr.h"
 #include "salr_internal.hpp"   // the two halves of the encoder
@@ -486,6 +489,87 @@ PyObject* py_grad_norm(PyObject*, PyObject* const* v, Py_ssize_t n) {
     SALR_CATCH
 }
 
+// A sequence of tensors (or None for some of them); None itself: no sequence.
+struct TensorList {
+    PyObject* fast = nullptr;
+    Py_ssize_t size = 0;
+    TensorList(PyObject* o, const char* name) {
+        if (o == Py_None) return;
+        fast = PySequence_Fast(o, name);
+        if (!fast) throw PyFailure{};
+        size = PySequence_Fast_GET_SIZE(fast);
+    }
+    ~TensorList() { Py_XDECREF(fast); }
+    TensorList(const TensorList&) = delete;
+    TensorList& operator=(const TensorList&) = delete;
+    const at::Tensor& at(Py_ssize_t i, const char* name) const { return tensor_of(PySequence_Fast_GET_ITEM(fast, i), name); }
+};
+
+// step_list(grads, params, copies, exp_avg, exp_avg_sq, scales) -> (plan on the device, chunks, param_type, grad_type, state_bits)
+//   all but grads None: a list for the norm only
+PyObject* py_step_list(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    SALR_TRY
+    need_args(n, 6, "step_list");
+    static const char* const names[6] = {"grads", "params", "copies", "exp_avg", "exp_avg_sq", "scales"};
+    const TensorList grads(v[0], names[0]), params(v[1], names[1]), copies(v[2], names[2]), m(v[3], names[3]), sq(v[4], names[4]), scales(v[5], names[5]);
+    const Py_ssize_t count = grads.size;
+    if (count == 0) fail(PyExc_ValueError, "no %s", "tensors");
+    for (const TensorList* l : {&params, &copies, &m, &sq, &scales})
+        if (l->fast && l->size != count) fail(PyExc_ValueError, "lists of different %s", "lengths");
+    const bool step = params.fast != nullptr;
+    if (step && (!m.fast || !sq.fast)) fail(PyExc_TypeError, "%s and exp_avg_sq must be given", "exp_avg");
+    const at::Tensor& first = grads.at(0, "grad");
+    if (!first.defined()) fail(PyExc_TypeError, "%s must be a tensor", "grad");
+    const at::Device device = first.device();
+    const auto type_of = [](at::ScalarType t, const char* name) {
+        if (t != at::kFloat && t != at::kBFloat16) fail(PyExc_TypeError, "%s must be fp32 or bf16", name);
+        return t == at::kFloat ? SALR_F32 : SALR_BF16;
+    };
+    const at::ScalarType grad_type = first.scalar_type(), param_type = step ? params.at(0, "param").scalar_type() : at::kFloat;
+    const at::ScalarType state_type = step ? m.at(0, "exp_avg").scalar_type() : at::kFloat;
+    const salr_type_t gt = type_of(grad_type, "grads"), pt = type_of(param_type, "params");
+    if (state_type != at::kFloat && state_type != at::kFloat8_e4m3fn) fail(PyExc_TypeError, "%s must be fp32 or float8_e4m3fn", "exp_avg");
+    const int bits = !step ? 0 : state_type == at::kFloat ? 32 : 8;
+    if (step && (scales.fast != nullptr) != (bits == 8)) fail(PyExc_ValueError, "%s go with states in 8 bits", "scales");
+    const auto pointer = [&](const at::Tensor& t, at::ScalarType type, int64_t size, const char* name) -> void* {
+        if (!t.defined()) fail(PyExc_TypeError, "%s must be a tensor", name);
+        if (t.scalar_type() != type) fail(PyExc_TypeError, "%s: unexpected dtype", name);
+        if (!t.is_cuda()) fail(PyExc_TypeError, "%s must be a CUDA tensor", name);
+        if (!t.is_contiguous()) fail(PyExc_TypeError, "%s must be contiguous", name);
+        if (t.device() != device) fail(PyExc_ValueError, "%s: tensors on different devices", name);
+        if (t.numel() != size) fail(PyExc_ValueError, "%s: another number of elements than its gradient wants", name);
+        return t.data_ptr();
+    };
+    std::vector<salr_step_tensor_t> table((size_t)count);
+    std::vector<int64_t> counts((size_t)count);
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        salr_step_tensor_t& t = table[(size_t)i];
+        const at::Tensor& g = grads.at(i, "grad");
+        t = salr_step_tensor_t{};
+        t.count = counts[(size_t)i] = g.defined() ? g.numel() : 0;
+        t.grad = pointer(g, grad_type, t.count, "grad");
+        if (!step) continue;
+        t.param = pointer(params.at(i, "param"), param_type, t.count, "param");
+        t.exp_avg = pointer(m.at(i, "exp_avg"), state_type, t.count, "exp_avg");
+        t.exp_avg_sq = pointer(sq.at(i, "exp_avg_sq"), state_type, t.count, "exp_avg_sq");
+        if (copies.fast && copies.at(i, "copy").defined()) t.copy = static_cast<uint16_t*>(pointer(copies.at(i, "copy"), at::kBFloat16, t.count, "copy"));
+        if (scales.fast)
+            t.scales = static_cast<float*>(pointer(scales.at(i, "scales"), at::kFloat, 2 * ((t.count + salr::kStepBlock - 1) / salr::kStepBlock), "scales"));
+    }
+    const size_t need = salr_step_plan_bytes(counts.data(), count);
+    if (need == (size_t)-1) check(SALR_ERR_SHAPE, "salr_step_plan");
+    at::Tensor host = at::empty({(int64_t)(need < 64 ? 64 : need)}, at::TensorOptions().dtype(at::kByte));
+    int64_t chunks = 0;
+    check(salr_step_plan(table.data(), count, pt, gt, bits, host.data_ptr(), need, &chunks), "salr_step_plan");
+    at::Tensor plan;
+    {
+        Gil release;
+        plan = host.to(device);
+    }
+    return Py_BuildValue("NLiii", THPVariable_Wrap(std::move(plan)), (long long)chunks, (int)pt, (int)gt, bits);
+    SALR_CATCH
+}
+
 PyObject* py_set_error(PyObject*, PyObject* cls) {
     Py_XINCREF(cls);
     Py_XSETREF(g_salr_error, cls);
@@ -500,6 +584,7 @@ PyMethodDef kMethods[] = {
     SALR_FAST("mask", py_mask),
     SALR_FAST("decode", py_decode),
     SALR_FAST("linear_cross_entropy", py_linear_cross_entropy),
+    SALR_FAST("step_list", py_step_list),
     SALR_FAST("adamw_step", py_adamw_step),
     SALR_FAST("grad_norm", py_grad_norm),
     {"encode", py_encode, METH_O, nullptr},
