@@ -310,6 +310,25 @@ def test_offsets_past_32_bits():
     assert (dh.double() - dref).norm() < 5e-3 * dref.norm()
 
 
+def test_no_hidden_size():
+    """An empty contraction: all logits are 0."""
+    import paper_2601_16991_amd as salr
+    h, w = torch.empty(5, 0, dtype=torch.bfloat16, device=dev()), torch.empty(700, 0, dtype=torch.bfloat16, device=dev())
+    t = torch.tensor([0, 699, -1, 300, 700], device=dev())
+    loss, lse, dh, dw = salr.linear_cross_entropy(h, w, t, need_dw=True)
+    want = torch.log(torch.tensor(700.0)).item()
+    for x in (loss.cpu(), lse.cpu()):
+        assert torch.allclose(x[[0, 1, 3]], torch.full((3,), want), rtol=1e-6) and x[2] == 0 and torch.isnan(x[4])
+    assert dh.shape == (5, 0) and dw.shape == (700, 0)
+
+
+@pytest.mark.parametrize("need_dw", [False, True])
+def test_more_tokens_than_a_grid_dimension(need_dw):
+    T, K, V = 70001, 32, 300
+    h, w, t, g = _inputs(T, K, V, 17, std_w=0.3, sure=4.0)
+    _check(h, w, t, g, _run(h, w, t, g, True, need_dw), True, need_dw)
+
+
 def test_no_tokens():
     import paper_2601_16991_amd as salr
     h, w = torch.empty(0, 64, dtype=torch.bfloat16, device=dev()), torch.ones(300, 64, dtype=torch.bfloat16, device=dev())
