@@ -436,7 +436,7 @@ salr_status_t salr_concat_adapters(const uint16_t* const* a_list, const uint16_t
  *   dh         out  [T, K] bf16; NULL = not computed
  *   dw         out  [V, K] bf16; NULL = not computed (a frozen head)
  *   workspace  --   salr_linear_cross_entropy_workspace_bytes(T, K, V, want_dh, want_dw) bytes, 256-byte aligned; contents
- *                   unspecified.  It holds what the logits of a piece of the vocabulary become, up to 256 MiB (with dw up to 384 MiB), whatever V,
+ *                   unspecified.  It holds what the logits of a piece of the vocabulary become, up to 256 MiB (with dw up to 768 MiB), whatever V,
  *                   8 bytes per token and 256 (few tokens: 64) words of the vocabulary, and dh in fp32 (once or a few times)
  *
  * Precision: fp32 sums, maxima and logits; the probabilities are rounded to bf16 once, as operands of the matrix cores, and dh

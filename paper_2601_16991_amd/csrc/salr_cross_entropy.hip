@@ -12,8 +12,8 @@
 // The column of the target is left out of E and of the sum S' and joins at the end, dh = grad (E w - S' w_target) / (S' + e_target):
 // a token that is predicted well has 1 - p_target = S' / S to full precision, not the difference of rounded numbers.
 //
-// With dw G is needed itself.  Where E of the whole vocabulary in fp32 is no more than a piece may take, G is made from that; else the statistics
-// come first (a product more, on the logits) and the pieces hold G.
+// With dw G is needed itself.  Where the vocabulary is one piece (up to 128 M logits), E is kept in fp32 and G made from it; else the statistics come
+// first (a product more, on the logits: 1131 us against 925 for 1111 x 2720 x 50003) and the pieces hold G.
 //
 // Sums and statistics are fp32; E and G are rounded once to bf16, as operands of the matrix cores.
 // A masked token (target < 0) has loss 0 and gradient 0 whatever its hidden state holds.
@@ -515,8 +515,7 @@ CePlan ce_plan(int64_t T, int64_t K, int64_t V, bool want_dh, bool want_dw) {
     p.target_logit = take((size_t)T * 4);
     p.of_rows = take((size_t)T * sizeof(CeRow));
     if (pieces) p.e = take((size_t)T * p.piece * 2);
-    // with dw: E in fp32 where that is no more than a piece may take
-    p.holds_e32 = want_dw && p.piece == all && T * all * 4 <= kCePieceBytes;
+    p.holds_e32 = want_dw && p.piece == all;
     if (p.holds_e32) p.e32 = take((size_t)T * p.piece * 4);
     if (want_dh) p.sums = take((size_t)p.slices * T * K * 4);
     if (want_dw) p.h_live = take((size_t)T * K * 2);

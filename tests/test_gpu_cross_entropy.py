@@ -91,6 +91,26 @@ def test_several_pieces_of_the_vocabulary(need_dw):
     _check(h, w, t, g, _run(h, w, t, g, True, need_dw), True, need_dw)
 
 
+@pytest.mark.parametrize("need_dw", [False, True])
+@pytest.mark.parametrize("T,V", [(2100, 70001), (5000, 30011)])
+def test_more_logits_than_a_piece_holds(T, V, need_dw):
+    """More than 128 M logits: two pieces, the running maximum a step up in the second for some tokens and in the first for others."""
+    import paper_2601_16991_amd as salr
+    K = 32
+    assert T * V > 1 << 27
+    h, w, t, g = _inputs(T, K, V, 23)
+    w[:, 0] = 0.0
+    w[: V // 7, 0] = 60.0
+    w[-V // 9:, 0] = -60.0
+    h[0::4, 0] = 1.0
+    h[2::4, 0] = -1.0
+    h[1::4, 0] = 0.0
+    h[3::4, 0] = 0.25
+    h, w, t, g = [x.to(dev()) for x in (h, w, t, g)]
+    got = salr.linear_cross_entropy(h, w, t, g, need_dh=True, need_dw=need_dw)
+    _check(h, w, t, g, got, True, need_dw)
+
+
 @pytest.mark.parametrize("T", [1, 40, 300])
 def test_no_gradient_of_the_loss_means_ones(T):
     h, w, t, _ = _inputs(T, 64, 900, 3)
