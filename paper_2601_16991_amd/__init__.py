@@ -642,11 +642,12 @@ GRAD_NORM_WORKSPACE_BYTES = 8192                      # SALR_GRAD_NORM_WORKSPACE
 
 
 class _StepList:
-    """The tensors of a step as salr_step_plan lays them out: checked and written once, copied to the device, read by every call."""
+    """The tensors of a step as salr_step_plan lays them out: checked and written once, copied to the device, read by every call.
+    ``tensors`` holds them for the calls, which raise ValueError once one has other memory than it had (``p.data = ...``)."""
 
     def __init__(self, grads, params=None, copies=None, exp_avg=None, exp_avg_sq=None, scales=None):
-        self._keep = (grads, params, copies, exp_avg, exp_avg_sq, scales)
-        self.plan, self.chunks, self.param_type, self.grad_type, self.state_bits = _native().step_list(*self._keep)
+        self.plan, self.chunks, self.param_type, self.grad_type, self.state_bits, self.tensors = _native().step_list(
+            grads, params, copies, exp_avg, exp_avg_sq, scales)
 
 
 class GradNorm:
@@ -656,12 +657,16 @@ class GradNorm:
 
     def __init__(self, grads, _list=None):
         self._list = _list or _StepList(list(grads))
-        self._workspace = torch.zeros(GRAD_NORM_WORKSPACE_BYTES, dtype=torch.uint8, device=self._list.plan.device)
+        # (copied, which is done on return: the first call may be on any stream)
+        self._workspace = torch.zeros(GRAD_NORM_WORKSPACE_BYTES, dtype=torch.uint8).to(self._list.plan.device)
         self._call = _native().grad_norm
 
     def __call__(self, max_norm: float = float("inf"), out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         l = self._list
-        got = self._call(l.plan, l.chunks, l.grad_type, max_norm, self._workspace, out, _handle(stream))
+        if out is None and stream is not None:
+            with torch.cuda.stream(stream):
+                out = torch.empty(2, device=l.plan.device)
+        got = self._call(l.plan, l.chunks, l.grad_type, max_norm, self._workspace, out, _handle(stream), l.tensors)
         return got if out is None else out
 
 
@@ -677,7 +682,8 @@ def adamw_states(params, bits: int = 32):
 
 
 class AdamW:
-    """AdamW over many tensors in one launch a step.
+    """AdamW over many tensors in one launch a step.  The tensors keep their memory: a step raises ValueError where one has other memory
+    than when the object was made.
 
     params        fp32 or bf16 tensors, updated in place
     grads         their gradients (fp32 or bf16), read where they are at every step: a backward pass writes into them
@@ -695,13 +701,11 @@ class AdamW:
             exp_avg, exp_avg_sq, scales = adamw_states(params, bits)
         self.params, self.grads, self.exp_avg, self.exp_avg_sq, self.scales, self.copies = params, grads, exp_avg, exp_avg_sq, scales, copies
         self._list = _StepList(grads, params, copies, exp_avg, exp_avg_sq, scales)
-        self._norm = None
+        self._norm = GradNorm(None, self._list)
         self._call = _native().adamw_step
 
     def grad_norm(self, max_norm: float = float("inf"), stream=None) -> torch.Tensor:
         """[norm, factor] of the gradients (see ``GradNorm``); ``grad_norm(c)[1:]`` is a ``grad_scale`` for ``step``."""
-        if self._norm is None:
-            self._norm = GradNorm(None, self._list)
         return self._norm(max_norm, None, stream)
 
     def step(self, lr: float, step: int, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.0,
@@ -710,4 +714,4 @@ class AdamW:
         not finite nothing changes.  ``seed``: of the random rounding of 8-bit states, another one every step."""
         l = self._list
         self._call(l.plan, l.chunks, l.param_type, l.grad_type, l.state_bits, lr, beta1, beta2, eps, weight_decay, step, seed, grad_scale,
-                   _handle(stream))
+                   _handle(stream), l.tensors)

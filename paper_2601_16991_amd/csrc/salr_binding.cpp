@@ -12,6 +12,8 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <memory>
+#include <utility>
 #include <vector>
 
 #include "salr.h"
@@ -440,10 +442,29 @@ double double_of(PyObject* o) {
     return x;
 }
 
-// adamw_step(plan, chunks, param_type, grad_type, state_bits, lr, beta1, beta2, eps, weight_decay, step, seed, grad_scale, stream)
+// The tensors whose addresses a plan holds, so that a call refuses it once one of them has other memory.
+struct StepTensors {
+    static constexpr const char* kName = "salr.step_tensors";
+    std::vector<std::pair<at::Tensor, const void*>> all;
+    static void check(PyObject* capsule) {
+        const auto* t = static_cast<const StepTensors*>(PyCapsule_GetPointer(capsule, kName));
+        if (!t) throw PyFailure{};
+        for (const auto& [tensor, at] : t->all)
+            if (tensor.const_data_ptr() != at) fail(PyExc_ValueError, "a tensor of the list has other %s than when the list was made", "memory");
+    }
+    static PyObject* capsule(std::unique_ptr<StepTensors> t) {
+        PyObject* c = PyCapsule_New(t.get(), kName, [](PyObject* o) { delete static_cast<StepTensors*>(PyCapsule_GetPointer(o, kName)); });
+        if (!c) throw PyFailure{};
+        t.release();
+        return c;
+    }
+};
+
+// adamw_step(plan, chunks, param_type, grad_type, state_bits, lr, beta1, beta2, eps, weight_decay, step, seed, grad_scale, stream, tensors)
 PyObject* py_adamw_step(PyObject*, PyObject* const* v, Py_ssize_t n) {
     SALR_TRY
-    need_args(n, 14, "adamw_step");
+    need_args(n, 15, "adamw_step");
+    StepTensors::check(v[14]);
     const uint8_t* plan = device_ptr<uint8_t>(tensor_of(v[0], "plan"), kU8, "plan");
     const int64_t chunks = int_of(v[1]);
     const salr_type_t pt = static_cast<salr_type_t>(int_of(v[2])), gt = static_cast<salr_type_t>(int_of(v[3]));
@@ -464,10 +485,11 @@ PyObject* py_adamw_step(PyObject*, PyObject* const* v, Py_ssize_t n) {
     SALR_CATCH
 }
 
-// grad_norm(plan, chunks, grad_type, max_norm, workspace, out, stream) -> out, allocated like the workspace where it is None
+// grad_norm(plan, chunks, grad_type, max_norm, workspace, out, stream, tensors) -> out, allocated like the workspace where it is None
 PyObject* py_grad_norm(PyObject*, PyObject* const* v, Py_ssize_t n) {
     SALR_TRY
-    need_args(n, 7, "grad_norm");
+    need_args(n, 8, "grad_norm");
+    StepTensors::check(v[7]);
     const uint8_t* plan = device_ptr<uint8_t>(tensor_of(v[0], "plan"), kU8, "plan");
     const int64_t chunks = int_of(v[1]);
     const salr_type_t gt = static_cast<salr_type_t>(int_of(v[2]));
@@ -505,7 +527,7 @@ struct TensorList {
     const at::Tensor& at(Py_ssize_t i, const char* name) const { return tensor_of(PySequence_Fast_GET_ITEM(fast, i), name); }
 };
 
-// step_list(grads, params, copies, exp_avg, exp_avg_sq, scales) -> (plan on the device, chunks, param_type, grad_type, state_bits)
+// step_list(grads, params, copies, exp_avg, exp_avg_sq, scales) -> (plan on the device, chunks, param_type, grad_type, state_bits, tensors)
 //   all but grads None: a list for the norm only
 PyObject* py_step_list(PyObject*, PyObject* const* v, Py_ssize_t n) {
     SALR_TRY
@@ -531,6 +553,7 @@ PyObject* py_step_list(PyObject*, PyObject* const* v, Py_ssize_t n) {
     if (state_type != at::kFloat && state_type != at::kFloat8_e4m3fn) fail(PyExc_TypeError, "%s must be fp32 or float8_e4m3fn", "exp_avg");
     const int bits = !step ? 0 : state_type == at::kFloat ? 32 : 8;
     if (step && (scales.fast != nullptr) != (bits == 8)) fail(PyExc_ValueError, "%s go with states in 8 bits", "scales");
+    auto tensors = std::make_unique<StepTensors>();
     const auto pointer = [&](const at::Tensor& t, at::ScalarType type, int64_t size, const char* name) -> void* {
         if (!t.defined()) fail(PyExc_TypeError, "%s must be a tensor", name);
         if (t.scalar_type() != type) fail(PyExc_TypeError, "%s: unexpected dtype", name);
@@ -538,6 +561,7 @@ PyObject* py_step_list(PyObject*, PyObject* const* v, Py_ssize_t n) {
         if (!t.is_contiguous()) fail(PyExc_TypeError, "%s must be contiguous", name);
         if (t.device() != device) fail(PyExc_ValueError, "%s: tensors on different devices", name);
         if (t.numel() != size) fail(PyExc_ValueError, "%s: another number of elements than its gradient wants", name);
+        tensors->all.emplace_back(t, t.const_data_ptr());
         return t.data_ptr();
     };
     std::vector<salr_step_tensor_t> table((size_t)count);
@@ -566,7 +590,8 @@ PyObject* py_step_list(PyObject*, PyObject* const* v, Py_ssize_t n) {
         Gil release;
         plan = host.to(device);
     }
-    return Py_BuildValue("NLiii", THPVariable_Wrap(std::move(plan)), (long long)chunks, (int)pt, (int)gt, bits);
+    PyObject* held = StepTensors::capsule(std::move(tensors));
+    return Py_BuildValue("NLiiiN", THPVariable_Wrap(std::move(plan)), (long long)chunks, (int)pt, (int)gt, bits, held);
     SALR_CATCH
 }
 

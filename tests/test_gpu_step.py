@@ -287,6 +287,41 @@ def test_on_another_stream_and_in_a_graph():
         assert same()
 
 
+def test_norm_on_a_stream_that_is_not_current():
+    import paper_2601_16991_amd as salr
+    grads = [torch.full((5000,), 2.0, device=dev()), torch.full((20000,), 2.0, device=dev())]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    opt = salr.AdamW([torch.zeros_like(g) for g in grads], grads)
+    got = [salr.GradNorm(grads)(1.0, stream=side), opt.grad_norm(1.0, stream=side)]
+    side.synchronize()
+    with torch.cuda.stream(side):
+        for norm in got:
+            assert ref.close(float(norm[0]), (4.0 * 25000) ** 0.5)
+
+
+def test_tensors_with_other_memory_are_refused():
+    import paper_2601_16991_amd as salr
+    for moved in ("param", "grad", "exp_avg"):
+        p, g = torch.ones(64, device=dev()), torch.ones(64, device=dev())
+        opt = salr.AdamW([p], [g])
+        norm = salr.GradNorm([g])
+        opt.step(lr=1e-3, step=1)
+        t = {"param": p, "grad": g, "exp_avg": opt.exp_avg[0]}[moved]
+        before = p.clone()
+        t.data = t.clone()
+        with pytest.raises(ValueError):
+            opt.step(lr=1e-3, step=2)
+        if moved == "grad":
+            with pytest.raises(ValueError):
+                norm(1.0)
+        else:
+            assert float(norm(1.0)[0]) == 8.0
+        assert torch.equal(p, before)
+        salr.AdamW([p], [g], opt.exp_avg, opt.exp_avg_sq).step(lr=1e-3, step=2)
+        assert not torch.equal(p, before)
+
+
 def test_refusals():
     import paper_2601_16991_amd as salr
     p, g = torch.zeros(64, device=dev()), torch.zeros(64, device=dev())
