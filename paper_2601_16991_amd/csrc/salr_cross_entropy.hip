@@ -188,11 +188,16 @@ __global__ __launch_bounds__(Shape::kThreads) void ce_logits_kernel(const uint16
         }
     }
     if constexpr (kBf16) {
-        constexpr int kVecs = kN / 8, kRowsAtOnce = Shape::kThreads / kVecs;   // 16 bytes a lane
+        // 16 bytes a lane; of wide tiles not kept in this XCD's cache, where h and w are: 784 x 768 x 106368 with dh 327 us for 336, 4096 x 4096 x
+        // 131072 1 % (a small E is: 48 x 512 x 4099 24.8 us and 25.3)
+        constexpr int kVecs = kN / 8, kRowsAtOnce = Shape::kThreads / kVecs;
         const int vec = threadIdx.x % kVecs;
         for (int row = threadIdx.x / kVecs; row < kM; row += kRowsAtOnce) {
             if (m0 + row >= T) break;
-            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + (m0 + row) * pitch + n0 + 8 * vec) = *reinterpret_cast<const uint4*>(lds + row * kOutPitch + 16 * vec);
+            const u32x4 q = *reinterpret_cast<const u32x4*>(lds + row * kOutPitch + 16 * vec);
+            u32x4* to = reinterpret_cast<u32x4*>(static_cast<uint16_t*>(out) + (m0 + row) * pitch + n0 + 8 * vec);
+            if constexpr (kN == 256) __builtin_nontemporal_store(q, to);
+            else *to = q;
         }
     }
 }
@@ -314,6 +319,7 @@ __global__ __launch_bounds__(1024) void ce_rows_kernel(CeRowArgs a) {
 }
 
 // G from E in fp32 and the tiles' references, eight columns a thread, up to a whole step of columns.  Bound by memory (1111 x 50003: 57 us, 5.9 TB/s).
+// E is read for the last time, not kept in the caches: 2000 x 2048 x 65536 1099 us a call for 1128, smaller ones level.
 __global__ __launch_bounds__(256) void ce_gradients_kernel(const float* __restrict__ e, int64_t T, int64_t columns, int64_t pitch, const float2* __restrict__ stats,
                                                            int width, const CeRow* __restrict__ rows, const int64_t* __restrict__ targets,
                                                            uint16_t* __restrict__ out) {
@@ -321,10 +327,10 @@ __global__ __launch_bounds__(256) void ce_gradients_kernel(const float* __restri
     if (n >= (columns + kProductStep - 1) / kProductStep * kProductStep) return;
     const CeRow of = rows[t];
     const int64_t target = targets[t];
-    const float4* from = reinterpret_cast<const float4*>(e + t * pitch + n);
-    const float4 a = from[0], b = from[1];
+    const f32x4* from = reinterpret_cast<const f32x4*>(e + t * pitch + n);
+    const f32x4 a = __builtin_nontemporal_load(from), b = __builtin_nontemporal_load(from + 1);
     const float by = stats[n / width * T + t].x - of.M;
-    float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 #pragma unroll
     for (int c = 0; c < 8; ++c) x[c] = n + c == target ? -of.beta : of.alpha * times_power(x[c], by);
     const uint4 q = make_uint4(pack_two_bf16(x[0], x[1]), pack_two_bf16(x[2], x[3]), pack_two_bf16(x[4], x[5]), pack_two_bf16(x[6], x[7]));
@@ -421,7 +427,7 @@ __global__ __launch_bounds__(Shape::kThreads) void ce_dw_kernel(const uint16_t* 
     const TileSource<true, 256, Shape::kWaves> gs(gr + m0, pitch, pitch - m0, T, wave, lane);
     const TileSource<true, 256, Shape::kWaves> hs(h + n0, K, K - n0, T, wave, lane);
     tile_product<Shape, true, true>(gs, hs, 0, (int)((T + kProductStep - 1) / kProductStep), lds, acc);
-    // through LDS, so that rows leave as whole vectors, side by side
+    // through LDS, so that rows leave as whole vectors, side by side, and not into the caches, where G and h are (315 x 7872 x 44416 639 us a call for 668)
     constexpr int kOutPitch = 512 + 16;
 #pragma unroll
     for (int i = 0; i < kMI; ++i)
@@ -433,7 +439,7 @@ __global__ __launch_bounds__(Shape::kThreads) void ce_dw_kernel(const uint16_t* 
     const int vec = threadIdx.x % 32;
     if (n0 + 8 * vec >= K) return;
     for (int row = threadIdx.x / 32; row < 256 && m0 + row < columns; row += Shape::kThreads / 32)
-        *reinterpret_cast<uint4*>(dw + (m0 + row) * K + n0 + 8 * vec) = *reinterpret_cast<const uint4*>(lds + row * kOutPitch + 16 * vec);
+        __builtin_nontemporal_store(*reinterpret_cast<const u32x4*>(lds + row * kOutPitch + 16 * vec), reinterpret_cast<u32x4*>(dw + (m0 + row) * K + n0 + 8 * vec));
 }
 
 // Hidden states with those of masked tokens as zeros: G is zero there, but not what it is multiplied by.
