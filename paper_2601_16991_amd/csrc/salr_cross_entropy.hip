@@ -47,6 +47,15 @@ __device__ __forceinline__ float tile_exponent(float most) { return kReferenceSt
 // x 2^by for a whole `by` that may be -infinity; 2^-128 is no normal number, so not by multiplying.
 __device__ __forceinline__ float times_power(float x, float by) { return __builtin_amdgcn_ldexpf(x, (int)fminf(fmaxf(by, -1000.f), 1000.f)); }
 
+// Of the four lanes that hold a row's columns: all of them get `with` of the four, without a trip through LDS.
+template <class With>
+__device__ __forceinline__ float over_groups(float x, With with) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = with(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return with(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
 // l = h w^T of one tile and what becomes of it.  `w`: the piece's first row, `columns` of it exist; `pitch`: of `out` [T][pitch].
 // 2048 x 4096 x 131072, statistics: 1600 us a call, 1376 TFLOP/s (the product by itself, with its result stored, takes the library 1545); E of 4096 x 32768: 860 us,
 // 1280 TFLOP/s.  A tile of 256 x 256 has 9 us outside the k loop without E and 15 with it: start and first loads 3, the exponentials and statistics 5 to 6,
@@ -131,8 +140,7 @@ __global__ __launch_bounds__(Shape::kThreads) void ce_logits_kernel(const uint16
             for (int j = 0; j < kNI; ++j)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) most = fmaxf(most, acc[i][j][r]);
-            most = fmaxf(most, __shfl_xor(most, 16));
-            most = fmaxf(most, __shfl_xor(most, 32));
+            most = over_groups(most, [](float a, float b) { return fmaxf(a, b); });
             if (g == 0) largest[wn * kM + 16 * (wm * kMI + i) + i16] = most;
         }
         __syncthreads();
@@ -181,8 +189,7 @@ __global__ __launch_bounds__(Shape::kThreads) void ce_logits_kernel(const uint16
                 *reinterpret_cast<uint2*>(lds + row * kOutPitch + 32 * (wn * kNI + j) + 8 * g) = make_uint2(pack_two_bf16(e[0], e[1]), pack_two_bf16(e[2], e[3]));
         }
         if constexpr (kMode != kGradients) {
-            sum += __shfl_xor(sum, 16);
-            sum += __shfl_xor(sum, 32);
+            sum = over_groups(sum, [](float a, float b) { return a + b; });
             if (g == 0) sums[wn * kM + row] = sum;
         }
     }
