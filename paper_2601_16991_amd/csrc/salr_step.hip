@@ -77,10 +77,11 @@ __device__ __forceinline__ void store_eight(void* base, int i, int left, const f
             to[0] = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
             to[1] = make_uint4(__float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7]));
         } else {
-            uint32_t e[8];
+            typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));   // (rounded to nearest, ties to even)
+            uint32_t e[4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) e[j] = f32_to_bf16_rne(x[j]);
-            to[0] = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+            for (int j = 0; j < 4; ++j) e[j] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x[2 * j], (__bf16)x[2 * j + 1]});
+            to[0] = make_uint4(e[0], e[1], e[2], e[3]);
         }
     } else {
 #pragma unroll
@@ -152,13 +153,9 @@ __device__ __forceinline__ uint32_t random20(uint32_t position, uint32_t key) {
 // x in [0, 448 and a little] to a value of the 8-bit type, up with the probability of what is cut off.
 __device__ __forceinline__ float random_round(float x, uint32_t bits20) {
 #pragma clang fp contract(off)
-    const bool low = x < 0x1p-6f;   // subnormal there, spacing 2^-9: as that of the values from 2^-6 on
-    const float t = low ? x + 0x1p-6f : x;
-    float y = __uint_as_float((__float_as_uint(t) + bits20) & ~0xFFFFFu);
-    y = low ? y - 0x1p-6f : y;
-    y = y > kFp8Most ? kFp8Most : y;
-    y = y < 0x1p-9f ? 0x1p-9f : y;
-    return x > 0.f ? y : x;   // (a NaN stays one)
+    const float up = x < 0x1p-6f ? 0x1p-6f : 0.f;   // subnormal there, spacing 2^-9: as that of the values from 2^-6 on
+    const float y = __uint_as_float((__float_as_uint(x + up) + bits20) & ~0xFFFFFu) - up;
+    return x > 0.f ? __builtin_amdgcn_fmed3f(y, 0x1p-9f, kFp8Most) : x;   // (a NaN stays one)
 }
 
 struct StepScalars {
