@@ -57,9 +57,9 @@ __device__ __forceinline__ float over_groups(float x, With with) {
 }
 
 // l = h w^T of one tile and what becomes of it.  `w`: the piece's first row, `columns` of it exist; `pitch`: of `out` [T][pitch].
-// 2048 x 4096 x 131072, statistics: 1600 us a call, 1376 TFLOP/s (the product by itself, with its result stored, takes the library 1545); E of 4096 x 32768: 860 us,
-// 1280 TFLOP/s.  A tile of 256 x 256 has 9 us outside the k loop without E and 15 with it: start and first loads 3, the exponentials and statistics 5 to 6,
-// E through LDS and out.  Up to 64 tokens the head's bytes count: 1 x 4096 x 131072 174 us, 6.2 TB/s.
+// 2048 x 4096 x 131072, statistics: 1565 us a call, 1405 TFLOP/s (the product by itself, with its result stored, takes the library 1515 to 1545); E of
+// 4096 x 32768: 836 us, 1315 TFLOP/s.  A tile of 256 x 256 has 7 us outside the k loop without E and 12 with it: start and first loads 3, the exponentials and
+// statistics 4, E through LDS and out.  Up to 64 tokens the head's bytes count: 1 x 4096 x 131072 174 us, 6.2 TB/s.
 template <class Shape, int kMode>
 __global__ __launch_bounds__(Shape::kThreads) void ce_logits_kernel(const uint16_t* __restrict__ h, int64_t T, int64_t K, const uint16_t* __restrict__ w,
                                                         int64_t columns, int64_t first, const int64_t* __restrict__ targets, int m_tiles, int n_tiles,
@@ -337,7 +337,7 @@ __global__ __launch_bounds__(1024) void ce_rows_kernel(CeRowArgs a) {
     a.rows[t] = CeRow{M, alpha, beta, target >= 0};
 }
 
-// G from E in fp32 and the tiles' references, eight columns a thread, up to a whole step of columns.  Bound by memory (1111 x 50003: 57 us, 5.9 TB/s).
+// G from E in fp32 and the tiles' references, eight columns a thread, up to a whole step of columns.  Bound by memory (1111 x 50003: 60 us, 5.6 TB/s).
 // E is read for the last time, not kept in the caches: 2000 x 2048 x 65536 1099 us a call for 1128, smaller ones level.
 __global__ __launch_bounds__(256) void ce_gradients_kernel(const float* __restrict__ e, int64_t T, int64_t columns, int64_t pitch, const float2* __restrict__ stats,
                                                            int width, const CeRow* __restrict__ rows, const int64_t* __restrict__ targets,
@@ -427,7 +427,8 @@ __global__ __launch_bounds__(256) void ce_dh_finish_kernel(const float* __restri
     *reinterpret_cast<uint4*>(dh + t * K + k) = q;
 }
 
-// dw of a piece: G^T h, both operands across the contraction.  1111 x 2720 x 50003: 290 us, 1040 TFLOP/s; of the 35 us of a tile its 18 steps take 26.
+// dw of a piece: G^T h, both operands across the contraction.  1111 x 2720 x 50003: 285 us, 1060 TFLOP/s; of the 34 us of a tile its 18 steps take 26.
+// With few tokens the stores count: 315 x 7872 x 44416 7 us of steps in the 16 of a tile.
 template <class Shape>
 __global__ __launch_bounds__(Shape::kThreads) void ce_dw_kernel(const uint16_t* __restrict__ gr, int64_t T, int64_t pitch, const uint16_t* __restrict__ h, int64_t K,
                                                     int64_t columns, int m_tiles, int n_tiles, uint16_t* __restrict__ dw) {

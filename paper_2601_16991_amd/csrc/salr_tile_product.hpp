@@ -149,9 +149,11 @@ struct TileShape {
 // Requests are spread over the products, because a burst of them holds the waves up (4 to 6 % of a call): P's into the slot just left, in
 // the second half; Q's, where it has a slot more, in the first half of the next step (3 % of a call).
 //
-// On 256 x 256 tiles the chip's power is the limit: 4096 x 4096 x 32768 with Q transposed 787 us, 1400 TFLOP/s, at 1.8 GHz of 2.4 with the matrix cores busy 74 %
-// of the cycles, LDS 28 %, no bank conflicts.  Of 1675 us (2048 x 4096 x 131072) 335 are the loads' (64 KB a step cross from an L2 to each CU), 125 the reads
+// On 256 x 256 tiles the chip's power is the limit: 4096 x 4096 x 32768 with Q transposed 777 us, 1415 TFLOP/s, at 1.8 GHz of 2.4 with the matrix cores busy 73 %
+// of the cycles, LDS 27 %, no bank conflicts.  In a loop of nothing but products the instruction of 32 x 32 x 16 is 13 % slower than this one.  Of 1675 us (2048 x 4096 x 131072) 335 are the loads' (64 KB a step cross from an L2 to each CU), 125 the reads
 // from LDS.  128 x 256 tiles: 0.9 us a step for 1.56, where they make a round of the CUs shorter.
+// A workgroup makes one tile: going on to the next, its first steps requested before the stores, is 1 to 2 % slower, since loads and stores are waited for
+// together, where those of a workgroup that has ended drain behind the next one's start.
 // (Eight waves of 128 x 64, two a SIMD: four of 128 x 128 read a third less from LDS and are 5 to 7 % slower, a SIMD's one wave stands at every barrier.)
 template <class Shape, bool kPColumns, bool kQColumns>
 __device__ __forceinline__ void tile_product(const TileSource<kPColumns, Shape::kM, Shape::kWaves>& ps, const TileSource<kQColumns, Shape::kN, Shape::kWaves>& qs,
