@@ -153,7 +153,7 @@ __global__ __launch_bounds__(Shape::kThreads) void ce_logits_kernel(const uint16
         if constexpr (kMode == kGradients) {
             if (m0 + row < T) of = rows[m0 + row];
             M = of.M, alpha = of.alpha;
-            if (__any(!of.live)) {   // a masked token: alpha and M are 0
+            if (__any(!of.live)) {   // a masked token: M and alpha are 0 in its CeRow, l here, whatever h held
 #pragma unroll
                 for (int j = 0; j < kNI; ++j)
 #pragma unroll
@@ -334,7 +334,7 @@ __global__ __launch_bounds__(1024) void ce_rows_kernel(CeRowArgs a) {
     }
     a.loss[t] = loss;
     a.lse[t] = lse;
-    a.rows[t] = CeRow{M, alpha, beta, target >= 0};
+    a.rows[t] = CeRow{target >= 0 ? M : 0.f, alpha, beta, target >= 0};   // (2^-M of a masked token may leave fp32, and 0 times infinity is NaN)
 }
 
 // G from E in fp32 and the tiles' references, eight columns a thread, up to a whole step of columns.  Bound by memory (1111 x 50003: 60 us, 5.6 TB/s).
