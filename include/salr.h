@@ -489,7 +489,10 @@ salr_status_t salr_step_plan(const salr_step_tensor_t* tensors, int64_t n, salr_
  * (salr_grad_norm gives NaN for gradients whose norm is not finite).  States in 8 bits: a block of 128 elements keeps, in fp32, the
  * largest |m| and sqrt(v) over 448; m is rounded to the nearest of the 8-bit values, sqrt(v) up or down at random so that its mean is
  * right (from the element's place in the list and `seed`: a run with the same seeds gives the same results), and to the
- * smallest of them rather than to zero.  A block whose largest magnitude is below 2^-100 is stored as zeros.
+ * smallest of them rather than to zero.  `seed` has to be another one every step (`step` serves): the same random bits each time would
+ * round the same way each time, and averages that move by less than a value's spacing would stay where they are (a captured
+ * graph keeps `step` and `seed` as they were at its capture, and so does every replay).  A block whose largest magnitude is below 2^-100 is
+ * stored as zeros.
  *
  *   plan, chunks          the list, on the device; of the types and state_bits that it was made for
  *   step                  number of this step, from 1 on

@@ -709,9 +709,13 @@ class AdamW:
         return self._norm(max_norm, None, stream)
 
     def step(self, lr: float, step: int, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.0,
-             grad_scale: Optional[torch.Tensor] = None, seed: int = 0, stream=None) -> None:
+             grad_scale: Optional[torch.Tensor] = None, seed: Optional[int] = None, stream=None) -> None:
         """Step number ``step`` (from 1 on).  ``grad_scale``: one fp32 on the device that the gradients are multiplied by; where it is
-        not finite nothing changes.  ``seed``: of the random rounding of 8-bit states, another one every step."""
+        not finite nothing changes.  ``seed``: of the random rounding of 8-bit states, None: ``step``.  A caller that gives one gives another
+        one every step: with the same random bits step after step the averages would stay where they are.  (A captured graph replays the
+        numbers of its capture.)"""
         l = self._list
+        if seed is None:
+            seed = step
         self._call(l.plan, l.chunks, l.param_type, l.grad_type, l.state_bits, lr, beta1, beta2, eps, weight_decay, step, seed, grad_scale,
                    _handle(stream), l.tensors)
