@@ -157,6 +157,19 @@ def _ptr(t: Optional[torch.Tensor], kinds, name: str) -> Optional[int]:
     return t.data_ptr() if t.numel() > 0 else None
 
 
+def _workspace(workspace: Optional[torch.Tensor], like: torch.Tensor) -> Tuple[Optional[int], int]:
+    """Address and bytes of a caller's workspace (of any type, on the device of ``like``)."""
+    if workspace is None:
+        return None, 0
+    if not workspace.is_cuda:
+        raise TypeError("workspace must be a CUDA tensor")
+    if not workspace.is_contiguous():
+        raise TypeError("workspace must be contiguous")
+    if like.is_cuda and workspace.device != like.device:
+        raise ValueError("workspace: tensors on different devices")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
 def _stream(stream) -> Optional[int]:
     s = torch.cuda.current_stream() if stream is None else stream
     return s.cuda_stream or None
@@ -382,8 +395,7 @@ def salr_sparse_lowrank_linear_backward(x: Optional[torch.Tensor], dy: torch.Ten
     for name, t, shape in (("x", x, (M, K)), ("dx", dx, (M, K)), ("da", da, (K, R)), ("db", db, (R, N))):
         if t is not None and tuple(t.shape) != shape:
             raise ValueError(f"{name} must be {shape}")
-    ws_ptr = None if workspace is None else workspace.data_ptr()
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    ws_ptr, ws_bytes = _workspace(workspace, dy)
     st = lib().salr_sparse_lowrank_linear_backward(
         _ptr(x, _BF16_TYPES, "x"), _ptr(dy, _BF16_TYPES, "dy"), M, K, N, _ptr(bitmap, _U32_TYPES, "bitmap"),
         _ptr(values, _BF16_TYPES, "values"), _ptr(row_offsets, _U32_TYPES, "row_offsets"),
@@ -412,8 +424,7 @@ class PreparedLinear:
         if slice_table is not None and (two_of_four or slice_table.numel() != N * 16):
             raise ValueError("slice table")
         self._keep = (x, bitmap, values, row_offsets, a_cat, b_cat, y, workspace, slice_table)
-        ws_ptr = None if workspace is None else workspace.data_ptr()
-        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+        ws_ptr, ws_bytes = _workspace(workspace, x)
         table = () if slice_table is None else (_ptr(slice_table, _U32_TYPES, "slice_table"),)
         self._args = (_ptr(x, _BF16_TYPES, "x"), M, K, N, _ptr(bitmap, _U32_TYPES, "bitmap"),
                       _ptr(values, _BF16_TYPES, "values"), _ptr(row_offsets, _U32_TYPES, "row_offsets")) + table + (
@@ -442,8 +453,7 @@ class PreparedQsalrLinear:
         if codes.numel() != (nnz + 1) // 2 or scales.numel() != (nnz + 63) // 64:
             raise ValueError("codes / scales do not match nnz")
         self._keep = (x, bitmap, codes, scales, row_offsets, a_cat, b_cat, y, workspace)
-        ws_ptr = None if workspace is None else workspace.data_ptr()
-        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+        ws_ptr, ws_bytes = _workspace(workspace, x)
         self._args = (_ptr(x, _BF16_TYPES, "x"), M, K, N, _ptr(bitmap, _U32_TYPES, "bitmap"),
                       _ptr(codes, (torch.uint8,), "codes"), _ptr(scales, _BF16_TYPES, "scales"),
                       _ptr(row_offsets, _U32_TYPES, "row_offsets"), nnz, _ptr(a_cat, _BF16_TYPES, "a_cat"),
@@ -527,7 +537,7 @@ def salr_residual_adapter(e: torch.Tensor, r: int, oversample: int, power_iterat
                                      _ptr(omega, (torch.float32,), "omega"), _ptr(a_res, _BF16_TYPES, "a_res"),
                                      _ptr(b_res, _BF16_TYPES, "b_res"),
                                      None if sigma is None else _ptr(sigma, (torch.float32,), "sigma"),
-                                     workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream))
+                                     *_workspace(workspace, e), _stream(stream))
     _check(st, "salr_residual_adapter")
 
 
@@ -620,8 +630,7 @@ def salr_linear_cross_entropy(h: torch.Tensor, w: torch.Tensor, targets: torch.T
                            ("lse", lse, (T,)), ("dh", dh, (T, K)), ("dw", dw, (V, K))):
         if t is not None and tuple(t.shape) != shape:
             raise ValueError(f"{name} must be {shape}")
-    ws_ptr = None if workspace is None else workspace.data_ptr()
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    ws_ptr, ws_bytes = _workspace(workspace, h)
     st = lib().salr_linear_cross_entropy(
         _ptr(h, _BF16_TYPES, "h"), T, K, _ptr(w, _BF16_TYPES, "w"), V, _ptr(targets, (torch.int64,), "targets"),
         _ptr(grad_loss, (torch.float32,), "grad_loss"), _ptr(loss, (torch.float32,), "loss"), _ptr(lse, (torch.float32,), "lse"),

@@ -123,9 +123,12 @@ struct Workspace {
     void* ptr = nullptr;
     size_t bytes = 0;
 
-    void given(PyObject* o) {
+    void given(PyObject* o, const at::Tensor& like) {
         const at::Tensor& t = tensor_of(o, "workspace");
         if (!t.defined()) return;
+        if (!t.is_cuda()) fail(PyExc_TypeError, "%s must be a CUDA tensor", "workspace");
+        if (!t.is_contiguous()) fail(PyExc_TypeError, "%s must be contiguous", "workspace");
+        if (t.device() != like.device()) fail(PyExc_ValueError, "%s: tensors on different devices", "workspace");
         ptr = t.data_ptr();
         bytes = (size_t)t.numel() * t.element_size();
     }
@@ -202,7 +205,7 @@ PyObject* py_linear(PyObject*, PyObject* const* v, Py_ssize_t n) {
         table = device_ptr<uint32_t>(st, kU32, "slice_table");
     }
     Workspace ws;
-    ws.given(v[9]);
+    ws.given(v[9], x);
     if (v[8] == Py_None) {   // (a call that brings its y allocates nothing)
         // Less than the query tells is the caller's choice of the path without a decoded weight.
         const size_t told = form == 2 ? salr_linear_2of4_workspace_bytes(l.M, l.K, l.N, l.R) : salr_linear_workspace_bytes(l.M, l.K, l.N, l.R);
@@ -244,7 +247,7 @@ PyObject* py_qsalr_linear(PyObject*, PyObject* const* v, Py_ssize_t n) {
     const uint16_t* sp = device_ptr<uint16_t>(tensor_of(v[3], "scales"), kBf16, "scales");
     uint16_t* yp = device_ptr<uint16_t>(y, kBf16, "y");
     Workspace ws;
-    ws.given(v[9]);
+    ws.given(v[9], x);
     if (v[9] == Py_None && v[8] == Py_None) {
         const size_t told = salr_qsalr_linear_workspace_bytes(l.M, l.K, l.N, l.R, nnz);
         const size_t want = salr_qsalr_linear_workspace_bytes_fastest(l.M, l.K, l.N, l.R, nnz);
@@ -413,7 +416,7 @@ PyObject* py_linear_cross_entropy(PyObject*, PyObject* const* v, Py_ssize_t n) {
     if (need_dh) dh = empty_on({T, K}, h.scalar_type(), h);
     if (need_dw) dw = empty_on({V, K}, w.scalar_type(), h);
     Workspace ws;
-    ws.given(v[6]);
+    ws.given(v[6], h);
     if (v[6] == Py_None) ws.allocate(salr_linear_cross_entropy_workspace_bytes(T, K, V, need_dh, need_dw), h);
     float *lp = device_ptr<float>(loss, kF32, "loss"), *sp = device_ptr<float>(lse, kF32, "lse");
     // (an output without elements has no memory, and is asked for all the same: the workspace was sized with it)
