@@ -180,6 +180,13 @@ def _handle(stream) -> Optional[int]:
     return None if stream is None else stream.cuda_stream
 
 
+def _on(stream, device):
+    """The stream argument of a call on tensors of ``device``: None or a stream of that GPU."""
+    if stream is not None and stream.device != device:
+        raise ValueError("stream: of another device than the tensors")
+    return stream
+
+
 def _check(status: int, where: str) -> None:
     if status != SALR_OK:
         raise SalrError(status, where)
@@ -630,12 +637,14 @@ def salr_linear_cross_entropy(h: torch.Tensor, w: torch.Tensor, targets: torch.T
                            ("lse", lse, (T,)), ("dh", dh, (T, K)), ("dw", dw, (V, K))):
         if t is not None and tuple(t.shape) != shape:
             raise ValueError(f"{name} must be {shape}")
-    ws_ptr, ws_bytes = _workspace(workspace, h)
-    st = lib().salr_linear_cross_entropy(
-        _ptr(h, _BF16_TYPES, "h"), T, K, _ptr(w, _BF16_TYPES, "w"), V, _ptr(targets, (torch.int64,), "targets"),
-        _ptr(grad_loss, (torch.float32,), "grad_loss"), _ptr(loss, (torch.float32,), "loss"), _ptr(lse, (torch.float32,), "lse"),
-        _ptr(dh, _BF16_TYPES, "dh"), _ptr(dw, _BF16_TYPES, "dw"), ws_ptr, ws_bytes, _stream(stream))
-    _check(st, "salr_linear_cross_entropy")
+    args = (_ptr(h, _BF16_TYPES, "h"), T, K, _ptr(w, _BF16_TYPES, "w"), V, _ptr(targets, (torch.int64,), "targets"),
+            _ptr(grad_loss, (torch.float32,), "grad_loss"), _ptr(loss, (torch.float32,), "loss"), _ptr(lse, (torch.float32,), "lse"),
+            _ptr(dh, _BF16_TYPES, "dh"), _ptr(dw, _BF16_TYPES, "dw"), *_workspace(workspace, h))
+    for name, t in (("w", w), ("targets", targets), ("grad_loss", grad_loss), ("loss", loss), ("lse", lse), ("dh", dh), ("dw", dw)):
+        if t is not None and t.device != h.device:
+            raise ValueError(f"{name}: tensors on different devices")
+    with torch.cuda.device(h.device):
+        _check(lib().salr_linear_cross_entropy(*args, _stream(_on(stream, h.device))), "salr_linear_cross_entropy")
 
 
 def linear_cross_entropy(h, w, targets, grad_loss=None, need_dh=True, need_dw=False, workspace=None):
@@ -673,9 +682,9 @@ class GradNorm:
     def __call__(self, max_norm: float = float("inf"), out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         l = self._list
         if out is None and stream is not None:
-            with torch.cuda.stream(stream):
+            with torch.cuda.stream(_on(stream, l.plan.device)):
                 out = torch.empty(2, device=l.plan.device)
-        got = self._call(l.plan, l.chunks, l.grad_type, max_norm, self._workspace, out, _handle(stream), l.tensors)
+        got = self._call(l.plan, l.chunks, l.grad_type, max_norm, self._workspace, out, _handle(_on(stream, l.plan.device)), l.tensors)
         return got if out is None else out
 
 
@@ -727,4 +736,4 @@ class AdamW:
         if seed is None:
             seed = step
         self._call(l.plan, l.chunks, l.param_type, l.grad_type, l.state_bits, lr, beta1, beta2, eps, weight_decay, step, seed, grad_scale,
-                   _handle(stream), l.tensors)
+                   _handle(_on(stream, l.plan.device)), l.tensors)

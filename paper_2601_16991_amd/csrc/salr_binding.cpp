@@ -8,6 +8,7 @@
 #include <ATen/hip/EmptyTensor.h>
 #include <ATen/ops/empty.h>
 #include <ATen/core/Tensor.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -62,6 +63,10 @@ T* device_ptr(const at::Tensor& t, Kind kind, const char* name) {
 
 void need_matrix(const at::Tensor& t, const char* name) {
     if (!t.defined() || t.dim() != 2) fail(PyExc_ValueError, "%s must be a matrix", name);
+}
+
+void need_device(const at::Tensor& t, const at::Device& device, const char* name) {
+    if (t.defined() && t.device() != device) fail(PyExc_ValueError, "%s: tensors on different devices", name);
 }
 
 void* stream_of(PyObject* o) {   // None: the current stream; else a stream handle as an integer (0 = default stream)
@@ -410,7 +415,10 @@ PyObject* py_linear_cross_entropy(PyObject*, PyObject* const* v, Py_ssize_t n) {
     const uint16_t *hp = device_ptr<uint16_t>(h, kBf16, "h"), *wp = device_ptr<uint16_t>(w, kBf16, "w");
     const int64_t* tp = device_ptr<int64_t>(targets, kI64, "targets");
     const float* gp = device_ptr<float>(grad, kF32, "grad_loss");
-    if (!h.is_cuda()) fail(PyExc_TypeError, "%s must be a CUDA tensor", "h");
+    need_device(w, h.device(), "w");
+    need_device(targets, h.device(), "targets");
+    need_device(grad, h.device(), "grad_loss");
+    const c10::DeviceGuard on(h.device());   // outputs, stream and launches are that GPU's, whichever is current
     const bool need_dh = PyObject_IsTrue(v[4]) == 1, need_dw = PyObject_IsTrue(v[5]) == 1;
     at::Tensor loss = empty_on({T}, at::kFloat, h), lse = empty_on({T}, at::kFloat, h), dh, dw;
     if (need_dh) dh = empty_on({T, K}, h.scalar_type(), h);
@@ -468,12 +476,16 @@ PyObject* py_adamw_step(PyObject*, PyObject* const* v, Py_ssize_t n) {
     SALR_TRY
     need_args(n, 15, "adamw_step");
     StepTensors::check(v[14]);
-    const uint8_t* plan = device_ptr<uint8_t>(tensor_of(v[0], "plan"), kU8, "plan");
+    const at::Tensor& list = tensor_of(v[0], "plan");
+    if (!list.defined()) fail(PyExc_TypeError, "%s must be a tensor", "plan");
+    const uint8_t* plan = device_ptr<uint8_t>(list, kU8, "plan");
     const int64_t chunks = int_of(v[1]);
     const salr_type_t pt = static_cast<salr_type_t>(int_of(v[2])), gt = static_cast<salr_type_t>(int_of(v[3]));
     const at::Tensor& scale = tensor_of(v[12], "grad_scale");
     if (scale.defined() && scale.numel() != 1) fail(PyExc_ValueError, "%s must be one value", "grad_scale");
     const float* sp = device_ptr<float>(scale, kF32, "grad_scale");
+    need_device(scale, list.device(), "grad_scale");
+    const c10::DeviceGuard on(list.device());
     const int bits = (int)int_of(v[4]);
     const double lr = double_of(v[5]), b1 = double_of(v[6]), b2 = double_of(v[7]), eps = double_of(v[8]), decay = double_of(v[9]);
     const int64_t step = int_of(v[10]), seed = int_of(v[11]);
@@ -493,16 +505,21 @@ PyObject* py_grad_norm(PyObject*, PyObject* const* v, Py_ssize_t n) {
     SALR_TRY
     need_args(n, 8, "grad_norm");
     StepTensors::check(v[7]);
-    const uint8_t* plan = device_ptr<uint8_t>(tensor_of(v[0], "plan"), kU8, "plan");
+    const at::Tensor& list = tensor_of(v[0], "plan");
+    if (!list.defined()) fail(PyExc_TypeError, "%s must be a tensor", "plan");
+    const uint8_t* plan = device_ptr<uint8_t>(list, kU8, "plan");
     const int64_t chunks = int_of(v[1]);
     const salr_type_t gt = static_cast<salr_type_t>(int_of(v[2]));
     const float max_norm = (float)double_of(v[3]);
     const at::Tensor& ws = tensor_of(v[4], "workspace");
     uint8_t* wp = device_ptr<uint8_t>(ws, kU8, "workspace");
     if (!ws.defined()) fail(PyExc_TypeError, "%s must be a tensor", "workspace");
+    need_device(ws, list.device(), "workspace");
+    const c10::DeviceGuard on(list.device());
     at::Tensor out = v[5] == Py_None ? empty_on({2}, at::kFloat, ws) : tensor_of(v[5], "out");
     if (out.numel() != 2) fail(PyExc_ValueError, "%s must hold two values", "out");
     float* op = device_ptr<float>(out, kF32, "out");
+    need_device(out, list.device(), "out");
     void* stream = stream_of(v[6]);
     salr_status_t st;
     {
