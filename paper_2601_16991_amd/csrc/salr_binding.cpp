@@ -13,6 +13,8 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
+#include <initializer_list>
 #include <memory>
 #include <utility>
 #include <vector>
@@ -457,11 +459,27 @@ double double_of(PyObject* o) {
 struct StepTensors {
     static constexpr const char* kName = "salr.step_tensors";
     std::vector<std::pair<at::Tensor, const void*>> all;
-    static void check(PyObject* capsule) {
-        const auto* t = static_cast<const StepTensors*>(PyCapsule_GetPointer(capsule, kName));
+    std::vector<at::Tensor> states;   // those whose only owner may be the optimiser
+    void* home = nullptr;             // the stream that was current when the list was made: its memory goes back to that stream's work
+    std::vector<void*> step_on, norm_on;   // other streams that the calls ran on
+    static StepTensors& check(PyObject* capsule) {
+        auto* t = static_cast<StepTensors*>(PyCapsule_GetPointer(capsule, kName));
         if (!t) throw PyFailure{};
         for (const auto& [tensor, at] : t->all)
             if (tensor.const_data_ptr() != at) fail(PyExc_ValueError, "a tensor of the list has other %s than when the list was made", "memory");
+        return *t;
+    }
+    // What the list's owner holds is used on `stream`: it is handed to nobody else before that is done, even if the owner goes first.  (Told
+    // to the allocator once for a stream and a tensor: it remembers.)
+    void uses(std::vector<void*>& known, void* stream, std::initializer_list<const at::Tensor*> owned, bool with_states) const {
+        if (stream == home || std::find(known.begin(), known.end(), stream) != known.end()) return;
+        const auto tell = [stream](const at::Tensor& t) {   // (a stream that is known by its handle has it as its id)
+            t.record_stream(c10::Stream(c10::Stream::UNSAFE, t.device(), reinterpret_cast<intptr_t>(stream)));
+        };
+        for (const at::Tensor* t : owned) tell(*t);
+        if (with_states)
+            for (const at::Tensor& t : states) tell(t);
+        known.push_back(stream);
     }
     static PyObject* capsule(std::unique_ptr<StepTensors> t) {
         PyObject* c = PyCapsule_New(t.get(), kName, [](PyObject* o) { delete static_cast<StepTensors*>(PyCapsule_GetPointer(o, kName)); });
@@ -475,7 +493,7 @@ struct StepTensors {
 PyObject* py_adamw_step(PyObject*, PyObject* const* v, Py_ssize_t n) {
     SALR_TRY
     need_args(n, 15, "adamw_step");
-    StepTensors::check(v[14]);
+    StepTensors& held = StepTensors::check(v[14]);
     const at::Tensor& list = tensor_of(v[0], "plan");
     if (!list.defined()) fail(PyExc_TypeError, "%s must be a tensor", "plan");
     const uint8_t* plan = device_ptr<uint8_t>(list, kU8, "plan");
@@ -490,6 +508,7 @@ PyObject* py_adamw_step(PyObject*, PyObject* const* v, Py_ssize_t n) {
     const double lr = double_of(v[5]), b1 = double_of(v[6]), b2 = double_of(v[7]), eps = double_of(v[8]), decay = double_of(v[9]);
     const int64_t step = int_of(v[10]), seed = int_of(v[11]);
     void* stream = stream_of(v[13]);
+    held.uses(held.step_on, stream, {&list}, true);
     salr_status_t st;
     {
         Gil release;
@@ -504,7 +523,7 @@ PyObject* py_adamw_step(PyObject*, PyObject* const* v, Py_ssize_t n) {
 PyObject* py_grad_norm(PyObject*, PyObject* const* v, Py_ssize_t n) {
     SALR_TRY
     need_args(n, 8, "grad_norm");
-    StepTensors::check(v[7]);
+    StepTensors& held = StepTensors::check(v[7]);
     const at::Tensor& list = tensor_of(v[0], "plan");
     if (!list.defined()) fail(PyExc_TypeError, "%s must be a tensor", "plan");
     const uint8_t* plan = device_ptr<uint8_t>(list, kU8, "plan");
@@ -521,6 +540,7 @@ PyObject* py_grad_norm(PyObject*, PyObject* const* v, Py_ssize_t n) {
     float* op = device_ptr<float>(out, kF32, "out");
     need_device(out, list.device(), "out");
     void* stream = stream_of(v[6]);
+    held.uses(held.norm_on, stream, {&list, &ws}, false);
     salr_status_t st;
     {
         Gil release;
@@ -597,6 +617,8 @@ PyObject* py_step_list(PyObject*, PyObject* const* v, Py_ssize_t n) {
         t.exp_avg = pointer(m.at(i, "exp_avg"), state_type, t.count, "exp_avg");
         t.exp_avg_sq = pointer(sq.at(i, "exp_avg_sq"), state_type, t.count, "exp_avg_sq");
         if (copies.fast && copies.at(i, "copy").defined()) t.copy = static_cast<uint16_t*>(pointer(copies.at(i, "copy"), at::kBFloat16, t.count, "copy"));
+        for (const TensorList* l : {&m, &sq}) tensors->states.push_back(l->at(i, "state"));
+        if (scales.fast) tensors->states.push_back(scales.at(i, "scales"));
         if (scales.fast)
             t.scales = static_cast<float*>(pointer(scales.at(i, "scales"), at::kFloat, 2 * ((t.count + salr::kStepBlock - 1) / salr::kStepBlock), "scales"));
     }
@@ -605,6 +627,8 @@ PyObject* py_step_list(PyObject*, PyObject* const* v, Py_ssize_t n) {
     at::Tensor host = at::empty({(int64_t)(need < 64 ? 64 : need)}, at::TensorOptions().dtype(at::kByte));
     int64_t chunks = 0;
     check(salr_step_plan(table.data(), count, pt, gt, bits, host.data_ptr(), need, &chunks), "salr_step_plan");
+    const c10::DeviceGuard on(device);
+    tensors->home = stream_of(Py_None);
     at::Tensor plan;
     {
         Gil release;

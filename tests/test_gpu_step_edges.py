@@ -43,3 +43,26 @@ def test_no_seed_means_the_number_of_the_step():
         return torch.cat([x.view(torch.uint8).cpu() for x in opt.exp_avg_sq])
     assert torch.equal(go(), go(own=True))
     assert torch.equal(go(seed=0), go(seed=0)) and not torch.equal(go(), go(seed=0))
+
+
+def test_a_list_outlives_its_owner_until_its_stream_is_done():
+    """An object that is dropped right after its call on a side stream: its memory is not handed to the other stream's tensors while the
+    call waits there.  (They are only allocated here, never written.)"""
+    import paper_2601_16991_amd as salr
+    grads = [torch.full((5000,), 2.0, device=dev()), torch.full((20000,), 2.0, device=dev())]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    norm = salr.GradNorm(grads)
+    opt = salr.AdamW([torch.zeros_like(g) for g in grads], grads)
+    params = opt.params
+    held = {norm._list.plan.data_ptr(), norm._workspace.data_ptr(), opt._list.plan.data_ptr(), *(x.data_ptr() for x in opt.exp_avg + opt.exp_avg_sq)}
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)
+        got = norm(1.0)
+    opt.step(lr=0.5, step=1, stream=side)
+    del norm, opt
+    taken = [torch.empty(n, dtype=torch.uint8, device=dev()) for n in (64, 256, 512, 8192, 20000, 80000) for _ in range(64)]
+    busy = not side.query()
+    assert not held & {x.data_ptr() for x in taken}
+    side.synchronize()
+    assert busy and ref.close(float(got[0]), (4.0 * 25000) ** 0.5) and all(bool((p < -0.49).all()) for p in params)
