@@ -452,6 +452,8 @@ salr_status_t salr_linear_cross_entropy(const uint16_t* h, int64_t T, int64_t K,
 
 /*
  * The list of tensors that salr_adamw_step and salr_grad_norm go through in one launch, whatever their number and sizes.
+ * Every tensor is in it once, and none that a step writes (all but grad) overlaps another: the records are gone through at the same time, in no
+ * order (not checked here; a weight that is used in several places is one tensor with the sum of its gradients).
  * salr_step_plan writes it to HOST memory (salr_step_plan_bytes(counts, n) bytes) and copies nothing to the device: the caller does,
  * once, and hands the device copy (16-byte aligned) to the calls below for as long as the tensors stay where they are.
  */

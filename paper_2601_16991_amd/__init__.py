@@ -701,7 +701,8 @@ def adamw_states(params, bits: int = 32):
 
 class AdamW:
     """AdamW over many tensors in one launch a step.  The tensors keep their memory: a step raises ValueError where one has other memory
-    than when the object was made.
+    than when the object was made.  Each is in the lists once (ValueError where memory that a step writes is another tensor's too): a weight that
+    is used in several places is one tensor with the sum of its gradients.
 
     params        fp32 or bf16 tensors, updated in place
     grads         their gradients (fp32 or bf16), read where they are at every step: a backward pass writes into them

@@ -567,6 +567,23 @@ struct TensorList {
     const at::Tensor& at(Py_ssize_t i, const char* name) const { return tensor_of(PySequence_Fast_GET_ITEM(fast, i), name); }
 };
 
+// Memory of a list's tensor.  What a step writes may be no other tensor's, in whole or in part: the records are gone through at once.
+struct StepRange {
+    uintptr_t begin, end;
+    bool written;
+    const char* name;
+};
+const char* written_twice(std::vector<StepRange>& ranges) {   // the name of a tensor that shares such memory, or null
+    std::sort(ranges.begin(), ranges.end(), [](const StepRange& a, const StepRange& b) { return a.begin < b.begin; });
+    uintptr_t any = 0, written = 0;   // ends of those before
+    for (const StepRange& r : ranges) {
+        if (r.begin < (r.written ? any : written)) return r.name;
+        any = std::max(any, r.end);
+        if (r.written) written = std::max(written, r.end);
+    }
+    return nullptr;
+}
+
 // step_list(grads, params, copies, exp_avg, exp_avg_sq, scales) -> (plan on the device, chunks, param_type, grad_type, state_bits, tensors)
 //   all but grads None: a list for the norm only
 PyObject* py_step_list(PyObject*, PyObject* const* v, Py_ssize_t n) {
@@ -594,7 +611,8 @@ PyObject* py_step_list(PyObject*, PyObject* const* v, Py_ssize_t n) {
     const int bits = !step ? 0 : state_type == at::kFloat ? 32 : 8;
     if (step && (scales.fast != nullptr) != (bits == 8)) fail(PyExc_ValueError, "%s go with states in 8 bits", "scales");
     auto tensors = std::make_unique<StepTensors>();
-    const auto pointer = [&](const at::Tensor& t, at::ScalarType type, int64_t size, const char* name) -> void* {
+    std::vector<StepRange> ranges;
+    const auto pointer = [&](const at::Tensor& t, at::ScalarType type, int64_t size, const char* name, bool written = true) -> void* {
         if (!t.defined()) fail(PyExc_TypeError, "%s must be a tensor", name);
         if (t.scalar_type() != type) fail(PyExc_TypeError, "%s: unexpected dtype", name);
         if (!t.is_cuda()) fail(PyExc_TypeError, "%s must be a CUDA tensor", name);
@@ -602,6 +620,8 @@ PyObject* py_step_list(PyObject*, PyObject* const* v, Py_ssize_t n) {
         if (t.device() != device) fail(PyExc_ValueError, "%s: tensors on different devices", name);
         if (t.numel() != size) fail(PyExc_ValueError, "%s: another number of elements than its gradient wants", name);
         tensors->all.emplace_back(t, t.const_data_ptr());
+        const uintptr_t at = reinterpret_cast<uintptr_t>(t.const_data_ptr());
+        if (size > 0) ranges.push_back({at, at + t.nbytes(), written, name});
         return t.data_ptr();
     };
     std::vector<salr_step_tensor_t> table((size_t)count);
@@ -611,7 +631,7 @@ PyObject* py_step_list(PyObject*, PyObject* const* v, Py_ssize_t n) {
         const at::Tensor& g = grads.at(i, "grad");
         t = salr_step_tensor_t{};
         t.count = counts[(size_t)i] = g.defined() ? g.numel() : 0;
-        t.grad = pointer(g, grad_type, t.count, "grad");
+        t.grad = pointer(g, grad_type, t.count, "grad", false);
         if (!step) continue;
         t.param = pointer(params.at(i, "param"), param_type, t.count, "param");
         t.exp_avg = pointer(m.at(i, "exp_avg"), state_type, t.count, "exp_avg");
@@ -622,6 +642,7 @@ PyObject* py_step_list(PyObject*, PyObject* const* v, Py_ssize_t n) {
         if (scales.fast)
             t.scales = static_cast<float*>(pointer(scales.at(i, "scales"), at::kFloat, 2 * ((t.count + salr::kStepBlock - 1) / salr::kStepBlock), "scales"));
     }
+    if (const char* name = written_twice(ranges)) fail(PyExc_ValueError, "%s: shares memory with another tensor of the list", name);
     const size_t need = salr_step_plan_bytes(counts.data(), count);
     if (need == (size_t)-1) check(SALR_ERR_SHAPE, "salr_step_plan");
     at::Tensor host = at::empty({(int64_t)(need < 64 ? 64 : need)}, at::TensorOptions().dtype(at::kByte));

@@ -66,3 +66,28 @@ def test_a_list_outlives_its_owner_until_its_stream_is_done():
     assert not held & {x.data_ptr() for x in taken}
     side.synchronize()
     assert busy and ref.close(float(got[0]), (4.0 * 25000) ** 0.5) and all(bool((p < -0.49).all()) for p in params)
+
+
+def test_memory_that_would_be_written_twice_is_refused():
+    """A tied weight, a slice of another tensor, one tensor in two roles.  Gradients are only read: they may be the same."""
+    import paper_2601_16991_amd as salr
+    flat = torch.zeros(4096, device=dev())
+    p, q, g = flat[:1024], flat[1024:2048], torch.ones(1024, device=dev())
+    new = lambda: torch.zeros(1024, device=dev())
+    for params, grads, kw in (
+        ([p, p], [g, g.clone()], {}),                                              # tied
+        ([flat[:1024], flat[1020:2044]], [g, g.clone()], {}),                      # the last four of one, the first four of the other
+        ([flat[:2048], flat[1024:1032]], [torch.ones(2048, device=dev()), g[:8]], {}),   # one inside the other
+        ([p], [p], {}),                                                            # its own gradient
+        ([p], [g], {"exp_avg": [q], "exp_avg_sq": [q]}),
+        ([p, q], [g, g], {"exp_avg": [new(), p], "exp_avg_sq": [new(), new()]}),
+        ([p], [g], {"copies": [p.view(torch.bfloat16)[:1024]]}),
+        ([p, q], [g, new()], {"exp_avg": [new(), new()], "exp_avg_sq": [new(), g]}),    # a state that is a gradient
+    ):
+        with pytest.raises(ValueError, match="shares memory with another tensor"):
+            salr.AdamW(params, grads, **kw)
+    salr.AdamW([p, q, flat[2048:2056]], [g, g, g[:8]]).step(lr=1.0, step=1)
+    salr.AdamW([p, flat[:0], q], [g, g[:0], g]).step(lr=1.0, step=1)
+    assert float(salr.GradNorm([g, g])(1.0)[0]) == float(torch.tensor(2048.0).sqrt())   # fp32's
+    torch.cuda.synchronize()
+    assert (flat[2056:] == 0).all() and (flat[:2056] != 0).all()
