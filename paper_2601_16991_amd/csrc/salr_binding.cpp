@@ -458,15 +458,20 @@ double double_of(PyObject* o) {
 // The tensors whose addresses a plan holds, so that a call refuses it once one of them has other memory.
 struct StepTensors {
     static constexpr const char* kName = "salr.step_tensors";
-    std::vector<std::pair<at::Tensor, const void*>> all;
+    struct Member {
+        at::Tensor tensor;
+        const void* at;
+        bool written;
+    };
+    std::vector<Member> all;
     std::vector<at::Tensor> states;   // those whose only owner may be the optimiser
     void* home = nullptr;             // the stream that was current when the list was made: its memory goes back to that stream's work
     std::vector<void*> step_on, norm_on;   // other streams that the calls ran on
     static StepTensors& check(PyObject* capsule) {
         auto* t = static_cast<StepTensors*>(PyCapsule_GetPointer(capsule, kName));
         if (!t) throw PyFailure{};
-        for (const auto& [tensor, at] : t->all)
-            if (tensor.const_data_ptr() != at) fail(PyExc_ValueError, "a tensor of the list has other %s than when the list was made", "memory");
+        for (const Member& x : t->all)
+            if (x.tensor.const_data_ptr() != x.at) fail(PyExc_ValueError, "a tensor of the list has other %s than when the list was made", "memory");
         return *t;
     }
     // What the list's owner holds is used on `stream`: it is handed to nobody else before that is done, even if the owner goes first.  (Told
@@ -480,6 +485,11 @@ struct StepTensors {
         if (with_states)
             for (const at::Tensor& t : states) tell(t);
         known.push_back(stream);
+    }
+    // A step changes its tensors in place: autograd sees by their versions that what it saved of them is another value now.
+    void changed() const {
+        for (const Member& x : all)
+            if (x.written && !x.tensor.is_inference()) x.tensor.unsafeGetTensorImpl()->bump_version();
     }
     static PyObject* capsule(std::unique_ptr<StepTensors> t) {
         PyObject* c = PyCapsule_New(t.get(), kName, [](PyObject* o) { delete static_cast<StepTensors*>(PyCapsule_GetPointer(o, kName)); });
@@ -515,6 +525,7 @@ PyObject* py_adamw_step(PyObject*, PyObject* const* v, Py_ssize_t n) {
         st = salr_adamw_step(plan, chunks, pt, gt, bits, lr, b1, b2, eps, decay, step, seed, sp, stream);
     }
     check(st, "salr_adamw_step");
+    held.changed();
     Py_RETURN_NONE;
     SALR_CATCH
 }
@@ -619,7 +630,7 @@ PyObject* py_step_list(PyObject*, PyObject* const* v, Py_ssize_t n) {
         if (!t.is_contiguous()) fail(PyExc_TypeError, "%s must be contiguous", name);
         if (t.device() != device) fail(PyExc_ValueError, "%s: tensors on different devices", name);
         if (t.numel() != size) fail(PyExc_ValueError, "%s: another number of elements than its gradient wants", name);
-        tensors->all.emplace_back(t, t.const_data_ptr());
+        tensors->all.push_back({t, t.const_data_ptr(), written});
         const uintptr_t at = reinterpret_cast<uintptr_t>(t.const_data_ptr());
         if (size > 0) ranges.push_back({at, at + t.nbytes(), written, name});
         return t.data_ptr();

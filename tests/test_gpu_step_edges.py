@@ -91,3 +91,22 @@ def test_memory_that_would_be_written_twice_is_refused():
     assert float(salr.GradNorm([g, g])(1.0)[0]) == float(torch.tensor(2048.0).sqrt())   # fp32's
     torch.cuda.synchronize()
     assert (flat[2056:] == 0).all() and (flat[:2056] != 0).all()
+
+
+def test_autograd_sees_that_a_step_changed_what_it_saved():
+    import paper_2601_16991_amd as salr
+    p = torch.ones(300, device=dev(), requires_grad=True)
+    g, copy = torch.ones(300, device=dev()), torch.empty(300, dtype=torch.bfloat16, device=dev())
+    opt = salr.AdamW([p], [g], copies=[copy])
+    before = [x._version for x in (p, copy, opt.exp_avg[0], opt.exp_avg_sq[0], g)]
+    loss = (p * p).sum()
+    opt.step(lr=1e-2, step=1)
+    assert [x._version - b for x, b in zip((p, copy, opt.exp_avg[0], opt.exp_avg_sq[0], g), before)] == [1, 1, 1, 1, 0]
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    opt.grad_norm(1.0)
+    assert p._version == before[0] + 1
+    with torch.inference_mode():
+        q = torch.ones(300, device=dev())
+        salr.AdamW([q], [g.clone()]).step(lr=1e-2, step=1)
+        assert (q != 1).all()
