@@ -821,7 +821,8 @@ static_assert(sizeof(StepChunk) == 64, "a plan's size is told in these");
 constexpr int64_t kStepBlock = 128;     // elements that share two scales
 constexpr int64_t kStepChunk = 8192;    // elements of a record
 constexpr int64_t kStepMaxCount = (int64_t)1 << 42;
-constexpr int64_t kStepMaxChunks = 536870911LL;   // gridDim.x, four workgroups each
+constexpr int64_t kStepMaxChunks = 536870911LL;   // records, 32 GiB of them
+constexpr int64_t kMostThreads = 0xFFFFFFFFLL;    // of a launch along one dimension
 constexpr int kGradNormBlocks = 512;    // workgroups of the norm, one partial sum each (two to a CU)
 static_assert(256 + kGradNormBlocks * 8 <= SALR_GRAD_NORM_WORKSPACE_BYTES, "room for the partial sums");
 struct AdamwArgs {

@@ -362,8 +362,14 @@ hipError_t launch_adamw(const StepChunk* plan, int64_t chunks, bool param32, boo
                                                  {adamw_kernel<false, true, false>, adamw_kernel<false, true, true>}},
                                                 {{adamw_kernel<true, false, false>, adamw_kernel<true, false, true>},
                                                  {adamw_kernel<true, true, false>, adamw_kernel<true, true, true>}}};
-    hipLaunchKernelGGL(kernels[param32][grad32][eight], dim3((unsigned)(chunks * kStepParts)), dim3(256), 0, stream, plan, h, a.grad_scale);
-    return hipGetLastError();
+    constexpr int64_t kAtOnce = kMostThreads / (kStepParts * 256);   // records: 34 G elements
+    for (int64_t first = 0; first < chunks; first += kAtOnce) {
+        const int64_t here = chunks - first < kAtOnce ? chunks - first : kAtOnce;
+        hipLaunchKernelGGL(kernels[param32][grad32][eight], dim3((unsigned)(here * kStepParts)), dim3(256), 0, stream, plan + first, h, a.grad_scale);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_grad_norm(const StepChunk* plan, int64_t chunks, bool grad32, float max_norm, float* out, void* workspace, hipStream_t stream) {

@@ -110,3 +110,27 @@ def test_autograd_sees_that_a_step_changed_what_it_saved():
         q = torch.ones(300, device=dev())
         salr.AdamW([q], [g.clone()]).step(lr=1e-2, step=1)
         assert (q != 1).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_more_records_than_a_launch_has_threads_for(bits):
+    """2^22 records and some, all of them empty (64 zero bytes) but the first, those around 2^22 and the last."""
+    import paper_2601_16991_amd as salr
+    at = [0, 4194302, 4194303, 4194304, 4194400]
+    gen = torch.Generator().manual_seed(8)
+    grads = [torch.randn(500 + i, generator=gen).to(dev()) for i in range(len(at))]
+    few = salr.AdamW([torch.ones_like(g) for g in grads], grads, bits=bits)
+    many = salr.AdamW([torch.ones_like(g) for g in grads], grads, bits=bits)
+    plan = torch.zeros(at[-1] + 1, 64, dtype=torch.uint8, device=dev())
+    plan[at] = many._list.plan[:64 * len(at)].view(len(at), 64)
+    few.step(lr=1e-2, step=1)
+    l = many._list
+    assert salr.lib().salr_adamw_step(plan.data_ptr(), at[-1] + 1, l.param_type, l.grad_type, l.state_bits, 1e-2, 0.9, 0.999, 1e-8, 0.0, 1, 1, None,
+                                      None) == salr.SALR_OK
+    ws, out = torch.zeros(salr.GRAD_NORM_WORKSPACE_BYTES, dtype=torch.uint8, device=dev()), torch.empty(2, device=dev())
+    assert salr.lib().salr_grad_norm(plan.data_ptr(), at[-1] + 1, l.grad_type, 1.0, out.data_ptr(), ws.data_ptr(), ws.numel(), None) == salr.SALR_OK
+    torch.cuda.synchronize()
+    for a, b in zip(few.params + few.exp_avg + few.exp_avg_sq, many.params + many.exp_avg + many.exp_avg_sq):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    want = float(torch.sqrt(sum(g.double().square().sum() for g in grads)))
+    assert abs(float(out[0]) / want - 1) < 2.0 ** -23
