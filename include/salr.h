@@ -428,7 +428,9 @@ salr_status_t salr_concat_adapters(const uint16_t* const* a_list, const uint16_t
  *     G[t][v] = grad_loss[t] * (exp(l[t][v] - lse[t]) - [v == targets[t]]),   dh = G * w,   dw = G^T * h
  *
  *   h          in   [T, K] bf16 hidden states; K % 8 == 0, K <= 2^22 (else SHAPE)
- *   w          in   [V, K] bf16, the head (rows along K, as the weight of a PyTorch linear); 1 <= V < 2^31 where T > 0 (else SHAPE)
+ *   w          in   [V, K] bf16, the head (rows along K, as the weight of a PyTorch linear); 1 <= V < 2^31 where T > 0 (else SHAPE).
+ *                   SHAPE too where a launch would have 2^32 threads: 2^23 tiles of 128 or 256 tokens and 256 words, T * K / 8 >= 2^32 with
+ *                   a gradient, T >= 2^24 with dw on a vocabulary of at most 256 words
  *   targets    in   [T] int64.  A negative target masks its token: loss, lse, and the gradient are 0 there, whatever the hidden
  *                   state holds (NaN and infinities too).  A target >= V gives NaN in the token's loss, lse and gradients.
  *   grad_loss  in   [T] fp32, the gradient of what is minimised with respect to loss[t] (1 / tokens for the mean); NULL: ones

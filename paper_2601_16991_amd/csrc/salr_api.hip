@@ -47,12 +47,12 @@ bool qsalr_decodes_codes(int64_t M, int64_t K, int64_t N, int64_t nnz) {
 bool misaligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 bool is_type(salr_type_t t) { return t == SALR_F32 || t == SALR_BF16; }
 
-// Sizes that salr_linear_cross_entropy takes: whole vectors along K, offsets within a tile of 256 rows and all grids in 31 bits.
-bool cross_entropy_sizes_ok(int64_t T, int64_t K, int64_t V) {
-    constexpr int64_t most = 2147483647LL, tile = 256;
+// Sizes that salr_linear_cross_entropy takes: whole vectors along K, offsets within a tile of 256 rows in 32 bits, launches that a GPU takes.
+bool cross_entropy_plan(int64_t T, int64_t K, int64_t V, bool want_dh, bool want_dw, salr::CePlan* plan) {
+    constexpr int64_t most = 2147483647LL;
     if (K % 8 != 0 || K > ((int64_t)1 << 22) || T > most || V > most || (T > 0 && V < 1)) return false;
-    const int64_t m = (T + 15) / 16, n = (V + tile - 1) / tile, k = (K + tile - 1) / tile;
-    return (m == 0 || n <= most / m) && (k == 0 || n <= most / k) && (k == 0 || m <= most / k / 256) && T * (K / 8 + 1) / 256 <= most;
+    *plan = salr::ce_plan(T, K, V, want_dh, want_dw);
+    return salr::ce_launches_fit(*plan, T, K, V, want_dh, want_dw);
 }
 
 }  // namespace
@@ -469,8 +469,8 @@ salr_status_t salr_sparse_lowrank_linear_backward(const uint16_t* x, const uint1
 }
 
 size_t salr_linear_cross_entropy_workspace_bytes(int64_t T, int64_t K, int64_t V, int want_dh, int want_dw) {
-    if (T < 0 || K < 0 || V < 0 || !cross_entropy_sizes_ok(T, K, V)) return 0;
-    return salr::ce_plan(T, K, V, want_dh != 0, want_dw != 0).bytes;
+    salr::CePlan plan;
+    return T < 0 || K < 0 || V < 0 || !cross_entropy_plan(T, K, V, want_dh != 0, want_dw != 0, &plan) ? 0 : plan.bytes;
 }
 
 salr_status_t salr_linear_cross_entropy(const uint16_t* h, int64_t T, int64_t K, const uint16_t* w, int64_t V, const int64_t* targets,
@@ -481,8 +481,8 @@ salr_status_t salr_linear_cross_entropy(const uint16_t* h, int64_t T, int64_t K,
     if (misaligned(h, 16) || misaligned(w, 16) || misaligned(dh, 16) || misaligned(dw, 16) || misaligned(workspace, 256) || misaligned(targets, 8) ||
         misaligned(grad_loss, 4) || misaligned(loss, 4) || misaligned(lse, 4))
         return SALR_ERR_INVALID_ARG;
-    if (!cross_entropy_sizes_ok(T, K, V)) return SALR_ERR_SHAPE;
-    const salr::CePlan plan = salr::ce_plan(T, K, V, dh != nullptr, dw != nullptr);
+    salr::CePlan plan;
+    if (!cross_entropy_plan(T, K, V, dh != nullptr, dw != nullptr, &plan)) return SALR_ERR_SHAPE;
     if (workspace_bytes < plan.bytes) return SALR_ERR_CAPACITY;
     if (plan.bytes > 0 && !workspace) return SALR_ERR_INVALID_ARG;
     if (T == 0 && (!dw || V == 0)) return SALR_OK;

@@ -551,6 +551,21 @@ CePlan ce_plan(int64_t T, int64_t K, int64_t V, bool want_dh, bool want_dw) {
     return p;
 }
 
+// Whether every launch of such a call keeps below 2^32 threads.  (Tiles are taken at the 512 threads of the largest; the narrow ones of 256 are
+// few.)
+bool ce_launches_fit(const CePlan& p, int64_t T, int64_t K, int64_t V, bool want_dh, bool want_dw) {
+    const auto tiles_fit = [](int64_t a, int64_t b, int64_t c) {
+        constexpr int64_t most = kMostThreads / 512 / kProductXcds * kProductXcds;   // (the grid is a multiple of the XCDs)
+        return a == 0 || b == 0 || (b <= most / a && c <= most / (a * b));
+    };
+    const int64_t k_tiles = ceil_div(K, 256), columns = want_dh && !want_dw ? (V < p.piece ? V : p.piece) : V;
+    if (!tiles_fit(p.m_tiles, ceil_div(columns, p.width), 1) || T > kMostThreads / 1024 * 64) return false;
+    if (want_dh && !tiles_fit(ceil_div(T, p.dh_rows), k_tiles, p.slices)) return false;
+    if (want_dw && !tiles_fit(ceil_div(V < p.piece ? V : p.piece, 256), k_tiles, 1)) return false;
+    if ((want_dh || want_dw) && T * (K / 8) > kMostThreads / 256 * 256) return false;
+    return !p.holds_e32 || T <= kMostThreads / 256;
+}
+
 namespace {
 
 struct CeRun {   // one call

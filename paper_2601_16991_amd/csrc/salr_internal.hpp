@@ -861,6 +861,7 @@ struct CePlan {
     size_t bytes;
 };
 CePlan ce_plan(int64_t T, int64_t K, int64_t V, bool want_dh, bool want_dw);
+bool ce_launches_fit(const CePlan& p, int64_t T, int64_t K, int64_t V, bool want_dh, bool want_dw);
 hipError_t launch_cross_entropy(const CeArgs& a, void* workspace);
 
 }  // namespace salr
