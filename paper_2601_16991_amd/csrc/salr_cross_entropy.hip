@@ -29,7 +29,7 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
 enum CeMode { kStatistics, kExponentials, kExponentials32, kGradients };   // what a tile of logits becomes: nothing but its statistics, E in bf16 or fp32, G
 
 struct CeRow {   // of a token, once its statistics are complete
-    float M, alpha, beta;   // G = alpha 2^(l log2 e - M), of the target's column -beta
+    float M, alpha, beta;   // G = alpha 2^(l log2 e - M), of the target's column -beta; M at or above the reference of E by a whole number
     int32_t live;
 };
 
@@ -318,7 +318,7 @@ __global__ __launch_bounds__(1024) void ce_rows_kernel(CeRowArgs a) {
     // S' = sum of 2^(l log2 e - M) over the other columns, e the target's (M may lie below the target's own exponent)
     const int64_t target = a.targets[t];
     const float nan = __builtin_nanf("");
-    float loss = 0.f, lse = 0.f, alpha = 0.f, beta = 0.f;
+    float loss = 0.f, lse = 0.f, alpha = 0.f, beta = 0.f, above = M;
     if (target >= a.V) {
         loss = lse = alpha = beta = nan;
     } else if (target >= 0) {
@@ -328,13 +328,16 @@ __global__ __launch_bounds__(1024) void ce_rows_kernel(CeRowArgs a) {
         lse = kLn2 * (M + top) + logf(total);
         const float ratio = rest / e;   // (where the target is far below the others it leaves fp32)
         loss = ratio < 1e6f ? log1pf(ratio) : lse - l;
-        alpha = sum == 0.f ? 0.f : times_power(gl / total, -top);
+        // alpha times 2^-top would leave fp32 where the target is far above the others: top goes to M, as long as that is exact
+        const bool exact = fabsf(M) <= 0x1p23f && top <= 1000.f;
+        above = exact ? M + top : M;
+        alpha = sum == 0.f ? 0.f : times_power(gl / total, exact ? 0.f : -top);
         beta = gl * (rest / total);
         if (!(total > 0.f && total < inf)) loss = lse = alpha = beta = nan;
     }
     a.loss[t] = loss;
     a.lse[t] = lse;
-    a.rows[t] = CeRow{target >= 0 ? M : 0.f, alpha, beta, target >= 0};   // (2^-M of a masked token may leave fp32, and 0 times infinity is NaN)
+    a.rows[t] = CeRow{target >= 0 ? above : 0.f, alpha, beta, target >= 0};   // (2^-M of a masked token may leave fp32, and 0 times infinity is NaN)
 }
 
 // G from E in fp32 and the tiles' references, eight columns a thread, up to a whole step of columns.  Bound by memory (1111 x 50003: 60 us, 5.6 TB/s).
@@ -403,8 +406,8 @@ __global__ __launch_bounds__(Shape::kThreads) void ce_dh_kernel(const uint16_t* 
 // dh from the slices' sums, eight columns a thread.  kPlain: the sums are dh itself.  Bound by memory (4096 x 4096, one slice: 21 us, 5.6 TB/s).
 template <bool kPlain>
 __global__ __launch_bounds__(256) void ce_dh_finish_kernel(const float* __restrict__ sums, int slices, int64_t T, int64_t K, const CeRow* __restrict__ rows,
-                                                           const int64_t* __restrict__ targets, int64_t V, const uint16_t* __restrict__ w,
-                                                           uint16_t* __restrict__ dh) {
+                                                           const float2* __restrict__ running, const int64_t* __restrict__ targets, int64_t V,
+                                                           const uint16_t* __restrict__ w, uint16_t* __restrict__ dh) {
     const int64_t per_row = K / 8, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (id >= T * per_row) return;
     const int64_t t = id / per_row, k = (id - t * per_row) * 8;
@@ -418,9 +421,10 @@ __global__ __launch_bounds__(256) void ce_dh_finish_kernel(const float* __restri
         x[0] += a.x, x[1] += a.y, x[2] += a.z, x[3] += a.w, x[4] += b.x, x[5] += b.y, x[6] += b.z, x[7] += b.w;
     }
     if constexpr (!kPlain) {
+        const float reference = running[t].x, by = (reference == -__builtin_inff() ? 0.f : reference) - of.M;   // of E, below of.M
         const uint4 wt = target >= 0 && target < V ? *reinterpret_cast<const uint4*>(w + target * K + k) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int c = 0; c < 8; ++c) x[c] = of.alpha * x[c] - of.beta * bf16_bits_to_f32(unit_elem(wt, c));
+        for (int c = 0; c < 8; ++c) x[c] = times_power(of.alpha * x[c], by) - of.beta * bf16_bits_to_f32(unit_elem(wt, c));
     }
     uint4 q = make_uint4(pack_two_bf16(x[0], x[1]), pack_two_bf16(x[2], x[3]), pack_two_bf16(x[4], x[5]), pack_two_bf16(x[6], x[7]));
     if (target < 0) q = make_uint4(0, 0, 0, 0);
@@ -631,7 +635,7 @@ struct CeRun {   // one call
     void dh_finish() const {
         if (units() == 0) return;
         hipLaunchKernelGGL(ce_dh_finish_kernel<kPlain>, dim3(units()), dim3(256), 0, a.stream, at<const float>(p.sums), (int)p.slices, a.T, a.K,
-                           at<const CeRow>(p.of_rows), a.targets, a.V, a.w, a.dh);
+                           at<const CeRow>(p.of_rows), at<const float2>(p.running), a.targets, a.V, a.w, a.dh);
     }
     void gradients() const {
         const unsigned across = (unsigned)ceil_div(a.V, 2048);
