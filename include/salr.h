@@ -443,7 +443,7 @@ salr_status_t salr_concat_adapters(const uint16_t* const* a_list, const uint16_t
  *
  * Precision: fp32 sums, maxima and logits; the probabilities are rounded to bf16 once, as operands of the matrix cores, and dh
  * and dw at the end.  The probability of the target stays out of that: 1 - p is summed, not subtracted.  A logit that is NaN or
- * +infinite makes the token's results NaN.  Results are the same bit for bit from call to call.
+ * +infinite (2^127 and more may count as that) makes the token's results NaN; one of -infinity, or far below the others, has probability 0.  Results are the same bit for bit from call to call.
  * Errors: INVALID_ARG (null where data is required, negative size, a pointer that is not 16-byte aligned (targets, grad_loss, loss and lse:
  * not aligned to their type)), SHAPE, CAPACITY, HIP.  The workspace query returns 0 for sizes the call would refuse.
  */

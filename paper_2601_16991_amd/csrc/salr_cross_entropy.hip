@@ -30,7 +30,7 @@ enum CeMode { kStatistics, kExponentials, kExponentials32, kGradients };   // wh
 
 struct CeRow {   // of a token, once its statistics are complete
     float M, alpha, beta;   // G = alpha 2^(l log2 e - M), of the target's column -beta; M at or above the reference of E by a whole number
-    int32_t live;
+    int32_t live;   // 0: masked, 2: M is twice a large logit, else 1
 };
 
 __device__ __forceinline__ uint32_t pack_two_bf16(float a, float b) {
@@ -41,8 +41,12 @@ __device__ __forceinline__ uint32_t pack_two_bf16(float a, float b) {
 
 // The reference of a tile's row: the multiple of 128 next to its largest exponent, so that its E lie below 2^65.  bf16 and fp32 hold those
 // as well as numbers below 1, and hardly any row has tiles of two references: with logits within 44 of zero it is 0.
-constexpr float kReferenceStep = 128.f;
-__device__ __forceinline__ float tile_exponent(float most) { return kReferenceStep * rintf(most * (kLog2e / kReferenceStep)); }
+// Logits of 2^30 and more (-1e30 rules a word out) are 128 or further apart where they differ, and fp32 has no multiples of 128 much above: there
+// the reference is twice the largest logit, E 1 where l is that one, else 0.  (2^127 and more counts as infinite.)
+constexpr float kReferenceStep = 128.f, kLargeLogit = 0x1p30f, kLargeReference = 2.f * kLargeLogit;
+__device__ __forceinline__ float tile_exponent(float most) {
+    return fabsf(most) < kLargeLogit ? kReferenceStep * rintf(most * (kLog2e / kReferenceStep)) : 2.f * most;
+}
 
 // x 2^by for a whole `by` that may be -infinity; 2^-128 is no normal number, so not by multiplying.
 __device__ __forceinline__ float times_power(float x, float by) { return __builtin_amdgcn_ldexpf(x, (int)fminf(fmaxf(by, -1000.f), 1000.f)); }
@@ -132,7 +136,11 @@ __global__ __launch_bounds__(Shape::kThreads) void ce_logits_kernel(const uint16
             }
         }
     }
+    // Whether this wave has to look for large references.  One with logits below 2^30 alone has not: where the tile's is large all the same, it is
+    // that of a far larger logit, and E is 0.
+    bool some_large = false;
     if constexpr (kMode != kGradients) {
+        bool large = false;
 #pragma unroll
         for (int i = 0; i < kMI; ++i) {
             float most = -__builtin_inff();
@@ -141,8 +149,10 @@ __global__ __launch_bounds__(Shape::kThreads) void ce_logits_kernel(const uint16
 #pragma unroll
                 for (int r = 0; r < 4; ++r) most = fmaxf(most, acc[i][j][r]);
             most = over_groups(most, [](float a, float b) { return fmaxf(a, b); });
+            large |= fabsf(most) >= kLargeLogit;   // (-infinity, no column: rows past the end are zeros)
             if (g == 0) largest[wn * kM + 16 * (wm * kMI + i) + i16] = most;
         }
+        some_large = __any(large);
         __syncthreads();
     }
 #pragma unroll
@@ -153,11 +163,12 @@ __global__ __launch_bounds__(Shape::kThreads) void ce_logits_kernel(const uint16
         if constexpr (kMode == kGradients) {
             if (m0 + row < T) of = rows[m0 + row];
             M = of.M, alpha = of.alpha;
-            if (__any(!of.live)) {   // a masked token: M and alpha are 0 in its CeRow, l here, whatever h held
+            if (__any(of.live != 1)) {   // a masked token: M and alpha are 0 in its CeRow, l here, whatever h held
 #pragma unroll
                 for (int j = 0; j < kNI; ++j)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) acc[i][j][r] = of.live ? acc[i][j][r] : 0.f;
+                some_large = __any(of.live == 2);
             }
         } else {
             float most = largest[row];
@@ -165,6 +176,16 @@ __global__ __launch_bounds__(Shape::kThreads) void ce_logits_kernel(const uint16
             for (int q = 1; q < kWN; ++q) most = fmaxf(most, largest[q * kM + row]);
             M = tile_exponent(most);
             M = M == -__builtin_inff() ? 0.f : M;   // (nothing in the row: every E is 2^-inf)
+        }
+        if (__builtin_expect(some_large, 0)) {
+            const bool large = fabsf(M) >= kLargeReference && fabsf(M) < __builtin_inff();
+            const float most = 0.5f * M;
+#pragma unroll
+            for (int j = 0; j < kNI; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (large) acc[i][j][r] = acc[i][j][r] == most ? 0.f : -__builtin_inff();
+            M = large ? 0.f : M;
         }
         float sum = 0.f;
 #pragma unroll
@@ -283,8 +304,9 @@ __global__ __launch_bounds__(1024) void ce_rows_kernel(CeRowArgs a) {
         // four at a time, its lanes through the columns.
         for (int n0 = 0; n0 < a.n_tiles; n0 += kParts) {
             const int n = n0 + first_tile;
-            const float behind = here && n < a.n_tiles ? M - a.stats[(int64_t)n * a.T + t].x : 0.f;
-            uint64_t todo = __ballot(behind > 0.f && behind < inf);
+            const float reference = here && n < a.n_tiles ? a.stats[(int64_t)n * a.T + t].x : -inf;   // (-infinity: every E is 0)
+            const float behind = reference > -inf ? M - reference : 0.f;
+            uint64_t todo = __ballot(behind > 0.f);
             while (todo != 0) {
                 uint2* at[4] = {};
                 uint2 q[4];
@@ -322,10 +344,13 @@ __global__ __launch_bounds__(1024) void ce_rows_kernel(CeRowArgs a) {
     if (target >= a.V) {
         loss = lse = alpha = beta = nan;
     } else if (target >= 0) {
-        const float l = a.target_logit[t], up = fmaf(l, kLog2e, -M), top = up > 0.f || all.M == -inf ? ceilf(up) : 0.f;
+        const float l = a.target_logit[t], off = l - 0.5f * M;
+        const bool large = fabsf(M) >= kLargeReference;   // M is twice a logit then
+        const float up = !large ? fmaf(l, kLog2e, -M) : off > kLargeLogit && l < inf ? kLargeLogit : off * kLog2e;
+        const float top = up > 0.f || all.M == -inf ? ceilf(up) : 0.f;
         const float e = __builtin_amdgcn_exp2f(up - top), rest = times_power(sum, -top), total = rest + e;
         const float gl = a.grad_loss != nullptr ? a.grad_loss[t] : 1.f;
-        lse = kLn2 * (M + top) + logf(total);
+        lse = (!large ? kLn2 * (M + top) : top > 0.f ? l : 0.5f * M) + logf(total);
         const float ratio = rest / e;   // (where the target is far below the others it leaves fp32)
         loss = ratio < 1e6f ? log1pf(ratio) : lse - l;
         // alpha times 2^-top would leave fp32 where the target is far above the others: top goes to M, as long as that is exact
@@ -337,7 +362,7 @@ __global__ __launch_bounds__(1024) void ce_rows_kernel(CeRowArgs a) {
     }
     a.loss[t] = loss;
     a.lse[t] = lse;
-    a.rows[t] = CeRow{target >= 0 ? above : 0.f, alpha, beta, target >= 0};   // (2^-M of a masked token may leave fp32, and 0 times infinity is NaN)
+    a.rows[t] = CeRow{target >= 0 ? above : 0.f, alpha, beta, target < 0 ? 0 : fabsf(M) >= kLargeReference ? 2 : 1};   // (2^-M of a masked token may leave fp32, and 0 times infinity is NaN)
 }
 
 // G from E in fp32 and the tiles' references, eight columns a thread, up to a whole step of columns.  Bound by memory (1111 x 50003: 60 us, 5.6 TB/s).
