@@ -1,5 +1,5 @@
 """Fine-tunes the adapters of SALR layers under a frozen language-model head: the layers' forward and backward pass, the head's
-loss without its logits, clipping, and an optimiser step over all adapters, each on the GPU through the library's kernels.
+loss without storing its logits, clipping, and an optimiser step over all adapters, each on the GPU through the library's kernels.
 
     python examples/finetune_adapters.py --steps 60 --bits 8
 

@@ -422,7 +422,8 @@ salr_status_t salr_concat_adapters(const uint16_t* const* a_list, const uint16_t
  * What a fine-tuning step needs on either side of the layers: the loss of a language-model head with the gradient that
  * salr_sparse_lowrank_linear_backward starts from, the norm of the gradients it ends with, and the optimiser step that uses them.
  *
- * salr_linear_cross_entropy -- softmax cross entropy of the logits l = h * w^T [T, V], which are never stored:
+ * salr_linear_cross_entropy -- softmax cross entropy of the logits l = h * w^T [T, V].  They are not stored, and of their
+ * exponentials (where a gradient is wanted) a bounded part at a time, see workspace:
  *
  *     lse[t] = log sum_v exp(l[t][v]),   loss[t] = lse[t] - l[t][targets[t]],
  *     G[t][v] = grad_loss[t] * (exp(l[t][v] - lse[t]) - [v == targets[t]]),   dh = G * w,   dw = G^T * h
@@ -437,9 +438,15 @@ salr_status_t salr_concat_adapters(const uint16_t* const* a_list, const uint16_t
  *   loss, lse  out  [T] fp32
  *   dh         out  [T, K] bf16; NULL = not computed
  *   dw         out  [V, K] bf16; NULL = not computed (a frozen head)
- *   workspace  --   salr_linear_cross_entropy_workspace_bytes(T, K, V, want_dh, want_dw) bytes, 256-byte aligned; contents
- *                   unspecified.  It holds what the logits of a piece of the vocabulary become, up to 256 MiB (with dw up to 768 MiB), whatever V,
- *                   8 bytes per token and 256 (few tokens: 64) words of the vocabulary, and dh in fp32 (once or a few times)
+ *   workspace  --   salr_linear_cross_entropy_workspace_bytes(T, K, V, want_dh, want_dw) bytes, 256-byte aligned; contents unspecified.
+ *                   It holds, whatever V:
+ *                     a gradient wanted   the exponentials of a piece of the logits in bf16, 2 bytes each: up to 256 MiB (512 T bytes where that
+ *                                         is more: a piece has 256 words at least)
+ *                     dw                  where all T * V logits are one piece (128 M of them), the same in fp32 as well: 6 bytes a logit in
+ *                                         all, up to 768 MiB, more than the logits would take.  And a copy of h, 2 T K bytes
+ *                     dh                  its sums in fp32, 4 T K bytes, 1 to 16 times (up to 64 tokens: 64)
+ *                   and 32 bytes a token with 8 per token and 256 words (64 words where tokens or words are few) of the vocabulary, with dh alone
+ *                   of a piece
  *
  * Precision: fp32 sums, maxima and logits; the probabilities are rounded to bf16 once, as operands of the matrix cores, and dh
  * and dw at the end.  The probability of the target stays out of that: 1 - p is summed, not subtracted.  A logit that is NaN or

@@ -648,7 +648,9 @@ def salr_linear_cross_entropy(h: torch.Tensor, w: torch.Tensor, targets: torch.T
 
 
 def linear_cross_entropy(h, w, targets, grad_loss=None, need_dh=True, need_dw=False, workspace=None):
-    """(loss, lse, dh, dw) of softmax cross entropy on the logits h w^T, which are never stored; entries not asked for are None.
+    """(loss, lse, dh, dw) of softmax cross entropy on the logits h w^T, which are not stored; entries not asked for are None.  The workspace
+    (allocated for the call where it is None) is small for the loss alone, with dh about 256 MiB at most, with dw up to 768 MiB, each with a few
+    times the size of h: see salr_linear_cross_entropy_workspace_bytes.
 
     h [T, K] and w [V, K] bf16, targets [T] int64 (negative: the token is masked), grad_loss [T] fp32 (None: ones) the gradient of
     what is minimised with respect to each token's loss."""

@@ -1,4 +1,4 @@
-// Softmax cross entropy of a language-model head, l = h w^T, without keeping the logits:
+// Softmax cross entropy of a language-model head, l = h w^T, without storing the logits:
 //
 //   loss_t = lse_t - l[t, target_t],   dh = G w,   dw = G^T h,   G = grad_t (softmax(l) - onehot(target))
 //

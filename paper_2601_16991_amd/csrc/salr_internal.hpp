@@ -836,7 +836,7 @@ void write_step_plan(const salr_step_tensor_t* tensors, int64_t n, bool param32,
 hipError_t launch_adamw(const StepChunk* plan, int64_t chunks, bool param32, bool grad32, bool eight, const AdamwArgs& a, hipStream_t stream);
 hipError_t launch_grad_norm(const StepChunk* plan, int64_t chunks, bool grad32, float max_norm, float* out, void* workspace, hipStream_t stream);
 
-// ---- Softmax cross entropy of a head without its logits (salr_cross_entropy.hip)
+// ---- Softmax cross entropy of a head, logits not stored (salr_cross_entropy.hip)
 constexpr int64_t kCePieceBytes = (int64_t)256 << 20;   // E of a piece of the vocabulary, see ce_plan
 struct CeArgs {
     const uint16_t* h;

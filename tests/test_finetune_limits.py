@@ -42,3 +42,25 @@ MOST_TILES = (1 << 23) - 8
 def test_launches_fit(salr, T, K, V, dh, dw, taken):
     assert _call(salr, T, K, V, dh, dw) == (salr.SALR_ERR_CAPACITY if taken else salr.SALR_ERR_SHAPE)
     assert (salr.salr_linear_cross_entropy_workspace_bytes(T, K, V, dh, dw) > 0) == taken
+
+
+@pytest.mark.parametrize("dh,dw", [(False, False), (True, False), (False, True), (True, True)])
+@pytest.mark.parametrize("T,K,V", [(1, 4096, 131072), (48, 512, 4099), (64, 8192, 131072), (1111, 2720, 50003), (2000, 2048, 65536), (4096, 4096, 131072),
+                                   (16384, 8192, 131072), (524288, 64, 300), (600000, 64, 256), (600000, 64, 5000), (1, 8, 1 << 30)])
+def test_workspace_is_what_its_terms_add_up_to(salr, T, K, V, dh, dw):
+    """The terms that the header names, each at its most: nothing grows with T * V but the statistics, 8 bytes per token and tile of words."""
+    words = (V + 255) // 256 * 256
+    cap = max(1, (256 << 20) // (512 * T)) * 256      # words of the largest piece
+    one_piece = words <= cap
+    need = 32 * T + 8 * T * (min(words, cap) if dh and not dw else words) // (64 if T <= 64 or words <= 96 * 256 else 256)
+    if dh or dw:
+        need += 2 * T * min(words, cap)
+    assert not (dh or dw) or 2 * T * min(words, cap) <= max(256 << 20, 512 * T)
+    if dw:
+        need += (4 * T * words if one_piece else 0) + 2 * T * K
+    if dh:
+        need += 4 * T * K * (64 if T <= 64 else 16)
+    got = salr.salr_linear_cross_entropy_workspace_bytes(T, K, V, dh, dw)
+    assert 0 < got <= need + 9 * 256
+    if dw and one_piece:
+        assert got >= 6 * T * V
