@@ -30,7 +30,7 @@ enum CeMode { kStatistics, kExponentials, kExponentials32, kGradients };   // wh
 
 struct CeRow {   // of a token, once its statistics are complete
     float M, alpha, beta;   // G = alpha 2^(l log2 e - M), of the target's column -beta; M at or above the reference of E by a whole number
-    int32_t live;   // 0: masked, 2: M is twice a large logit, else 1
+    int32_t live;
 };
 
 __device__ __forceinline__ uint32_t pack_two_bf16(float a, float b) {
@@ -40,12 +40,16 @@ __device__ __forceinline__ uint32_t pack_two_bf16(float a, float b) {
 }
 
 // The reference of a tile's row: the multiple of 128 next to its largest exponent, so that its E lie below 2^65.  bf16 and fp32 hold those
-// as well as numbers below 1, and hardly any row has tiles of two references: with logits within 44 of zero it is 0.
+// as well as numbers below 1, and hardly any row has tiles of two references: with logits within 44 of zero it is 0.  What is 2^-62 of the row's largest
+// and less may be 0 then, which a sum over the words does not see.  E in fp32, which becomes operands of a sum over the tokens (dw: a word's may all be
+// small), is kept from the largest exponent itself on, down to 2^-126 of it.
 // Logits of 2^30 and more (-1e30 rules a word out) are 128 or further apart where they differ, and fp32 has no multiples of 128 much above: there
 // the reference is twice the largest logit, E 1 where l is that one, else 0.  (2^127 and more counts as infinite.)
 constexpr float kReferenceStep = 128.f, kLargeLogit = 0x1p30f, kLargeReference = 2.f * kLargeLogit;
+template <int kMode>
 __device__ __forceinline__ float tile_exponent(float most) {
-    return fabsf(most) < kLargeLogit ? kReferenceStep * rintf(most * (kLog2e / kReferenceStep)) : 2.f * most;
+    constexpr float kStep = kMode == kExponentials32 ? 1.f : kReferenceStep;
+    return fabsf(most) < kLargeLogit ? kStep * rintf(most * (kLog2e / kStep)) : 2.f * most;
 }
 
 // x 2^by for a whole `by` that may be -infinity; 2^-128 is no normal number, so not by multiplying.
@@ -136,11 +140,7 @@ __global__ __launch_bounds__(Shape::kThreads) void ce_logits_kernel(const uint16
             }
         }
     }
-    // Whether this wave has to look for large references.  One with logits below 2^30 alone has not: where the tile's is large all the same, it is
-    // that of a far larger logit, and E is 0.
-    bool some_large = false;
     if constexpr (kMode != kGradients) {
-        bool large = false;
 #pragma unroll
         for (int i = 0; i < kMI; ++i) {
             float most = -__builtin_inff();
@@ -149,10 +149,8 @@ __global__ __launch_bounds__(Shape::kThreads) void ce_logits_kernel(const uint16
 #pragma unroll
                 for (int r = 0; r < 4; ++r) most = fmaxf(most, acc[i][j][r]);
             most = over_groups(most, [](float a, float b) { return fmaxf(a, b); });
-            large |= fabsf(most) >= kLargeLogit;   // (-infinity, no column: rows past the end are zeros)
             if (g == 0) largest[wn * kM + 16 * (wm * kMI + i) + i16] = most;
         }
-        some_large = __any(large);
         __syncthreads();
     }
 #pragma unroll
@@ -163,37 +161,28 @@ __global__ __launch_bounds__(Shape::kThreads) void ce_logits_kernel(const uint16
         if constexpr (kMode == kGradients) {
             if (m0 + row < T) of = rows[m0 + row];
             M = of.M, alpha = of.alpha;
-            if (__any(of.live != 1)) {   // a masked token: M and alpha are 0 in its CeRow, l here, whatever h held
+            if (__any(!of.live)) {   // a masked token: M and alpha are 0 in its CeRow, l here, whatever h held
 #pragma unroll
                 for (int j = 0; j < kNI; ++j)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) acc[i][j][r] = of.live ? acc[i][j][r] : 0.f;
-                some_large = __any(of.live == 2);
             }
         } else {
             float most = largest[row];
 #pragma unroll
             for (int q = 1; q < kWN; ++q) most = fmaxf(most, largest[q * kM + row]);
-            M = tile_exponent(most);
+            M = tile_exponent<kMode>(most);
             M = M == -__builtin_inff() ? 0.f : M;   // (nothing in the row: every E is 2^-inf)
         }
-        if (__builtin_expect(some_large, 0)) {
-            const bool large = fabsf(M) >= kLargeReference && fabsf(M) < __builtin_inff();
-            const float most = 0.5f * M;
-#pragma unroll
-            for (int j = 0; j < kNI; ++j)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (large) acc[i][j][r] = acc[i][j][r] == most ? 0.f : -__builtin_inff();
-            M = large ? 0.f : M;
-        }
+        const bool large = fabsf(M) >= kLargeReference;   // E = 2^(l - that logit): 1 or 0
+        const float slope = large ? 1.f : kLog2e, origin = large ? 0.5f * M : M;
         float sum = 0.f;
 #pragma unroll
         for (int j = 0; j < kNI; ++j) {
             float e[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                e[r] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], kLog2e, -M));
+                e[r] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], slope, -origin));
                 if constexpr (kMode == kGradients) e[r] *= alpha;
             }
             if constexpr (kMode == kGradients) {
@@ -224,7 +213,7 @@ __global__ __launch_bounds__(Shape::kThreads) void ce_logits_kernel(const uint16
                 most = fmaxf(most, largest[q * kM + row]);
                 sum += sums[q * kM + row];
             }
-            stats[(int64_t)at.nt * T + m0 + row] = make_float2(tile_exponent(most), sum);
+            stats[(int64_t)at.nt * T + m0 + row] = make_float2(tile_exponent<kMode>(most), sum);
         }
     }
     if constexpr (kBf16) {
@@ -260,7 +249,7 @@ struct CeRowArgs {
     CeRow* rows;
 };
 
-// Maximum of references and the sum with respect to it.  References are multiples of 128, -infinity (no column), +infinity or NaN.
+// Maximum of references and the sum with respect to it.  References are whole numbers, -infinity (no column) or +infinity.
 struct CeSum {
     float M, sum, least;   // least: smallest reference of a tile that has one
     __device__ __forceinline__ void add(float M2, float sum2, float least2) {
@@ -353,16 +342,18 @@ __global__ __launch_bounds__(1024) void ce_rows_kernel(CeRowArgs a) {
         lse = (!large ? kLn2 * (M + top) : top > 0.f ? l : 0.5f * M) + logf(total);
         const float ratio = rest / e;   // (where the target is far below the others it leaves fp32)
         loss = ratio < 1e6f ? log1pf(ratio) : lse - l;
-        // alpha times 2^-top would leave fp32 where the target is far above the others: top goes to M, as long as that is exact
-        const bool exact = fabsf(M) <= 0x1p23f && top <= 1000.f;
-        above = exact ? M + top : M;
-        alpha = sum == 0.f ? 0.f : times_power(gl / total, exact ? 0.f : -top);
+        // 2^-top and the exponent of the sum go to M, as long as that is exact, so that 2^(l log2 e - M) is as small as G is and no smaller:
+        // alpha times 2^-top would leave fp32 where the target is far above the others, 2^(l log2 e - M) where M is far above them all
+        const bool exact = fabsf(M) <= 0x1p23f && top <= 1000.f && total > 0.f && total < inf;
+        const float whole = exact ? (float)__builtin_amdgcn_frexp_expf(total) : 0.f;
+        above = exact ? M + top + whole : M;
+        alpha = sum == 0.f ? 0.f : exact ? gl / times_power(total, -whole) : times_power(gl / total, -top);
         beta = gl * (rest / total);
         if (!(total > 0.f && total < inf)) loss = lse = alpha = beta = nan;
     }
     a.loss[t] = loss;
     a.lse[t] = lse;
-    a.rows[t] = CeRow{target >= 0 ? above : 0.f, alpha, beta, target < 0 ? 0 : fabsf(M) >= kLargeReference ? 2 : 1};   // (2^-M of a masked token may leave fp32, and 0 times infinity is NaN)
+    a.rows[t] = CeRow{target >= 0 ? above : 0.f, alpha, beta, target >= 0};   // (2^-M of a masked token may leave fp32, and 0 times infinity is NaN)
 }
 
 // G from E in fp32 and the tiles' references, eight columns a thread, up to a whole step of columns.  Bound by memory (1111 x 50003: 60 us, 5.6 TB/s).

@@ -139,3 +139,33 @@ def test_large_logits_in_several_pieces():
             off = 2.0 ** -6 * ((G7.abs() * g[7].abs()).double()[:, None] * h[7].double().abs()[None] + clean.double().abs()) + 1e-4   # (fp32 sums of 4200 terms)
             assert ((dw.double() - want).abs() <= off).all()
             assert (dw[20000:21000] == 0).all()
+
+
+@pytest.mark.parametrize("need_dw", [False, True])
+def test_references_that_rise_and_fall_from_piece_to_piece(need_dw):
+    """Three pieces of the vocabulary, in blocks of 50000 words whose logits lie near -60, 0 and 60 in turn, for other tokens near 60, 0 and
+    -60: the running reference (-128, 0, 128) rises late, early or in between, and tiles fall behind it."""
+    T, K, V = 1100, 32, 260003
+    assert 2 * ((256 << 20) // (512 * T)) * 256 < V <= 3 * ((256 << 20) // (512 * T)) * 256
+    h, w, t, g = base._inputs(T, K, V, 51)
+    w[:, 0] = (torch.arange(V) // 50000 % 3 - 1).bfloat16()
+    h[:, 0] = 0.0
+    h[0::4, 0] = 60.0
+    h[2::4, 0] = -60.0
+    h, w, t, g = [x.to(dev()) for x in (h, w, t, g)]
+    base._check(h, w, t, g, _on_device(need_dw, h, w, t, g), True, need_dw)
+
+
+@pytest.mark.parametrize("T,V,block", [(300, 26003, 5000), (1100, 260003, 50000)])
+@pytest.mark.parametrize("high", [40.0, 50.0, 60.0])
+def test_words_that_are_unlikely_for_every_token_get_their_gradient(high, T, V, block):
+    """A third of the words has probabilities of 1e-17 to 1e-30 where one of h's components is not zero: dw of that component is the sum of these, which
+    bf16 and fp32 hold."""
+    K = 32
+    h, w, t, g = base._inputs(T, K, V, 51)
+    w[:, 0] = (torch.arange(V) // block % 3 - 1).bfloat16()
+    h[:, 0] = 0.0
+    h[0::4, 0] = high
+    h[2::4, 0] = -high
+    h, w, t, g = [x.to(dev()) for x in (h, w, t, g)]
+    base._check(h, w, t, g, _on_device(True, h, w, t, g), True, True)
