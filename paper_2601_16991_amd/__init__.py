@@ -181,8 +181,8 @@ def _handle(stream) -> Optional[int]:
 
 
 def _on(stream, device):
-    """The stream argument of a call on tensors of ``device``: None or a stream of that GPU."""
-    if stream is not None and stream.device != device:
+    """The stream argument of a call on tensors of ``device``."""
+    if stream.device != device:
         raise ValueError("stream: of another device than the tensors")
     return stream
 
@@ -644,7 +644,7 @@ def salr_linear_cross_entropy(h: torch.Tensor, w: torch.Tensor, targets: torch.T
         if t is not None and t.device != h.device:
             raise ValueError(f"{name}: tensors on different devices")
     with torch.cuda.device(h.device):
-        _check(lib().salr_linear_cross_entropy(*args, _stream(_on(stream, h.device))), "salr_linear_cross_entropy")
+        _check(lib().salr_linear_cross_entropy(*args, _stream(None if stream is None else _on(stream, h.device))), "salr_linear_cross_entropy")
 
 
 def linear_cross_entropy(h, w, targets, grad_loss=None, need_dh=True, need_dw=False, workspace=None):
@@ -672,8 +672,9 @@ class _StepList:
 
 class GradNorm:
     """The norm of many gradients at once: ``GradNorm(grads)(max_norm)`` is a tensor [norm, min(1, max_norm / (norm + 1e-6))], the second
-    value NaN where the norm is not finite.  The tensors are read where they are at every call, on the stream that is current then;
-    calls that overlap on different streams need a ``GradNorm`` each."""
+    value NaN where the norm is not finite.  The tensors are read where they are at every call, on the stream that is current then; where one
+    has other memory than when the object was made the call raises ValueError (making the list costs what ``AdamW`` tells).  An object has one
+    workspace: calls on different streams that may overlap need an object each, or their sums are wrong."""
 
     def __init__(self, grads, _list=None):
         self._list = _list or _StepList(list(grads))
@@ -683,10 +684,12 @@ class GradNorm:
 
     def __call__(self, max_norm: float = float("inf"), out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         l = self._list
-        if out is None and stream is not None:
-            with torch.cuda.stream(_on(stream, l.plan.device)):
-                out = torch.empty(2, device=l.plan.device)
-        got = self._call(l.plan, l.chunks, l.grad_type, max_norm, self._workspace, out, _handle(_on(stream, l.plan.device)), l.tensors)
+        if stream is not None:
+            _on(stream, l.plan.device)
+            if out is None:
+                with torch.cuda.stream(stream):
+                    out = torch.empty(2, device=l.plan.device)
+        got = self._call(l.plan, l.chunks, l.grad_type, max_norm, self._workspace, out, _handle(stream), l.tensors)
         return got if out is None else out
 
 
@@ -705,6 +708,10 @@ class AdamW:
     """AdamW over many tensors in one launch a step.  The tensors keep their memory: a step raises ValueError where one has other memory
     than when the object was made.  Each is in the lists once (ValueError where memory that a step writes is another tensor's too): a weight that
     is used in several places is one tensor with the sum of its gradients.
+
+    The list is laid out and copied to the GPU when the object is made: about 50 us on the host for 14 tensors and 150 for 448, against 4 and
+    17 us for a step.  So gradients that stay (a backward pass that writes into them, ``zero_grad(set_to_none=False)``) cost nothing, while a
+    program that has new ones every step makes an object every step, with the states of the last one.
 
     params        fp32 or bf16 tensors, updated in place
     grads         their gradients (fp32 or bf16), read where they are at every step: a backward pass writes into them
@@ -726,7 +733,8 @@ class AdamW:
         self._call = _native().adamw_step
 
     def grad_norm(self, max_norm: float = float("inf"), stream=None) -> torch.Tensor:
-        """[norm, factor] of the gradients (see ``GradNorm``); ``grad_norm(c)[1:]`` is a ``grad_scale`` for ``step``."""
+        """[norm, factor] of the gradients (see ``GradNorm``); ``grad_norm(c)[1:]`` is a ``grad_scale`` for ``step``.  The object has one workspace
+        for it: calls on different streams must not overlap (a ``GradNorm`` of its own for each stream can)."""
         return self._norm(max_norm, None, stream)
 
     def step(self, lr: float, step: int, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.0,
@@ -739,4 +747,4 @@ class AdamW:
         if seed is None:
             seed = step
         self._call(l.plan, l.chunks, l.param_type, l.grad_type, l.state_bits, lr, beta1, beta2, eps, weight_decay, step, seed, grad_scale,
-                   _handle(_on(stream, l.plan.device)), l.tensors)
+                   None if stream is None else _on(stream, l.plan.device).cuda_stream, l.tensors)

@@ -461,7 +461,7 @@ struct StepTensors {
     struct Member {
         at::Tensor tensor;
         const void* at;
-        bool written;
+        bool counted;   // written by a step, and not an inference tensor: those have no version
     };
     std::vector<Member> all;
     std::vector<at::Tensor> states;   // those whose only owner may be the optimiser
@@ -489,7 +489,7 @@ struct StepTensors {
     // A step changes its tensors in place: autograd sees by their versions that what it saved of them is another value now.
     void changed() const {
         for (const Member& x : all)
-            if (x.written && !x.tensor.is_inference()) x.tensor.unsafeGetTensorImpl()->bump_version();
+            if (x.counted) x.tensor.unsafeGetTensorImpl()->bump_version();
     }
     static PyObject* capsule(std::unique_ptr<StepTensors> t) {
         PyObject* c = PyCapsule_New(t.get(), kName, [](PyObject* o) { delete static_cast<StepTensors*>(PyCapsule_GetPointer(o, kName)); });
@@ -630,7 +630,7 @@ PyObject* py_step_list(PyObject*, PyObject* const* v, Py_ssize_t n) {
         if (!t.is_contiguous()) fail(PyExc_TypeError, "%s must be contiguous", name);
         if (t.device() != device) fail(PyExc_ValueError, "%s: tensors on different devices", name);
         if (t.numel() != size) fail(PyExc_ValueError, "%s: another number of elements than its gradient wants", name);
-        tensors->all.push_back({t, t.const_data_ptr(), written});
+        tensors->all.push_back({t, t.const_data_ptr(), written && !t.is_inference()});
         const uintptr_t at = reinterpret_cast<uintptr_t>(t.const_data_ptr());
         if (size > 0) ranges.push_back({at, at + t.nbytes(), written, name});
         return t.data_ptr();
