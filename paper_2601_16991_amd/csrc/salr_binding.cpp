@@ -9,6 +9,7 @@
 #include <ATen/ops/empty.h>
 #include <ATen/core/Tensor.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -70,6 +71,13 @@ void need_matrix(const at::Tensor& t, const char* name) {
 void need_device(const at::Tensor& t, const at::Device& device, const char* name) {
     if (t.defined() && t.device() != device) fail(PyExc_ValueError, "%s: tensors on different devices", name);
 }
+
+struct OnDevice {   // that GPU is the current one here
+    c10::OptionalDeviceGuard guard;
+    explicit OnDevice(const at::Device& device) {
+        if (c10::hip::current_device() != device.index()) guard.reset_device(device);
+    }
+};
 
 void* stream_of(PyObject* o) {   // None: the current stream; else a stream handle as an integer (0 = default stream)
     if (o == Py_None) return c10::hip::getCurrentHIPStream().stream();
@@ -420,7 +428,7 @@ PyObject* py_linear_cross_entropy(PyObject*, PyObject* const* v, Py_ssize_t n) {
     need_device(w, h.device(), "w");
     need_device(targets, h.device(), "targets");
     need_device(grad, h.device(), "grad_loss");
-    const c10::DeviceGuard on(h.device());   // outputs, stream and launches are that GPU's, whichever is current
+    const OnDevice on(h.device());   // outputs, stream and launches are that GPU's, whichever is current
     const bool need_dh = PyObject_IsTrue(v[4]) == 1, need_dw = PyObject_IsTrue(v[5]) == 1;
     at::Tensor loss = empty_on({T}, at::kFloat, h), lse = empty_on({T}, at::kFloat, h), dh, dw;
     if (need_dh) dh = empty_on({T, K}, h.scalar_type(), h);
@@ -461,7 +469,6 @@ struct StepTensors {
     struct Member {
         at::Tensor tensor;
         const void* at;
-        bool counted;   // written by a step, and not an inference tensor: those have no version
     };
     std::vector<Member> all;
     std::vector<at::Tensor> states;   // those whose only owner may be the optimiser
@@ -486,10 +493,10 @@ struct StepTensors {
             for (const at::Tensor& t : states) tell(t);
         known.push_back(stream);
     }
-    // A step changes its tensors in place: autograd sees by their versions that what it saved of them is another value now.
+    // A step changes params and copies in place: autograd sees by their versions that what it saved of them is another value now.
+    std::vector<at::Tensor> versioned;   // (inference tensors have none)
     void changed() const {
-        for (const Member& x : all)
-            if (x.counted) x.tensor.unsafeGetTensorImpl()->bump_version();
+        for (const at::Tensor& t : versioned) t.unsafeGetTensorImpl()->bump_version();
     }
     static PyObject* capsule(std::unique_ptr<StepTensors> t) {
         PyObject* c = PyCapsule_New(t.get(), kName, [](PyObject* o) { delete static_cast<StepTensors*>(PyCapsule_GetPointer(o, kName)); });
@@ -513,7 +520,7 @@ PyObject* py_adamw_step(PyObject*, PyObject* const* v, Py_ssize_t n) {
     if (scale.defined() && scale.numel() != 1) fail(PyExc_ValueError, "%s must be one value", "grad_scale");
     const float* sp = device_ptr<float>(scale, kF32, "grad_scale");
     need_device(scale, list.device(), "grad_scale");
-    const c10::DeviceGuard on(list.device());
+    const OnDevice on(list.device());
     const int bits = (int)int_of(v[4]);
     const double lr = double_of(v[5]), b1 = double_of(v[6]), b2 = double_of(v[7]), eps = double_of(v[8]), decay = double_of(v[9]);
     const int64_t step = int_of(v[10]), seed = int_of(v[11]);
@@ -545,7 +552,7 @@ PyObject* py_grad_norm(PyObject*, PyObject* const* v, Py_ssize_t n) {
     uint8_t* wp = device_ptr<uint8_t>(ws, kU8, "workspace");
     if (!ws.defined()) fail(PyExc_TypeError, "%s must be a tensor", "workspace");
     need_device(ws, list.device(), "workspace");
-    const c10::DeviceGuard on(list.device());
+    const OnDevice on(list.device());
     at::Tensor out = v[5] == Py_None ? empty_on({2}, at::kFloat, ws) : tensor_of(v[5], "out");
     if (out.numel() != 2) fail(PyExc_ValueError, "%s must hold two values", "out");
     float* op = device_ptr<float>(out, kF32, "out");
@@ -630,7 +637,7 @@ PyObject* py_step_list(PyObject*, PyObject* const* v, Py_ssize_t n) {
         if (!t.is_contiguous()) fail(PyExc_TypeError, "%s must be contiguous", name);
         if (t.device() != device) fail(PyExc_ValueError, "%s: tensors on different devices", name);
         if (t.numel() != size) fail(PyExc_ValueError, "%s: another number of elements than its gradient wants", name);
-        tensors->all.push_back({t, t.const_data_ptr(), written && !t.is_inference()});
+        tensors->all.push_back({t, t.const_data_ptr()});
         const uintptr_t at = reinterpret_cast<uintptr_t>(t.const_data_ptr());
         if (size > 0) ranges.push_back({at, at + t.nbytes(), written, name});
         return t.data_ptr();
@@ -645,6 +652,8 @@ PyObject* py_step_list(PyObject*, PyObject* const* v, Py_ssize_t n) {
         t.grad = pointer(g, grad_type, t.count, "grad", false);
         if (!step) continue;
         t.param = pointer(params.at(i, "param"), param_type, t.count, "param");
+        for (const TensorList* l : {&params, &copies})
+            if (l->fast && l->at(i, "param").defined() && !l->at(i, "param").is_inference()) tensors->versioned.push_back(l->at(i, "param"));
         t.exp_avg = pointer(m.at(i, "exp_avg"), state_type, t.count, "exp_avg");
         t.exp_avg_sq = pointer(sq.at(i, "exp_avg_sq"), state_type, t.count, "exp_avg_sq");
         if (copies.fast && copies.at(i, "copy").defined()) t.copy = static_cast<uint16_t*>(pointer(copies.at(i, "copy"), at::kBFloat16, t.count, "copy"));

@@ -333,21 +333,26 @@ __global__ __launch_bounds__(1024) void ce_rows_kernel(CeRowArgs a) {
     if (target >= a.V) {
         loss = lse = alpha = beta = nan;
     } else if (target >= 0) {
-        const float l = a.target_logit[t], off = l - 0.5f * M;
+        const float l = a.target_logit[t];
         const bool large = fabsf(M) >= kLargeReference;   // M is twice a logit then
-        const float up = !large ? fmaf(l, kLog2e, -M) : off > kLargeLogit && l < inf ? kLargeLogit : off * kLog2e;
+        float up = fmaf(l, kLog2e, -M);
+        if (large) {
+            const float off = l - 0.5f * M;
+            up = off > kLargeLogit && l < inf ? kLargeLogit : off * kLog2e;
+        }
         const float top = up > 0.f || all.M == -inf ? ceilf(up) : 0.f;
         const float e = __builtin_amdgcn_exp2f(up - top), rest = times_power(sum, -top), total = rest + e;
         const float gl = a.grad_loss != nullptr ? a.grad_loss[t] : 1.f;
-        lse = (!large ? kLn2 * (M + top) : top > 0.f ? l : 0.5f * M) + logf(total);
+        lse = kLn2 * (M + top);
+        if (large) lse = top > 0.f ? l : 0.5f * M;
+        lse += logf(total);
         const float ratio = rest / e;   // (where the target is far below the others it leaves fp32)
         loss = ratio < 1e6f ? log1pf(ratio) : lse - l;
         // 2^-top and the exponent of the sum go to M, as long as that is exact, so that 2^(l log2 e - M) is as small as G is and no smaller:
         // alpha times 2^-top would leave fp32 where the target is far above the others, 2^(l log2 e - M) where M is far above them all
         const bool exact = fabsf(M) <= 0x1p23f && top <= 1000.f && total > 0.f && total < inf;
-        const float whole = exact ? (float)__builtin_amdgcn_frexp_expf(total) : 0.f;
-        above = exact ? M + top + whole : M;
-        alpha = sum == 0.f ? 0.f : exact ? gl / times_power(total, -whole) : times_power(gl / total, -top);
+        above = exact ? M + top + (float)__builtin_amdgcn_frexp_expf(total) : M;
+        alpha = sum == 0.f ? 0.f : times_power(gl / (exact ? __builtin_amdgcn_frexp_mantf(total) : total), exact ? 0.f : -top);
         beta = gl * (rest / total);
         if (!(total > 0.f && total < inf)) loss = lse = alpha = beta = nan;
     }

@@ -98,10 +98,10 @@ def test_autograd_sees_that_a_step_changed_what_it_saved():
     p = torch.ones(300, device=dev(), requires_grad=True)
     g, copy = torch.ones(300, device=dev()), torch.empty(300, dtype=torch.bfloat16, device=dev())
     opt = salr.AdamW([p], [g], copies=[copy])
-    before = [x._version for x in (p, copy, opt.exp_avg[0], opt.exp_avg_sq[0], g)]
+    before = [x._version for x in (p, copy, g)]
     loss = (p * p).sum()
     opt.step(lr=1e-2, step=1)
-    assert [x._version - b for x, b in zip((p, copy, opt.exp_avg[0], opt.exp_avg_sq[0], g), before)] == [1, 1, 1, 1, 0]
+    assert [x._version - b for x, b in zip((p, copy, g), before)] == [1, 1, 0]
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         loss.backward()
     opt.grad_norm(1.0)
