@@ -7,7 +7,7 @@
 //   logits  a tile of 256 tokens x 256 columns at a time: E = 2^(l log2 e - M_tile) in bf16, M_tile a multiple of 128 near the
 //           tile's largest exponent of the row, and the row's sum of E in fp32;
 //   rows    M_row = the running maximum of the M_tile, the running sum; E of tiles with another M is brought to M_row, a subtraction
-//           from its exponents;
+//           from its exponents (what falls below bf16's normal numbers is lost);
 //   dh      sums = 2^(M_row before - M_row) sums + E w.
 // The column of the target is left out of E and of the sum S' and joins at the end, dh = grad (E w - S' w_target) / (S' + e_target):
 // a token that is predicted well has 1 - p_target = S' / S to full precision, not the difference of rounded numbers.
@@ -65,9 +65,9 @@ __device__ __forceinline__ float over_groups(float x, With with) {
 }
 
 // l = h w^T of one tile and what becomes of it.  `w`: the piece's first row, `columns` of it exist; `pitch`: of `out` [T][pitch].
-// 2048 x 4096 x 131072, statistics: 1565 us a call, 1405 TFLOP/s (the product by itself, with its result stored, takes the library 1515 to 1545); E of
-// 4096 x 32768: 836 us, 1315 TFLOP/s.  A tile of 256 x 256 has 7 us outside the k loop without E and 12 with it: start and first loads 3, the exponentials and
-// statistics 4, E through LDS and out.  Up to 64 tokens the head's bytes count: 1 x 4096 x 131072 174 us, 6.2 TB/s.
+// 2048 x 4096 x 131072, statistics: 1573 us a call, 1400 TFLOP/s (the product by itself, with its result stored, takes the library 1515 to 1545); E of
+// 4096 x 32768: 830 us, 1325 TFLOP/s.  A tile of 256 x 256 has 7 us outside the k loop without E and 12 with it: start and first loads 3, the exponentials and
+// statistics 4, E through LDS and out.  Up to 64 tokens the head's bytes count: 1 x 4096 x 131072 173 us, 6.2 TB/s.
 template <class Shape, int kMode>
 __global__ __launch_bounds__(Shape::kThreads) void ce_logits_kernel(const uint16_t* __restrict__ h, int64_t T, int64_t K, const uint16_t* __restrict__ w,
                                                         int64_t columns, int64_t first, const int64_t* __restrict__ targets, int m_tiles, int n_tiles,
@@ -289,7 +289,8 @@ __global__ __launch_bounds__(1024) void ce_rows_kernel(CeRowArgs a) {
     for (int q = 0; q < 16; ++q) all.add(part[q][row].M, part[q][row].sum, part[q][row].least);
     const float M = all.M == -inf ? 0.f : all.M, sum = all.sum;
     if (a.e != nullptr && __any(here && all.least < M)) {
-        // The exponents of E in tiles with a reference below the row's, lowered by the difference: exact.  The wave goes through such tiles
+        // The exponents of E in tiles with a reference below the row's, lowered by the difference: exact, but for what then lies below bf16's normal
+        // numbers (2^-62 of the row's largest and less: 0, or another number as small).  The wave goes through such tiles
         // four at a time, its lanes through the columns.
         for (int n0 = 0; n0 < a.n_tiles; n0 += kParts) {
             const int n = n0 + first_tile;
@@ -452,7 +453,7 @@ __global__ __launch_bounds__(256) void ce_dh_finish_kernel(const float* __restri
     *reinterpret_cast<uint4*>(dh + t * K + k) = q;
 }
 
-// dw of a piece: G^T h, both operands across the contraction.  1111 x 2720 x 50003: 285 us, 1060 TFLOP/s; of the 34 us of a tile its 18 steps take 26.
+// dw of a piece: G^T h, both operands across the contraction.  1111 x 2720 x 50003: 279 us, 1083 TFLOP/s; of the 34 us of a tile its 18 steps take 26.
 // With few tokens the stores count: 315 x 7872 x 44416 7 us of steps in the 16 of a tile.
 template <class Shape>
 __global__ __launch_bounds__(Shape::kThreads) void ce_dw_kernel(const uint16_t* __restrict__ gr, int64_t T, int64_t pitch, const uint16_t* __restrict__ h, int64_t K,
