@@ -430,8 +430,8 @@ salr_status_t salr_concat_adapters(const uint16_t* const* a_list, const uint16_t
  *
  *   h          in   [T, K] bf16 hidden states; K % 8 == 0, K <= 2^22 (else SHAPE)
  *   w          in   [V, K] bf16, the head (rows along K, as the weight of a PyTorch linear); 1 <= V < 2^31 where T > 0 (else SHAPE).
- *                   SHAPE too where a launch would have 2^32 threads: 2^23 tiles of 128 or 256 tokens and 256 words, T * K / 8 >= 2^32 with
- *                   a gradient, T >= 2^24 with dw on a vocabulary of at most 256 words
+ *                   SHAPE too where a launch would have 2^32 threads: 2^23 tiles of 256 words and up to 256 tokens, T * K / 8 >= 2^32
+ *                   with a gradient, T >= 2^24 with dw on a vocabulary of at most 256 words
  *   targets    in   [T] int64.  A negative target masks its token: loss, lse, and the gradient are 0 there, whatever the hidden
  *                   state holds (NaN and infinities too).  A target >= V gives NaN in the token's loss, lse and gradients.
  *   grad_loss  in   [T] fp32, the gradient of what is minimised with respect to loss[t] (1 / tokens for the mean); NULL: ones
@@ -450,7 +450,8 @@ salr_status_t salr_concat_adapters(const uint16_t* const* a_list, const uint16_t
  *
  * Precision: fp32 sums, maxima and logits; the probabilities are rounded to bf16 once, as operands of the matrix cores, and dh
  * and dw at the end.  The probability of the target stays out of that: 1 - p is summed, not subtracted.  A logit that is NaN or
- * +infinite (2^127 and more may count as that) makes the token's results NaN; one of -infinity, or far below the others, has probability 0.  Results are the same bit for bit from call to call.
+ * +infinite (2^127 and more may count as that) makes the token's results NaN; one of -infinity, or far below the others, has
+ * probability 0.  Results are the same bit for bit from call to call.
  * Errors: INVALID_ARG (null where data is required, negative size, a pointer that is not 16-byte aligned (targets, grad_loss, loss and lse:
  * not aligned to their type)), SHAPE, CAPACITY, HIP.  The workspace query returns 0 for sizes the call would refuse.
  */
