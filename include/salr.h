@@ -531,6 +531,121 @@ salr_status_t salr_grad_norm(const void* plan, int64_t chunks, salr_type_t grad_
                              size_t workspace_bytes, void* stream);
 
 /*
+ * What is on either side of a layer when its adapters are trained, or served to many requests: dropout, layer norm, adapters that differ from
+ * token to token.  Activations here may start at any element's address (a row of an odd length does); they are fp32 or bf16 where a type is asked for.
+ *
+ * salr_dropout -- y[i] = residual[i] + (keep(i) ? x[i] / (1 - q) : 0), the sum in fp32 and rounded once.  The mask is not stored: the gradient of x
+ * is the same call on the gradient of y, without the residual (whose gradient is that of y), with the same p, seed and offset.
+ *
+ * keep(i) is (16 bits of i) >= c with c = floor(65536 p + 0.5); q = c / 65536 is what p becomes.  The bits are Philox4x32-10 (Salmon, Moraes, Dror
+ * and Shaw, 2011) of the counter (i / 8, offset), 64 bits each, low words first, with the seed as key (low word first): element i has the half i % 2, the
+ * lower one first, of word i / 2 % 4.  Another seed, or another offset under one seed (a layer's number, a step's), gives other bits.
+ *
+ *   x            in   [count] of `type`
+ *   residual     in   [count] of `type`, or NULL
+ *   seed_device  in   one int64 on the device that is read instead of `seed` when the kernel runs, or NULL.  A captured graph keeps `seed` and `offset` as
+ *                     they were at its capture: a program that replays a step changes *seed_device between the replays
+ *   y            out  [count] of `type`; may be x or residual, else overlaps neither
+ * Errors: INVALID_ARG (null where data is required, negative count, a type that is none, p outside [0, 1) or with c = 65536, a pointer that is
+ * not aligned to its type, y overlapping x or residual in part), SHAPE (count > 2^42), HIP.
+ */
+salr_status_t salr_dropout(const void* x, const void* residual, int64_t count, salr_type_t type, double p, int64_t seed, const int64_t* seed_device,
+                           int64_t offset, void* y, void* stream);
+
+/*
+ * salr_layer_norm -- for every row of s = x, or s = x + residual, rounded to `type` as it is stored in `sum`:
+ *
+ *     mean = sum_k s[k] / K,   rstd = 1 / sqrt(sum_k (s[k] - mean)^2 / K + eps),   y[k] = (s[k] - mean) * rstd * weight[k] + bias[k]
+ *
+ *   x         in   [T, K] of `type`;  0 <= K <= 32768, T < 2^22 (else SHAPE)
+ *   residual  in   [T, K] of `type`, or NULL
+ *   weight    in   [K] of `weight_type`
+ *   bias      in   [K] of `weight_type`, or NULL (zeros)
+ *   y         out  [T, K] of `type`; may be x or residual
+ *   sum       out  [T, K] of `type`: s, what the next residual and the backward pass take; may be x or residual, not y.  NULL iff residual is
+ *   mean      out  [T] fp32, or NULL
+ *   rstd      out  [T] fp32, or NULL
+ * Sums are fp32, squares are of differences to the mean.  A row with an infinity or NaN gives NaN, other rows are not touched by it.
+ * Errors: INVALID_ARG (null where data is required, negative size, a type that is none, eps negative or not finite, a pointer that is not
+ * aligned to its type, sum without residual or the other way round, an output that overlaps an input in part or another output), SHAPE, HIP.
+ *
+ * salr_layer_norm_backward -- with xhat = (x - mean) * rstd and g = dy * weight:
+ *
+ *     dx = rstd * (g - sum_k g[k] / K - xhat * sum_k (g[k] xhat[k]) / K) + dsum,   dw = sum over rows of dy * xhat,   db = sum over rows of dy
+ *
+ *   dy, x        in   [T, K] of `type`; x is what was normalised: `sum` where there was a residual
+ *   weight       in   [K] of `weight_type`
+ *   mean, rstd   in   [T] fp32
+ *   dsum         in   [T, K] of `type`, a gradient that reaches s past the norm (the residual stream's), or NULL
+ *   dx           out  [T, K] of `type` (the gradient of x and of residual alike); may be dy, x or dsum; NULL = not computed
+ *   dw, db       out  [K] of `weight_type`, fp32 sums rounded once; NULL = not computed (a frozen norm).  T == 0 writes zeros
+ *   workspace    --   salr_layer_norm_backward_workspace_bytes(T, K, dw or db wanted) bytes, 16-byte aligned; contents unspecified
+ * Results are the same bit for bit from call to call.
+ * Errors: as above, and CAPACITY.  The workspace query returns 0 for sizes the call would refuse.
+ */
+salr_status_t salr_layer_norm(const void* x, const void* residual, const void* weight, const void* bias, int64_t T, int64_t K, salr_type_t type,
+                              salr_type_t weight_type, double eps, void* y, void* sum, float* mean, float* rstd, void* stream);
+size_t salr_layer_norm_backward_workspace_bytes(int64_t T, int64_t K, int want_weights);
+salr_status_t salr_layer_norm_backward(const void* dy, const void* x, const void* weight, const float* mean, const float* rstd, const void* dsum, int64_t T,
+                                       int64_t K, salr_type_t type, salr_type_t weight_type, void* dx, void* dw, void* db, void* workspace,
+                                       size_t workspace_bytes, void* stream);
+
+/*
+ * Adapters of many requests beside one shared layer: salr_sparse_lowrank_linear applies one pair to the whole batch; here every token names its own.
+ * The list lies on the device: the caller fills an array of these records, has it checked, and copies it there once, for as long as the
+ * adapters stay where they are.
+ */
+typedef struct {
+    const uint16_t* a;   /* [K, rank] bf16                                                                      */
+    const uint16_t* b;   /* [rank, N] bf16                                                                      */
+    uint16_t* da;        /* [K, rank] bf16, gradient of a: written by the backward pass; NULL = not computed    */
+    uint16_t* db;        /* [rank, N] bf16, gradient of b; NULL = not computed                                  */
+    int64_t rank;        /* 0 .. 256; at 0 the pointers are not looked at                                       */
+} salr_adapter_t;
+
+/*
+ * salr_adapter_list_check -- whether the n records of a HOST array can be used; *max_rank gets the largest rank, which the calls want to know.  No
+ * gradient may overlap another tensor of the list (not checked here).
+ * Errors: INVALID_ARG (null where data is required, n or a rank negative, a pointer that is not 16-byte aligned), SHAPE (n > 65533),
+ * UNSUPPORTED (a rank above 256).
+ */
+salr_status_t salr_adapter_list_check(const salr_adapter_t* adapters, int64_t n, int64_t* max_rank);
+
+/*
+ * salr_adapters_add -- y[t] = base[t] + (x[t] A_i) B_i with i = ids[t]; a token with a negative id has no adapter: y[t] = base[t].
+ * An id that is not below n gives NaN in its token's row.
+ *
+ *   list, n, max_rank  the records, on the device (8-byte aligned), their number (at least 1) and largest rank
+ *   x          in   [T, K] bf16;  T < 2^28, K and N <= 2^22 (else SHAPE)
+ *   ids        in   [T] int32
+ *   base       in   [T, N] bf16, the shared layer's output; NULL = zeros
+ *   y          out  [T, N] bf16; may be base, overlaps x and base in no other way
+ *   workspace  --   salr_adapters_add_workspace_bytes(T, K, N, n, max_rank) bytes, 256-byte aligned; contents unspecified
+ *
+ * salr_adapters_backward -- the adjoint:
+ *
+ *     dx[t] = dx_base[t] + (dy[t] B_i^T) A_i^T,    dA_i = sum over i's tokens of x[t]^T (dy[t] B_i^T),    dB_i = sum over them of (x[t] A_i)^T dy[t]
+ *
+ *   x          in   as above; may be NULL where want_gradients is 0
+ *   dy         in   [T, N] bf16
+ *   dx_base    in   [T, K] bf16, the shared layer's dx; NULL = zeros
+ *   dx         out  [T, K] bf16; may be dx_base; NULL = not computed.  NaN for a token whose id is not below n, which is in no adapter's gradient
+ *   want_gradients  not 0: da and db of every record that has them are written; those of an adapter without a token as zeros
+ *   workspace  --   salr_adapters_backward_workspace_bytes(T, K, N, n, max_rank, want_gradients) bytes, 256-byte aligned
+ *
+ * bf16 in and out, fp32 sums; x A and dy B^T are rounded to bf16 once, as the layer's are.  Results are the same bit for bit from call to call.
+ * Errors of both: INVALID_ARG (null where data is required, negative size, n < 1, max_rank outside [0, 256], a misaligned pointer (x, base, y, dy, dx_base,
+ * dx: to 2 bytes; ids: to 4), an output that overlaps an input otherwise than told), SHAPE, CAPACITY, HIP.  The queries return 0 for sizes that are refused.
+ */
+size_t salr_adapters_add_workspace_bytes(int64_t T, int64_t K, int64_t N, int64_t n, int64_t max_rank);
+salr_status_t salr_adapters_add(const salr_adapter_t* list, int64_t n, int64_t max_rank, const uint16_t* x, int64_t T, int64_t K, int64_t N,
+                                const int32_t* ids, const uint16_t* base, uint16_t* y, void* workspace, size_t workspace_bytes, void* stream);
+size_t salr_adapters_backward_workspace_bytes(int64_t T, int64_t K, int64_t N, int64_t n, int64_t max_rank, int want_gradients);
+salr_status_t salr_adapters_backward(const salr_adapter_t* list, int64_t n, int64_t max_rank, const uint16_t* x, const uint16_t* dy, int64_t T,
+                                     int64_t K, int64_t N, const int32_t* ids, const uint16_t* dx_base, uint16_t* dx, int want_gradients,
+                                     void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Measurement hook (not part of the method): when both events are non-NULL, the next calls of
  * salr_sparse_lowrank_linear on this host thread attach the two events to the launch of the fused
  * decode+GEMM kernel: `start_event` takes the time the kernel begins executing and `stop_event` the

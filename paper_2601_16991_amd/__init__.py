@@ -33,6 +33,11 @@ class StepTensor(ctypes.Structure):
     _fields_ = [("param", _vp), ("copy", _vp), ("grad", _vp), ("exp_avg", _vp), ("exp_avg_sq", _vp), ("scales", _vp), ("count", _i64)]
 
 
+class Adapter(ctypes.Structure):
+    """salr_adapter_t of include/salr.h."""
+    _fields_ = [("a", _vp), ("b", _vp), ("da", _vp), ("db", _vp), ("rank", _i64)]
+
+
 class SalrError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = int(status)
@@ -124,6 +129,25 @@ def lib() -> ctypes.CDLL:
         L.salr_adamw_step.argtypes = [_vp, _i64, ctypes.c_int, ctypes.c_int, ctypes.c_int, *[ctypes.c_double] * 5, _i64, _i64, _vp, _vp]
         L.salr_grad_norm.restype = ctypes.c_int
         L.salr_grad_norm.argtypes = [_vp, _i64, ctypes.c_int, ctypes.c_float, _vp, _vp, ctypes.c_size_t, _vp]
+        L.salr_dropout.restype = ctypes.c_int
+        L.salr_dropout.argtypes = [_vp, _vp, _i64, ctypes.c_int, ctypes.c_double, _i64, _vp, _i64, _vp, _vp]
+        L.salr_layer_norm.restype = ctypes.c_int
+        L.salr_layer_norm.argtypes = [_vp, _vp, _vp, _vp, _i64, _i64, ctypes.c_int, ctypes.c_int, ctypes.c_double, _vp, _vp, _vp, _vp, _vp]
+        L.salr_layer_norm_backward_workspace_bytes.restype = ctypes.c_size_t
+        L.salr_layer_norm_backward_workspace_bytes.argtypes = [_i64, _i64, ctypes.c_int]
+        L.salr_layer_norm_backward.restype = ctypes.c_int
+        L.salr_layer_norm_backward.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _i64, _i64, ctypes.c_int, ctypes.c_int, _vp, _vp, _vp, _vp,
+                                               ctypes.c_size_t, _vp]
+        L.salr_adapter_list_check.restype = ctypes.c_int
+        L.salr_adapter_list_check.argtypes = [ctypes.POINTER(Adapter), _i64, ctypes.POINTER(_i64)]
+        L.salr_adapters_add_workspace_bytes.restype = ctypes.c_size_t
+        L.salr_adapters_add_workspace_bytes.argtypes = [_i64, _i64, _i64, _i64, _i64]
+        L.salr_adapters_add.restype = ctypes.c_int
+        L.salr_adapters_add.argtypes = [_vp, _i64, _i64, _vp, _i64, _i64, _i64, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
+        L.salr_adapters_backward_workspace_bytes.restype = ctypes.c_size_t
+        L.salr_adapters_backward_workspace_bytes.argtypes = [_i64, _i64, _i64, _i64, _i64, ctypes.c_int]
+        L.salr_adapters_backward.restype = ctypes.c_int
+        L.salr_adapters_backward.argtypes = [_vp, _i64, _i64, _vp, _vp, _i64, _i64, _i64, _vp, _vp, _vp, ctypes.c_int, _vp, ctypes.c_size_t, _vp]
         L.salr_set_kernel_timing_events.restype = None
         L.salr_set_kernel_timing_events.argtypes = [_vp, _vp]
         _lib = L
@@ -748,3 +772,134 @@ class AdamW:
             seed = step
         self._call(l.plan, l.chunks, l.param_type, l.grad_type, l.state_bits, lr, beta1, beta2, eps, weight_decay, step, seed, grad_scale,
                    None if stream is None else _on(stream, l.plan.device).cuda_stream, l.tensors)
+
+
+# ---- on either side of a layer: dropout, layer norm, adapters of many requests
+
+def _within(stream, device):
+    """A stream argument for calls that allocate: that stream is the current one meanwhile."""
+    return torch.cuda.stream(None if stream is None else _on(stream, device))
+
+
+def salr_dropout(x: torch.Tensor, residual: Optional[torch.Tensor], p: float, seed, offset: int, y: torch.Tensor, stream=None) -> None:
+    """Enqueue y = dropout(x) (+ residual), fp32 or bf16; y may be x or residual."""
+    if y is None:
+        raise TypeError("y must be a tensor")
+    _native().dropout(x, residual, p, seed, offset, y, None if stream is None else _on(stream, x.device).cuda_stream)
+
+
+def dropout(x: torch.Tensor, p: float, seed, offset: int = 0, residual: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """residual + (keep ? x / (1 - p) : 0), newly allocated; x and residual fp32 or bf16, contiguous, of any shape.
+
+    Which elements stay follows from their positions, ``seed`` and ``offset`` (Philox4x32-10; p is taken in steps of 2^-16): no mask is stored, and
+    the gradient of x is ``dropout(dy, p, seed, offset)`` (with another gradient of x as ``residual`` where there is one).  ``seed``: a number, or an int64
+    tensor of one on the GPU that is read when the kernel runs: a captured graph has other masks at every replay where that changes in between."""
+    with _within(stream, x.device):
+        return _native().dropout(x, residual, p, seed, offset, None, None)
+
+
+def salr_layer_norm(x: torch.Tensor, residual: Optional[torch.Tensor], weight: torch.Tensor, bias: Optional[torch.Tensor], eps: float, y: torch.Tensor,
+                    sum: Optional[torch.Tensor], mean: Optional[torch.Tensor], rstd: Optional[torch.Tensor], stream=None) -> None:
+    """Enqueue the layer norm of x [T, K], or of sum = x + residual; mean, rstd fp32 [T] or None."""
+    _native().layer_norm(x, residual, weight, bias, eps, y, sum, mean, rstd, None if stream is None else _on(stream, x.device).cuda_stream, False)
+
+
+def layer_norm(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, eps: float = 1e-5, residual: Optional[torch.Tensor] = None,
+               stream=None):
+    """(y, sum, mean, rstd): the layer norm of every row of x [T, K], or of sum = x + residual (None without a residual), which the next residual and
+    ``layer_norm_backward`` take.  x and residual fp32 or bf16, weight and bias [K] fp32 or bf16; K up to 32768."""
+    with _within(stream, x.device):
+        return _native().layer_norm(x, residual, weight, bias, eps, None, None, None, None, None, True)
+
+
+def salr_layer_norm_backward_workspace_bytes(T: int, K: int, want_weights: bool) -> int:
+    return int(lib().salr_layer_norm_backward_workspace_bytes(T, K, int(want_weights)))
+
+
+def salr_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                             dsum: Optional[torch.Tensor], dx: Optional[torch.Tensor], dw: Optional[torch.Tensor], db: Optional[torch.Tensor],
+                             workspace: Optional[torch.Tensor], stream=None) -> None:
+    """Enqueue the gradient of the layer norm: dx [T, K] (may be dy, x or dsum), dw and db [K]; None = not computed."""
+    for name, t in (("dx", dx), ("dw", dw), ("db", db)):
+        if t is not None and not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name} must be a tensor")
+    with _within(stream, x.device):
+        _native().layer_norm_backward(dy, x, weight, mean, rstd, dsum, dx, dw, db, workspace, None)
+
+
+def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                        dsum: Optional[torch.Tensor] = None, need_dx: bool = True, need_dw: bool = False, need_db: bool = False,
+                        workspace: Optional[torch.Tensor] = None, stream=None):
+    """(dx, dw, db); entries not asked for are None.  x is what was normalised (``sum`` where there was a residual), mean and rstd as ``layer_norm`` gave
+    them; ``dsum``: a gradient that reaches x past the norm, added to dx."""
+    with _within(stream, x.device):
+        return _native().layer_norm_backward(dy, x, weight, mean, rstd, dsum, True if need_dx else None, True if need_dw else None,
+                                             True if need_db else None, workspace, None)
+
+
+def salr_adapters_add_workspace_bytes(T: int, K: int, N: int, n: int, max_rank: int) -> int:
+    return int(lib().salr_adapters_add_workspace_bytes(T, K, N, n, max_rank))
+
+
+def salr_adapters_backward_workspace_bytes(T: int, K: int, N: int, n: int, max_rank: int, want_gradients: bool) -> int:
+    return int(lib().salr_adapters_backward_workspace_bytes(T, K, N, n, max_rank, int(want_gradients)))
+
+
+class AdapterSet:
+    """Adapters of many requests beside one shared layer [K -> N]: a list of pairs A_i [K, r_i], B_i [r_i, N] (bf16, ranks up to 256, each its own), of
+    which every token of a batch names one by its place in the list, or none by a negative id.  ``linear`` applies one pair to all tokens; here
+
+        y[t] = base[t] + (x[t] A_i) B_i,  i = ids[t]
+
+    The set is laid out and copied to the GPU when the object is made.  The tensors keep their memory: a call raises ValueError where one has other
+    memory than it had then; values may change (an optimiser's copies).  An id that is not below the number of adapters gives NaN in its token's row.
+
+    da, db   bf16 tensors of the shapes of a and b (or None for a pair that is frozen) that ``backward`` writes, as ``AdamW`` reads gradients where
+             they are.  None of them may share memory with another tensor of the set.
+    """
+
+    def __init__(self, a: Sequence[torch.Tensor], b: Sequence[torch.Tensor], da: Optional[Sequence[Optional[torch.Tensor]]] = None,
+                 db: Optional[Sequence[Optional[torch.Tensor]]] = None):
+        self.a, self.b = list(a), list(b)
+        self.da, self.db = (None if x is None else list(x) for x in (da, db))
+        got = _native().adapter_list(self.a, self.b, self.da, self.db)
+        self._list, self.n, self.K, self.N, self.max_rank, self._tensors = got
+        self._first = (self._list, self.n, self.K, self.N, self.max_rank, self._tensors)
+        self._add, self._backward = _native().adapters_add, _native().adapters_backward
+
+    def workspace_bytes(self, T: int) -> int:
+        """Of a workspace for ``add`` on T tokens."""
+        return salr_adapters_add_workspace_bytes(T, self.K, self.N, self.n, self.max_rank)
+
+    def backward_workspace_bytes(self, T: int) -> int:
+        """Of a workspace for ``backward`` on T tokens."""
+        return salr_adapters_backward_workspace_bytes(T, self.K, self.N, self.n, self.max_rank, True)
+
+    def add(self, x: torch.Tensor, ids: torch.Tensor, base: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+            workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """base + (x A_i) B_i for every token: x [T, K] bf16, ids [T] int32, base [T, N] bf16 (None: zeros).  ``out`` may be ``base``; None: allocated, as
+        the workspace is."""
+        if stream is None:
+            got = self._add(*self._first, x, ids, base, out, workspace, None)
+        else:
+            with _within(stream, self._list.device):
+                got = self._add(*self._first, x, ids, base, out, workspace, None)
+        return got if out is None else out
+
+    def linear(self, x: torch.Tensor, bitmap: torch.Tensor, values: torch.Tensor, row_offsets: torch.Tensor, ids: torch.Tensor,
+               workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The shared SALR layer with every token's own adapter: x What^T + (x A_i) B_i.  ``workspace``: of the layer (see ``linear``)."""
+        y = linear(x, bitmap, values, row_offsets, None, None, workspace)
+        return self.add(x, ids, y, out=y)
+
+    def backward(self, dy: torch.Tensor, x: Optional[torch.Tensor], ids: torch.Tensor, dx_base: Optional[torch.Tensor] = None,
+                 dx: Optional[torch.Tensor] = None, need_dx: bool = True, need_gradients: bool = True, workspace: Optional[torch.Tensor] = None,
+                 stream=None):
+        """(dx, da, db): dx = dx_base + (dy B_i^T) A_i^T in ``dx`` (which may be ``dx_base``; None: allocated), the gradients in the tensors that the set was
+        made with, those of an adapter without a token as zeros.  ``x``: what ``add`` had (None where only dx is asked for)."""
+        if need_gradients and self.da is None and self.db is None:
+            raise ValueError("a set made without da and db has no place for gradients")
+        out = (True if dx is None else dx) if need_dx else None
+        with _within(stream, self._list.device):
+            got = self._backward(*self._first, x, ids, dy, dx_base, out, need_gradients, workspace, None)
+        return got, self.da if need_gradients else None, self.db if need_gradients else None

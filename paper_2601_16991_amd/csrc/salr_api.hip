@@ -4,6 +4,7 @@
 #include "salr_internal.hpp"
 
 #include <atomic>
+#include <initializer_list>
 #include <limits>
 
 namespace {
@@ -53,6 +54,22 @@ bool cross_entropy_plan(int64_t T, int64_t K, int64_t V, bool want_dh, bool want
     if (K % 8 != 0 || K > ((int64_t)1 << 22) || T > most || V > most || (T > 0 && V < 1)) return false;
     *plan = salr::ce_plan(T, K, V, want_dh, want_dw);
     return salr::ce_launches_fit(*plan, T, K, V, want_dh, want_dw);
+}
+
+// Whether [a, a + bytes) and [b, b + bytes_b) share memory; in any other way than by being the same.
+bool overlaps(const void* a, size_t bytes, const void* b, size_t bytes_b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return a && b && bytes > 0 && bytes_b > 0 && x < y + bytes_b && y < x + bytes;
+}
+bool overlaps_in_part(const void* a, const void* b, size_t bytes) { return a != b && overlaps(a, bytes, b, bytes); }
+
+bool layer_norm_sizes(int64_t T, int64_t K) { return T <= salr::kLayerNormMostT && K <= salr::kLayerNormMostK; }
+
+// Sizes of the calls on adapters of many requests.
+salr_status_t adapters_sizes(int64_t T, int64_t K, int64_t N, int64_t n, int64_t max_rank) {
+    if (T < 0 || K < 0 || N < 0 || n < 1 || max_rank < 0 || max_rank > kMaxRank) return SALR_ERR_INVALID_ARG;
+    if (T > salr::kAdaptersMostT || K > salr::kAdaptersMostColumns || N > salr::kAdaptersMostColumns || n > salr::kAdaptersMostCount) return SALR_ERR_SHAPE;
+    return SALR_OK;
 }
 
 }  // namespace
@@ -544,6 +561,146 @@ salr_status_t salr_grad_norm(const void* plan, int64_t chunks, salr_type_t grad_
     if (workspace_bytes < SALR_GRAD_NORM_WORKSPACE_BYTES) return SALR_ERR_CAPACITY;
     const hipError_t e = salr::launch_grad_norm(static_cast<const salr::StepChunk*>(plan), chunks, grad_type == SALR_F32, max_norm, out, workspace,
                                                 static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SALR_OK : SALR_ERR_HIP;
+}
+
+salr_status_t salr_dropout(const void* x, const void* residual, int64_t count, salr_type_t type, double p, int64_t seed, const int64_t* seed_device,
+                           int64_t offset, void* y, void* stream) {
+    if (count < 0 || !is_type(type) || !(p >= 0.0 && p < 1.0)) return SALR_ERR_INVALID_ARG;
+    const uint32_t cut = (uint32_t)(p * 65536.0 + 0.5);
+    if (cut >= 65536) return SALR_ERR_INVALID_ARG;
+    if (count == 0) return SALR_OK;
+    const uintptr_t size = type == SALR_F32 ? 4 : 2;
+    if (!x || !y || misaligned(x, size) || misaligned(residual, size) || misaligned(y, size) || misaligned(seed_device, 8)) return SALR_ERR_INVALID_ARG;
+    if (count > (int64_t)1 << 42) return SALR_ERR_SHAPE;
+    if (overlaps_in_part(x, y, (size_t)count * size) || overlaps_in_part(residual, y, (size_t)count * size)) return SALR_ERR_INVALID_ARG;
+    const salr::DropoutArgs args{x, residual, count, cut, seed, seed_device, offset, y, type == SALR_F32};
+    const hipError_t e = salr::launch_dropout(args, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SALR_OK : SALR_ERR_HIP;
+}
+
+salr_status_t salr_layer_norm(const void* x, const void* residual, const void* weight, const void* bias, int64_t T, int64_t K, salr_type_t type,
+                              salr_type_t weight_type, double eps, void* y, void* sum, float* mean, float* rstd, void* stream) {
+    if (T < 0 || K < 0 || !is_type(type) || !is_type(weight_type) || !(eps >= 0.0 && eps <= std::numeric_limits<float>::max())) return SALR_ERR_INVALID_ARG;
+    if (!layer_norm_sizes(T, K)) return SALR_ERR_SHAPE;
+    if (T == 0 || K == 0) return SALR_OK;
+    const uintptr_t size = type == SALR_F32 ? 4 : 2, wsize = weight_type == SALR_F32 ? 4 : 2;
+    const size_t bytes = (size_t)(T * K) * size, wbytes = (size_t)K * wsize, stats = (size_t)T * 4;
+    if (!x || !weight || !y || (residual != nullptr) != (sum != nullptr)) return SALR_ERR_INVALID_ARG;
+    for (const void* p : {x, residual, static_cast<const void*>(y), static_cast<const void*>(sum)})
+        if (misaligned(p, size)) return SALR_ERR_INVALID_ARG;
+    if (misaligned(weight, wsize) || misaligned(bias, wsize) || misaligned(mean, 4) || misaligned(rstd, 4)) return SALR_ERR_INVALID_ARG;
+    for (const void* out : {static_cast<const void*>(y), static_cast<const void*>(sum)}) {
+        if (overlaps_in_part(out, x, bytes) || overlaps_in_part(out, residual, bytes) || overlaps(out, bytes, weight, wbytes) || overlaps(out, bytes, bias, wbytes) ||
+            overlaps(out, bytes, mean, stats) || overlaps(out, bytes, rstd, stats))
+            return SALR_ERR_INVALID_ARG;
+    }
+    if (overlaps(y, bytes, sum, bytes) || overlaps(mean, stats, rstd, stats)) return SALR_ERR_INVALID_ARG;
+    for (const float* out : {mean, rstd})
+        if (overlaps(out, stats, x, bytes) || overlaps(out, stats, residual, bytes) || overlaps(out, stats, weight, wbytes) || overlaps(out, stats, bias, wbytes))
+            return SALR_ERR_INVALID_ARG;
+    const salr::LayerNormArgs args{x, residual, weight, bias, T, (int)K, (float)eps, y, sum, mean, rstd, type == SALR_F32, weight_type == SALR_F32};
+    const hipError_t e = salr::launch_layer_norm(args, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SALR_OK : SALR_ERR_HIP;
+}
+
+size_t salr_layer_norm_backward_workspace_bytes(int64_t T, int64_t K, int want_weights) {
+    if (T <= 0 || K <= 0 || !layer_norm_sizes(T, K) || !want_weights) return 0;
+    return (size_t)(salr::layer_norm_parts(T, K) * K) * 2 * sizeof(float);
+}
+
+salr_status_t salr_layer_norm_backward(const void* dy, const void* x, const void* weight, const float* mean, const float* rstd, const void* dsum, int64_t T,
+                                       int64_t K, salr_type_t type, salr_type_t weight_type, void* dx, void* dw, void* db, void* workspace,
+                                       size_t workspace_bytes, void* stream) {
+    if (T < 0 || K < 0 || !is_type(type) || !is_type(weight_type)) return SALR_ERR_INVALID_ARG;
+    if (!layer_norm_sizes(T, K)) return SALR_ERR_SHAPE;
+    const bool weights = dw != nullptr || db != nullptr;
+    if (K == 0 || (T == 0 && !weights) || (!dx && !weights)) return SALR_OK;
+    if (T > 0 && (!dy || !x || !weight || !mean || !rstd)) return SALR_ERR_INVALID_ARG;
+    const uintptr_t size = type == SALR_F32 ? 4 : 2, wsize = weight_type == SALR_F32 ? 4 : 2;
+    const size_t bytes = (size_t)(T * K) * size, wbytes = (size_t)K * wsize, stats = (size_t)T * 4;
+    for (const void* p : {dy, x, dsum, static_cast<const void*>(dx)})
+        if (misaligned(p, size)) return SALR_ERR_INVALID_ARG;
+    for (const void* p : {weight, static_cast<const void*>(dw), static_cast<const void*>(db)})
+        if (misaligned(p, wsize)) return SALR_ERR_INVALID_ARG;
+    if (misaligned(mean, 4) || misaligned(rstd, 4) || misaligned(workspace, 16)) return SALR_ERR_INVALID_ARG;
+    if (overlaps_in_part(dx, dy, bytes) || overlaps_in_part(dx, x, bytes) || overlaps_in_part(dx, dsum, bytes) || overlaps(dx, bytes, weight, wbytes) ||
+        overlaps(dx, bytes, mean, stats) || overlaps(dx, bytes, rstd, stats) || overlaps(dw, wbytes, db, wbytes))
+        return SALR_ERR_INVALID_ARG;
+    for (const void* out : {dw, db})   // (written by a second launch: after weight, mean and rstd have been read, but dx is out by then)
+        if (overlaps(out, wbytes, dx, bytes) || overlaps(out, wbytes, dy, bytes) || overlaps(out, wbytes, x, bytes) || overlaps(out, wbytes, dsum, bytes) ||
+            overlaps(out, wbytes, weight, wbytes) || overlaps(out, wbytes, mean, stats) || overlaps(out, wbytes, rstd, stats))
+            return SALR_ERR_INVALID_ARG;
+    const size_t need = salr_layer_norm_backward_workspace_bytes(T, K, weights);
+    if (workspace_bytes < need) return SALR_ERR_CAPACITY;
+    if (need > 0 && !workspace) return SALR_ERR_INVALID_ARG;
+    const salr::LayerNormGradArgs args{dy, x, weight, mean, rstd, dsum, T, (int)K, dx, static_cast<float*>(workspace), type == SALR_F32, weight_type == SALR_F32};
+    const hipError_t e = salr::launch_layer_norm_backward(args, dw, db, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? SALR_OK : SALR_ERR_HIP;
+}
+
+salr_status_t salr_adapter_list_check(const salr_adapter_t* adapters, int64_t n, int64_t* max_rank) {
+    if (n < 0 || (n > 0 && !adapters) || !max_rank) return SALR_ERR_INVALID_ARG;
+    if (n > salr::kAdaptersMostCount) return SALR_ERR_SHAPE;
+    int64_t most = 0;
+    for (int64_t i = 0; i < n; ++i) {
+        const salr_adapter_t& a = adapters[i];
+        if (a.rank < 0) return SALR_ERR_INVALID_ARG;
+        if (a.rank > kMaxRank) return SALR_ERR_UNSUPPORTED;
+        if (a.rank == 0) continue;
+        if (!a.a || !a.b || misaligned(a.a, 16) || misaligned(a.b, 16) || misaligned(a.da, 16) || misaligned(a.db, 16)) return SALR_ERR_INVALID_ARG;
+        if (a.rank > most) most = a.rank;
+    }
+    *max_rank = most;
+    return SALR_OK;
+}
+
+size_t salr_adapters_add_workspace_bytes(int64_t T, int64_t K, int64_t N, int64_t n, int64_t max_rank) {
+    if (adapters_sizes(T, K, N, n, max_rank) != SALR_OK || T == 0 || N == 0) return 0;
+    return salr::request_adapters_plan(T, K, N, n, max_rank, false, false).bytes;
+}
+
+salr_status_t salr_adapters_add(const salr_adapter_t* list, int64_t n, int64_t max_rank, const uint16_t* x, int64_t T, int64_t K, int64_t N,
+                                const int32_t* ids, const uint16_t* base, uint16_t* y, void* workspace, size_t workspace_bytes, void* stream) {
+    const salr_status_t st = adapters_sizes(T, K, N, n, max_rank);
+    if (st != SALR_OK) return st;
+    if (T == 0 || N == 0) return SALR_OK;
+    if (!list || (K > 0 && !x) || !ids || !y) return SALR_ERR_INVALID_ARG;
+    if (misaligned(list, 8) || misaligned(x, 2) || misaligned(ids, 4) || misaligned(base, 2) || misaligned(y, 2) || misaligned(workspace, 256)) return SALR_ERR_INVALID_ARG;
+    const size_t bytes = (size_t)(T * N) * 2;
+    if (overlaps_in_part(y, base, bytes) || overlaps(y, bytes, x, (size_t)(T * K) * 2) || overlaps(y, bytes, ids, (size_t)T * 4)) return SALR_ERR_INVALID_ARG;
+    const salr::RequestAdaptersPlan plan = salr::request_adapters_plan(T, K, N, n, max_rank, false, false);
+    if (workspace_bytes < plan.bytes) return SALR_ERR_CAPACITY;
+    if (!workspace) return SALR_ERR_INVALID_ARG;
+    const salr::RequestAdaptersArgs args{list, n, x, nullptr, T, K, N, ids, base, y, false, workspace, static_cast<hipStream_t>(stream)};
+    const hipError_t e = salr::launch_request_adapters(args, plan);
+    return e == hipSuccess ? SALR_OK : SALR_ERR_HIP;
+}
+
+size_t salr_adapters_backward_workspace_bytes(int64_t T, int64_t K, int64_t N, int64_t n, int64_t max_rank, int want_gradients) {
+    if (adapters_sizes(T, K, N, n, max_rank) != SALR_OK) return 0;
+    return salr::request_adapters_plan(T, K, N, n, max_rank, true, want_gradients != 0).bytes;
+}
+
+salr_status_t salr_adapters_backward(const salr_adapter_t* list, int64_t n, int64_t max_rank, const uint16_t* x, const uint16_t* dy, int64_t T,
+                                     int64_t K, int64_t N, const int32_t* ids, const uint16_t* dx_base, uint16_t* dx, int want_gradients,
+                                     void* workspace, size_t workspace_bytes, void* stream) {
+    const salr_status_t st = adapters_sizes(T, K, N, n, max_rank);
+    if (st != SALR_OK) return st;
+    if (!want_gradients && (!dx || T == 0 || K == 0)) return SALR_OK;
+    if (!list || (T > 0 && (!ids || (N > 0 && !dy) || (want_gradients && K > 0 && !x)))) return SALR_ERR_INVALID_ARG;
+    if (misaligned(list, 8) || misaligned(x, 2) || misaligned(dy, 2) || misaligned(ids, 4) || misaligned(dx_base, 2) || misaligned(dx, 2) ||
+        misaligned(workspace, 256))
+        return SALR_ERR_INVALID_ARG;
+    const size_t bytes = (size_t)(T * K) * 2;
+    if (overlaps_in_part(dx, dx_base, bytes) || overlaps(dx, bytes, x, bytes) || overlaps(dx, bytes, dy, (size_t)(T * N) * 2) ||
+        overlaps(dx, bytes, ids, (size_t)T * 4))
+        return SALR_ERR_INVALID_ARG;
+    const salr::RequestAdaptersPlan plan = salr::request_adapters_plan(T, K, N, n, max_rank, true, want_gradients != 0);
+    if (workspace_bytes < plan.bytes) return SALR_ERR_CAPACITY;
+    if (!workspace) return SALR_ERR_INVALID_ARG;
+    const salr::RequestAdaptersArgs args{list, n, x, dy, T, K, N, ids, dx_base, K > 0 ? dx : nullptr, want_gradients != 0, workspace, static_cast<hipStream_t>(stream)};
+    const hipError_t e = salr::launch_request_adapters_backward(args, plan);
     return e == hipSuccess ? SALR_OK : SALR_ERR_HIP;
 }
 

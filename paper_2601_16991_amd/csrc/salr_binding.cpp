@@ -680,6 +680,316 @@ PyObject* py_step_list(PyObject*, PyObject* const* v, Py_ssize_t n) {
     SALR_CATCH
 }
 
+// ---- what is beside a layer: dropout, layer norm, adapters of many requests
+
+salr_type_t float_type(const at::Tensor& t, const char* name) {
+    if (t.scalar_type() == at::kFloat) return SALR_F32;
+    if (!dtype_ok(t.scalar_type(), kBf16)) fail(PyExc_TypeError, "%s must be fp32 or bf16", name);
+    return SALR_BF16;
+}
+
+// A tensor of the type, shape and device of `like`; undefined where it is None.
+const at::Tensor& alike(PyObject* o, const at::Tensor& like, const char* name) {
+    const at::Tensor& t = tensor_of(o, name);
+    if (!t.defined()) return t;
+    if (t.scalar_type() != like.scalar_type()) fail(PyExc_TypeError, "%s: unexpected dtype", name);
+    if (t.sizes() != like.sizes()) fail(PyExc_ValueError, "%s: unexpected shape", name);
+    if (!t.is_cuda()) fail(PyExc_TypeError, "%s must be a CUDA tensor", name);
+    if (!t.is_contiguous()) fail(PyExc_TypeError, "%s must be contiguous", name);
+    need_device(t, like.device(), name);
+    return t;
+}
+void* address(const at::Tensor& t) { return t.defined() && t.numel() > 0 ? t.data_ptr() : nullptr; }
+
+const at::Tensor& given_float(PyObject* o, const char* name) {
+    const at::Tensor& t = tensor_of(o, name);
+    if (!t.defined()) fail(PyExc_TypeError, "%s must be a tensor", name);
+    if (!t.is_cuda()) fail(PyExc_TypeError, "%s must be a CUDA tensor", name);
+    if (!t.is_contiguous()) fail(PyExc_TypeError, "%s must be contiguous", name);
+    return t;
+}
+
+PyObject* tuple_of(std::initializer_list<const at::Tensor*> results) {   // None for those that are not defined
+    PyObject* out = PyTuple_New((Py_ssize_t)results.size());
+    if (!out) throw PyFailure{};
+    Py_ssize_t i = 0;
+    for (const at::Tensor* t : results) {
+        if (!t->defined()) Py_INCREF(Py_None);
+        PyTuple_SET_ITEM(out, i++, t->defined() ? THPVariable_Wrap(*t) : Py_None);
+    }
+    return out;
+}
+
+// dropout(x, residual, p, seed, offset, y, stream) -> y, allocated where it is None; seed: a number, or a tensor of one on the device
+PyObject* py_dropout(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    SALR_TRY
+    need_args(n, 7, "dropout");
+    const at::Tensor& x = given_float(v[0], "x");
+    const salr_type_t type = float_type(x, "x");
+    const at::Tensor& residual = alike(v[1], x, "residual");
+    const double p = double_of(v[2]);
+    int64_t seed = 0;
+    const int64_t* seed_device = nullptr;
+    if (THPVariable_Check(v[3])) {
+        const at::Tensor& t = tensor_of(v[3], "seed");
+        if (t.numel() != 1) fail(PyExc_ValueError, "%s must be one value", "seed");
+        seed_device = device_ptr<int64_t>(t, kI64, "seed");
+        need_device(t, x.device(), "seed");
+    } else {
+        seed = int_of(v[3]);
+    }
+    const int64_t offset = int_of(v[4]);
+    const OnDevice on(x.device());
+    at::Tensor y = v[5] == Py_None ? empty_on(x.sizes(), x.scalar_type(), x) : alike(v[5], x, "y");
+    void* stream = stream_of(v[6]);
+    salr_status_t st;
+    {
+        Gil release;
+        st = salr_dropout(address(x), address(residual), x.numel(), type, p, seed, seed_device, offset, address(y), stream);
+    }
+    check(st, "salr_dropout");
+    return result(v[5], std::move(y));
+    SALR_CATCH
+}
+
+const at::Tensor& weights_of(PyObject* o, int64_t K, const at::Tensor& like, const char* name) {
+    const at::Tensor& t = tensor_of(o, name);
+    if (!t.defined()) return t;
+    if (t.dim() != 1 || t.size(0) != K) fail(PyExc_ValueError, "%s must be [K]", name);
+    if (!t.is_cuda()) fail(PyExc_TypeError, "%s must be a CUDA tensor", name);
+    if (!t.is_contiguous()) fail(PyExc_TypeError, "%s must be contiguous", name);
+    need_device(t, like.device(), name);
+    float_type(t, name);
+    return t;
+}
+float* row_values(PyObject* o, int64_t T, const at::Tensor& like, const char* name, bool needed) {
+    const at::Tensor& t = tensor_of(o, name);
+    if (!t.defined() && needed) fail(PyExc_TypeError, "%s must be a tensor", name);
+    if (t.defined() && (t.dim() != 1 || t.size(0) != T)) fail(PyExc_ValueError, "%s must be [T]", name);
+    need_device(t, like.device(), name);
+    return device_ptr<float>(t, kF32, name);
+}
+
+// layer_norm(x, residual, weight, bias, eps, y, sum, mean, rstd, stream, allocate) -> (y, sum, mean, rstd); allocate: those outputs are None and made
+PyObject* py_layer_norm(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    SALR_TRY
+    need_args(n, 11, "layer_norm");
+    const at::Tensor& x = given_float(v[0], "x");
+    need_matrix(x, "x");
+    const int64_t T = x.size(0), K = x.size(1);
+    const salr_type_t type = float_type(x, "x");
+    const at::Tensor& residual = alike(v[1], x, "residual");
+    const at::Tensor &weight = weights_of(v[2], K, x, "weight"), &bias = weights_of(v[3], K, x, "bias");
+    if (!weight.defined()) fail(PyExc_TypeError, "%s must be a tensor", "weight");
+    const salr_type_t wtype = float_type(weight, "weight");
+    if (bias.defined() && bias.scalar_type() != weight.scalar_type()) fail(PyExc_TypeError, "%s: of another type than weight", "bias");
+    const double eps = double_of(v[4]);
+    const OnDevice on(x.device());
+    at::Tensor y, sum, mean, rstd;
+    float *mp, *rp;
+    if (PyObject_IsTrue(v[10]) == 1) {
+        y = empty_on({T, K}, x.scalar_type(), x);
+        if (residual.defined()) sum = empty_on({T, K}, x.scalar_type(), x);
+        mean = empty_on({T}, at::kFloat, x);
+        rstd = empty_on({T}, at::kFloat, x);
+        mp = static_cast<float*>(address(mean));
+        rp = static_cast<float*>(address(rstd));
+    } else {
+        y = alike(v[5], x, "y");
+        sum = alike(v[6], x, "sum");
+        if (!y.defined()) fail(PyExc_TypeError, "%s must be a tensor", "y");
+        mp = row_values(v[7], T, x, "mean", false);
+        rp = row_values(v[8], T, x, "rstd", false);
+    }
+    void* stream = stream_of(v[9]);
+    salr_status_t st;
+    {
+        Gil release;
+        st = salr_layer_norm(address(x), address(residual), address(weight), address(bias), T, K, type, wtype, eps, address(y), address(sum), mp, rp, stream);
+    }
+    check(st, "salr_layer_norm");
+    return tuple_of({&y, &sum, &mean, &rstd});
+    SALR_CATCH
+}
+
+// layer_norm_backward(dy, x, weight, mean, rstd, dsum, dx, dw, db, workspace, stream) -> (dx, dw, db); True for one of the three: made, None: not computed
+PyObject* py_layer_norm_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    SALR_TRY
+    need_args(n, 11, "layer_norm_backward");
+    const at::Tensor& x = given_float(v[1], "x");
+    need_matrix(x, "x");
+    const int64_t T = x.size(0), K = x.size(1);
+    const salr_type_t type = float_type(x, "x");
+    const at::Tensor &dy = alike(v[0], x, "dy"), &weight = weights_of(v[2], K, x, "weight"), &dsum = alike(v[5], x, "dsum");
+    if (!dy.defined()) fail(PyExc_TypeError, "%s must be a tensor", "dy");
+    if (!weight.defined()) fail(PyExc_TypeError, "%s must be a tensor", "weight");
+    const salr_type_t wtype = float_type(weight, "weight");
+    const float *mean = row_values(v[3], T, x, "mean", true), *rstd = row_values(v[4], T, x, "rstd", true);
+    const OnDevice on(x.device());
+    const auto output = [&](PyObject* o, const at::Tensor& like, const char* name) {
+        return o == Py_True ? empty_on(like.sizes(), like.scalar_type(), x) : at::Tensor(alike(o, like, name));
+    };
+    at::Tensor dx = output(v[6], x, "dx"), dw = output(v[7], weight, "dw"), db = output(v[8], weight, "db");
+    Workspace ws;
+    ws.given(v[9], x);
+    if (v[9] == Py_None) ws.allocate(salr_layer_norm_backward_workspace_bytes(T, K, dw.defined() || db.defined()), x);
+    void* stream = stream_of(v[10]);
+    salr_status_t st;
+    {
+        Gil release;
+        st = salr_layer_norm_backward(address(dy), address(x), address(weight), mean, rstd, address(dsum), T, K, type, wtype, address(dx), address(dw),
+                                      address(db), ws.ptr, ws.bytes, stream);
+    }
+    check(st, "salr_layer_norm_backward");
+    return tuple_of({&dx, &dw, &db});
+    SALR_CATCH
+}
+
+// adapter_list(a, b, da, db) -> (records on the device, n, K, N, max_rank, tensors)
+PyObject* py_adapter_list(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    SALR_TRY
+    need_args(n, 4, "adapter_list");
+    const TensorList as(v[0], "a"), bs(v[1], "b"), das(v[2], "da"), dbs(v[3], "db");
+    const Py_ssize_t count = as.size;
+    if (count == 0) fail(PyExc_ValueError, "no %s", "adapters");
+    for (const TensorList* l : {&bs, &das, &dbs})
+        if ((l->fast || l == &bs) && l->size != count) fail(PyExc_ValueError, "lists of different %s", "lengths");
+    const at::Tensor &a0 = as.at(0, "a"), &b0 = bs.at(0, "b");
+    need_matrix(a0, "a");
+    need_matrix(b0, "b");
+    const at::Device device = a0.device();
+    const int64_t K = a0.size(0), N = b0.size(1);
+    if (K == 0 || N == 0) fail(PyExc_ValueError, "a layer without %s", "features");
+    auto tensors = std::make_unique<StepTensors>();
+    std::vector<StepRange> ranges;
+    const auto pointer = [&](const at::Tensor& t, int64_t rows, int64_t cols, const char* name, bool written) -> uint16_t* {
+        need_matrix(t, name);
+        if (!t.is_cuda()) fail(PyExc_TypeError, "%s must be a CUDA tensor", name);
+        if (!dtype_ok(t.scalar_type(), kBf16)) fail(PyExc_TypeError, "%s must be bf16", name);
+        if (!t.is_contiguous()) fail(PyExc_TypeError, "%s must be contiguous", name);
+        if (t.device() != device) fail(PyExc_ValueError, "%s: tensors on different devices", name);
+        if (t.size(0) != rows || t.size(1) != cols) fail(PyExc_ValueError, "%s: unexpected shape", name);
+        tensors->all.push_back({t, t.const_data_ptr()});
+        tensors->states.push_back(t);
+        if (written && !t.is_inference()) tensors->versioned.push_back(t);
+        const uintptr_t at = reinterpret_cast<uintptr_t>(t.const_data_ptr());
+        if (t.numel() > 0) ranges.push_back({at, at + t.nbytes(), written, name});
+        return static_cast<uint16_t*>(address(t));
+    };
+    std::vector<salr_adapter_t> table((size_t)count);
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        salr_adapter_t& t = table[(size_t)i];
+        const at::Tensor& a = as.at(i, "a");
+        need_matrix(a, "a");
+        t.rank = a.size(1);
+        t.a = pointer(a, K, t.rank, "a", false);
+        t.b = pointer(bs.at(i, "b"), t.rank, N, "b", false);
+        t.da = das.fast && das.at(i, "da").defined() ? pointer(das.at(i, "da"), K, t.rank, "da", true) : nullptr;
+        t.db = dbs.fast && dbs.at(i, "db").defined() ? pointer(dbs.at(i, "db"), t.rank, N, "db", true) : nullptr;
+    }
+    if (const char* name = written_twice(ranges)) fail(PyExc_ValueError, "%s: shares memory with another tensor of the list", name);
+    int64_t max_rank = 0;
+    check(salr_adapter_list_check(table.data(), count, &max_rank), "salr_adapter_list_check");
+    at::Tensor host = at::empty({(int64_t)(table.size() * sizeof(salr_adapter_t))}, at::TensorOptions().dtype(at::kByte));
+    std::copy_n(reinterpret_cast<const uint8_t*>(table.data()), host.numel(), static_cast<uint8_t*>(host.data_ptr()));
+    const c10::DeviceGuard on(device);
+    tensors->home = stream_of(Py_None);
+    at::Tensor list;
+    {
+        Gil release;
+        list = host.to(device);
+    }
+    PyObject* held = StepTensors::capsule(std::move(tensors));
+    return Py_BuildValue("NnLLLN", THPVariable_Wrap(std::move(list)), count, (long long)K, (long long)N, (long long)max_rank, held);
+    SALR_CATCH
+}
+
+struct AdapterCall {   // list, n, K, N, max_rank, tensors, x, ids: the first arguments of the calls on a list
+    StepTensors& held;
+    const at::Tensor &list, &x, &ids;
+    int64_t n, K, N, max_rank, T = 0;
+    explicit AdapterCall(PyObject* const* v, const at::Tensor& rows)
+        : held(StepTensors::check(v[5])), list(tensor_of(v[0], "list")), x(tensor_of(v[6], "x")), ids(tensor_of(v[7], "ids")), n(int_of(v[1])),
+          K(int_of(v[2])), N(int_of(v[3])), max_rank(int_of(v[4])) {
+        if (!list.defined()) fail(PyExc_TypeError, "%s must be a tensor", "list");
+        if (!rows.defined()) fail(PyExc_TypeError, "%s must be a tensor", "x");
+        need_matrix(rows, "x");
+        T = rows.size(0);
+        if (x.defined()) matrix(x, K, "x");
+        if (!ids.defined() || ids.dim() != 1 || ids.size(0) != T) fail(PyExc_ValueError, "%s must be [T]", "ids");
+        if (ids.scalar_type() != at::kInt) fail(PyExc_TypeError, "%s must be int32", "ids");
+        device_ptr<uint32_t>(ids, kU32, "ids");
+        need_device(ids, list.device(), "ids");
+    }
+    void matrix(const at::Tensor& t, int64_t columns, const char* name) const {   // [T, columns] bf16 where it is defined
+        if (!t.defined()) return;
+        need_matrix(t, name);
+        if (t.size(0) != T || t.size(1) != columns) fail(PyExc_ValueError, "%s: unexpected shape", name);
+        device_ptr<uint16_t>(t, kBf16, name);
+        need_device(t, list.device(), name);
+    }
+    const salr_adapter_t* records() const { return static_cast<const salr_adapter_t*>(list.data_ptr()); }
+};
+
+// adapters_add(list, n, K, N, max_rank, tensors, x, ids, base, y, workspace, stream) -> y, allocated where it is None
+PyObject* py_adapters_add(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    SALR_TRY
+    need_args(n, 12, "adapters_add");
+    const AdapterCall c(v, tensor_of(v[6], "x"));
+    const at::Tensor& base = tensor_of(v[8], "base");
+    c.matrix(base, c.N, "base");
+    const OnDevice on(c.list.device());
+    at::Tensor y = v[9] == Py_None ? empty_on({c.T, c.N}, c.x.scalar_type(), c.x) : tensor_of(v[9], "y");
+    c.matrix(y, c.N, "y");
+    Workspace ws;
+    ws.given(v[10], c.x);
+    if (v[10] == Py_None) ws.allocate(salr_adapters_add_workspace_bytes(c.T, c.K, c.N, c.n, c.max_rank), c.x);
+    void* stream = stream_of(v[11]);
+    c.held.uses(c.held.step_on, stream, {&c.list}, true);
+    salr_status_t st;
+    {
+        Gil release;
+        st = salr_adapters_add(c.records(), c.n, c.max_rank, static_cast<uint16_t*>(address(c.x)), c.T, c.K, c.N, static_cast<int32_t*>(address(c.ids)),
+                               static_cast<uint16_t*>(address(base)), static_cast<uint16_t*>(address(y)), ws.ptr, ws.bytes, stream);
+    }
+    check(st, "salr_adapters_add");
+    return result(v[9], std::move(y));
+    SALR_CATCH
+}
+
+// adapters_backward(list, n, K, N, max_rank, tensors, x, ids, dy, dx_base, dx, want_gradients, workspace, stream) -> dx; True for dx: made, None: not computed
+PyObject* py_adapters_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    SALR_TRY
+    need_args(n, 14, "adapters_backward");
+    const at::Tensor& dy = tensor_of(v[8], "dy");
+    const AdapterCall c(v, dy);
+    c.matrix(dy, c.N, "dy");
+    const bool gradients = PyObject_IsTrue(v[11]) == 1;
+    if (gradients && !c.x.defined()) fail(PyExc_TypeError, "%s must be a tensor", "x");
+    const at::Tensor& dx_base = tensor_of(v[9], "dx_base");
+    c.matrix(dx_base, c.K, "dx_base");
+    const OnDevice on(c.list.device());
+    at::Tensor dx = v[10] == Py_True ? empty_on({c.T, c.K}, dy.scalar_type(), dy) : tensor_of(v[10], "dx");
+    c.matrix(dx, c.K, "dx");
+    Workspace ws;
+    ws.given(v[12], dy);
+    if (v[12] == Py_None) ws.allocate(salr_adapters_backward_workspace_bytes(c.T, c.K, c.N, c.n, c.max_rank, gradients), dy);
+    void* stream = stream_of(v[13]);
+    c.held.uses(c.held.step_on, stream, {&c.list}, true);
+    salr_status_t st;
+    {
+        Gil release;
+        st = salr_adapters_backward(c.records(), c.n, c.max_rank, static_cast<uint16_t*>(address(c.x)), static_cast<uint16_t*>(address(dy)), c.T, c.K, c.N,
+                                    static_cast<int32_t*>(address(c.ids)), static_cast<uint16_t*>(address(dx_base)), static_cast<uint16_t*>(address(dx)),
+                                    gradients, ws.ptr, ws.bytes, stream);
+    }
+    check(st, "salr_adapters_backward");
+    if (gradients) c.held.changed();
+    if (!dx.defined()) Py_RETURN_NONE;
+    return THPVariable_Wrap(std::move(dx));
+    SALR_CATCH
+}
+
 PyObject* py_set_error(PyObject*, PyObject* cls) {
     Py_XINCREF(cls);
     Py_XSETREF(g_salr_error, cls);
@@ -697,6 +1007,12 @@ PyMethodDef kMethods[] = {
     SALR_FAST("step_list", py_step_list),
     SALR_FAST("adamw_step", py_adamw_step),
     SALR_FAST("grad_norm", py_grad_norm),
+    SALR_FAST("dropout", py_dropout),
+    SALR_FAST("layer_norm", py_layer_norm),
+    SALR_FAST("layer_norm_backward", py_layer_norm_backward),
+    SALR_FAST("adapter_list", py_adapter_list),
+    SALR_FAST("adapters_add", py_adapters_add),
+    SALR_FAST("adapters_backward", py_adapters_backward),
     {"encode", py_encode, METH_O, nullptr},
     {"set_error", py_set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},

@@ -864,4 +864,81 @@ CePlan ce_plan(int64_t T, int64_t K, int64_t V, bool want_dh, bool want_dw);
 bool ce_launches_fit(const CePlan& p, int64_t T, int64_t K, int64_t V, bool want_dh, bool want_dw);
 hipError_t launch_cross_entropy(const CeArgs& a, void* workspace);
 
+// ---- Dropout (salr_dropout.hip)
+struct DropoutArgs {
+    const void* x;
+    const void* residual;
+    int64_t count;
+    uint32_t cut;            // of 65536: elements whose 16 random bits are below it are dropped
+    int64_t seed;
+    const int64_t* seed_at;  // read instead of seed where it is not null
+    int64_t offset;
+    void* y;
+    bool f32;
+};
+hipError_t launch_dropout(const DropoutArgs& a, hipStream_t stream);
+
+// ---- Layer norm (salr_layer_norm.hip)
+constexpr int64_t kLayerNormMostK = 32768;         // a row is held in the registers of up to sixteen waves
+constexpr int64_t kLayerNormMostT = (1 << 22) - 1; // workgroups of up to 1024 threads, fewer than 2^32 of them in a launch
+constexpr int64_t kLayerNormParts = 256;           // workgroups that sum dw and db: one a CU
+struct LayerNormArgs {
+    const void* x;
+    const void* residual;
+    const void* weight;
+    const void* bias;
+    int64_t T;
+    int K;
+    float eps;
+    void* y;
+    void* sum;
+    float* mean;
+    float* rstd;
+    bool f32, w32;
+};
+struct LayerNormGradArgs {
+    const void* dy;
+    const void* x;
+    const void* weight;
+    const float* mean;
+    const float* rstd;
+    const void* dsum;
+    int64_t T;
+    int K;
+    void* dx;
+    float* part;   // [2][parts][K]
+    bool f32, w32;
+};
+int64_t layer_norm_parts(int64_t T, int64_t K);
+hipError_t launch_layer_norm(const LayerNormArgs& a, hipStream_t stream);
+hipError_t launch_layer_norm_backward(const LayerNormGradArgs& a, void* dw, void* db, hipStream_t stream);
+
+// ---- Adapters of many requests (salr_request_adapters.hip)
+constexpr int64_t kAdaptersMostT = ((int64_t)1 << 28) - 1, kAdaptersMostColumns = (int64_t)1 << 22, kAdaptersMostCount = 65533;
+struct RequestAdaptersPlan {
+    bool direct;             // few tokens: a workgroup finds its own among the ids; else a launch in front orders them
+    int64_t rows, tiles;     // tokens of a tile, tiles of the launches
+    int64_t t_rows;          // rows of the products with the first factor
+    int rpad;                // their columns
+    int slices_x, slices_dy; // slices of K and N that they are summed over
+    size_t order, starts, counts, part_x, part_dy, t_x, t_dy;   // offsets in the workspace
+    size_t bytes;
+};
+RequestAdaptersPlan request_adapters_plan(int64_t T, int64_t K, int64_t N, int64_t n, int64_t max_rank, bool backward, bool want_dadb);
+struct RequestAdaptersArgs {
+    const salr_adapter_t* list;   // on the device
+    int64_t n;
+    const uint16_t* x;
+    const uint16_t* dy;           // backward
+    int64_t T, K, N;
+    const int32_t* ids;
+    const uint16_t* base;
+    uint16_t* out;                // y, or dx (may be null in the backward pass)
+    bool want_dadb;
+    void* workspace;
+    hipStream_t stream;
+};
+hipError_t launch_request_adapters(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p);
+hipError_t launch_request_adapters_backward(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p);
+
 }  // namespace salr

@@ -1,0 +1,298 @@
+// Layer norm of a row s of K values, s = x or the stored sum x + residual, and its gradient:
+//
+//   mean = sum s / K,  rstd = 1 / sqrt(sum (s - mean)^2 / K + eps),  xhat = (s - mean) rstd,  y = xhat w + b
+//   g = dy w,  dx = rstd (g - sum g / K - xhat sum (g xhat) / K) + dsum,  dw = sum over rows of dy xhat,  db = sum over rows of dy
+//
+// What bounds both is memory: every matrix crosses it once.  A team of 1 to 16 waves holds a row in registers, as it lies in memory (8 or 16
+// bytes of registers for four elements), each lane one to four vectors of eight elements; sums go over the lanes in registers and over the
+// team's waves through LDS.  The variance is summed from differences to the mean in a second pass over the registers: squares alone lose
+// what a large mean hides.  Sums are fp32.
+//
+// dw and db: a workgroup of sixteen waves goes through rows, its lanes keep the sums of their columns; the teams of a workgroup are added in LDS,
+// in order, and the workgroups' sums, at most kLayerNormParts of them, by a second launch: no atomics, the same bits every time.
+#include <type_traits>
+
+#include "salr_eight.hpp"
+#include "salr_internal.hpp"
+
+namespace salr {
+
+// Sum over the wave, in every lane: within rows of 16 lanes, then over the rows.
+__device__ __forceinline__ float wave_sum(float v) {
+    const auto add = [](float a, int b) { return a + __int_as_float(b); };
+    v = add(v, __builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x111, 0xf, 0xf, false));
+    v = add(v, __builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x112, 0xf, 0xf, false));
+    v = add(v, __builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x114, 0xf, 0xf, false));
+    v = add(v, __builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x118, 0xf, 0xf, false));
+    v = add(v, __builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x142, 0xa, 0xf, false));
+    v = add(v, __builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x143, 0xc, 0xf, false));
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), kWave - 1));
+}
+
+// Sum over a team of kTeam waves, every wave of the workgroup calling it.  `slots` (kSums floats a wave) are another set at every call until
+// two barriers have passed.
+template <int kTeam, int kSums>
+__device__ __forceinline__ void team_sum(float (&v)[kSums], float* slots) {
+#pragma unroll
+    for (int i = 0; i < kSums; ++i) v[i] = wave_sum(v[i]);
+    if constexpr (kTeam > 1) {
+        const int wave = threadIdx.x >> 6, first = wave / kTeam * kTeam;
+        if (lane_id() == 0)
+#pragma unroll
+            for (int i = 0; i < kSums; ++i) slots[wave * kSums + i] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kSums; ++i) {
+            float s = 0.f;
+#pragma unroll
+            for (int t = 0; t < kTeam; ++t) s += slots[(first + t) * kSums + i];
+            v[i] = s;
+        }
+    }
+}
+
+// Eight weights from element i on, in fp32.
+__device__ __forceinline__ void load_weights(const void* w, bool w32, int i, int left, float (&out)[8]) {
+    if (w32) {
+        const Eight<true> q = load_eight<true, false, false>(w, i, left);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) out[j] = q.get(j);
+    } else {
+        const Eight<false> q = load_eight<false, false, false>(w, i, left);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) out[j] = q.get(j);
+    }
+}
+
+template <bool k32, int kTeam, int kUnits>
+__global__ __launch_bounds__(kTeam < 4 ? 256 : 64 * kTeam) void layer_norm_kernel(LayerNormArgs a) {
+    constexpr int kWaves = kTeam < 4 ? 4 : kTeam, kTeams = kWaves / kTeam;
+    __shared__ float slots[2][kWaves];
+    const int team = threadIdx.x / (64 * kTeam), at = threadIdx.x % (64 * kTeam), K = a.K;
+    const int64_t row = (int64_t)blockIdx.x * kTeams + team;
+    const bool live = row < a.T;   // (the others go through the barriers)
+    const int64_t start = (live ? row : 0) * K * (k32 ? 4 : 2);
+    const char* x = static_cast<const char*>(a.x) + start;
+    const char* residual = static_cast<const char*>(a.residual) + start;
+    char* y = static_cast<char*>(a.y) + start;
+    float s[kUnits][8], sums[1] = {0.f};
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+        const int i = 8 * (at + 64 * kTeam * u), left = live ? K - i : 0;
+        const Eight<k32> q = load_eight<k32, false, false>(x, i, left);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[u][j] = q.get(j);
+    }
+    if (a.residual != nullptr) {
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const int i = 8 * (at + 64 * kTeam * u), left = live ? K - i : 0;
+            const Eight<k32> q = load_eight<k32, false, false>(residual, i, left);
+            // the sum is rounded as it is stored, and the norm is of that: so is the gradient, which reads it back
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                s[u][j] += q.get(j);
+                if constexpr (!k32) s[u][j] = (float)(__bf16)s[u][j];
+            }
+            if (left > 0) store_eight<k32, false>(static_cast<char*>(a.sum) + start, i, left, s[u]);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sums[0] += s[u][j];
+    team_sum<kTeam>(sums, slots[0]);
+    const float mean = sums[0] / (float)K;
+    sums[0] = 0.f;
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+        const int left = K - 8 * (at + 64 * kTeam * u);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float d = j < left ? s[u][j] - mean : 0.f;
+            sums[0] = fmaf(d, d, sums[0]);
+        }
+    }
+    team_sum<kTeam>(sums, slots[1]);
+    const float rstd = 1.f / sqrtf(sums[0] / (float)K + a.eps);
+    if (!live) return;
+    if (at == 0) {
+        if (a.mean != nullptr) a.mean[row] = mean;
+        if (a.rstd != nullptr) a.rstd[row] = rstd;
+    }
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+        const int i = 8 * (at + 64 * kTeam * u), left = K - i;
+        if (left <= 0) break;
+        float w[8], b[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        load_weights(a.weight, a.w32, i, left, w);
+        if (a.bias != nullptr) load_weights(a.bias, a.w32, i, left, b);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = fmaf((s[u][j] - mean) * rstd, w[j], b[j]);
+        store_eight<k32, false>(y, i, left, w);
+    }
+}
+
+// kWeights: dw and db too, the workgroup's sums of them as part[0][blockIdx.x][K] and part[1][..].  lds: K floats where a workgroup has several teams.
+template <bool k32, int kTeam, int kUnits, bool kWeights>
+__global__ __launch_bounds__(kWeights ? 1024 : kTeam < 4 ? 256 : 64 * kTeam) void layer_norm_backward_kernel(LayerNormGradArgs a) {
+    constexpr int kWaves = kWeights ? 16 : kTeam < 4 ? 4 : kTeam, kTeams = kWaves / kTeam;
+    __shared__ float slots[2][kWaves * 2];
+    extern __shared__ float totals[];
+    const int team = threadIdx.x / (64 * kTeam), at = threadIdx.x % (64 * kTeam), K = a.K;
+    float dw[kWeights ? kUnits : 1][8] = {}, db[kWeights ? kUnits : 1][8] = {};
+    int parity = 0;
+    for (int64_t row0 = (int64_t)blockIdx.x * kTeams; row0 < a.T; row0 += (int64_t)gridDim.x * kTeams, parity ^= 1) {   // the same for the workgroup
+        const int64_t row = row0 + team;
+        const bool live = row < a.T;
+        const int64_t start = (live ? row : 0) * K * (k32 ? 4 : 2);
+        const char *x = static_cast<const char*>(a.x) + start, *dy = static_cast<const char*>(a.dy) + start;
+        const float mean = live ? a.mean[row] : 0.f, rstd = live ? a.rstd[row] : 0.f;
+        Eight<k32> xq[kUnits], dyq[kUnits], dsq[kUnits];
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const int i = 8 * (at + 64 * kTeam * u), left = live ? K - i : 0;
+            xq[u] = load_eight<k32, false, false>(x, i, left);
+            dyq[u] = load_eight<k32, false, false>(dy, i, left);
+            if (a.dx != nullptr && a.dsum != nullptr) dsq[u] = load_eight<k32, false, false>(static_cast<const char*>(a.dsum) + start, i, left);
+        }
+        float sums[2] = {0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const int i = 8 * (at + 64 * kTeam * u), left = live ? K - i : 0;
+            float w[8] = {};
+            if (left > 0 && a.dx != nullptr) load_weights(a.weight, a.w32, i, left, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float d = dyq[u].get(j), xhat = j < left ? (xq[u].get(j) - mean) * rstd : 0.f, g = d * w[j];
+                sums[0] += g;
+                sums[1] = fmaf(g, xhat, sums[1]);
+                if constexpr (kWeights) {
+                    dw[u][j] = fmaf(d, xhat, dw[u][j]);
+                    db[u][j] += d;
+                }
+            }
+        }
+        if (a.dx == nullptr) continue;   // the same for the launch
+        team_sum<kTeam>(sums, slots[parity]);
+        const float g_mean = sums[0] / (float)K, along = sums[1] / (float)K;
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const int i = 8 * (at + 64 * kTeam * u), left = live ? K - i : 0;
+            if (left <= 0) break;
+            float w[8];
+            load_weights(a.weight, a.w32, i, left, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float xhat = (xq[u].get(j) - mean) * rstd;
+                w[j] = rstd * (fmaf(-xhat, along, dyq[u].get(j) * w[j] - g_mean));
+                if (a.dsum != nullptr) w[j] += dsq[u].get(j);
+            }
+            store_eight<k32, false>(static_cast<char*>(a.dx) + start, i, left, w);
+        }
+    }
+    if constexpr (kWeights) {
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            float* part = a.part + ((int64_t)which * gridDim.x + blockIdx.x) * K;
+            for (int t = 0; t < kTeams; ++t) {   // the teams one after the other
+                if (t == team) {
+#pragma unroll
+                    for (int u = 0; u < kUnits; ++u) {
+                        const int i = 8 * (at + 64 * kTeam * u);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            if (i + j >= K) break;
+                            float s = which == 0 ? dw[u][j] : db[u][j];
+                            if (t > 0) s += totals[i + j];
+                            if (t < kTeams - 1) totals[i + j] = s;
+                            else part[i + j] = s;
+                        }
+                    }
+                }
+                if constexpr (kTeams > 1) __syncthreads();
+            }
+        }
+    }
+}
+
+// dw (y 0) and db (y 1) from the workgroups' sums, 64 columns a workgroup, every sixteenth part a wave.  parts 0: zeros.
+__global__ __launch_bounds__(1024) void layer_norm_parts_kernel(const float* part, int parts, int K, bool w32, void* dw, void* db) {
+    __shared__ float sums[16][64];
+    const int lane = lane_id(), wave = threadIdx.x >> 6;
+    void* out = blockIdx.y == 0 ? dw : db;
+    if (out == nullptr) return;   // the same for the workgroup
+    const int c = blockIdx.x * 64 + lane;
+    const float* from = part + (int64_t)blockIdx.y * parts * K;
+    float s = 0.f;
+    if (c < K)
+#pragma unroll 8
+        for (int p = wave; p < parts; p += 16) s += from[(int64_t)p * K + c];
+    sums[wave][lane] = s;
+    __syncthreads();
+    if (wave != 0 || c >= K) return;
+#pragma unroll
+    for (int w = 1; w < 16; ++w) s += sums[w][lane];
+    if (w32) static_cast<float*>(out)[c] = s;
+    else static_cast<uint16_t*>(out)[c] = f32_to_bf16_rne(s);
+}
+
+// The team for rows of K: as few waves as hold a row with two vectors a lane.
+template <typename Run>
+void with_team(int64_t K, Run run) {
+    using std::integral_constant;
+    if (K <= 512) run(integral_constant<int, 1>(), integral_constant<int, 1>());
+    else if (K <= 1024) run(integral_constant<int, 1>(), integral_constant<int, 2>());
+    else if (K <= 2048) run(integral_constant<int, 2>(), integral_constant<int, 2>());
+    else if (K <= 4096) run(integral_constant<int, 4>(), integral_constant<int, 2>());
+    else if (K <= 8192) run(integral_constant<int, 8>(), integral_constant<int, 2>());
+    else if (K <= 16384) run(integral_constant<int, 16>(), integral_constant<int, 2>());
+    else run(integral_constant<int, 16>(), integral_constant<int, 4>());
+}
+
+int layer_norm_team(int64_t K) {
+    int team = 0;
+    with_team(K, [&](auto waves, auto) { team = waves; });
+    return team;
+}
+
+int64_t layer_norm_parts(int64_t T, int64_t K) {
+    const int64_t teams = 16 / layer_norm_team(K), groups = (T + teams - 1) / teams;
+    return groups < kLayerNormParts ? groups : kLayerNormParts;
+}
+
+hipError_t launch_layer_norm(const LayerNormArgs& a, hipStream_t stream) {
+    with_team(a.K, [&](auto waves, auto units) {
+        constexpr int kTeam = waves, kUnits = units, kTeams = kTeam < 4 ? 4 / kTeam : 1;
+        const dim3 grid((unsigned)((a.T + kTeams - 1) / kTeams)), block(64 * kTeam * kTeams);
+        if (a.f32) hipLaunchKernelGGL((layer_norm_kernel<true, kTeam, kUnits>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((layer_norm_kernel<false, kTeam, kUnits>), grid, block, 0, stream, a);
+    });
+    return hipGetLastError();
+}
+
+hipError_t launch_layer_norm_backward(const LayerNormGradArgs& a, void* dw, void* db, hipStream_t stream) {
+    const bool weights = dw != nullptr || db != nullptr;
+    const int64_t parts = layer_norm_parts(a.T, a.K);
+    if (a.T > 0 && (weights || a.dx != nullptr))
+        with_team(a.K, [&](auto waves, auto units) {
+            constexpr int kTeam = waves, kUnits = units;
+            const auto run = [&](auto kernel, int64_t groups, int threads, size_t lds) {
+                hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3((unsigned)threads), lds, stream, a);
+            };
+            if (weights) {
+                const size_t lds = kTeam < 16 ? (size_t)a.K * 4 : 0;
+                if (a.f32) run(layer_norm_backward_kernel<true, kTeam, kUnits, true>, parts, 1024, lds);
+                else run(layer_norm_backward_kernel<false, kTeam, kUnits, true>, parts, 1024, lds);
+            } else {
+                constexpr int kTeams = kTeam < 4 ? 4 / kTeam : 1;
+                if (a.f32) run(layer_norm_backward_kernel<true, kTeam, kUnits, false>, (a.T + kTeams - 1) / kTeams, 64 * kTeam * kTeams, 0);
+                else run(layer_norm_backward_kernel<false, kTeam, kUnits, false>, (a.T + kTeams - 1) / kTeams, 64 * kTeam * kTeams, 0);
+            }
+        });
+    if (weights)
+        hipLaunchKernelGGL(layer_norm_parts_kernel, dim3((unsigned)((a.K + 63) / 64), 2), dim3(1024), 0, stream, a.part, (int)parts, a.K, a.w32, dw, db);
+    return hipGetLastError();
+}
+
+}  // namespace salr
