@@ -616,7 +616,7 @@ salr_status_t salr_adapter_list_check(const salr_adapter_t* adapters, int64_t n,
  * An id that is not below n gives NaN in its token's row.
  *
  *   list, n, max_rank  the records, on the device (8-byte aligned), their number (at least 1) and largest rank
- *   x          in   [T, K] bf16;  T < 2^28, K and N <= 2^22 (else SHAPE)
+ *   x          in   [T, K] bf16;  T < 2^28, K and N from 8 to 2^22 (else SHAPE)
  *   ids        in   [T] int32
  *   base       in   [T, N] bf16, the shared layer's output; NULL = zeros
  *   y          out  [T, N] bf16; may be base, overlaps x and base in no other way
@@ -633,7 +633,9 @@ salr_status_t salr_adapter_list_check(const salr_adapter_t* adapters, int64_t n,
  *   want_gradients  not 0: da and db of every record that has them are written; those of an adapter without a token as zeros
  *   workspace  --   salr_adapters_backward_workspace_bytes(T, K, N, n, max_rank, want_gradients) bytes, 256-byte aligned
  *
- * bf16 in and out, fp32 sums; x A and dy B^T are rounded to bf16 once, as the layer's are.  Results are the same bit for bit from call to call.
+ * bf16 in and out, fp32 sums; x A and dy B^T go into the second product as two bf16 values each (16 bits of mantissa).  Results are the same bit for bit
+ * from call to call.  A token's infinity or NaN, or an adapter's, makes infinities or NaN of its own results only (and NaN of some that would be
+ * infinite: an infinite factor meets the second value, which may be zero).
  * Errors of both: INVALID_ARG (null where data is required, negative size, n < 1, max_rank outside [0, 256], a misaligned pointer (x, base, y, dy, dx_base,
  * dx: to 2 bytes; ids: to 4), an output that overlaps an input otherwise than told), SHAPE, CAPACITY, HIP.  The queries return 0 for sizes that are refused.
  */

@@ -778,7 +778,7 @@ class AdamW:
 
 def _within(stream, device):
     """A stream argument for calls that allocate: that stream is the current one meanwhile."""
-    return torch.cuda.stream(None if stream is None else _on(stream, device))
+    return torch.cuda.stream(_on(stream, device))
 
 
 def salr_dropout(x: torch.Tensor, residual: Optional[torch.Tensor], p: float, seed, offset: int, y: torch.Tensor, stream=None) -> None:
@@ -794,6 +794,8 @@ def dropout(x: torch.Tensor, p: float, seed, offset: int = 0, residual: Optional
     Which elements stay follows from their positions, ``seed`` and ``offset`` (Philox4x32-10; p is taken in steps of 2^-16): no mask is stored, and
     the gradient of x is ``dropout(dy, p, seed, offset)`` (with another gradient of x as ``residual`` where there is one).  ``seed``: a number, or an int64
     tensor of one on the GPU that is read when the kernel runs: a captured graph has other masks at every replay where that changes in between."""
+    if stream is None:
+        return _native().dropout(x, residual, p, seed, offset, None, None)
     with _within(stream, x.device):
         return _native().dropout(x, residual, p, seed, offset, None, None)
 
@@ -808,6 +810,8 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tenso
                stream=None):
     """(y, sum, mean, rstd): the layer norm of every row of x [T, K], or of sum = x + residual (None without a residual), which the next residual and
     ``layer_norm_backward`` take.  x and residual fp32 or bf16, weight and bias [K] fp32 or bf16; K up to 32768."""
+    if stream is None:
+        return _native().layer_norm(x, residual, weight, bias, eps, None, None, None, None, None, True)
     with _within(stream, x.device):
         return _native().layer_norm(x, residual, weight, bias, eps, None, None, None, None, None, True)
 
@@ -823,8 +827,7 @@ def salr_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Te
     for name, t in (("dx", dx), ("dw", dw), ("db", db)):
         if t is not None and not isinstance(t, torch.Tensor):
             raise TypeError(f"{name} must be a tensor")
-    with _within(stream, x.device):
-        _native().layer_norm_backward(dy, x, weight, mean, rstd, dsum, dx, dw, db, workspace, None)
+    _native().layer_norm_backward(dy, x, weight, mean, rstd, dsum, dx, dw, db, workspace, None if stream is None else _on(stream, x.device).cuda_stream)
 
 
 def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
@@ -832,9 +835,11 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor,
                         workspace: Optional[torch.Tensor] = None, stream=None):
     """(dx, dw, db); entries not asked for are None.  x is what was normalised (``sum`` where there was a residual), mean and rstd as ``layer_norm`` gave
     them; ``dsum``: a gradient that reaches x past the norm, added to dx."""
+    args = (dy, x, weight, mean, rstd, dsum, True if need_dx else None, True if need_dw else None, True if need_db else None, workspace, None)
+    if stream is None:
+        return _native().layer_norm_backward(*args)
     with _within(stream, x.device):
-        return _native().layer_norm_backward(dy, x, weight, mean, rstd, dsum, True if need_dx else None, True if need_dw else None,
-                                             True if need_db else None, workspace, None)
+        return _native().layer_norm_backward(*args)
 
 
 def salr_adapters_add_workspace_bytes(T: int, K: int, N: int, n: int, max_rank: int) -> int:
@@ -900,6 +905,10 @@ class AdapterSet:
         if need_gradients and self.da is None and self.db is None:
             raise ValueError("a set made without da and db has no place for gradients")
         out = (True if dx is None else dx) if need_dx else None
-        with _within(stream, self._list.device):
-            got = self._backward(*self._first, x, ids, dy, dx_base, out, need_gradients, workspace, None)
+        args = (*self._first, x, ids, dy, dx_base, out, need_gradients, workspace, None)
+        if stream is None:
+            got = self._backward(*args)
+        else:
+            with _within(stream, self._list.device):
+                got = self._backward(*args)
         return got, self.da if need_gradients else None, self.db if need_gradients else None

@@ -68,7 +68,8 @@ bool layer_norm_sizes(int64_t T, int64_t K) { return T <= salr::kLayerNormMostT 
 // Sizes of the calls on adapters of many requests.
 salr_status_t adapters_sizes(int64_t T, int64_t K, int64_t N, int64_t n, int64_t max_rank) {
     if (T < 0 || K < 0 || N < 0 || n < 1 || max_rank < 0 || max_rank > kMaxRank) return SALR_ERR_INVALID_ARG;
-    if (T > salr::kAdaptersMostT || K > salr::kAdaptersMostColumns || N > salr::kAdaptersMostColumns || n > salr::kAdaptersMostCount) return SALR_ERR_SHAPE;
+    const auto fits = [](int64_t columns) { return columns >= salr::kAdaptersLeastColumns && columns <= salr::kAdaptersMostColumns; };
+    if (T > salr::kAdaptersMostT || !fits(K) || !fits(N) || n > salr::kAdaptersMostCount) return SALR_ERR_SHAPE;
     return SALR_OK;
 }
 
@@ -656,7 +657,7 @@ salr_status_t salr_adapter_list_check(const salr_adapter_t* adapters, int64_t n,
 }
 
 size_t salr_adapters_add_workspace_bytes(int64_t T, int64_t K, int64_t N, int64_t n, int64_t max_rank) {
-    if (adapters_sizes(T, K, N, n, max_rank) != SALR_OK || T == 0 || N == 0) return 0;
+    if (adapters_sizes(T, K, N, n, max_rank) != SALR_OK || T == 0) return 0;
     return salr::request_adapters_plan(T, K, N, n, max_rank, false, false).bytes;
 }
 
@@ -664,8 +665,8 @@ salr_status_t salr_adapters_add(const salr_adapter_t* list, int64_t n, int64_t m
                                 const int32_t* ids, const uint16_t* base, uint16_t* y, void* workspace, size_t workspace_bytes, void* stream) {
     const salr_status_t st = adapters_sizes(T, K, N, n, max_rank);
     if (st != SALR_OK) return st;
-    if (T == 0 || N == 0) return SALR_OK;
-    if (!list || (K > 0 && !x) || !ids || !y) return SALR_ERR_INVALID_ARG;
+    if (T == 0) return SALR_OK;
+    if (!list || !x || !ids || !y) return SALR_ERR_INVALID_ARG;
     if (misaligned(list, 8) || misaligned(x, 2) || misaligned(ids, 4) || misaligned(base, 2) || misaligned(y, 2) || misaligned(workspace, 256)) return SALR_ERR_INVALID_ARG;
     const size_t bytes = (size_t)(T * N) * 2;
     if (overlaps_in_part(y, base, bytes) || overlaps(y, bytes, x, (size_t)(T * K) * 2) || overlaps(y, bytes, ids, (size_t)T * 4)) return SALR_ERR_INVALID_ARG;
@@ -687,8 +688,8 @@ salr_status_t salr_adapters_backward(const salr_adapter_t* list, int64_t n, int6
                                      void* workspace, size_t workspace_bytes, void* stream) {
     const salr_status_t st = adapters_sizes(T, K, N, n, max_rank);
     if (st != SALR_OK) return st;
-    if (!want_gradients && (!dx || T == 0 || K == 0)) return SALR_OK;
-    if (!list || (T > 0 && (!ids || (N > 0 && !dy) || (want_gradients && K > 0 && !x)))) return SALR_ERR_INVALID_ARG;
+    if (!want_gradients && (!dx || T == 0)) return SALR_OK;
+    if (!list || (T > 0 && (!ids || !dy || (want_gradients && !x)))) return SALR_ERR_INVALID_ARG;
     if (misaligned(list, 8) || misaligned(x, 2) || misaligned(dy, 2) || misaligned(ids, 4) || misaligned(dx_base, 2) || misaligned(dx, 2) ||
         misaligned(workspace, 256))
         return SALR_ERR_INVALID_ARG;
@@ -699,7 +700,7 @@ salr_status_t salr_adapters_backward(const salr_adapter_t* list, int64_t n, int6
     const salr::RequestAdaptersPlan plan = salr::request_adapters_plan(T, K, N, n, max_rank, true, want_gradients != 0);
     if (workspace_bytes < plan.bytes) return SALR_ERR_CAPACITY;
     if (!workspace) return SALR_ERR_INVALID_ARG;
-    const salr::RequestAdaptersArgs args{list, n, x, dy, T, K, N, ids, dx_base, K > 0 ? dx : nullptr, want_gradients != 0, workspace, static_cast<hipStream_t>(stream)};
+    const salr::RequestAdaptersArgs args{list, n, x, dy, T, K, N, ids, dx_base, dx, want_gradients != 0, workspace, static_cast<hipStream_t>(stream)};
     const hipError_t e = salr::launch_request_adapters_backward(args, plan);
     return e == hipSuccess ? SALR_OK : SALR_ERR_HIP;
 }

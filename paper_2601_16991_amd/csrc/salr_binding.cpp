@@ -859,7 +859,6 @@ PyObject* py_adapter_list(PyObject*, PyObject* const* v, Py_ssize_t n) {
     need_matrix(b0, "b");
     const at::Device device = a0.device();
     const int64_t K = a0.size(0), N = b0.size(1);
-    if (K == 0 || N == 0) fail(PyExc_ValueError, "a layer without %s", "features");
     auto tensors = std::make_unique<StepTensors>();
     std::vector<StepRange> ranges;
     const auto pointer = [&](const at::Tensor& t, int64_t rows, int64_t cols, const char* name, bool written) -> uint16_t* {
@@ -887,6 +886,7 @@ PyObject* py_adapter_list(PyObject*, PyObject* const* v, Py_ssize_t n) {
         t.da = das.fast && das.at(i, "da").defined() ? pointer(das.at(i, "da"), K, t.rank, "da", true) : nullptr;
         t.db = dbs.fast && dbs.at(i, "db").defined() ? pointer(dbs.at(i, "db"), t.rank, N, "db", true) : nullptr;
     }
+    if (K < salr::kAdaptersLeastColumns || N < salr::kAdaptersLeastColumns) check(SALR_ERR_SHAPE, "AdapterSet");
     if (const char* name = written_twice(ranges)) fail(PyExc_ValueError, "%s: shares memory with another tensor of the list", name);
     int64_t max_rank = 0;
     check(salr_adapter_list_check(table.data(), count, &max_rank), "salr_adapter_list_check");

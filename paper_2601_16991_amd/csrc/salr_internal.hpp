@@ -915,6 +915,7 @@ hipError_t launch_layer_norm_backward(const LayerNormGradArgs& a, void* dw, void
 
 // ---- Adapters of many requests (salr_request_adapters.hip)
 constexpr int64_t kAdaptersMostT = ((int64_t)1 << 28) - 1, kAdaptersMostColumns = (int64_t)1 << 22, kAdaptersMostCount = 65533;
+constexpr int64_t kAdaptersLeastColumns = 8;   // one vector
 struct RequestAdaptersPlan {
     bool direct;             // few tokens: a workgroup finds its own among the ids; else a launch in front orders them
     int64_t rows, tiles;     // tokens of a tile, tiles of the launches

@@ -8,7 +8,7 @@
 // team's waves through LDS.  The variance is summed from differences to the mean in a second pass over the registers: squares alone lose
 // what a large mean hides.  Sums are fp32.
 //
-// dw and db: a workgroup of sixteen waves goes through rows, its lanes keep the sums of their columns; the teams of a workgroup are added in LDS,
+// dw and db: a workgroup of eight waves or more goes through rows, its lanes keep the sums of their columns; the teams of a workgroup are added in LDS,
 // in order, and the workgroups' sums, at most kLayerNormParts of them, by a second launch: no atomics, the same bits every time.
 #include <type_traits>
 
@@ -51,20 +51,32 @@ __device__ __forceinline__ void team_sum(float (&v)[kSums], float* slots) {
     }
 }
 
-// Eight weights from element i on, in fp32.
+// Eight elements of a row from i on, of which `left` are there; kWhole: all or none of them.
+template <bool k32, bool kWhole>
+__device__ __forceinline__ Eight<k32> row_eight(const void* row, int i, int left) {
+    if constexpr (kWhole) {
+        Eight<k32> zero{};
+        return left > 0 ? load_eight<k32, false, false>(row, i, 8) : zero;
+    } else {
+        return load_eight<k32, false, false>(row, i, left);
+    }
+}
+
+// The same of weights, in fp32.
+template <bool kWhole>
 __device__ __forceinline__ void load_weights(const void* w, bool w32, int i, int left, float (&out)[8]) {
     if (w32) {
-        const Eight<true> q = load_eight<true, false, false>(w, i, left);
+        const Eight<true> q = row_eight<true, kWhole>(w, i, left);
 #pragma unroll
         for (int j = 0; j < 8; ++j) out[j] = q.get(j);
     } else {
-        const Eight<false> q = load_eight<false, false, false>(w, i, left);
+        const Eight<false> q = row_eight<false, kWhole>(w, i, left);
 #pragma unroll
         for (int j = 0; j < 8; ++j) out[j] = q.get(j);
     }
 }
 
-template <bool k32, int kTeam, int kUnits>
+template <bool k32, int kTeam, int kUnits, bool kWhole>
 __global__ __launch_bounds__(kTeam < 4 ? 256 : 64 * kTeam) void layer_norm_kernel(LayerNormArgs a) {
     constexpr int kWaves = kTeam < 4 ? 4 : kTeam, kTeams = kWaves / kTeam;
     __shared__ float slots[2][kWaves];
@@ -79,7 +91,7 @@ __global__ __launch_bounds__(kTeam < 4 ? 256 : 64 * kTeam) void layer_norm_kerne
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
         const int i = 8 * (at + 64 * kTeam * u), left = live ? K - i : 0;
-        const Eight<k32> q = load_eight<k32, false, false>(x, i, left);
+        const Eight<k32> q = row_eight<k32, kWhole>(x, i, left);
 #pragma unroll
         for (int j = 0; j < 8; ++j) s[u][j] = q.get(j);
     }
@@ -87,14 +99,14 @@ __global__ __launch_bounds__(kTeam < 4 ? 256 : 64 * kTeam) void layer_norm_kerne
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
             const int i = 8 * (at + 64 * kTeam * u), left = live ? K - i : 0;
-            const Eight<k32> q = load_eight<k32, false, false>(residual, i, left);
+            const Eight<k32> q = row_eight<k32, kWhole>(residual, i, left);
             // the sum is rounded as it is stored, and the norm is of that: so is the gradient, which reads it back
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 s[u][j] += q.get(j);
                 if constexpr (!k32) s[u][j] = (float)(__bf16)s[u][j];
             }
-            if (left > 0) store_eight<k32, false>(static_cast<char*>(a.sum) + start, i, left, s[u]);
+            if (left > 0) store_eight<k32, false>(static_cast<char*>(a.sum) + start, i, kWhole ? 8 : left, s[u]);
         }
     }
 #pragma unroll
@@ -109,7 +121,7 @@ __global__ __launch_bounds__(kTeam < 4 ? 256 : 64 * kTeam) void layer_norm_kerne
         const int left = K - 8 * (at + 64 * kTeam * u);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float d = j < left ? s[u][j] - mean : 0.f;
+            const float d = (kWhole ? 0 : j) < left ? s[u][j] - mean : 0.f;
             sums[0] = fmaf(d, d, sums[0]);
         }
     }
@@ -125,46 +137,72 @@ __global__ __launch_bounds__(kTeam < 4 ? 256 : 64 * kTeam) void layer_norm_kerne
         const int i = 8 * (at + 64 * kTeam * u), left = K - i;
         if (left <= 0) break;
         float w[8], b[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        load_weights(a.weight, a.w32, i, left, w);
-        if (a.bias != nullptr) load_weights(a.bias, a.w32, i, left, b);
+        load_weights<kWhole>(a.weight, a.w32, i, left, w);
+        if (a.bias != nullptr) load_weights<kWhole>(a.bias, a.w32, i, left, b);
 #pragma unroll
         for (int j = 0; j < 8; ++j) w[j] = fmaf((s[u][j] - mean) * rstd, w[j], b[j]);
-        store_eight<k32, false>(y, i, left, w);
+        store_eight<k32, false>(y, i, kWhole ? 8 : left, w);
     }
 }
 
-// kWeights: dw and db too, the workgroup's sums of them as part[0][blockIdx.x][K] and part[1][..].  lds: K floats where a workgroup has several teams.
-template <bool k32, int kTeam, int kUnits, bool kWeights>
-__global__ __launch_bounds__(kWeights ? 1024 : kTeam < 4 ? 256 : 64 * kTeam) void layer_norm_backward_kernel(LayerNormGradArgs a) {
-    constexpr int kWaves = kWeights ? 16 : kTeam < 4 ? 4 : kTeam, kTeams = kWaves / kTeam;
+// kWeights: dw and db too, the workgroup's sums of them as part[0][blockIdx.x][K] and part[1][..]; a row's requests are then out while the one before is
+// worked on (kAhead), since a workgroup has its CU to itself.  lds: K floats where a workgroup has several teams.
+template <int kTeam, bool kWeights>
+constexpr int grad_waves() { return kWeights ? 8 : kTeam < 4 ? 4 : kTeam; }
+
+template <bool k32, int kTeam, int kUnits, bool kWhole, bool kWeights>
+__global__ __launch_bounds__((64 * grad_waves<kTeam, kWeights>())) void layer_norm_backward_kernel(LayerNormGradArgs a) {
+    constexpr int kWaves = grad_waves<kTeam, kWeights>(), kTeams = kWaves / kTeam;
+    constexpr bool kAhead = kWeights && kUnits <= 2;
     __shared__ float slots[2][kWaves * 2];
     extern __shared__ float totals[];
     const int team = threadIdx.x / (64 * kTeam), at = threadIdx.x % (64 * kTeam), K = a.K;
-    float dw[kWeights ? kUnits : 1][8] = {}, db[kWeights ? kUnits : 1][8] = {};
-    int parity = 0;
-    for (int64_t row0 = (int64_t)blockIdx.x * kTeams; row0 < a.T; row0 += (int64_t)gridDim.x * kTeams, parity ^= 1) {   // the same for the workgroup
-        const int64_t row = row0 + team;
+    const bool want_dx = a.dx != nullptr, add = want_dx && a.dsum != nullptr;
+    float dw[kWeights ? kUnits : 1][8] = {}, db[kWeights ? kUnits : 1][8] = {}, w[kUnits][8] = {};
+    if (want_dx)
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const int i = 8 * (at + 64 * kTeam * u);
+            load_weights<kWhole>(a.weight, a.w32, i, K - i, w[u]);
+        }
+    struct Row {
+        Eight<k32> x[kUnits], dy[kUnits], ds[kUnits];
+        float mean, rstd;
+    };
+    const auto request = [&](Row& r, int64_t row) {
         const bool live = row < a.T;
         const int64_t start = (live ? row : 0) * K * (k32 ? 4 : 2);
-        const char *x = static_cast<const char*>(a.x) + start, *dy = static_cast<const char*>(a.dy) + start;
-        const float mean = live ? a.mean[row] : 0.f, rstd = live ? a.rstd[row] : 0.f;
-        Eight<k32> xq[kUnits], dyq[kUnits], dsq[kUnits];
+        r.mean = live ? a.mean[row] : 0.f;
+        r.rstd = live ? a.rstd[row] : 0.f;
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
             const int i = 8 * (at + 64 * kTeam * u), left = live ? K - i : 0;
-            xq[u] = load_eight<k32, false, false>(x, i, left);
-            dyq[u] = load_eight<k32, false, false>(dy, i, left);
-            if (a.dx != nullptr && a.dsum != nullptr) dsq[u] = load_eight<k32, false, false>(static_cast<const char*>(a.dsum) + start, i, left);
+            r.x[u] = row_eight<k32, kWhole>(static_cast<const char*>(a.x) + start, i, left);
+            r.dy[u] = row_eight<k32, kWhole>(static_cast<const char*>(a.dy) + start, i, left);
+            if (add) r.ds[u] = row_eight<k32, kWhole>(static_cast<const char*>(a.dsum) + start, i, left);
+        }
+    };
+    const int64_t stride = (int64_t)gridDim.x * kTeams;
+    Row next;
+    if constexpr (kAhead) request(next, (int64_t)blockIdx.x * kTeams + team);
+    int parity = 0;
+    for (int64_t row0 = (int64_t)blockIdx.x * kTeams; row0 < a.T; row0 += stride, parity ^= 1) {   // the same for the workgroup
+        const int64_t row = row0 + team;
+        const bool live = row < a.T;
+        Row r;
+        if constexpr (kAhead) {
+            r = next;
+            if (row0 + stride < a.T) request(next, row + stride);
+        } else {
+            request(r, row);
         }
         float sums[2] = {0.f, 0.f};
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
-            const int i = 8 * (at + 64 * kTeam * u), left = live ? K - i : 0;
-            float w[8] = {};
-            if (left > 0 && a.dx != nullptr) load_weights(a.weight, a.w32, i, left, w);
+            const int left = live ? K - 8 * (at + 64 * kTeam * u) : 0;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float d = dyq[u].get(j), xhat = j < left ? (xq[u].get(j) - mean) * rstd : 0.f, g = d * w[j];
+                const float d = r.dy[u].get(j), xhat = (kWhole ? 0 : j) < left ? (r.x[u].get(j) - r.mean) * r.rstd : 0.f, g = d * w[u][j];
                 sums[0] += g;
                 sums[1] = fmaf(g, xhat, sums[1]);
                 if constexpr (kWeights) {
@@ -173,22 +211,22 @@ __global__ __launch_bounds__(kWeights ? 1024 : kTeam < 4 ? 256 : 64 * kTeam) voi
                 }
             }
         }
-        if (a.dx == nullptr) continue;   // the same for the launch
+        if (!want_dx) continue;   // the same for the launch
         team_sum<kTeam>(sums, slots[parity]);
         const float g_mean = sums[0] / (float)K, along = sums[1] / (float)K;
+        char* dx = static_cast<char*>(a.dx) + (live ? row : 0) * K * (k32 ? 4 : 2);
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
             const int i = 8 * (at + 64 * kTeam * u), left = live ? K - i : 0;
             if (left <= 0) break;
-            float w[8];
-            load_weights(a.weight, a.w32, i, left, w);
+            float v[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float xhat = (xq[u].get(j) - mean) * rstd;
-                w[j] = rstd * (fmaf(-xhat, along, dyq[u].get(j) * w[j] - g_mean));
-                if (a.dsum != nullptr) w[j] += dsq[u].get(j);
+                const float xhat = (r.x[u].get(j) - r.mean) * r.rstd;
+                v[j] = r.rstd * (fmaf(-xhat, along, r.dy[u].get(j) * w[u][j] - g_mean));
+                if (add) v[j] += r.ds[u].get(j);
             }
-            store_eight<k32, false>(static_cast<char*>(a.dx) + start, i, left, w);
+            store_eight<k32, false>(dx, i, kWhole ? 8 : left, v);
         }
     }
     if constexpr (kWeights) {
@@ -202,7 +240,7 @@ __global__ __launch_bounds__(kWeights ? 1024 : kTeam < 4 ? 256 : 64 * kTeam) voi
                         const int i = 8 * (at + 64 * kTeam * u);
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
-                            if (i + j >= K) break;
+                            if (i + (kWhole ? 0 : j) >= K) break;
                             float s = which == 0 ? dw[u][j] : db[u][j];
                             if (t > 0) s += totals[i + j];
                             if (t < kTeams - 1) totals[i + j] = s;
@@ -250,23 +288,37 @@ void with_team(int64_t K, Run run) {
     else run(integral_constant<int, 16>(), integral_constant<int, 4>());
 }
 
-int layer_norm_team(int64_t K) {
-    int team = 0;
-    with_team(K, [&](auto waves, auto) { team = waves; });
-    return team;
+// The team that sums dw and db too: eight waves at most, whose lanes have 256 registers each for their columns' sums.
+template <typename Run>
+void with_grad_team(int64_t K, Run run) {
+    using std::integral_constant;
+    if (K <= 8192) with_team(K, run);
+    else if (K <= 16384) run(integral_constant<int, 8>(), integral_constant<int, 4>());
+    else run(integral_constant<int, 8>(), integral_constant<int, 8>());
 }
 
 int64_t layer_norm_parts(int64_t T, int64_t K) {
-    const int64_t teams = 16 / layer_norm_team(K), groups = (T + teams - 1) / teams;
+    int team = 0;
+    with_grad_team(K, [&](auto waves, auto) { team = waves; });
+    const int64_t teams = 8 / team, groups = (T + teams - 1) / teams;
     return groups < kLayerNormParts ? groups : kLayerNormParts;
+}
+
+template <typename Run>
+void with_whole(int64_t K, Run run) {   // rows of whole vectors
+    if (K % 8 == 0) run(std::true_type());
+    else run(std::false_type());
 }
 
 hipError_t launch_layer_norm(const LayerNormArgs& a, hipStream_t stream) {
     with_team(a.K, [&](auto waves, auto units) {
-        constexpr int kTeam = waves, kUnits = units, kTeams = kTeam < 4 ? 4 / kTeam : 1;
-        const dim3 grid((unsigned)((a.T + kTeams - 1) / kTeams)), block(64 * kTeam * kTeams);
-        if (a.f32) hipLaunchKernelGGL((layer_norm_kernel<true, kTeam, kUnits>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((layer_norm_kernel<false, kTeam, kUnits>), grid, block, 0, stream, a);
+        with_whole(a.K, [&](auto whole) {
+            constexpr int kTeam = waves, kUnits = units, kTeams = kTeam < 4 ? 4 / kTeam : 1;
+            constexpr bool kWhole = decltype(whole)::value;
+            const dim3 grid((unsigned)((a.T + kTeams - 1) / kTeams)), block(64 * kTeam * kTeams);
+            if (a.f32) hipLaunchKernelGGL((layer_norm_kernel<true, kTeam, kUnits, kWhole>), grid, block, 0, stream, a);
+            else hipLaunchKernelGGL((layer_norm_kernel<false, kTeam, kUnits, kWhole>), grid, block, 0, stream, a);
+        });
     });
     return hipGetLastError();
 }
@@ -274,21 +326,27 @@ hipError_t launch_layer_norm(const LayerNormArgs& a, hipStream_t stream) {
 hipError_t launch_layer_norm_backward(const LayerNormGradArgs& a, void* dw, void* db, hipStream_t stream) {
     const bool weights = dw != nullptr || db != nullptr;
     const int64_t parts = layer_norm_parts(a.T, a.K);
-    if (a.T > 0 && (weights || a.dx != nullptr))
+    const auto run = [&](auto kernel, int64_t groups, int threads, size_t lds) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3((unsigned)threads), lds, stream, a);
+    };
+    if (a.T > 0 && weights)
+        with_grad_team(a.K, [&](auto waves, auto units) {
+            with_whole(a.K, [&](auto whole) {
+                constexpr int kTeam = waves, kUnits = units;
+                constexpr bool kWhole = decltype(whole)::value;
+                const size_t lds = kTeam < 8 ? (size_t)a.K * 4 : 0;
+                if (a.f32) run(layer_norm_backward_kernel<true, kTeam, kUnits, kWhole, true>, parts, 512, lds);
+                else run(layer_norm_backward_kernel<false, kTeam, kUnits, kWhole, true>, parts, 512, lds);
+            });
+        });
+    else if (a.T > 0 && a.dx != nullptr)
         with_team(a.K, [&](auto waves, auto units) {
-            constexpr int kTeam = waves, kUnits = units;
-            const auto run = [&](auto kernel, int64_t groups, int threads, size_t lds) {
-                hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3((unsigned)threads), lds, stream, a);
-            };
-            if (weights) {
-                const size_t lds = kTeam < 16 ? (size_t)a.K * 4 : 0;
-                if (a.f32) run(layer_norm_backward_kernel<true, kTeam, kUnits, true>, parts, 1024, lds);
-                else run(layer_norm_backward_kernel<false, kTeam, kUnits, true>, parts, 1024, lds);
-            } else {
-                constexpr int kTeams = kTeam < 4 ? 4 / kTeam : 1;
-                if (a.f32) run(layer_norm_backward_kernel<true, kTeam, kUnits, false>, (a.T + kTeams - 1) / kTeams, 64 * kTeam * kTeams, 0);
-                else run(layer_norm_backward_kernel<false, kTeam, kUnits, false>, (a.T + kTeams - 1) / kTeams, 64 * kTeam * kTeams, 0);
-            }
+            with_whole(a.K, [&](auto whole) {
+                constexpr int kTeam = waves, kUnits = units, kThreads = 64 * grad_waves<kTeam, false>(), kTeams = kThreads / 64 / kTeam;
+                constexpr bool kWhole = decltype(whole)::value;
+                if (a.f32) run(layer_norm_backward_kernel<true, kTeam, kUnits, kWhole, false>, (a.T + kTeams - 1) / kTeams, kThreads, 0);
+                else run(layer_norm_backward_kernel<false, kTeam, kUnits, kWhole, false>, (a.T + kTeams - 1) / kTeams, kThreads, 0);
+            });
         });
     if (weights)
         hipLaunchKernelGGL(layer_norm_parts_kernel, dim3((unsigned)((a.K + 63) / 64), 2), dim3(1024), 0, stream, a.part, (int)parts, a.K, a.w32, dw, db);

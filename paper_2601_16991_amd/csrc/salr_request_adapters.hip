@@ -9,11 +9,16 @@
 //   more                         a launch in front orders the tokens by adapter (stable: sums over tokens have an order); a workgroup finds the
 //                                adapter of its tile of 64 in the counts
 // Then  narrow_kernel  t = in * factor (K or N columns down to r; fp32 sums over slices of the columns),
-//       wide_kernel    out = base + t * factor (r up to N or K columns), t rounded to bf16 as the layer rounds its own,
+//       wide_kernel    out = base + t * factor (r up to N or K columns),
 //       outer_kernel   the adapters' gradients, sums over tokens.
+// t goes into the second product as two bf16 values, t rounded and what is left of it: 16 bits of mantissa, so that results are as good as their own
+// rounding (with t rounded once, as the layer does, errors were 1.4 times that).  In wide_kernel the second value is free: an instruction
+// that takes eight values a lane has room for four ranks of both.
 // All on the matrix cores, though memory bounds each (2 r products a byte of x and out at most): tiles of 16 fill them however few rows are live, and
 // what an adapter's factors lack in alignment or length is zeros in LDS.  Results do not depend on which other tokens a call holds, save that
 // the number of slices follows from its sizes.
+#include <type_traits>
+
 #include "salr_adapter_t.hpp"
 #include "salr_eight.hpp"
 #include "salr_internal.hpp"
@@ -24,7 +29,6 @@ namespace {
 
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef u32x2_t AnyUint2 __attribute__((aligned(2)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 // LDS of one wave alone: what was written is read by its other lanes, what was read may be written again.  (Its accesses are done in order;
 // this keeps the compiler to it.)
@@ -102,47 +106,122 @@ __device__ __forceinline__ int64_t place_of(const Tile& tile, const int* rows, i
     return kDirect ? rows[j] : tile.first + j;
 }
 
-__device__ __forceinline__ uint4 eight_of(const uint16_t* row, int64_t c, int64_t C) {   // columns c .. c + 7 of a row of C, zeros behind it
-    const int64_t left = C - c;
-    return load_eight<false, false, false>(row + c, 0, left < 8 ? (int)left : 8).q[0];
+// Sixteen bytes at any element's address of global memory.  (Said to the compiler: a pointer out of a record could point anywhere, and loads through
+// such pointers are waited for together with LDS'.)
+__device__ __forceinline__ uint4 load16(const uint16_t* p) {
+    typedef const AnyUint4 __attribute__((address_space(1))) * Global;
+    return __builtin_bit_cast(uint4, *(Global)(uintptr_t)p);
+}
+
+// The eight values `by` places on, zeros behind the first `left` of them.
+__device__ __forceinline__ uint4 from_place(uint4 q, int by, int left) {
+    uint64_t lo = q.x | (uint64_t)q.y << 32, hi = q.z | (uint64_t)q.w << 32;
+    const int bits = 16 * (by & 3);
+    lo = by & 4 ? hi : lo;
+    hi = by & 4 ? 0 : hi;
+    lo = lo >> bits | (hi << 1) << (63 - bits);
+    hi >>= bits;
+    const int a = left < 0 ? 0 : left < 4 ? left : 4, b = left < 4 ? 0 : left < 8 ? left - 4 : 4;
+    lo &= a == 4 ? ~(uint64_t)0 : ((uint64_t)1 << (16 * a)) - 1;
+    hi &= b == 4 ? ~(uint64_t)0 : ((uint64_t)1 << (16 * b)) - 1;
+    return make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
+}
+
+// Columns c .. c + 7 of the row of C >= 8 that starts at element `start` of a matrix of `total`, in two steps, so that nothing waits for a request until it
+// is used: raw_eight asks for them, in one request without a branch (kWhole, C % 8 == 0: at the row's last vector where c is past it; else pulled back
+// from the matrix' end where it would leave it), and true_eight makes of what came the row's values, and zeros behind them, wherever c is.
+template <bool kWhole>
+__device__ __forceinline__ uint4 raw_eight(const uint16_t* m, int64_t start, int c, int C, int64_t total) {
+    if constexpr (kWhole) {
+        return load16(m + start + (c < C ? c : C - 8));
+    } else {
+        const int64_t at = start + (c < C ? c : C - 1);
+        return load16(m + (at < total - 8 ? at : total - 8));
+    }
+}
+template <bool kWhole>
+__device__ __forceinline__ uint4 true_eight(uint4 q, int64_t start, int c, int C, int64_t total) {
+    if constexpr (kWhole) {
+        return c < C ? q : make_uint4(0, 0, 0, 0);
+    } else {
+        const int64_t at = start + (c < C ? c : C - 1), past = at - (total - 8);
+        return from_place(q, past > 0 ? (int)past : 0, C - c);
+    }
+}
+
+// Ranks r .. r + 7 of a row of a factor A [C, rank], likewise; behind the last rank whatever comes, but nothing from behind the matrix.
+__device__ __forceinline__ uint4 raw_ranks(const uint16_t* m, int64_t row, int r, int rank, int64_t total) {
+    const int64_t at = row * rank + r;
+    return load16(m + (at < total - 8 ? at : total - 8));
+}
+__device__ __forceinline__ uint4 true_ranks(uint4 q, int64_t row, int r, int rank, int64_t total) {
+    if ((rank & 7) == 0) return q;   // (whole vectors are pulled back only where r >= rank)
+    const int64_t past = row * rank + r - (total - 8);
+    return from_place(q, past > 0 ? past < 8 ? (int)past : 7 : 0, 8);
+}
+
+// Four values as bf16 and what that leaves of them, as bf16 too.
+__device__ __forceinline__ uint4 two_halves(f32x4 v) {
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        hi[e] = f32_to_bf16_rne(v[e]);
+        const float rest = v[e] - bf16_bits_to_f32(hi[e]);
+        lo[e] = fabsf(rest) <= fabsf(v[e]) ? f32_to_bf16_rne(rest) : 0u;   // (infinite or NaN: all of it is in the first)
+    }
+    return make_uint4(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16, lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
 }
 
 }  // namespace
 
 // A workgroup a group: counts the tokens of the groups before its own, then puts its own in order.  Every group goes through all ids, which
-// stay in the caches; no workgroup waits for another.
+// stay in the caches; no workgroup waits for another.  A thread takes eight ids side by side, so that up to 8192 tokens are read once.
+constexpr int kOrderEach = 8;
 __global__ __launch_bounds__(1024) void order_tokens_kernel(const int32_t* ids, int T, int n, int32_t* order, int32_t* starts, int32_t* counts) {
     __shared__ uint32_t scratch[17];
-    __shared__ int total[2];
-    const int group = blockIdx.x;
-    if (threadIdx.x < 2) total[threadIdx.x] = 0;
-    __syncthreads();
+    __shared__ int total[2][16];
+    const int group = blockIdx.x, wave = threadIdx.x >> 6;
     int less = 0, same = 0;
-    for (int t = threadIdx.x; t < T; t += 1024) {
-        const int g = group_of(ids[t], n);
-        less += g < group;
-        same += g == group;
-    }
+    uint32_t mine = 0;   // of the ids looked at last
+    const auto look = [&](int64_t t0) {
+        mine = 0;
+        int g[kOrderEach];
+#pragma unroll
+        for (int j = 0; j < kOrderEach; ++j) {
+            const int64_t t = t0 + kOrderEach * threadIdx.x + j;
+            g[j] = t < T ? group_of(ids[t], n) : 2147483647;
+        }
+#pragma unroll
+        for (int j = 0; j < kOrderEach; ++j) {
+            less += g[j] < group;
+            mine |= (uint32_t)(g[j] == group) << j;
+        }
+        same += __popc(mine);
+    };
+    for (int64_t t0 = 0; t0 < T; t0 += 1024 * kOrderEach) look(t0);
     less = (int)last_lane(wave_inclusive_scan((uint32_t)less));
     same = (int)last_lane(wave_inclusive_scan((uint32_t)same));
-    if (lane_id() == 0) {   // (whole numbers: in any order)
-        atomicAdd(&total[0], less);
-        atomicAdd(&total[1], same);
+    if (lane_id() == 0) {
+        total[0][wave] = less;
+        total[1][wave] = same;
     }
     __syncthreads();
-    int at = total[0];
-    const int count = total[1];
+    int at = 0, count = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+        at += total[0][w];
+        count += total[1][w];
+    }
     if (threadIdx.x == 0) {
         starts[group] = at;
         counts[group] = count;
     }
     if (count == 0) return;
-    for (int t0 = 0; t0 < T; t0 += 1024) {
-        const int t = t0 + threadIdx.x;
-        const bool mine = t < T && group_of(ids[t], n) == group;
+    for (int64_t t0 = 0; t0 < T; t0 += 1024 * kOrderEach) {
+        if (T > 1024 * kOrderEach) look(t0);
         uint32_t here;
-        const uint32_t place = block_exclusive_scan<1024>(mine ? 1u : 0u, scratch, here);
-        if (mine) order[at + place] = t;
+        uint32_t place = at + block_exclusive_scan<1024>(__popc(mine), scratch, here);
+        for (uint32_t left = mine; left != 0; left &= left - 1) order[place++] = (int32_t)(t0 + kOrderEach * threadIdx.x + __builtin_ctz(left));
         at += (int)here;
     }
 }
@@ -158,75 +237,90 @@ struct NarrowArgs {
 };
 
 // part[z][row][r] = sum over the columns c of slice z of in[row][c] * factor(c, r).  Workgroup (tile, slice); its four waves take every fourth step
-// of 32 columns, with 16 kMB rows and 16 kRT ranks each (more ranks: another pass), and are added through LDS, in order.  in's rows are the A
-// operand of 16x16x32 MFMAs as they lie; A's [32 columns, ranks], which lie the wrong way round, go through LDS and its transposing
+// of 64 columns, with 16 kMB rows and 16 kRT ranks each (more ranks: another pass), and are added through LDS, in order.  in's rows are the A
+// operand of 16x16x32 MFMAs as they lie; A's [64 columns, ranks], which lie the wrong way round, go through LDS and its transposing
 // read, B's [ranks, columns] are the B operand as they lie.  A step's requests are out while the one before is multiplied.
-template <bool kDirect, int kMB, int kRT>
-__global__ __launch_bounds__(256) void narrow_kernel(NarrowArgs a) {
-    constexpr int kPitch = 16 * kRT + 8, kSumPitch = 16 * kRT + 4;
-    __shared__ int rows[16 * kMB];
-    __shared__ __align__(16) uint16_t stages[4][32 * kPitch];
-    __shared__ __align__(16) float sums[16 * kMB * kSumPitch];
+template <int kMB, int kRT>
+struct NarrowLds {
+    static constexpr int kPitch = 16 * kRT + 8, kSumPitch = 16 * kRT + 4, kStage = 64 * kPitch;
+    static constexpr int kSumBytes = 16 * kMB * kSumPitch * 4, kStageBytes = 4 * kStage * 2, kBytes = kSumBytes > kStageBytes ? kSumBytes : kStageBytes;
+};
+
+template <bool kDirect, int kMB, int kRT, bool kWhole, bool second>   // second: dy with B
+__device__ __forceinline__ void narrow_tile(const NarrowArgs& a, const Tile& tile, const int* rows, char* lds) {
+    typedef NarrowLds<kMB, kRT> Lds;
+    constexpr int kPitch = Lds::kPitch, kSumPitch = Lds::kSumPitch, kStage = Lds::kStage;
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i16 = lane & 15, g = lane >> 4;
-    const Tile tile = find_tile<kDirect, 16 * kMB>(a.tokens, rows);
-    if (tile.group < 0 || tile.group >= a.tokens.n) return;
-    const bool second = (int)blockIdx.y >= a.slices[0];
     const int z = second ? (int)blockIdx.y - a.slices[0] : (int)blockIdx.y, slices = second ? a.slices[1] : a.slices[0];
     const uint16_t* in = second ? a.in[1] : a.in[0];
-    const int64_t C = second ? a.C[1] : a.C[0];
+    const int C = (int)(second ? a.C[1] : a.C[0]);
+    const int64_t in_total = (int64_t)a.tokens.T * C;
     float* part = (second ? a.part[1] : a.part[0]) + (int64_t)z * a.t_rows * a.rpad;
     const salr_adapter_t& adapter = a.tokens.list[tile.group];
     const int rank = (int)adapter.rank;
     const uint16_t* factor = second ? adapter.b : adapter.a;
-    const int steps = (int)((C + 31) >> 5), s_begin = (int)((int64_t)steps * z / slices), s_end = (int)((int64_t)steps * (z + 1) / slices);
-    const uint16_t* row[kMB];
+    const int64_t factor_total = (int64_t)rank * C;
+    const int steps = (C + 63) >> 6, s_begin = (int)((int64_t)steps * z / slices), s_end = (int)((int64_t)steps * (z + 1) / slices);
+    int64_t row[kMB];   // (behind the last token the first one's: what comes of it is not stored)
 #pragma unroll
-    for (int mb = 0; mb < kMB; ++mb) {
-        const int token = rows[16 * mb + i16];
-        row[mb] = token < 0 ? nullptr : in + (int64_t)token * C;
-    }
-    uint16_t* stage = stages[wave];
+    for (int mb = 0; mb < kMB; ++mb) row[mb] = (int64_t)rows[16 * mb + i16 < tile.count ? 16 * mb + i16 : 0] * C;
+    uint16_t* stage = reinterpret_cast<uint16_t*>(lds) + wave * kStage;
+    float* sums = reinterpret_cast<float*>(lds);
     for (int rb = 0; rb < rank; rb += 16 * kRT) {
         const int rts = (rank - rb + 15) / 16 < kRT ? (rank - rb + 15) / 16 : kRT;
         f32x4 acc[kMB][kRT] = {};
-        uint4 xq[kMB], fq[kRT];
+        uint4 xq[2][kMB], fq[2][kRT];
         const auto request = [&](int s) {
-            const int64_t c = 32 * (int64_t)s;
+            const int c = 64 * s;
 #pragma unroll
-            for (int mb = 0; mb < kMB; ++mb) xq[mb] = row[mb] != nullptr ? eight_of(row[mb], c + 8 * g, C) : make_uint4(0, 0, 0, 0);
+            for (int u = 0; u < 2; ++u) {
 #pragma unroll
-            for (int rt = 0; rt < kRT; ++rt) {
-                fq[rt] = make_uint4(0, 0, 0, 0);
-                if (second) {
-                    const int r = rb + 16 * rt + i16;
-                    if (r < rank) fq[rt] = eight_of(factor + (int64_t)r * C, c + 8 * g, C);
-                } else {   // vector v of [32][16 kRT]
-                    const int v = lane + 64 * rt, k = v / (2 * kRT), r = rb + 8 * (v % (2 * kRT));
-                    if (c + k < C && r < rank) fq[rt] = eight_of(factor + (c + k) * rank, r, rank);
+                for (int mb = 0; mb < kMB; ++mb) xq[u][mb] = raw_eight<kWhole>(in, row[mb], c + 32 * u + 8 * g, C, in_total);
+#pragma unroll
+                for (int rt = 0; rt < kRT; ++rt) {
+                    if constexpr (second) {   // (behind the last rank its values again: what comes of them is dropped)
+                        const int r = rb + 16 * rt + i16;
+                        fq[u][rt] = raw_eight<kWhole>(factor, (int64_t)(r < rank ? r : rank - 1) * C, c + 32 * u + 8 * g, C, factor_total);
+                    } else {                  // vector v of [64][16 kRT]
+                        const int v = lane + 64 * (kRT * u + rt), k = c + v / (2 * kRT);
+                        fq[u][rt] = raw_ranks(factor, k < C ? k : C - 1, rb + 8 * (v % (2 * kRT)), rank, factor_total);
+                    }
                 }
             }
         };
         if (s_begin + wave < s_end) request(s_begin + wave);
         for (int s = s_begin + wave; s < s_end; s += 4) {
-            bf16x8 x[kMB], f[kRT];
+            bf16x8 x[2][kMB], f[2][kRT];
 #pragma unroll
-            for (int mb = 0; mb < kMB; ++mb) x[mb] = as_bf16x8(xq[mb]);
-            if (second) {
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int rt = 0; rt < kRT; ++rt) f[rt] = as_bf16x8(fq[rt]);
+                for (int mb = 0; mb < kMB; ++mb) x[u][mb] = as_bf16x8(true_eight<kWhole>(xq[u][mb], row[mb], 64 * s + 32 * u + 8 * g, C, in_total));
+            if constexpr (second) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int rt = 0; rt < kRT; ++rt) {
+                        const int r = rb + 16 * rt + i16;
+                        f[u][rt] = as_bf16x8(true_eight<kWhole>(fq[u][rt], (int64_t)(r < rank ? r : rank - 1) * C, 64 * s + 32 * u + 8 * g, C, factor_total));
+                    }
             } else {
 #pragma unroll
-                for (int rt = 0; rt < kRT; ++rt) {
-                    const int v = lane + 64 * rt;
-                    *reinterpret_cast<uint4*>(stage + v / (2 * kRT) * kPitch + 8 * (v % (2 * kRT))) = fq[rt];
-                }
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int rt = 0; rt < kRT; ++rt) {
+                        const int v = lane + 64 * (kRT * u + rt), k = 64 * s + v / (2 * kRT);
+                        const uint4 q = true_ranks(fq[u][rt], k < C ? k : C - 1, rb + 8 * (v % (2 * kRT)), rank, factor_total);
+                        *reinterpret_cast<uint4*>(stage + v / (2 * kRT) * kPitch + 8 * (v % (2 * kRT))) = k < C ? q : make_uint4(0, 0, 0, 0);
+                    }
                 wave_sync();
 #pragma unroll
-                for (int rt = 0; rt < kRT; ++rt) {
-                    const uint16_t* col = stage + (8 * g + (i16 >> 2)) * kPitch + 16 * rt + 4 * (i16 & 3);
-                    const uint2 lo = lds_read_tr4(col), hi = lds_read_tr4(col + 4 * kPitch);
-                    f[rt] = as_bf16x8(make_uint4(lo.x, lo.y, hi.x, hi.y));
-                }
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int rt = 0; rt < kRT; ++rt) {
+                        const uint16_t* col = stage + (32 * u + 8 * g + (i16 >> 2)) * kPitch + 16 * rt + 4 * (i16 & 3);
+                        const uint2 lo = lds_read_tr4(col), hi = lds_read_tr4(col + 4 * kPitch);
+                        f[u][rt] = as_bf16x8(make_uint4(lo.x, lo.y, hi.x, hi.y));
+                    }
                 wave_sync();
             }
             if (s + 4 < s_end) request(s + 4);
@@ -234,9 +328,11 @@ __global__ __launch_bounds__(256) void narrow_kernel(NarrowArgs a) {
             for (int rt = 0; rt < kRT; ++rt)
                 if (rt < rts)
 #pragma unroll
-                    for (int mb = 0; mb < kMB; ++mb)
-                        if (16 * mb < tile.count) acc[mb][rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[mb], f[rt], acc[mb][rt], 0, 0, 0);
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int mb = 0; mb < kMB; ++mb) acc[mb][rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[u][mb], f[u][rt], acc[mb][rt], 0, 0, 0);
         }
+        __syncthreads();   // the stages have been read: their place is the sums' now
         // accumulators: lane holds column i16 (rank), rows 4 g + e (tokens)
         for (int w = 0; w < 4; ++w) {
             if (w == wave)
@@ -262,10 +358,21 @@ __global__ __launch_bounds__(256) void narrow_kernel(NarrowArgs a) {
     }
 }
 
-// t = bf16(sum over the slices of part), four values a thread; y picks the product.
+template <bool kDirect, int kMB, int kRT, bool kWhole>
+__global__ __launch_bounds__(256, kMB == 1 ? 3 : 2) void narrow_kernel(NarrowArgs a) {
+    __shared__ int rows[16 * kMB];
+    __shared__ __align__(16) char lds[NarrowLds<kMB, kRT>::kBytes];
+    const Tile tile = find_tile<kDirect, 16 * kMB>(a.tokens, rows);
+    if (tile.group < 0 || tile.group >= a.tokens.n) return;
+    if constexpr (kDirect) narrow_tile<kDirect, kMB, kRT, kWhole, false>(a, tile, rows, lds);
+    else if ((int)blockIdx.y < a.slices[0]) narrow_tile<kDirect, kMB, kRT, kWhole, false>(a, tile, rows, lds);
+    else narrow_tile<kDirect, kMB, kRT, kWhole, true>(a, tile, rows, lds);
+}
+
+// t = the sum over the slices of part, four values a thread, as two_halves has them; y picks the product.
 struct SumArgs {
     const float* part[2];
-    uint16_t* t[2];
+    uint4* t[2];
     int slices[2];
     int64_t count;   // of a slice
 };
@@ -273,19 +380,18 @@ __global__ __launch_bounds__(256) void sum_slices_kernel(SumArgs a) {
     const bool second = blockIdx.y == 1;
     const float* part = second ? a.part[1] : a.part[0];
     const int slices = second ? a.slices[1] : a.slices[0];
-    const int64_t i = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x);
-    if (i >= a.count) return;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (4 * i >= a.count) return;
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int z = 0; z < slices; ++z) s += *reinterpret_cast<const f32x4*>(part + z * a.count + i);
-    uint16_t* to = (second ? a.t[1] : a.t[0]) + i;
-    *reinterpret_cast<uint2*>(to) = make_uint2(f32_to_bf16_rne(s[0]) | (uint32_t)f32_to_bf16_rne(s[1]) << 16, f32_to_bf16_rne(s[2]) | (uint32_t)f32_to_bf16_rne(s[3]) << 16);
+#pragma unroll 8
+    for (int z = 0; z < slices; ++z) s += *reinterpret_cast<const f32x4*>(part + z * a.count + 4 * i);
+    (second ? a.t[1] : a.t[0])[i] = two_halves(s);
 }
 
 struct WideArgs {
     Tokens tokens;
     const float* part;      // [slices][t_rows][rpad], summed here; or, slices 0,
-    const uint16_t* t;      // [t_rows][rpad]
+    const uint4* t;         // [t_rows][rpad / 4], as two_halves has them
     int slices;
     int64_t t_rows;
     int rpad;
@@ -296,27 +402,28 @@ struct WideArgs {
 };
 
 // out[row][c] = base[row][c] + sum over r of t[row][r] * factor(r, c).  Workgroup (tile, columns): t's rows once into LDS, then each wave takes 64
-// columns at a time, the factor's part of them, zeros where ranks or columns end, through LDS of its own (64 ranks a pass).  The product is
-// formed transposed, columns of out as rows of 16x16x16 MFMAs, and which column a row stands for is chosen so that a lane ends up with 16
-// columns of one token side by side (row m of tile j is column 16 (m / 4) + 4 j + m % 4): out is read and written in whole vectors.
+// columns at a time, the factor's part of them, zeros where ranks or columns end, through LDS of its own (kPass ranks a pass), the next one's on their
+// way meanwhile.  The product is formed transposed, columns of out as rows of 16x16x32 MFMAs, and which column a row stands for is chosen so that a
+// lane ends up with 16 columns of one token side by side (row m of tile j is column 16 (m / 4) + 4 j + m % 4): out is read and written in
+// whole vectors.  An instruction takes 16 ranks: four of a lane with t's first half and the same four with its second.
 // kFactorA: the factor is A [C, r] (dx), else B [r, C] (y).
-template <bool kDirect, int kMB, int kMostR, bool kFactorA>
-__global__ __launch_bounds__(256) void wide_kernel(WideArgs a) {
-    constexpr int kTPitch = kMostR + 8, kPitch = 64 + 8;
+template <bool kDirect, int kMB, int kMostR, bool kFactorA, bool kWhole>
+__global__ __launch_bounds__(256, kMB == 1 ? 3 : kMostR > 64 ? 1 : 2) void wide_kernel(WideArgs a) {
+    constexpr int kTPitch = 2 * kMostR + 8, kPass = kMostR < 64 ? kMostR : 64, kVectors = kPass / 8, kPitch = kFactorA ? kPass + 8 : 64 + 8;
     __shared__ int rows[16 * kMB];
     __shared__ __align__(16) uint16_t t[16 * kMB * kTPitch];
-    __shared__ __align__(16) uint16_t stages[4][64 * kPitch];
+    __shared__ __align__(16) uint16_t stages[4][(kFactorA ? 64 : kPass) * kPitch];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i16 = lane & 15, g = lane >> 4;
     const Tile tile = find_tile<kDirect, 16 * kMB>(a.tokens, rows);
     if (tile.group < 0) return;
-    const int64_t c_begin = (int64_t)blockIdx.y * a.per_group, c_end = c_begin + a.per_group < a.C ? c_begin + a.per_group : a.C;
+    const int C = (int)a.C, c_begin = (int)(blockIdx.y * a.per_group), c_end = c_begin + a.per_group < C ? (int)(c_begin + a.per_group) : C;
     if (tile.group >= a.tokens.n) {   // no adapter: base as it is; an id that is none: NaN
         const bool none = tile.group == a.tokens.n;
         if (none && a.base == a.out) return;
-        const int width = (int)((c_end - c_begin + 7) >> 3);
+        const int width = (c_end - c_begin + 7) >> 3;
         for (int i = threadIdx.x; i < tile.count * width; i += 256) {
-            const int64_t at = (int64_t)rows[i / width] * a.C, c = c_begin + 8 * (i % width);
-            const int left = c_end - c < 8 ? (int)(c_end - c) : 8;
+            const int64_t at = (int64_t)rows[i / width] * C;
+            const int c = c_begin + 8 * (i % width), left = c_end - c;
             Eight<false> q{{make_uint4(0, 0, 0, 0)}};
             if (none && a.base != nullptr) q = load_eight<false, false, false>(a.base + at + c, 0, left);
             float v[8];
@@ -329,85 +436,119 @@ __global__ __launch_bounds__(256) void wide_kernel(WideArgs a) {
     const salr_adapter_t& adapter = a.tokens.list[tile.group];
     const int rank = (int)adapter.rank, rank16 = (rank + 15) & ~15;
     const uint16_t* factor = kFactorA ? adapter.a : adapter.b;
+    const int64_t factor_total = (int64_t)rank * C;
+    uint4 q[kVectors];
+    const auto request = [&](int c0, int rb) {   // the factor's part for 64 columns and kPass ranks
+#pragma unroll
+        for (int v = 0; v < kVectors; ++v) {
+            if constexpr (kFactorA) {   // vectors of [64 columns][kPass ranks]
+                const int i = lane + 64 * v, k = c0 + i / kVectors;
+                q[v] = raw_ranks(factor, k < C ? k : C - 1, rb + 8 * (i % kVectors), rank, factor_total);
+            } else {                    // vectors of [kPass ranks][64 columns]
+                const int r = rb + 8 * v + (lane >> 3);
+                q[v] = raw_eight<kWhole>(factor, (int64_t)(r < rank ? r : rank - 1) * C, c0 + 8 * (lane & 7), C, factor_total);
+            }
+        }
+    };
+    const auto place = [&](uint16_t* stage, int c0, int rb) {   // what came of that into LDS, zeros behind the last rank
+#pragma unroll
+        for (int v = 0; v < kVectors; ++v) {
+            const int i = lane + 64 * v;
+            if constexpr (kFactorA) {
+                const int k = c0 + i / kVectors, r = rb + 8 * (i % kVectors);
+                const uint4 f = true_ranks(q[v], k < C ? k : C - 1, r, rank, factor_total);
+                *reinterpret_cast<uint4*>(stage + i / kVectors * kPitch + 8 * (i % kVectors)) = rank - r >= 8 ? f : from_place(f, 0, rank - r);
+            } else {
+                const int r = rb + 8 * v + (lane >> 3);
+                const uint4 f = true_eight<kWhole>(q[v], (int64_t)(r < rank ? r : rank - 1) * C, c0 + 8 * (lane & 7), C, factor_total);
+                *reinterpret_cast<uint4*>(stage + (i >> 3) * kPitch + 8 * (i & 7)) = r < rank ? f : make_uint4(0, 0, 0, 0);
+            }
+        }
+    };
+    int c0 = c_begin + 64 * wave, rb = 0;
+    if (c0 < c_end && rank > 0) request(c0, 0);
     for (int i = threadIdx.x; i < 16 * kMB * (rank16 / 4); i += 256) {
         const int j = i / (rank16 / 4), r = 4 * (i % (rank16 / 4));
-        uint2 q = make_uint2(0, 0);
+        uint4 h = make_uint4(0, 0, 0, 0);
         if (j < tile.count) {
             const int64_t at = place_of<kDirect>(tile, rows, j) * a.rpad + r;
             if (a.slices > 0) {
                 f32x4 s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
+#pragma unroll 8
                 for (int z = 0; z < a.slices; ++z) s += *reinterpret_cast<const f32x4*>(a.part + z * a.t_rows * a.rpad + at);
-                q = make_uint2(f32_to_bf16_rne(s[0]) | (uint32_t)f32_to_bf16_rne(s[1]) << 16, f32_to_bf16_rne(s[2]) | (uint32_t)f32_to_bf16_rne(s[3]) << 16);
+                h = two_halves(s);
             } else {
-                q = *reinterpret_cast<const uint2*>(a.t + at);
+                h = a.t[at >> 2];
             }
         }
-        *reinterpret_cast<uint2*>(t + j * kTPitch + r) = q;
+        *reinterpret_cast<uint4*>(t + j * kTPitch + 2 * r) = h;
     }
     __syncthreads();
     uint16_t* stage = stages[wave];
-    for (int64_t c0 = c_begin + 64 * wave; c0 < c_end; c0 += 256) {
-        f32x4 acc[kMB][4] = {};
-        for (int rb = 0; rb < rank; rb += 64) {
-            const int ranks = rank - rb < 64 ? rank - rb : 64, steps = (ranks + 15) / 16;
-            uint4 q[8];
+    const int64_t out_total = (int64_t)a.tokens.T * C;
+    int token[kMB];
 #pragma unroll
-            for (int v = 0; v < 8; ++v) {
-                if (v >= 2 * steps) break;
-                q[v] = make_uint4(0, 0, 0, 0);
-                if constexpr (kFactorA) {   // vectors of [64 columns][16 steps ranks]
-                    const int i = lane + 64 * v, k = i / (2 * steps), r = 8 * (i % (2 * steps));
-                    if (c0 + k < a.C && r < ranks) q[v] = eight_of(factor + (c0 + k) * rank, rb + r, rank);
-                } else {                    // vectors of [16 steps ranks][64 columns]
-                    const int r = 8 * v + (lane >> 3);
-                    if (r < ranks) q[v] = eight_of(factor + (int64_t)(rb + r) * a.C, c0 + 8 * (lane & 7), a.C);
-                }
+    for (int mb = 0; mb < kMB; ++mb) token[mb] = rows[16 * mb + i16];
+    f32x4 acc[kMB][4];
+    Eight<false> base[kMB][2] = {};
+    while (c0 < c_end) {
+        if (rb == 0) {
+#pragma unroll
+            for (int mb = 0; mb < kMB; ++mb) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[mb][j] = f32x4{0.f, 0.f, 0.f, 0.f};
             }
-            wave_sync();
+            if (a.base != nullptr) {
 #pragma unroll
-            for (int v = 0; v < 8; ++v) {
-                if (v >= 2 * steps) break;
-                const int i = lane + 64 * v;
-                if constexpr (kFactorA) *reinterpret_cast<uint4*>(stage + i / (2 * steps) * kPitch + 8 * (i % (2 * steps))) = q[v];
-                else *reinterpret_cast<uint4*>(stage + (i >> 3) * kPitch + 8 * (i & 7)) = q[v];
+                for (int mb = 0; mb < kMB; ++mb)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        base[mb][h].q[0] = raw_eight<kWhole>(a.base, (int64_t)(token[mb] < 0 ? 0 : token[mb]) * C, c0 + 16 * g + 8 * h, C, out_total);
             }
-            wave_sync();
+        }
+        const int steps = (rank - rb + 15) / 16 < kPass / 16 ? (rank - rb + 15) / 16 : kPass / 16;
+        if (rank > 0) place(stage, c0, rb);
+        wave_sync();
+        const int now = rb, c_now = c0;
+        rb += kPass;
+        if (rb >= rank) {
+            rb = 0;
+            c0 += 256;
+        }
+        if (c0 < c_end && rank > 0) request(c0, rb);
 #pragma unroll
-            for (int st = 0; st < 4; ++st) {
-                if (st >= steps) break;
-                uint2 tq[kMB];
+        for (int st = 0; st < kPass / 16; ++st) {
+            if (st < steps) {
+                uint4 tq[kMB];
 #pragma unroll
-                for (int mb = 0; mb < kMB; ++mb) tq[mb] = *reinterpret_cast<const uint2*>(t + (16 * mb + i16) * kTPitch + rb + 16 * st + 4 * g);
+                for (int mb = 0; mb < kMB; ++mb) tq[mb] = *reinterpret_cast<const uint4*>(t + (16 * mb + i16) * kTPitch + 2 * (now + 16 * st + 4 * g));
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     uint2 f;
                     if constexpr (kFactorA) f = *reinterpret_cast<const uint2*>(stage + (16 * (i16 >> 2) + 4 * j + (i16 & 3)) * kPitch + 16 * st + 4 * g);
                     else f = lds_read_tr4(stage + (16 * st + 4 * g + (i16 >> 2)) * kPitch + 16 * (i16 & 3) + 4 * j);
+                    const bf16x8 twice = as_bf16x8(make_uint4(f.x, f.y, f.x, f.y));
 #pragma unroll
                     for (int mb = 0; mb < kMB; ++mb)
-                        if (16 * mb < tile.count)
-                            acc[mb][j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, f), __builtin_bit_cast(s16x4, tq[mb]), acc[mb][j], 0, 0, 0);
+                        if (16 * mb < tile.count) acc[mb][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(twice, as_bf16x8(tq[mb]), acc[mb][j], 0, 0, 0);
                 }
             }
         }
-        // lane holds columns c0 + 16 g .. + 15 of token 16 mb + i16
+        wave_sync();
+        if (rb != 0) continue;
+        // lane holds columns c_now + 16 g .. + 15 of token 16 mb + i16
 #pragma unroll
         for (int mb = 0; mb < kMB; ++mb) {
-            const int token = rows[16 * mb + i16];
-            if (token < 0) continue;
+            if (token[mb] < 0) continue;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int64_t c = c0 + 16 * g + 8 * h;
-                const int left = a.C - c < 8 ? (int)(a.C - c) : 8;
+                const int c = c_now + 16 * g + 8 * h, left = C - c;
                 if (left <= 0) continue;
-                const int64_t at = (int64_t)token * a.C + c;
-                Eight<false> q{{make_uint4(0, 0, 0, 0)}};
-                if (a.base != nullptr) q = load_eight<false, false, false>(a.base + at, 0, left);
+                const Eight<false> from{{true_eight<kWhole>(base[mb][h].q[0], (int64_t)token[mb] * C, c, C, out_total)}};
                 float v[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = q.get(e) + acc[mb][2 * h + (e >> 2)][e & 3];
-                store_eight<false, false>(a.out + at, 0, left, v);
+                for (int e = 0; e < 8; ++e) v[e] = from.get(e) + acc[mb][2 * h + (e >> 2)][e & 3];
+                store_eight<false, false>(a.out + (int64_t)token[mb] * C + c, 0, kWhole ? 8 : left, v);
             }
         }
     }
@@ -416,96 +557,136 @@ __global__ __launch_bounds__(256) void wide_kernel(WideArgs a) {
 struct OuterArgs {
     Tokens tokens;
     const uint16_t* in[2];   // x (dA), dy (dB)
-    const uint16_t* s[2];    // dy B^T (dA), x A (dB): [T][rpad] by position
+    const uint4* s[2];       // dy B^T (dA), x A (dB): [T][rpad / 4] by position, as two_halves has them
     int64_t C[2];
     int rpad;
-    int blocks0;             // of 64 columns: of x
+    int blocks0;             // of kCols columns: of x
 };
 
-// dA_i [K, r] and dB_i [r, N], sums over the adapter's tokens: workgroup (64 columns of x or dy, adapter).  Both operands lie with the tokens as
+// dA_i [K, r] and dB_i [r, N], sums over the adapter's tokens: workgroup (kCols columns of x or dy, adapter).  Both operands lie with the tokens as
 // rows and are transposed by LDS' transposing read, 32 tokens a step and kBatch steps in flight.  Which of the two is the MFMA's first
 // operand is chosen so that a lane holds four values side by side of the result.  An adapter without tokens gets zeros.
-template <int kRT>
-__global__ __launch_bounds__(256) void outer_kernel(OuterArgs a) {
-    constexpr int kBatch = 4, kPitch = 64 + 8, kSPitch = 16 * kRT + 8;
-    __shared__ __align__(16) uint16_t in_tile[2][kBatch * 32 * kPitch];
-    __shared__ __align__(16) uint16_t s_tile[2][kBatch * 32 * kSPitch];
+template <int kRT, int kCols>
+struct OuterLds {
+    static constexpr int kBatch = 128 / kCols * 2, kTokens = 32 * kBatch, kPitch = kCols + 8, kSPitch = 32 * kRT + 8;
+    uint16_t in_tile[kTokens * kPitch];
+    uint16_t s_tile[kTokens * kSPitch];
+};
+
+template <int kRT, int kCols, bool kWhole, bool second>   // second: dB
+__device__ __forceinline__ void outer_tile(const OuterArgs& a, uint16_t* in_tile, uint16_t* s_tile) {
+    typedef OuterLds<kRT, kCols> Lds;
+    constexpr int kBatch = Lds::kBatch, kTokens = Lds::kTokens, kPitch = Lds::kPitch, kSPitch = Lds::kSPitch;
+    constexpr int kCT = kCols / 64, kX = kTokens * kCols / 8 / 256, kS = kTokens * 4 * kRT / 256, kAcross = kCols / 8;
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i16 = lane & 15, g = lane >> 4;
     const salr_adapter_t& adapter = a.tokens.list[blockIdx.y];
-    const bool second = (int)blockIdx.x >= a.blocks0;
     uint16_t* out = second ? adapter.db : adapter.da;
     if (out == nullptr) return;
     const int rank = (int)adapter.rank, count = a.tokens.counts[blockIdx.y], start = a.tokens.starts[blockIdx.y];
     const uint16_t* in = second ? a.in[1] : a.in[0];
-    const uint16_t* s = (second ? a.s[1] : a.s[0]) + (int64_t)start * a.rpad;
-    const int64_t C = second ? a.C[1] : a.C[0], c0 = 64 * (int64_t)((int)blockIdx.x - (second ? a.blocks0 : 0));
-    const int trow = threadIdx.x >> 3, tvec = threadIdx.x & 7;
+    const uint4* s = (second ? a.s[1] : a.s[0]) + (int64_t)start * (a.rpad / 4);
+    const int C = (int)(second ? a.C[1] : a.C[0]), c0 = kCols * ((int)blockIdx.x - (second ? a.blocks0 : 0));
+    const int64_t in_total = (int64_t)a.tokens.T * C;
+    const int trow = threadIdx.x / kAcross, tvec = threadIdx.x % kAcross;
     for (int rb = 0; rb < rank; rb += 16 * kRT) {
-        f32x4 acc[kRT] = {};
-        uint4 xq[kBatch], sq[kRT];
-        const auto request = [&](int b) {   // tokens b .. b + 32 kBatch - 1 of the adapter
+        f32x4 acc[kCT][kRT] = {};
+        uint4 xq[kX], sq[kS];
+        int token[kX];   // of the batch after the one requested last
+        int64_t row[kX];
+        const auto find = [&](int b) {
 #pragma unroll
-            for (int d = 0; d < kBatch; ++d) {
-                const int j = b + 32 * d + trow;
-                xq[d] = make_uint4(0, 0, 0, 0);
-                if (j < count) xq[d] = eight_of(in + (int64_t)a.tokens.order[start + j] * C, c0 + 8 * tvec, C);
-            }
-#pragma unroll
-            for (int v = 0; v < kRT; ++v) {
-                const int i = threadIdx.x + 256 * v, j = b + i / (2 * kRT), r = rb + 8 * (i % (2 * kRT));
-                sq[v] = make_uint4(0, 0, 0, 0);
-                if (j < count && r < a.rpad) sq[v] = *reinterpret_cast<const uint4*>(s + (int64_t)j * a.rpad + r);
+            for (int d = 0; d < kX; ++d) {
+                const int j = b + 256 / kAcross * d + trow;
+                token[d] = a.tokens.order[start + (j < count ? j : count - 1)];
             }
         };
-        if (count > 0) request(0);
-        int buf = 0;
-        for (int b = 0; b < count; b += 32 * kBatch, buf ^= 1) {
+        const auto request = [&](int b) {   // tokens b .. b + kTokens - 1 of the adapter
 #pragma unroll
-            for (int d = 0; d < kBatch; ++d) *reinterpret_cast<uint4*>(&in_tile[buf][(32 * d + trow) * kPitch + 8 * tvec]) = xq[d];
-#pragma unroll
-            for (int v = 0; v < kRT; ++v) {
-                const int i = threadIdx.x + 256 * v;
-                *reinterpret_cast<uint4*>(&s_tile[buf][i / (2 * kRT) * kSPitch + 8 * (i % (2 * kRT))]) = sq[v];
+            for (int d = 0; d < kX; ++d) {
+                row[d] = (int64_t)token[d] * C;
+                xq[d] = raw_eight<kWhole>(in, row[d], c0 + 8 * tvec, C, in_total);
             }
-            if (b + 32 * kBatch < count) request(b + 32 * kBatch);
-            __syncthreads();   // the tiles are complete; those of the other buffer have been read by everyone
+#pragma unroll
+            for (int v = 0; v < kS; ++v) {
+                const int i = threadIdx.x + 256 * v, j = b + i / (4 * kRT), quad = rb / 4 + i % (4 * kRT), across = a.rpad / 4;
+                sq[v] = s[(int64_t)(j < count ? j : count - 1) * across + (quad < across ? quad : across - 1)];
+            }
+            find(b + kTokens);
+        };
+        if (count > 0) {
+            find(0);
+            request(0);
+        }
+        for (int b = 0; b < count; b += kTokens) {
+            if (b > 0) __syncthreads();   // the tiles of the batch before have been read by everyone
+#pragma unroll
+            for (int d = 0; d < kX; ++d) {   // (zeros behind the last token, in both)
+                const int j = 256 / kAcross * d + trow;
+                const uint4 q = true_eight<kWhole>(xq[d], row[d], c0 + 8 * tvec, C, in_total);
+                *reinterpret_cast<uint4*>(&in_tile[j * kPitch + 8 * tvec]) = b + j < count ? q : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int v = 0; v < kS; ++v) {
+                const int i = threadIdx.x + 256 * v, j = i / (4 * kRT);
+                *reinterpret_cast<uint4*>(&s_tile[j * kSPitch + 8 * (i % (4 * kRT))]) = b + j < count ? sq[v] : make_uint4(0, 0, 0, 0);
+            }
+            if (b + kTokens < count) request(b + kTokens);
+            __syncthreads();
 #pragma unroll
             for (int d = 0; d < kBatch; ++d) {
-                if (b + 32 * d >= count) break;   // the same for the workgroup
-                const auto operand = [&](const uint16_t* tile, int pitch, int c) {
-                    const uint16_t* col = tile + (32 * d + 8 * g + (i16 >> 2)) * pitch + c + 4 * (i16 & 3);
+                if (b + 32 * d >= count) continue;   // the same for the workgroup
+                // four quads of a row side by side, or (s) every other one: the first halves, or the second
+                const auto operand = [&](const uint16_t* tile, int pitch, int c, int apart) {
+                    const uint16_t* col = tile + (32 * d + 8 * g + (i16 >> 2)) * pitch + c + apart * (i16 & 3);
                     const uint2 lo = lds_read_tr4(col), hi = lds_read_tr4(col + 4 * pitch);
                     return as_bf16x8(make_uint4(lo.x, lo.y, hi.x, hi.y));
                 };
-                const bf16x8 x = operand(in_tile[buf], kPitch, 16 * wave);
+                bf16x8 x[kCT];
 #pragma unroll
-                for (int rt = 0; rt < kRT; ++rt) {
-                    const bf16x8 f = operand(s_tile[buf], kSPitch, 16 * rt);
-                    acc[rt] = second ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, f, acc[rt], 0, 0, 0) : __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, x, acc[rt], 0, 0, 0);
-                }
+                for (int ct = 0; ct < kCT; ++ct) x[ct] = operand(in_tile, kPitch, 16 * (kCT * wave + ct), 4);
+#pragma unroll
+                for (int rt = 0; rt < kRT; ++rt)
+                    if (rb + 16 * rt < rank)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const bf16x8 f = operand(s_tile, kSPitch, 32 * rt + 4 * h, 8);
+#pragma unroll
+                            for (int ct = 0; ct < kCT; ++ct) {
+                                if constexpr (second) acc[ct][rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[ct], f, acc[ct][rt], 0, 0, 0);
+                                else acc[ct][rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, x[ct], acc[ct][rt], 0, 0, 0);
+                            }
+                        }
             }
         }
-        __syncthreads();   // before the next pass writes buffer 0 again
+        if (rb + 16 * kRT < rank) __syncthreads();   // before the next pass writes the tiles again
         // lane holds column i16 and rows 4 g + e of its accumulators: rows are columns of dy (dB) or ranks (dA)
 #pragma unroll
-        for (int rt = 0; rt < kRT; ++rt) {
-            const int r = rb + 16 * rt + (second ? i16 : 4 * g);
-            const int64_t c = c0 + 16 * wave + (second ? 4 * g : i16);
-            if (r >= rank || c >= C) continue;
-            const int64_t left = second ? C - c : rank - r;
-            uint16_t* to = second ? out + (int64_t)r * C + c : out + c * rank + r;
-            uint16_t e[4];
+        for (int ct = 0; ct < kCT; ++ct)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) e[i] = f32_to_bf16_rne(acc[rt][i]);
-            if (left >= 4) {
-                *reinterpret_cast<AnyUint2*>(to) = u32x2_t{e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16};
-            } else {
+            for (int rt = 0; rt < kRT; ++rt) {
+                const int r = rb + 16 * rt + (second ? i16 : 4 * g), c = c0 + 16 * (kCT * wave + ct) + (second ? 4 * g : i16);
+                if (r >= rank || c >= C) continue;
+                const int left = second ? C - c : rank - r;
+                uint16_t* to = second ? out + (int64_t)r * C + c : out + (int64_t)c * rank + r;
+                uint16_t e[4];
 #pragma unroll
-                for (int i = 0; i < 3; ++i)
-                    if (i < left) to[i] = e[i];
+                for (int i = 0; i < 4; ++i) e[i] = f32_to_bf16_rne(acc[ct][rt][i]);
+                if (left >= 4) {
+                    *reinterpret_cast<AnyUint2*>(to) = u32x2_t{e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16};
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 3; ++i)
+                        if (i < left) to[i] = e[i];
+                }
             }
-        }
     }
+}
+
+template <int kRT, int kCols, bool kWhole>
+__global__ __launch_bounds__(256, 3) void outer_kernel(OuterArgs a) {
+    __shared__ __align__(16) OuterLds<kRT, kCols> lds;
+    if ((int)blockIdx.x < a.blocks0) outer_tile<kRT, kCols, kWhole, false>(a, lds.in_tile, lds.s_tile);
+    else outer_tile<kRT, kCols, kWhole, true>(a, lds.in_tile, lds.s_tile);
 }
 
 // ---- host
@@ -514,9 +695,9 @@ namespace {
 
 size_t padded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 
-// Slices of a contraction of C columns: workgroups enough for the chip, two steps of 32 columns a wave at least (one where tokens are few).
+// Slices of a contraction of C columns: `want` workgroups, each of steps_least steps of 64 columns at least.
 int slices_of(int64_t C, int64_t tiles, int64_t want, int64_t steps_least) {
-    const int64_t steps = (C + 31) / 32;
+    const int64_t steps = (C + 63) / 64;
     int64_t s = (want + tiles - 1) / tiles;
     if (s > steps / steps_least) s = steps / steps_least;
     if (s > 32) s = 32;
@@ -536,26 +717,53 @@ void launch_order(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p) {
                        reinterpret_cast<int32_t*>(w + p.order), reinterpret_cast<int32_t*>(w + p.starts), reinterpret_cast<int32_t*>(w + p.counts));
 }
 
+template <typename Run>
+void with_whole(bool whole, Run run) {   // rows of whole vectors
+    if (whole) run(std::true_type());
+    else run(std::false_type());
+}
+
 void launch_narrow(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p, bool x_too, bool dy_too) {
     char* w = static_cast<char*>(a.workspace);
     NarrowArgs n{tokens_of(a, p), {a.x, a.dy}, {a.K, a.N}, {reinterpret_cast<float*>(w + p.part_x), reinterpret_cast<float*>(w + p.part_dy)},
                  {x_too ? p.slices_x : 0, dy_too ? p.slices_dy : 0}, p.t_rows, p.rpad};
     const dim3 grid((unsigned)p.tiles, (unsigned)(n.slices[0] + n.slices[1]));
     const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, a.stream, n); };
-    if (p.direct) p.rpad <= 16 ? run(narrow_kernel<true, 1, 1>) : p.rpad <= 32 ? run(narrow_kernel<true, 1, 2>) : run(narrow_kernel<true, 1, 4>);
-    else p.rpad <= 16 ? run(narrow_kernel<false, 4, 1>) : p.rpad <= 32 ? run(narrow_kernel<false, 4, 2>) : run(narrow_kernel<false, 4, 4>);
+    with_whole((!x_too || a.K % 8 == 0) && (!dy_too || a.N % 8 == 0), [&](auto whole) {
+        constexpr bool kWhole = decltype(whole)::value;
+        if (p.direct) p.rpad <= 16 ? run(narrow_kernel<true, 1, 1, kWhole>) : p.rpad <= 32 ? run(narrow_kernel<true, 1, 2, kWhole>) : run(narrow_kernel<true, 1, 4, kWhole>);
+        else p.rpad <= 16 ? run(narrow_kernel<false, 4, 1, kWhole>) : p.rpad <= 32 ? run(narrow_kernel<false, 4, 2, kWhole>) : run(narrow_kernel<false, 4, 4, kWhole>);
+    });
 }
 
 template <bool kFactorA>
-void launch_wide(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p, const float* part, const uint16_t* t, int slices, int64_t C) {
+void launch_wide(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p, const float* part, const uint4* t, int slices, int64_t C) {
     int64_t per_group = 256;
     while (p.tiles * ((C + 2 * per_group - 1) / (2 * per_group)) >= 1024) per_group *= 2;
     const WideArgs w{tokens_of(a, p), part, t, slices, p.t_rows, p.rpad, C, per_group, a.base, a.out};
     const dim3 grid((unsigned)p.tiles, (unsigned)((C + per_group - 1) / per_group));
     const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, a.stream, w); };
-    if constexpr (!kFactorA)
-        if (p.direct) return p.rpad <= 64 ? run(wide_kernel<true, 1, 64, false>) : run(wide_kernel<true, 1, 256, false>);
-    p.rpad <= 64 ? run(wide_kernel<false, 4, 64, kFactorA>) : run(wide_kernel<false, 4, 256, kFactorA>);
+    with_whole(C % 8 == 0, [&](auto whole) {
+        constexpr bool kWhole = decltype(whole)::value;
+        if constexpr (!kFactorA)
+            if (p.direct) {
+                p.rpad <= 32 ? run(wide_kernel<true, 1, 32, false, kWhole>) : p.rpad <= 64 ? run(wide_kernel<true, 1, 64, false, kWhole>) : run(wide_kernel<true, 1, 256, false, kWhole>);
+                return;
+            }
+        p.rpad <= 32 ? run(wide_kernel<false, 4, 32, kFactorA, kWhole>) : p.rpad <= 64 ? run(wide_kernel<false, 4, 64, kFactorA, kWhole>) : run(wide_kernel<false, 4, 256, kFactorA, kWhole>);
+    });
+}
+
+template <int kCols>
+void launch_outer(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p, const uint4* t_x, const uint4* t_dy) {
+    const int blocks0 = (int)((a.K + kCols - 1) / kCols), blocks1 = (int)((a.N + kCols - 1) / kCols);
+    const OuterArgs o{tokens_of(a, p), {a.x, a.dy}, {t_dy, t_x}, {a.K, a.N}, p.rpad, blocks0};
+    const dim3 grid((unsigned)(blocks0 + blocks1), (unsigned)a.n);
+    const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, a.stream, o); };
+    with_whole(a.K % 8 == 0 && a.N % 8 == 0, [&](auto whole) {
+        constexpr bool kWhole = decltype(whole)::value;
+        p.rpad <= 16 ? run(outer_kernel<1, kCols, kWhole>) : p.rpad <= 32 ? run(outer_kernel<2, kCols, kWhole>) : run(outer_kernel<4, kCols, kWhole>);
+    });
 }
 
 }  // namespace
@@ -570,8 +778,10 @@ RequestAdaptersPlan request_adapters_plan(int64_t T, int64_t K, int64_t N, int64
     p.rpad = (int)((max_rank + 15) / 16 * 16);
     if (p.rpad == 0) p.rpad = 16;
     const int64_t live = p.direct ? (n < T ? n : T) : (T + kTileTokens - 1) / kTileTokens + groups / 2;   // tiles to expect
-    p.slices_x = slices_of(K, live > 0 ? live : 1, p.direct ? 512 : 768, p.direct ? 4 : 8);
-    p.slices_dy = slices_of(N, live > 0 ? live : 1, p.direct ? 512 : 768, p.direct ? 4 : 8);
+    // of the backward pass' two products each has its share of the workgroups; few tokens: a step a wave will do
+    const int64_t want = p.direct ? 512 : 768, both = backward ? K + N : K;
+    p.slices_x = slices_of(K, live > 0 ? live : 1, want * K / both, p.direct ? 4 : 8);
+    p.slices_dy = slices_of(N, live > 0 ? live : 1, want * N / both, p.direct ? 4 : 8);
     size_t at = 0;
     const auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -587,8 +797,8 @@ RequestAdaptersPlan request_adapters_plan(int64_t T, int64_t K, int64_t N, int64
     if (!backward || want_dadb) p.part_x = take(row * 4 * p.slices_x);
     if (backward) {
         p.part_dy = take(row * 4 * p.slices_dy);
-        if (want_dadb) p.t_x = take(row * 2);
-        p.t_dy = take(row * 2);
+        if (want_dadb) p.t_x = take(row * 4);
+        p.t_dy = take(row * 4);
     }
     p.bytes = at;
     return p;
@@ -603,7 +813,7 @@ hipError_t launch_request_adapters(const RequestAdaptersArgs& a, const RequestAd
 
 hipError_t launch_request_adapters_backward(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p) {
     char* w = static_cast<char*>(a.workspace);
-    uint16_t *t_x = reinterpret_cast<uint16_t*>(w + p.t_x), *t_dy = reinterpret_cast<uint16_t*>(w + p.t_dy);
+    uint4 *t_x = reinterpret_cast<uint4*>(w + p.t_x), *t_dy = reinterpret_cast<uint4*>(w + p.t_dy);
     launch_order(a, p);
     if (a.T > 0) {
         launch_narrow(a, p, a.want_dadb, true);
@@ -612,11 +822,8 @@ hipError_t launch_request_adapters_backward(const RequestAdaptersArgs& a, const 
         if (a.out != nullptr) launch_wide<true>(a, p, nullptr, t_dy, 0, a.K);
     }
     if (a.want_dadb) {
-        const int blocks0 = (int)((a.K + 63) / 64), blocks1 = (int)((a.N + 63) / 64);
-        const OuterArgs o{tokens_of(a, p), {a.x, a.dy}, {t_dy, t_x}, {a.K, a.N}, p.rpad, blocks0};
-        const dim3 grid((unsigned)(blocks0 + blocks1), (unsigned)a.n);
-        const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, a.stream, o); };
-        p.rpad <= 16 ? run(outer_kernel<1>) : p.rpad <= 32 ? run(outer_kernel<2>) : run(outer_kernel<4>);
+        if ((a.K + a.N) / 128 * a.n >= 512) launch_outer<128>(a, p, t_x, t_dy);
+        else launch_outer<64>(a, p, t_x, t_dy);
     }
     return hipGetLastError();
 }

@@ -3,6 +3,7 @@ import numpy as np
 import torch
 
 U = 2.0 ** -24
+HALVES = 2.0 ** -16   # 2^-8 of 2^-8, of a value held as two bf16
 
 
 def half(dtype):
@@ -75,7 +76,8 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dsum):
 
 
 def adapters(x, ids, a, b, base):
-    """(y, tolerance before the last rounding): x A is summed in fp32 (K additions at most) and rounded to bf16, then r more."""
+    """(y, tolerance before the last rounding): x A is summed in fp32 (K additions at most) and taken as two bf16 values, the second within half a
+    step of what the first leaves; then 2 r additions more."""
     T, N = x.shape[0], b[0].shape[1]
     y = torch.zeros(T, N, dtype=torch.float64) if base is None else base.double().clone()
     size, tol = y.abs().clone(), torch.zeros_like(y)
@@ -85,10 +87,10 @@ def adapters(x, ids, a, b, base):
             continue
         xd, ad, bd = x[rows].double(), a[i].double(), b[i].double()
         t = xd @ ad
-        off = half(torch.bfloat16) * t.abs() * 1.01 + (ad.shape[0] + 40) * U * (xd.abs() @ ad.abs())
+        off = HALVES * t.abs() * 1.01 + (ad.shape[0] + 40) * U * (xd.abs() @ ad.abs())
         y[rows] += t @ bd
         size[rows] += t.abs() @ bd.abs()
-        tol[rows] += off @ bd.abs() + (ad.shape[1] + 2) * U * (1.01 * t.abs() @ bd.abs())
+        tol[rows] += off @ bd.abs() + (2 * ad.shape[1] + 2) * U * (1.01 * t.abs() @ bd.abs())
     y[ids >= len(a)] = float("nan")
     return y, tol + 2 * U * size
 
@@ -102,9 +104,9 @@ def adapters_backward(dy, x, ids, a, b, dx_base):
         rows = torch.nonzero(ids == i)[:, 0]
         xd, dyd, ad, bd = x[rows].double(), dy[rows].double(), a[i].double(), b[i].double()
         dt, t = dyd @ bd.t(), xd @ ad
-        off_dt = half(torch.bfloat16) * 1.01 * dt.abs() + (bd.shape[1] + 40) * U * (dyd.abs() @ bd.abs().t())
-        off_t = half(torch.bfloat16) * 1.01 * t.abs() + (ad.shape[0] + 40) * U * (xd.abs() @ ad.abs())
-        n = (len(rows) + 2) * U * 1.01
+        off_dt = HALVES * 1.01 * dt.abs() + (bd.shape[1] + 40) * U * (dyd.abs() @ bd.abs().t())
+        off_t = HALVES * 1.01 * t.abs() + (ad.shape[0] + 40) * U * (xd.abs() @ ad.abs())
+        n = (2 * len(rows) + 2) * U * 1.01
         da.append((xd.t() @ dt, xd.abs().t() @ (off_dt + n * dt.abs())))
         db.append((t.t() @ dyd, (off_t + n * t.abs()).t() @ dyd.abs()))
     return (dx, tol), da, db

@@ -116,7 +116,7 @@ def test_adapters_arguments(salr):
     for bad in sizes + (dict(list=None), dict(x=None), dict(ids=None), dict(dy=None), dict(ws=None), dict(list=at(0, 4)), dict(dy=at(3, 1)), dict(dx_base=at(4, 1)),
                         dict(dx=at(5, 1)), dict(dx=at(4, 2)), dict(dx=at(1)), dict(dx=at(3, -2)), dict(dx=at(2))):
         assert _grad(salr, **bad) == salr.SALR_ERR_INVALID_ARG, bad
-    for size in (dict(T=1 << 28), dict(K=(1 << 22) + 1), dict(N=(1 << 22) + 1), dict(n=65534)):
+    for size in (dict(T=1 << 28), dict(K=(1 << 22) + 1), dict(N=(1 << 22) + 1), dict(n=65534), dict(K=7), dict(N=7), dict(K=0), dict(N=0)):
         assert _add(salr, **size) == salr.SALR_ERR_SHAPE and _grad(salr, **size) == salr.SALR_ERR_SHAPE, size
     for T in (8, 300):
         need = salr.salr_adapters_add_workspace_bytes(T, 64, 96, 3, 16)
@@ -125,5 +125,5 @@ def test_adapters_arguments(salr):
         assert need > salr.salr_adapters_backward_workspace_bytes(T, 64, 96, 3, 16, False) > 0
         assert _grad(salr, T=T, bytes=need - 1) == salr.SALR_ERR_CAPACITY
     assert salr.salr_adapters_add_workspace_bytes(8, 64, 96, 0, 16) == 0 and salr.salr_adapters_backward_workspace_bytes(1 << 28, 64, 96, 1, 16, True) == 0
-    assert _add(salr, T=0, x=None) == salr.SALR_OK and _add(salr, N=0, y=None) == salr.SALR_OK
+    assert _add(salr, T=0, x=None) == salr.SALR_OK
     assert _grad(salr, want=0, dx=None, dy=None) == salr.SALR_OK and _grad(salr, want=0, T=0, dy=None) == salr.SALR_OK

@@ -49,7 +49,7 @@ def _set(salr, s, train=False):
     return salr.AdapterSet(a, b, *([[torch.full_like(t, 9.0) for t in l] for l in (a, b)] if train else []))
 
 
-SIZES = [(1, 64, 96), (1, 4096, 4096), (2, 33, 1), (5, 1, 65), (16, 512, 256), (17, 2720, 2731), (63, 100, 517), (64, 1030, 1024), (65, 64, 64), (130, 261, 300),
+SIZES = [(1, 64, 96), (1, 4096, 4096), (2, 33, 8), (5, 8, 65), (3, 9, 11), (16, 512, 256), (17, 2720, 2731), (63, 100, 517), (64, 1030, 1024), (65, 64, 64), (130, 261, 300),
          (300, 2720, 2731), (1000, 96, 4099), (700, 1600, 40)]
 
 
@@ -266,7 +266,7 @@ def test_streams(salr):
 
 def test_far_rows(salr):
     """Rows behind 2^31 elements."""
-    T, K, N = 600_000, 4, 4100
+    T, K, N = 600_000, 8, 4100
     a, b = [torch.randn(K, 2, device=dev()).bfloat16()], [torch.randn(2, N, device=dev()).bfloat16()]
     x = torch.randn(T, K, device=dev()).bfloat16()
     ids = torch.full((T,), -1, dtype=torch.int32, device=dev())
@@ -323,6 +323,8 @@ def test_refusals(salr):
     g = torch.empty_like(a[0])
     with pytest.raises(ValueError):
         salr.AdapterSet([a[0], a[0]], [b[0], b[0]], [g, g])
+    with pytest.raises(salr.SalrError):   # fewer than eight features
+        salr.AdapterSet([a[0][:7].contiguous()], [b[0]])
     with pytest.raises(salr.SalrError):   # a rank above 256
         salr.AdapterSet([torch.zeros(64, 257, dtype=torch.bfloat16, device=dev())], [torch.zeros(257, 64, dtype=torch.bfloat16, device=dev())])
     square = salr.AdapterSet([torch.zeros(64, 4, dtype=torch.bfloat16, device=dev())], [torch.zeros(4, 64, dtype=torch.bfloat16, device=dev())])
