@@ -606,7 +606,7 @@ typedef struct {
 /*
  * salr_adapter_list_check -- whether the n records of a HOST array can be used; *max_rank gets the largest rank, which the calls want to know.  No
  * gradient may overlap another tensor of the list (not checked here).
- * Errors: INVALID_ARG (null where data is required, n or a rank negative, a pointer that is not 16-byte aligned), SHAPE (n > 65533),
+ * Errors: INVALID_ARG (null where data is required, n or a rank negative, a pointer that is not 16-byte aligned), SHAPE (n > 4096),
  * UNSUPPORTED (a rank above 256).
  */
 salr_status_t salr_adapter_list_check(const salr_adapter_t* adapters, int64_t n, int64_t* max_rank);

@@ -914,15 +914,16 @@ hipError_t launch_layer_norm(const LayerNormArgs& a, hipStream_t stream);
 hipError_t launch_layer_norm_backward(const LayerNormGradArgs& a, void* dw, void* db, hipStream_t stream);
 
 // ---- Adapters of many requests (salr_request_adapters.hip)
-constexpr int64_t kAdaptersMostT = ((int64_t)1 << 28) - 1, kAdaptersMostColumns = (int64_t)1 << 22, kAdaptersMostCount = 65533;
+constexpr int64_t kAdaptersMostT = ((int64_t)1 << 28) - 1, kAdaptersMostColumns = (int64_t)1 << 22, kAdaptersMostCount = 4096;
 constexpr int64_t kAdaptersLeastColumns = 8;   // one vector
 struct RequestAdaptersPlan {
     bool direct;             // few tokens: a workgroup finds its own among the ids; else a launch in front orders them
     int64_t rows, tiles;     // tokens of a tile, tiles of the launches
+    int64_t live;            // of which so many are expected to hold tokens
     int64_t t_rows;          // rows of the products with the first factor
     int rpad;                // their columns
     int slices_x, slices_dy; // slices of K and N that they are summed over
-    size_t order, starts, counts, part_x, part_dy, t_x, t_dy;   // offsets in the workspace
+    size_t order, starts, counts, table, part_x, part_dy, t_x, t_dy;   // offsets in the workspace
     size_t bytes;
 };
 RequestAdaptersPlan request_adapters_plan(int64_t T, int64_t K, int64_t N, int64_t n, int64_t max_rank, bool backward, bool want_dadb);

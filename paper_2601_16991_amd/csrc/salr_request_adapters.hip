@@ -6,8 +6,7 @@
 // Tokens of one adapter are brought together into tiles, whose rows are read and written where they are: nothing is copied.
 //   up to kDirectTokens tokens   a workgroup is a token, finds its fellows among the ids by one comparison across the wave, and goes on if it
 //                                is the first of a tile of 16
-//   more                         a launch in front orders the tokens by adapter (stable: sums over tokens have an order); a workgroup finds the
-//                                adapter of its tile of 64 in the counts
+//   more                         a launch in front orders the tokens by adapter (stable: sums over tokens have an order) and writes a table of tiles of 64
 // Then  narrow_kernel  t = in * factor (K or N columns down to r; fp32 sums over slices of the columns),
 //       wide_kernel    out = base + t * factor (r up to N or K columns),
 //       outer_kernel   the adapters' gradients, sums over tokens.
@@ -47,6 +46,7 @@ struct Tokens {   // how a kernel finds its rows
     const int32_t* order;    // tokens by group: adapters, then those without one, then those whose id is none
     const int32_t* starts;   // [n + 2]
     const int32_t* counts;   // [n + 2]
+    const int4* tiles;       // group (-1: none), live rows, place of the first in `order`, 0
     int T, n;
 };
 
@@ -59,13 +59,13 @@ struct Tile {
     int first;   // of an ordered launch: position of the first
 };
 
-// The tile of this workgroup and, in rows[kRows] (LDS), its tokens, -1 behind the last.  Every thread calls it; ends with a barrier.
+// Tile `self` and, in rows[kRows] (LDS), its tokens, -1 behind the last.  Every thread calls it; ends with a barrier.
 template <bool kDirect, int kRows>
-__device__ __forceinline__ Tile find_tile(const Tokens& k, int* rows) {
+__device__ __forceinline__ Tile find_tile(const Tokens& k, int self, int* rows) {
     const int lane = lane_id();
     Tile tile{-1, 0, 0};
     if constexpr (kDirect) {
-        const int self = blockIdx.x, group = lane < k.T ? group_of(k.ids[lane], k.n) : -2;
+        const int group = lane < k.T ? group_of(k.ids[lane], k.n) : -2;
         const int mine = __builtin_amdgcn_readlane(group, self);
         const uint64_t same = __ballot(group == mine), below = same & (((uint64_t)1 << self) - 1);
         const int before = __popcll(below);
@@ -77,22 +77,8 @@ __device__ __forceinline__ Tile find_tile(const Tokens& k, int* rows) {
         __syncthreads();
         if (threadIdx.x < kWave && group == mine && place >= 0 && place < kRows) rows[place] = lane;
     } else {
-        int before = 0;   // tiles of the groups already looked at
-        for (int g0 = 0; g0 < k.n + 2; g0 += kWave) {
-            const int count = g0 + lane < k.n + 2 ? k.counts[g0 + lane] : 0;
-            const int tiles = (count + kRows - 1) / kRows, upto = before + (int)wave_inclusive_scan((uint32_t)tiles);
-            const uint64_t past = __ballot(upto > (int)blockIdx.x);
-            if (past != 0) {
-                const int at = __builtin_ctzll(past);
-                const int done = kRows * ((int)blockIdx.x - __builtin_amdgcn_readlane(upto - tiles, at));
-                const int left = __builtin_amdgcn_readlane(count, at) - done;
-                tile.group = g0 + at;
-                tile.count = left < kRows ? left : kRows;
-                tile.first = k.starts[tile.group] + done;
-                break;
-            }
-            before = __builtin_amdgcn_readlane(upto, kWave - 1);
-        }
+        const int4 t = k.tiles[self];
+        tile = Tile{t.x, t.y, t.z};
         if (tile.group < 0) return tile;
         if (threadIdx.x < kRows) rows[threadIdx.x] = (int)threadIdx.x < tile.count ? k.order[tile.first + threadIdx.x] : -1;
     }
@@ -176,8 +162,10 @@ __device__ __forceinline__ uint4 two_halves(f32x4 v) {
 
 // A workgroup a group: counts the tokens of the groups before its own, then puts its own in order.  Every group goes through all ids, which
 // stay in the caches; no workgroup waits for another.  A thread takes eight ids side by side, so that up to 8192 tokens are read once.
+// Group g, whose tokens start at place s, has the entries s / 64 + g and on of the table of tiles, up to the next group's, which are enough for its tiles
+// whatever s: so nobody has to know how many tiles the groups before have.  What is left over is marked as empty.
 constexpr int kOrderEach = 8;
-__global__ __launch_bounds__(1024) void order_tokens_kernel(const int32_t* ids, int T, int n, int32_t* order, int32_t* starts, int32_t* counts) {
+__global__ __launch_bounds__(1024) void order_tokens_kernel(const int32_t* ids, int T, int n, int32_t* order, int32_t* starts, int32_t* counts, int4* tiles) {
     __shared__ uint32_t scratch[17];
     __shared__ int total[2][16];
     const int group = blockIdx.x, wave = threadIdx.x >> 6;
@@ -186,10 +174,15 @@ __global__ __launch_bounds__(1024) void order_tokens_kernel(const int32_t* ids, 
     const auto look = [&](int64_t t0) {
         mine = 0;
         int g[kOrderEach];
+        typedef int Four __attribute__((ext_vector_type(4), aligned(4)));
+        const int64_t t = t0 + kOrderEach * threadIdx.x;
+        if (t + kOrderEach <= T) {
+            const Four lo = reinterpret_cast<const Four*>(ids + t)[0], hi = reinterpret_cast<const Four*>(ids + t)[1];
 #pragma unroll
-        for (int j = 0; j < kOrderEach; ++j) {
-            const int64_t t = t0 + kOrderEach * threadIdx.x + j;
-            g[j] = t < T ? group_of(ids[t], n) : 2147483647;
+            for (int j = 0; j < kOrderEach; ++j) g[j] = group_of(j < 4 ? lo[j] : hi[j - 4], n);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kOrderEach; ++j) g[j] = t + j < T ? group_of(ids[t + j], n) : 2147483647;
         }
 #pragma unroll
         for (int j = 0; j < kOrderEach; ++j) {
@@ -216,6 +209,11 @@ __global__ __launch_bounds__(1024) void order_tokens_kernel(const int32_t* ids, 
         starts[group] = at;
         counts[group] = count;
     }
+    const int entry = at / kTileTokens + group, entries = (at + count) / kTileTokens + group + 1 - entry;
+    for (int i = threadIdx.x; i < entries; i += 1024) {
+        const int left = count - kTileTokens * i;
+        tiles[entry + i] = make_int4(left > 0 ? group : -1, left < kTileTokens ? left : kTileTokens, at + kTileTokens * i, 0);
+    }
     if (count == 0) return;
     for (int64_t t0 = 0; t0 < T; t0 += 1024 * kOrderEach) {
         if (T > 1024 * kOrderEach) look(t0);
@@ -236,22 +234,29 @@ struct NarrowArgs {
     int rpad;
 };
 
-// part[z][row][r] = sum over the columns c of slice z of in[row][c] * factor(c, r).  Workgroup (tile, slice); its four waves take every fourth step
-// of 64 columns, with 16 kMB rows and 16 kRT ranks each (more ranks: another pass), and are added through LDS, in order.  in's rows are the A
-// operand of 16x16x32 MFMAs as they lie; A's [64 columns, ranks], which lie the wrong way round, go through LDS and its transposing
-// read, B's [ranks, columns] are the B operand as they lie.  A step's requests are out while the one before is multiplied.
+// part[z][row][r] = sum over the columns c of slice z of in[row][c] * factor(c, r).  A workgroup has a slice of a tile and goes through it by steps of 128
+// columns: rows of in and the factor's part come in by whole lines, four rows of 256 bytes a request, and through LDS (as MFMA operands straight from memory,
+// 16 rows of 64 bytes a request, they kept the address unit busy for 84 cycles a request instead of 23: 4096 tokens, 18432 columns, rank 32
+// 51 us).  The requests of two steps are out while one is multiplied.  16x16x32 MFMAs with in as A operand; A's [128 columns, ranks], which lie
+// the wrong way round, are read transposed.  Tiles of 64 rows: a wave has 16 of them; of 16 rows: each has 32 columns of a step, and their sums meet in LDS, in
+// order.  16 kRT ranks a pass.
 template <int kMB, int kRT>
 struct NarrowLds {
-    static constexpr int kPitch = 16 * kRT + 8, kSumPitch = 16 * kRT + 4, kStage = 64 * kPitch;
-    static constexpr int kSumBytes = 16 * kMB * kSumPitch * 4, kStageBytes = 4 * kStage * 2, kBytes = kSumBytes > kStageBytes ? kSumBytes : kStageBytes;
+    static constexpr int kCols = 128, kPitch = kCols + 8, kRankPitch = 16 * kRT + 8, kSumPitch = 16 * kRT + 4;
+    static constexpr int kIn = 16 * kMB * kPitch, kFactor = 16 * kRT * kPitch > kCols * kRankPitch ? 16 * kRT * kPitch : kCols * kRankPitch;
+    static constexpr int kSums = kMB == 1 ? 4 * 16 * kSumPitch : 1;
+    uint16_t in[kIn], factor[kFactor];
+    float sums[kSums];
+    int rows[16 * kMB];
 };
 
 template <bool kDirect, int kMB, int kRT, bool kWhole, bool second>   // second: dy with B
-__device__ __forceinline__ void narrow_tile(const NarrowArgs& a, const Tile& tile, const int* rows, char* lds) {
+__device__ __forceinline__ void narrow_tile(const NarrowArgs& a, const Tile& tile, int z, NarrowLds<kMB, kRT>& lds) {
     typedef NarrowLds<kMB, kRT> Lds;
-    constexpr int kPitch = Lds::kPitch, kSumPitch = Lds::kSumPitch, kStage = Lds::kStage;
+    constexpr int kPitch = Lds::kPitch, kRankPitch = Lds::kRankPitch, kSumPitch = Lds::kSumPitch, kParts = kMB == 1 ? 1 : 4;
+    static_assert(kMB == 1 || kMB == 4, "a block of rows for each wave, or one for all");
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i16 = lane & 15, g = lane >> 4;
-    const int z = second ? (int)blockIdx.y - a.slices[0] : (int)blockIdx.y, slices = second ? a.slices[1] : a.slices[0];
+    const int slices = second ? a.slices[1] : a.slices[0];
     const uint16_t* in = second ? a.in[1] : a.in[0];
     const int C = (int)(second ? a.C[1] : a.C[0]);
     const int64_t in_total = (int64_t)a.tokens.T * C;
@@ -260,113 +265,115 @@ __device__ __forceinline__ void narrow_tile(const NarrowArgs& a, const Tile& til
     const int rank = (int)adapter.rank;
     const uint16_t* factor = second ? adapter.b : adapter.a;
     const int64_t factor_total = (int64_t)rank * C;
-    const int steps = (C + 63) >> 6, s_begin = (int)((int64_t)steps * z / slices), s_end = (int)((int64_t)steps * (z + 1) / slices);
+    const int steps = (C + Lds::kCols - 1) / Lds::kCols, s_begin = (int)((int64_t)steps * z / slices), s_end = (int)((int64_t)steps * (z + 1) / slices);
+    const int vrow = threadIdx.x >> 4, vcol = 8 * (threadIdx.x & 15);
     int64_t row[kMB];   // (behind the last token the first one's: what comes of it is not stored)
 #pragma unroll
-    for (int mb = 0; mb < kMB; ++mb) row[mb] = (int64_t)rows[16 * mb + i16 < tile.count ? 16 * mb + i16 : 0] * C;
-    uint16_t* stage = reinterpret_cast<uint16_t*>(lds) + wave * kStage;
-    float* sums = reinterpret_cast<float*>(lds);
+    for (int i = 0; i < kMB; ++i) row[i] = (int64_t)lds.rows[16 * i + vrow < tile.count ? 16 * i + vrow : 0] * C;
     for (int rb = 0; rb < rank; rb += 16 * kRT) {
         const int rts = (rank - rb + 15) / 16 < kRT ? (rank - rb + 15) / 16 : kRT;
-        f32x4 acc[kMB][kRT] = {};
-        uint4 xq[2][kMB], fq[2][kRT];
-        const auto request = [&](int s) {
-            const int c = 64 * s;
+        f32x4 acc[kRT] = {};
+        struct Step {
+            uint4 x[kMB], f[kRT];
+        } ahead[2];
+        const auto request = [&](Step& q, int s) {
+            const int c = Lds::kCols * s;
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
+            for (int i = 0; i < kMB; ++i) q.x[i] = raw_eight<kWhole>(in, row[i], c + vcol, C, in_total);
 #pragma unroll
-                for (int mb = 0; mb < kMB; ++mb) xq[u][mb] = raw_eight<kWhole>(in, row[mb], c + 32 * u + 8 * g, C, in_total);
-#pragma unroll
-                for (int rt = 0; rt < kRT; ++rt) {
-                    if constexpr (second) {   // (behind the last rank its values again: what comes of them is dropped)
-                        const int r = rb + 16 * rt + i16;
-                        fq[u][rt] = raw_eight<kWhole>(factor, (int64_t)(r < rank ? r : rank - 1) * C, c + 32 * u + 8 * g, C, factor_total);
-                    } else {                  // vector v of [64][16 kRT]
-                        const int v = lane + 64 * (kRT * u + rt), k = c + v / (2 * kRT);
-                        fq[u][rt] = raw_ranks(factor, k < C ? k : C - 1, rb + 8 * (v % (2 * kRT)), rank, factor_total);
-                    }
+            for (int i = 0; i < kRT; ++i) {
+                if constexpr (second) {   // (behind the last rank its values again: what comes of them is dropped)
+                    const int r = rb + 16 * i + vrow;
+                    q.f[i] = raw_eight<kWhole>(factor, (int64_t)(r < rank ? r : rank - 1) * C, c + vcol, C, factor_total);
+                } else {                  // vector v of [128][16 kRT]
+                    const int v = threadIdx.x + 256 * i, k = c + v / (2 * kRT);
+                    q.f[i] = raw_ranks(factor, k < C ? k : C - 1, rb + 8 * (v % (2 * kRT)), rank, factor_total);
                 }
             }
         };
-        if (s_begin + wave < s_end) request(s_begin + wave);
-        for (int s = s_begin + wave; s < s_end; s += 4) {
-            bf16x8 x[2][kMB], f[2][kRT];
+        const auto step = [&](Step& q, int s) {
+            const int c = Lds::kCols * s;
+            if (s > s_begin) __syncthreads();   // the step before has been multiplied by every wave
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int i = 0; i < kMB; ++i) *reinterpret_cast<uint4*>(lds.in + (16 * i + vrow) * kPitch + vcol) = true_eight<kWhole>(q.x[i], row[i], c + vcol, C, in_total);
 #pragma unroll
-                for (int mb = 0; mb < kMB; ++mb) x[u][mb] = as_bf16x8(true_eight<kWhole>(xq[u][mb], row[mb], 64 * s + 32 * u + 8 * g, C, in_total));
-            if constexpr (second) {
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int rt = 0; rt < kRT; ++rt) {
-                        const int r = rb + 16 * rt + i16;
-                        f[u][rt] = as_bf16x8(true_eight<kWhole>(fq[u][rt], (int64_t)(r < rank ? r : rank - 1) * C, 64 * s + 32 * u + 8 * g, C, factor_total));
-                    }
-            } else {
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int rt = 0; rt < kRT; ++rt) {
-                        const int v = lane + 64 * (kRT * u + rt), k = 64 * s + v / (2 * kRT);
-                        const uint4 q = true_ranks(fq[u][rt], k < C ? k : C - 1, rb + 8 * (v % (2 * kRT)), rank, factor_total);
-                        *reinterpret_cast<uint4*>(stage + v / (2 * kRT) * kPitch + 8 * (v % (2 * kRT))) = k < C ? q : make_uint4(0, 0, 0, 0);
-                    }
-                wave_sync();
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int rt = 0; rt < kRT; ++rt) {
-                        const uint16_t* col = stage + (32 * u + 8 * g + (i16 >> 2)) * kPitch + 16 * rt + 4 * (i16 & 3);
-                        const uint2 lo = lds_read_tr4(col), hi = lds_read_tr4(col + 4 * kPitch);
-                        f[u][rt] = as_bf16x8(make_uint4(lo.x, lo.y, hi.x, hi.y));
-                    }
-                wave_sync();
+            for (int i = 0; i < kRT; ++i) {
+                if constexpr (second) {
+                    const int r = rb + 16 * i + vrow;
+                    *reinterpret_cast<uint4*>(lds.factor + (16 * i + vrow) * kPitch + vcol) =
+                        true_eight<kWhole>(q.f[i], (int64_t)(r < rank ? r : rank - 1) * C, c + vcol, C, factor_total);
+                } else {
+                    const int v = threadIdx.x + 256 * i, k = c + v / (2 * kRT);
+                    const uint4 f = true_ranks(q.f[i], k < C ? k : C - 1, rb + 8 * (v % (2 * kRT)), rank, factor_total);
+                    *reinterpret_cast<uint4*>(lds.factor + v / (2 * kRT) * kRankPitch + 8 * (v % (2 * kRT))) = k < C ? f : make_uint4(0, 0, 0, 0);
+                }
             }
-            if (s + 4 < s_end) request(s + 4);
+            if (s + 2 < s_end) request(q, s + 2);
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < kParts; ++u) {
+                const int block = kMB == 1 ? 0 : wave, col = 32 * (kMB == 1 ? wave : u);
+                const bf16x8 x = as_bf16x8(*reinterpret_cast<const uint4*>(lds.in + (16 * block + i16) * kPitch + col + 8 * g));
+#pragma unroll
+                for (int rt = 0; rt < kRT; ++rt) {
+                    if (rt >= rts) continue;
+                    uint4 f;
+                    if constexpr (second) {
+                        f = *reinterpret_cast<const uint4*>(lds.factor + (16 * rt + i16) * kPitch + col + 8 * g);
+                    } else {
+                        const uint16_t* from = lds.factor + (col + 8 * g + (i16 >> 2)) * kRankPitch + 16 * rt + 4 * (i16 & 3);
+                        const uint2 lo = lds_read_tr4(from), hi = lds_read_tr4(from + 4 * kRankPitch);
+                        f = make_uint4(lo.x, lo.y, hi.x, hi.y);
+                    }
+                    acc[rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, as_bf16x8(f), acc[rt], 0, 0, 0);
+                }
+            }
+        };
+        if (s_begin < s_end) request(ahead[0], s_begin);
+        if (s_begin + 1 < s_end) request(ahead[1], s_begin + 1);
+        for (int s = s_begin; s < s_end; s += 2) {
+            step(ahead[0], s);
+            if (s + 1 < s_end) step(ahead[1], s + 1);
+        }
+        // accumulators: lane holds column i16 (rank), rows 4 g + e (tokens).  Zeros behind the last rank (zero times an infinity of in is none).
+        if constexpr (kMB == 1) {
 #pragma unroll
             for (int rt = 0; rt < kRT; ++rt)
-                if (rt < rts)
 #pragma unroll
-                    for (int u = 0; u < 2; ++u)
-#pragma unroll
-                        for (int mb = 0; mb < kMB; ++mb) acc[mb][rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[u][mb], f[u][rt], acc[mb][rt], 0, 0, 0);
-        }
-        __syncthreads();   // the stages have been read: their place is the sums' now
-        // accumulators: lane holds column i16 (rank), rows 4 g + e (tokens)
-        for (int w = 0; w < 4; ++w) {
-            if (w == wave)
-#pragma unroll
-                for (int mb = 0; mb < kMB; ++mb)
-#pragma unroll
-                    for (int rt = 0; rt < kRT; ++rt)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            float* to = sums + (16 * mb + 4 * g + e) * kSumPitch + 16 * rt + i16;
-                            *to = w == 0 ? acc[mb][rt][e] : *to + acc[mb][rt][e];
-                        }
+                for (int e = 0; e < 4; ++e) lds.sums[(16 * wave + 4 * g + e) * kSumPitch + 16 * rt + i16] = acc[rt][e];
             __syncthreads();
-        }
-        for (int i = threadIdx.x; i < tile.count * rts * 4; i += 256) {
-            const int j = i / (rts * 4), c = 4 * (i % (rts * 4));
-            f32x4 v = *reinterpret_cast<const f32x4*>(sums + j * kSumPitch + c);
+            for (int i = threadIdx.x; i < tile.count * rts * 4; i += 256) {
+                const int j = i / (rts * 4), c = 4 * (i % (rts * 4));
+                f32x4 v = *reinterpret_cast<const f32x4*>(lds.sums + j * kSumPitch + c);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = rb + c + e < rank ? v[e] : 0.f;   // (zero times an infinity of in, where the ranks are padded)
-            *reinterpret_cast<f32x4*>(part + place_of<kDirect>(tile, rows, j) * a.rpad + rb + c) = v;
+                for (int w = 1; w < 4; ++w) v += *reinterpret_cast<const f32x4*>(lds.sums + (16 * w + j) * kSumPitch + c);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = rb + c + e < rank ? v[e] : 0.f;
+                *reinterpret_cast<f32x4*>(part + place_of<kDirect>(tile, lds.rows, j) * a.rpad + rb + c) = v;
+            }
+        } else {
+#pragma unroll
+            for (int rt = 0; rt < kRT; ++rt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int j = 16 * wave + 4 * g + e, r = rb + 16 * rt + i16;
+                    if (rt < rts && j < tile.count) part[place_of<kDirect>(tile, lds.rows, j) * a.rpad + r] = r < rank ? acc[rt][e] : 0.f;
+                }
         }
         __syncthreads();   // before the next pass
     }
 }
 
 template <bool kDirect, int kMB, int kRT, bool kWhole>
-__global__ __launch_bounds__(256, kMB == 1 ? 3 : 2) void narrow_kernel(NarrowArgs a) {
-    __shared__ int rows[16 * kMB];
-    __shared__ __align__(16) char lds[NarrowLds<kMB, kRT>::kBytes];
-    const Tile tile = find_tile<kDirect, 16 * kMB>(a.tokens, rows);
+__global__ __launch_bounds__(256, kRT < 4 ? 4 : 3) void narrow_kernel(NarrowArgs a) {
+    __shared__ __align__(16) NarrowLds<kMB, kRT> lds;
+    // slices side by side, then tiles: workgroups that run at a time read whole rows between them
+    const int slices = a.slices[0] + a.slices[1], slice = blockIdx.x % slices;
+    const Tile tile = find_tile<kDirect, 16 * kMB>(a.tokens, blockIdx.x / slices, lds.rows);
     if (tile.group < 0 || tile.group >= a.tokens.n) return;
-    if constexpr (kDirect) narrow_tile<kDirect, kMB, kRT, kWhole, false>(a, tile, rows, lds);
-    else if ((int)blockIdx.y < a.slices[0]) narrow_tile<kDirect, kMB, kRT, kWhole, false>(a, tile, rows, lds);
-    else narrow_tile<kDirect, kMB, kRT, kWhole, true>(a, tile, rows, lds);
+    if constexpr (kDirect) narrow_tile<kDirect, kMB, kRT, kWhole, false>(a, tile, slice, lds);
+    else if (slice < a.slices[0]) narrow_tile<kDirect, kMB, kRT, kWhole, false>(a, tile, slice, lds);
+    else narrow_tile<kDirect, kMB, kRT, kWhole, true>(a, tile, slice - a.slices[0], lds);
 }
 
 // t = the sum over the slices of part, four values a thread, as two_halves has them; y picks the product.
@@ -396,27 +403,31 @@ struct WideArgs {
     int64_t t_rows;
     int rpad;
     int64_t C;              // columns of out
-    int64_t per_group;      // of a workgroup, whole 256s
+    int per_group;          // of a workgroup, whole 256s
     const uint16_t* base;   // may be out, or null (zeros)
     uint16_t* out;
 };
 
-// out[row][c] = base[row][c] + sum over r of t[row][r] * factor(r, c).  Workgroup (tile, columns): t's rows once into LDS, then each wave takes 64
+// out[row][c] = base[row][c] + sum over r of t[row][r] * factor(r, c).  A workgroup has some columns of a tile: t's rows once into LDS, then each wave takes 64
 // columns at a time, the factor's part of them, zeros where ranks or columns end, through LDS of its own (kPass ranks a pass), the next one's on their
 // way meanwhile.  The product is formed transposed, columns of out as rows of 16x16x32 MFMAs, and which column a row stands for is chosen so that a
-// lane ends up with 16 columns of one token side by side (row m of tile j is column 16 (m / 4) + 4 j + m % 4): out is read and written in
-// whole vectors.  An instruction takes 16 ranks: four of a lane with t's first half and the same four with its second.
+// lane ends up with twice eight columns of one token side by side and four lanes with 64 bytes (row m of tile j is column 32 (j / 2) + 8 (m / 4)
+// + 4 (j % 2) + m % 4): out is read and written in whole vectors.  An instruction takes 16 ranks: four of a lane with t's first half and the same four with its second.
 // kFactorA: the factor is A [C, r] (dx), else B [r, C] (y).
-template <bool kDirect, int kMB, int kMostR, bool kFactorA, bool kWhole>
-__global__ __launch_bounds__(256, kMB == 1 ? 3 : kMostR > 64 ? 1 : 2) void wide_kernel(WideArgs a) {
-    constexpr int kTPitch = 2 * kMostR + 8, kPass = kMostR < 64 ? kMostR : 64, kVectors = kPass / 8, kPitch = kFactorA ? kPass + 8 : 64 + 8;
-    __shared__ int rows[16 * kMB];
-    __shared__ __align__(16) uint16_t t[16 * kMB * kTPitch];
+// kRows: of a tile; of 64, two waves have one half each.
+template <bool kDirect, int kRows, int kMostR, bool kFactorA, bool kWhole>
+__global__ __launch_bounds__(256, kMostR > 64 && kRows > 16 ? 1 : 4) void wide_kernel(WideArgs a) {
+    constexpr int kTPitch = 2 * kMostR + 8, kPass = 32, kVectors = kPass / 8, kPitch = kFactorA ? kPass + 8 : 64 + 8, kOutPitch = 64 + 8;
+    constexpr int kMB = kRows / 16 < 2 ? 1 : 2, kHalves = kRows / 16 / kMB, kStride = 256 / kHalves;   // blocks of rows of a wave, columns of a workgroup's step
+    __shared__ int rows[kRows];
+    __shared__ __align__(16) uint16_t t[kRows * kTPitch];
     __shared__ __align__(16) uint16_t stages[4][(kFactorA ? 64 : kPass) * kPitch];
+    static_assert(16 * kMB * kOutPitch <= (kFactorA ? 64 : kPass) * kPitch, "out goes through the factor's place");
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i16 = lane & 15, g = lane >> 4;
-    const Tile tile = find_tile<kDirect, 16 * kMB>(a.tokens, rows);
+    const int C = (int)a.C, across = (C + a.per_group - 1) / a.per_group;
+    const Tile tile = find_tile<kDirect, kRows>(a.tokens, blockIdx.x / across, rows);
     if (tile.group < 0) return;
-    const int C = (int)a.C, c_begin = (int)(blockIdx.y * a.per_group), c_end = c_begin + a.per_group < C ? (int)(c_begin + a.per_group) : C;
+    const int c_begin = (int)(blockIdx.x % across) * a.per_group, c_end = c_begin + a.per_group < C ? c_begin + a.per_group : C;
     if (tile.group >= a.tokens.n) {   // no adapter: base as it is; an id that is none: NaN
         const bool none = tile.group == a.tokens.n;
         if (none && a.base == a.out) return;
@@ -441,6 +452,7 @@ __global__ __launch_bounds__(256, kMB == 1 ? 3 : kMostR > 64 ? 1 : 2) void wide_
     const auto request = [&](int c0, int rb) {   // the factor's part for 64 columns and kPass ranks
 #pragma unroll
         for (int v = 0; v < kVectors; ++v) {
+            if (!kFactorA && rb + 8 * v >= rank16) continue;   // the same for the workgroup
             if constexpr (kFactorA) {   // vectors of [64 columns][kPass ranks]
                 const int i = lane + 64 * v, k = c0 + i / kVectors;
                 q[v] = raw_ranks(factor, k < C ? k : C - 1, rb + 8 * (i % kVectors), rank, factor_total);
@@ -460,14 +472,29 @@ __global__ __launch_bounds__(256, kMB == 1 ? 3 : kMostR > 64 ? 1 : 2) void wide_
                 *reinterpret_cast<uint4*>(stage + i / kVectors * kPitch + 8 * (i % kVectors)) = rank - r >= 8 ? f : from_place(f, 0, rank - r);
             } else {
                 const int r = rb + 8 * v + (lane >> 3);
+                if (rb + 8 * v >= rank16) continue;   // the same for the workgroup
                 const uint4 f = true_eight<kWhole>(q[v], (int64_t)(r < rank ? r : rank - 1) * C, c0 + 8 * (lane & 7), C, factor_total);
                 *reinterpret_cast<uint4*>(stage + (i >> 3) * kPitch + 8 * (i & 7)) = r < rank ? f : make_uint4(0, 0, 0, 0);
             }
         }
     };
-    int c0 = c_begin + 64 * wave, rb = 0;
-    if (c0 < c_end && rank > 0) request(c0, 0);
-    for (int i = threadIdx.x; i < 16 * kMB * (rank16 / 4); i += 256) {
+    const int64_t out_total = (int64_t)a.tokens.T * C;
+    const int first_row = wave % kHalves * 16 * kMB, vrow = lane >> 3, vcol = 8 * (lane & 7);
+    int64_t row[2 * kMB];   // of the vectors of out that this lane reads and writes, eight rows apart; behind the last token -1
+#pragma unroll
+    for (int i = 0; i < 2 * kMB; ++i) row[i] = rows[first_row + 8 * i + vrow] < 0 ? -1 : (int64_t)rows[first_row + 8 * i + vrow] * C;
+    uint4 base[2 * kMB] = {};
+    const auto request_base = [&](int c0) {   // (behind the last token any row: what comes of it is not stored)
+        if (a.base == nullptr) return;
+#pragma unroll
+        for (int i = 0; i < 2 * kMB; ++i) base[i] = raw_eight<kWhole>(a.base, row[i] < 0 ? 0 : row[i], c0 + vcol, C, out_total);
+    };
+    int c0 = c_begin + 64 * (wave / kHalves), rb = 0;
+    if (c0 < c_end) {
+        request_base(c0);
+        if (rank > 0) request(c0, 0);
+    }
+    for (int i = threadIdx.x; i < kRows * (rank16 / 4); i += 256) {
         const int j = i / (rank16 / 4), r = 4 * (i % (rank16 / 4));
         uint4 h = make_uint4(0, 0, 0, 0);
         if (j < tile.count) {
@@ -485,26 +512,14 @@ __global__ __launch_bounds__(256, kMB == 1 ? 3 : kMostR > 64 ? 1 : 2) void wide_
     }
     __syncthreads();
     uint16_t* stage = stages[wave];
-    const int64_t out_total = (int64_t)a.tokens.T * C;
-    int token[kMB];
-#pragma unroll
-    for (int mb = 0; mb < kMB; ++mb) token[mb] = rows[16 * mb + i16];
     f32x4 acc[kMB][4];
-    Eight<false> base[kMB][2] = {};
+    if (first_row >= tile.count) return;   // (no barrier follows)
     while (c0 < c_end) {
         if (rb == 0) {
 #pragma unroll
-            for (int mb = 0; mb < kMB; ++mb) {
+            for (int mb = 0; mb < kMB; ++mb)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) acc[mb][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-            }
-            if (a.base != nullptr) {
-#pragma unroll
-                for (int mb = 0; mb < kMB; ++mb)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-                        base[mb][h].q[0] = raw_eight<kWhole>(a.base, (int64_t)(token[mb] < 0 ? 0 : token[mb]) * C, c0 + 16 * g + 8 * h, C, out_total);
-            }
         }
         const int steps = (rank - rb + 15) / 16 < kPass / 16 ? (rank - rb + 15) / 16 : kPass / 16;
         if (rank > 0) place(stage, c0, rb);
@@ -513,7 +528,7 @@ __global__ __launch_bounds__(256, kMB == 1 ? 3 : kMostR > 64 ? 1 : 2) void wide_
         rb += kPass;
         if (rb >= rank) {
             rb = 0;
-            c0 += 256;
+            c0 += kStride;
         }
         if (c0 < c_end && rank > 0) request(c0, rb);
 #pragma unroll
@@ -521,12 +536,12 @@ __global__ __launch_bounds__(256, kMB == 1 ? 3 : kMostR > 64 ? 1 : 2) void wide_
             if (st < steps) {
                 uint4 tq[kMB];
 #pragma unroll
-                for (int mb = 0; mb < kMB; ++mb) tq[mb] = *reinterpret_cast<const uint4*>(t + (16 * mb + i16) * kTPitch + 2 * (now + 16 * st + 4 * g));
+                for (int mb = 0; mb < kMB; ++mb) tq[mb] = *reinterpret_cast<const uint4*>(t + (first_row + 16 * mb + i16) * kTPitch + 2 * (now + 16 * st + 4 * g));
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     uint2 f;
-                    if constexpr (kFactorA) f = *reinterpret_cast<const uint2*>(stage + (16 * (i16 >> 2) + 4 * j + (i16 & 3)) * kPitch + 16 * st + 4 * g);
-                    else f = lds_read_tr4(stage + (16 * st + 4 * g + (i16 >> 2)) * kPitch + 16 * (i16 & 3) + 4 * j);
+                    if constexpr (kFactorA) f = *reinterpret_cast<const uint2*>(stage + (32 * (j >> 1) + 8 * (i16 >> 2) + 4 * (j & 1) + (i16 & 3)) * kPitch + 16 * st + 4 * g);
+                    else f = lds_read_tr4(stage + (16 * st + 4 * g + (i16 >> 2)) * kPitch + 32 * (j >> 1) + 8 * (i16 & 3) + 4 * (j & 1));
                     const bf16x8 twice = as_bf16x8(make_uint4(f.x, f.y, f.x, f.y));
 #pragma unroll
                     for (int mb = 0; mb < kMB; ++mb)
@@ -536,21 +551,40 @@ __global__ __launch_bounds__(256, kMB == 1 ? 3 : kMostR > 64 ? 1 : 2) void wide_
         }
         wave_sync();
         if (rb != 0) continue;
-        // lane holds columns c_now + 16 g .. + 15 of token 16 mb + i16
+        // The accumulators hold columns 32 h + 8 g .. + 7 of row 16 mb + i16 in a lane.  base comes to them through the place of the factor in LDS, and out goes
+        // back through it: to memory whole lines.  (16 rows of 64 bytes a request, as the accumulators have them, 4096 tokens of 4096 columns
+        // took 23.8 us.)  base is used up before the next columns' is asked for.
 #pragma unroll
-        for (int mb = 0; mb < kMB; ++mb) {
-            if (token[mb] < 0) continue;
+        for (int i = 0; i < 2 * kMB; ++i)
+            *reinterpret_cast<uint4*>(stage + (8 * i + vrow) * kOutPitch + vcol) = true_eight<kWhole>(base[i], row[i] < 0 ? 0 : row[i], c_now + vcol, C, out_total);
+        wave_sync();
+        if (c0 < c_end) request_base(c0);
+#pragma unroll
+        for (int mb = 0; mb < kMB; ++mb)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int c = c_now + 16 * g + 8 * h, left = C - c;
-                if (left <= 0) continue;
-                const Eight<false> from{{true_eight<kWhole>(base[mb][h].q[0], (int64_t)token[mb] * C, c, C, out_total)}};
+                uint16_t* at = stage + (16 * mb + i16) * kOutPitch + 32 * h + 8 * g;
+                const Eight<false> from{{*reinterpret_cast<const uint4*>(at)}};
                 float v[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = from.get(e) + acc[mb][2 * h + (e >> 2)][e & 3];
-                store_eight<false, false>(a.out + (int64_t)token[mb] * C + c, 0, kWhole ? 8 : left, v);
+                store_eight<false>(at, 0, 8, v);
+            }
+        wave_sync();
+#pragma unroll
+        for (int i = 0; i < 2 * kMB; ++i) {
+            const int c = c_now + vcol, left = C - c;
+            const Eight<false> v{{*reinterpret_cast<const uint4*>(stage + (8 * i + vrow) * kOutPitch + vcol)}};
+            if (row[i] < 0 || left <= 0) continue;
+            if (kWhole || left >= 8) {
+                *reinterpret_cast<AnyUint4*>(a.out + row[i] + c) = __builtin_bit_cast(AlignedUint4, v.q[0]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 7; ++e)
+                    if (e < left) a.out[row[i] + c + e] = (uint16_t)unit_elem(v.q[0], e);
             }
         }
+        wave_sync();
     }
 }
 
@@ -568,7 +602,7 @@ struct OuterArgs {
 // operand is chosen so that a lane holds four values side by side of the result.  An adapter without tokens gets zeros.
 template <int kRT, int kCols>
 struct OuterLds {
-    static constexpr int kBatch = 128 / kCols * 2, kTokens = 32 * kBatch, kPitch = kCols + 8, kSPitch = 32 * kRT + 8;
+    static constexpr int kBatch = kCols == 64 ? 4 : 2, kTokens = 32 * kBatch, kPitch = kCols + 8, kSPitch = 32 * kRT + 8;
     uint16_t in_tile[kTokens * kPitch];
     uint16_t s_tile[kTokens * kSPitch];
 };
@@ -578,6 +612,7 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, uint16_t* in_tile
     typedef OuterLds<kRT, kCols> Lds;
     constexpr int kBatch = Lds::kBatch, kTokens = Lds::kTokens, kPitch = Lds::kPitch, kSPitch = Lds::kSPitch;
     constexpr int kCT = kCols / 64, kX = kTokens * kCols / 8 / 256, kS = kTokens * 4 * kRT / 256, kAcross = kCols / 8;
+    constexpr int kDeep = kRT < 4 ? 2 : 1;   // batches under way
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i16 = lane & 15, g = lane >> 4;
     const salr_adapter_t& adapter = a.tokens.list[blockIdx.y];
     uint16_t* out = second ? adapter.db : adapter.da;
@@ -590,9 +625,11 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, uint16_t* in_tile
     const int trow = threadIdx.x / kAcross, tvec = threadIdx.x % kAcross;
     for (int rb = 0; rb < rank; rb += 16 * kRT) {
         f32x4 acc[kCT][kRT] = {};
-        uint4 xq[kX], sq[kS];
+        struct Batch {
+            uint4 x[kX], s[kS];
+            int64_t row[kX];
+        } ahead[kDeep];
         int token[kX];   // of the batch after the one requested last
-        int64_t row[kX];
         const auto find = [&](int b) {
 #pragma unroll
             for (int d = 0; d < kX; ++d) {
@@ -600,37 +637,33 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, uint16_t* in_tile
                 token[d] = a.tokens.order[start + (j < count ? j : count - 1)];
             }
         };
-        const auto request = [&](int b) {   // tokens b .. b + kTokens - 1 of the adapter
+        const auto request = [&](Batch& q, int b) {   // tokens b .. b + kTokens - 1 of the adapter
 #pragma unroll
             for (int d = 0; d < kX; ++d) {
-                row[d] = (int64_t)token[d] * C;
-                xq[d] = raw_eight<kWhole>(in, row[d], c0 + 8 * tvec, C, in_total);
+                q.row[d] = (int64_t)token[d] * C;
+                q.x[d] = raw_eight<kWhole>(in, q.row[d], c0 + 8 * tvec, C, in_total);
             }
 #pragma unroll
             for (int v = 0; v < kS; ++v) {
                 const int i = threadIdx.x + 256 * v, j = b + i / (4 * kRT), quad = rb / 4 + i % (4 * kRT), across = a.rpad / 4;
-                sq[v] = s[(int64_t)(j < count ? j : count - 1) * across + (quad < across ? quad : across - 1)];
+                q.s[v] = s[(int64_t)(j < count ? j : count - 1) * across + (quad < across ? quad : across - 1)];
             }
             find(b + kTokens);
         };
-        if (count > 0) {
-            find(0);
-            request(0);
-        }
-        for (int b = 0; b < count; b += kTokens) {
+        const auto multiply = [&](Batch& q, int b) {
             if (b > 0) __syncthreads();   // the tiles of the batch before have been read by everyone
 #pragma unroll
             for (int d = 0; d < kX; ++d) {   // (zeros behind the last token, in both)
                 const int j = 256 / kAcross * d + trow;
-                const uint4 q = true_eight<kWhole>(xq[d], row[d], c0 + 8 * tvec, C, in_total);
-                *reinterpret_cast<uint4*>(&in_tile[j * kPitch + 8 * tvec]) = b + j < count ? q : make_uint4(0, 0, 0, 0);
+                const uint4 x = true_eight<kWhole>(q.x[d], q.row[d], c0 + 8 * tvec, C, in_total);
+                *reinterpret_cast<uint4*>(&in_tile[j * kPitch + 8 * tvec]) = b + j < count ? x : make_uint4(0, 0, 0, 0);
             }
 #pragma unroll
             for (int v = 0; v < kS; ++v) {
                 const int i = threadIdx.x + 256 * v, j = i / (4 * kRT);
-                *reinterpret_cast<uint4*>(&s_tile[j * kSPitch + 8 * (i % (4 * kRT))]) = b + j < count ? sq[v] : make_uint4(0, 0, 0, 0);
+                *reinterpret_cast<uint4*>(&s_tile[j * kSPitch + 8 * (i % (4 * kRT))]) = b + j < count ? q.s[v] : make_uint4(0, 0, 0, 0);
             }
-            if (b + kTokens < count) request(b + kTokens);
+            if (b + kDeep * kTokens < count) request(q, b + kDeep * kTokens);
             __syncthreads();
 #pragma unroll
             for (int d = 0; d < kBatch; ++d) {
@@ -657,6 +690,17 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, uint16_t* in_tile
                             }
                         }
             }
+        };
+        if (count > 0) {
+            find(0);
+            request(ahead[0], 0);
+            if constexpr (kDeep == 2)
+                if (kTokens < count) request(ahead[1], kTokens);
+        }
+        for (int b = 0; b < count; b += kDeep * kTokens) {
+            multiply(ahead[0], b);
+            if constexpr (kDeep == 2)
+                if (b + kTokens < count) multiply(ahead[1], b + kTokens);
         }
         if (rb + 16 * kRT < rank) __syncthreads();   // before the next pass writes the tiles again
         // lane holds column i16 and rows 4 g + e of its accumulators: rows are columns of dy (dB) or ranks (dA)
@@ -683,7 +727,7 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, uint16_t* in_tile
 }
 
 template <int kRT, int kCols, bool kWhole>
-__global__ __launch_bounds__(256, 3) void outer_kernel(OuterArgs a) {
+__global__ __launch_bounds__(256, 2) void outer_kernel(OuterArgs a) {
     __shared__ __align__(16) OuterLds<kRT, kCols> lds;
     if ((int)blockIdx.x < a.blocks0) outer_tile<kRT, kCols, kWhole, false>(a, lds.in_tile, lds.s_tile);
     else outer_tile<kRT, kCols, kWhole, true>(a, lds.in_tile, lds.s_tile);
@@ -695,10 +739,10 @@ namespace {
 
 size_t padded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 
-// Slices of a contraction of C columns: `want` workgroups, each of steps_least steps of 64 columns at least.
-int slices_of(int64_t C, int64_t tiles, int64_t want, int64_t steps_least) {
-    const int64_t steps = (C + 63) / 64;
-    int64_t s = (want + tiles - 1) / tiles;
+// Slices of a contraction of C columns: `want` of them, each of steps_least steps of 128 columns at least.
+int slices_of(int64_t C, int64_t want, int64_t steps_least) {
+    const int64_t steps = (C + 127) / 128;
+    int64_t s = want;
     if (s > steps / steps_least) s = steps / steps_least;
     if (s > 32) s = 32;
     return s < 1 ? 1 : (int)s;
@@ -707,14 +751,15 @@ int slices_of(int64_t C, int64_t tiles, int64_t want, int64_t steps_least) {
 Tokens tokens_of(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p) {
     const char* w = static_cast<const char*>(a.workspace);
     const auto at = [&](size_t offset) { return reinterpret_cast<const int32_t*>(w + offset); };
-    return p.direct ? Tokens{a.list, a.ids, nullptr, nullptr, nullptr, (int)a.T, (int)a.n}
-                    : Tokens{a.list, a.ids, at(p.order), at(p.starts), at(p.counts), (int)a.T, (int)a.n};
+    return p.direct ? Tokens{a.list, a.ids, nullptr, nullptr, nullptr, nullptr, (int)a.T, (int)a.n}
+                    : Tokens{a.list, a.ids, at(p.order), at(p.starts), at(p.counts), reinterpret_cast<const int4*>(w + p.table), (int)a.T, (int)a.n};
 }
 
 void launch_order(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p) {
     char* w = static_cast<char*>(a.workspace);
     hipLaunchKernelGGL(order_tokens_kernel, dim3((unsigned)a.n + 2), dim3(1024), 0, a.stream, a.ids, (int)a.T, (int)a.n,
-                       reinterpret_cast<int32_t*>(w + p.order), reinterpret_cast<int32_t*>(w + p.starts), reinterpret_cast<int32_t*>(w + p.counts));
+                       reinterpret_cast<int32_t*>(w + p.order), reinterpret_cast<int32_t*>(w + p.starts), reinterpret_cast<int32_t*>(w + p.counts),
+                       reinterpret_cast<int4*>(w + p.table));
 }
 
 template <typename Run>
@@ -727,7 +772,7 @@ void launch_narrow(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p, b
     char* w = static_cast<char*>(a.workspace);
     NarrowArgs n{tokens_of(a, p), {a.x, a.dy}, {a.K, a.N}, {reinterpret_cast<float*>(w + p.part_x), reinterpret_cast<float*>(w + p.part_dy)},
                  {x_too ? p.slices_x : 0, dy_too ? p.slices_dy : 0}, p.t_rows, p.rpad};
-    const dim3 grid((unsigned)p.tiles, (unsigned)(n.slices[0] + n.slices[1]));
+    const dim3 grid((unsigned)(p.tiles * (n.slices[0] + n.slices[1])));
     const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, a.stream, n); };
     with_whole((!x_too || a.K % 8 == 0) && (!dy_too || a.N % 8 == 0), [&](auto whole) {
         constexpr bool kWhole = decltype(whole)::value;
@@ -738,19 +783,19 @@ void launch_narrow(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p, b
 
 template <bool kFactorA>
 void launch_wide(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p, const float* part, const uint4* t, int slices, int64_t C) {
-    int64_t per_group = 256;
-    while (p.tiles * ((C + 2 * per_group - 1) / (2 * per_group)) >= 1024) per_group *= 2;
-    const WideArgs w{tokens_of(a, p), part, t, slices, p.t_rows, p.rpad, C, per_group, a.base, a.out};
-    const dim3 grid((unsigned)p.tiles, (unsigned)((C + per_group - 1) / per_group));
+    int64_t per_group = 256;   // as long as the chip has work for every place it has (six workgroups a CU, four of 64 tokens)
+    while (per_group < C && p.live * ((C + 2 * per_group - 1) / (2 * per_group)) >= (p.direct ? 1536 : 1024)) per_group *= 2;
+    const WideArgs w{tokens_of(a, p), part, t, slices, p.t_rows, p.rpad, C, (int)per_group, a.base, a.out};
+    const dim3 grid((unsigned)(p.tiles * ((C + per_group - 1) / per_group)));
     const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, a.stream, w); };
     with_whole(C % 8 == 0, [&](auto whole) {
         constexpr bool kWhole = decltype(whole)::value;
         if constexpr (!kFactorA)
             if (p.direct) {
-                p.rpad <= 32 ? run(wide_kernel<true, 1, 32, false, kWhole>) : p.rpad <= 64 ? run(wide_kernel<true, 1, 64, false, kWhole>) : run(wide_kernel<true, 1, 256, false, kWhole>);
+                p.rpad <= 32 ? run(wide_kernel<true, 16, 32, false, kWhole>) : p.rpad <= 64 ? run(wide_kernel<true, 16, 64, false, kWhole>) : run(wide_kernel<true, 16, 256, false, kWhole>);
                 return;
             }
-        p.rpad <= 32 ? run(wide_kernel<false, 4, 32, kFactorA, kWhole>) : p.rpad <= 64 ? run(wide_kernel<false, 4, 64, kFactorA, kWhole>) : run(wide_kernel<false, 4, 256, kFactorA, kWhole>);
+        p.rpad <= 32 ? run(wide_kernel<false, 64, 32, kFactorA, kWhole>) : p.rpad <= 64 ? run(wide_kernel<false, 64, 64, kFactorA, kWhole>) : run(wide_kernel<false, 64, 256, kFactorA, kWhole>);
     });
 }
 
@@ -773,15 +818,20 @@ RequestAdaptersPlan request_adapters_plan(int64_t T, int64_t K, int64_t N, int64
     p.direct = !backward && T <= kDirectTokens;
     p.rows = p.direct ? 16 : kTileTokens;
     const int64_t groups = n + 2 < T ? n + 2 : T;   // that hold a token
-    p.tiles = p.direct ? T : T / kTileTokens + groups;
+    p.tiles = p.direct ? T : T / kTileTokens + n + 2;
     p.t_rows = T;
     p.rpad = (int)((max_rank + 15) / 16 * 16);
     if (p.rpad == 0) p.rpad = 16;
-    const int64_t live = p.direct ? (n < T ? n : T) : (T + kTileTokens - 1) / kTileTokens + groups / 2;   // tiles to expect
-    // of the backward pass' two products each has its share of the workgroups; few tokens: a step a wave will do
-    const int64_t want = p.direct ? 512 : 768, both = backward ? K + N : K;
-    p.slices_x = slices_of(K, live > 0 ? live : 1, want * K / both, p.direct ? 4 : 8);
-    p.slices_dy = slices_of(N, live > 0 ? live : 1, want * N / both, p.direct ? 4 : 8);
+    p.live = p.direct ? (n < T ? n : T) : (T + kTileTokens - 1) / kTileTokens + groups / 2;   // tiles to expect
+    if (p.live == 0) p.live = 1;
+    if (p.direct) {
+        p.slices_x = slices_of(K, 1024 / p.live, 1);
+    } else {
+        // four workgroups a CU, all at once; the backward pass' two products take as long as each other
+        const int64_t all = 1024 / p.live, of_x = backward && want_dadb ? (all * K + (K + N) / 2) / (K + N) : 0;
+        p.slices_x = slices_of(K, backward ? of_x : all, 4);
+        p.slices_dy = slices_of(N, all - of_x, 4);
+    }
     size_t at = 0;
     const auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -792,6 +842,7 @@ RequestAdaptersPlan request_adapters_plan(int64_t T, int64_t K, int64_t N, int64
         p.order = take((size_t)T * 4);
         p.starts = take((size_t)(n + 2) * 4);
         p.counts = take((size_t)(n + 2) * 4);
+        p.table = take((size_t)p.tiles * 16);
     }
     const size_t row = (size_t)T * p.rpad;
     if (!backward || want_dadb) p.part_x = take(row * 4 * p.slices_x);
