@@ -234,8 +234,8 @@ struct NarrowArgs {
     int rpad;
 };
 
-// part[z][row][r] = sum over the columns c of slice z of in[row][c] * factor(c, r).  A workgroup has a slice of a tile and goes through it by steps of 128
-// columns: rows of in and the factor's part come in by whole lines, four rows of 256 bytes a request, and through LDS (as MFMA operands straight from memory,
+// part[z][row][r] = sum over the columns c of slice z of in[row][c] * factor(c, r).  A slice is every `slices`-th step of 128 columns, so that the
+// workgroups of a tile, one a slice, read side by side: rows of in and the factor's part come in by whole lines, four rows of 256 bytes a request, and through LDS (as MFMA operands straight from memory,
 // 16 rows of 64 bytes a request, they kept the address unit busy for 84 cycles a request instead of 23: 4096 tokens, 18432 columns, rank 32
 // 51 us).  The requests of two steps are out while one is multiplied.  16x16x32 MFMAs with in as A operand; A's [128 columns, ranks], which lie
 // the wrong way round, are read transposed.  Tiles of 64 rows: a wave has 16 of them; of 16 rows: each has 32 columns of a step, and their sums meet in LDS, in
@@ -265,7 +265,7 @@ __device__ __forceinline__ void narrow_tile(const NarrowArgs& a, const Tile& til
     const int rank = (int)adapter.rank;
     const uint16_t* factor = second ? adapter.b : adapter.a;
     const int64_t factor_total = (int64_t)rank * C;
-    const int steps = (C + Lds::kCols - 1) / Lds::kCols, s_begin = (int)((int64_t)steps * z / slices), s_end = (int)((int64_t)steps * (z + 1) / slices);
+    const int steps = (C + Lds::kCols - 1) / Lds::kCols;
     const int vrow = threadIdx.x >> 4, vcol = 8 * (threadIdx.x & 15);
     int64_t row[kMB];   // (behind the last token the first one's: what comes of it is not stored)
 #pragma unroll
@@ -293,7 +293,7 @@ __device__ __forceinline__ void narrow_tile(const NarrowArgs& a, const Tile& til
         };
         const auto step = [&](Step& q, int s) {
             const int c = Lds::kCols * s;
-            if (s > s_begin) __syncthreads();   // the step before has been multiplied by every wave
+            if (s > z) __syncthreads();   // the step before has been multiplied by every wave
 #pragma unroll
             for (int i = 0; i < kMB; ++i) *reinterpret_cast<uint4*>(lds.in + (16 * i + vrow) * kPitch + vcol) = true_eight<kWhole>(q.x[i], row[i], c + vcol, C, in_total);
 #pragma unroll
@@ -308,7 +308,7 @@ __device__ __forceinline__ void narrow_tile(const NarrowArgs& a, const Tile& til
                     *reinterpret_cast<uint4*>(lds.factor + v / (2 * kRT) * kRankPitch + 8 * (v % (2 * kRT))) = k < C ? f : make_uint4(0, 0, 0, 0);
                 }
             }
-            if (s + 2 < s_end) request(q, s + 2);
+            if (s + 2 * slices < steps) request(q, s + 2 * slices);
             __syncthreads();
 #pragma unroll
             for (int u = 0; u < kParts; ++u) {
@@ -329,11 +329,11 @@ __device__ __forceinline__ void narrow_tile(const NarrowArgs& a, const Tile& til
                 }
             }
         };
-        if (s_begin < s_end) request(ahead[0], s_begin);
-        if (s_begin + 1 < s_end) request(ahead[1], s_begin + 1);
-        for (int s = s_begin; s < s_end; s += 2) {
+        if (z < steps) request(ahead[0], z);
+        if (z + slices < steps) request(ahead[1], z + slices);
+        for (int s = z; s < steps; s += 2 * slices) {
             step(ahead[0], s);
-            if (s + 1 < s_end) step(ahead[1], s + 1);
+            if (s + slices < steps) step(ahead[1], s + slices);
         }
         // accumulators: lane holds column i16 (rank), rows 4 g + e (tokens).  Zeros behind the last rank (zero times an infinity of in is none).
         if constexpr (kMB == 1) {
@@ -403,7 +403,7 @@ struct WideArgs {
     int64_t t_rows;
     int rpad;
     int64_t C;              // columns of out
-    int per_group;          // of a workgroup, whole 256s
+    int per_group;          // of a workgroup, whole steps of its waves
     const uint16_t* base;   // may be out, or null (zeros)
     uint16_t* out;
 };
@@ -494,21 +494,29 @@ __global__ __launch_bounds__(256, kMostR > 64 && kRows > 16 ? 1 : 4) void wide_k
         request_base(c0);
         if (rank > 0) request(c0, 0);
     }
-    for (int i = threadIdx.x; i < kRows * (rank16 / 4); i += 256) {
-        const int j = i / (rank16 / 4), r = 4 * (i % (rank16 / 4));
-        uint4 h = make_uint4(0, 0, 0, 0);
-        if (j < tile.count) {
-            const int64_t at = place_of<kDirect>(tile, rows, j) * a.rpad + r;
-            if (a.slices > 0) {
-                f32x4 s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-                for (int z = 0; z < a.slices; ++z) s += *reinterpret_cast<const f32x4*>(a.part + z * a.t_rows * a.rpad + at);
-                h = two_halves(s);
-            } else {
-                h = a.t[at >> 2];
+    if (a.slices > 0) {   // four lanes share a quad's slices, every fourth each, and are of one mind
+        for (int i = threadIdx.x >> 2; i < kRows * (rank16 / 4); i += 64) {
+            const int j = i / (rank16 / 4), r = 4 * (i % (rank16 / 4)), first = threadIdx.x & 3;
+            f32x4 s = {0.f, 0.f, 0.f, 0.f};
+            if (j < tile.count) {
+                const float* from = a.part + place_of<kDirect>(tile, rows, j) * a.rpad + r;
+#pragma unroll 4
+                for (int z = first; z < a.slices; z += 4) s += *reinterpret_cast<const f32x4*>(from + z * a.t_rows * a.rpad);
             }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[e] += __shfl_xor(s[e], 1);
+                s[e] += __shfl_xor(s[e], 2);
+            }
+            if (first == 0) *reinterpret_cast<uint4*>(t + j * kTPitch + 2 * r) = two_halves(s);
         }
-        *reinterpret_cast<uint4*>(t + j * kTPitch + 2 * r) = h;
+    } else {
+        for (int i = threadIdx.x; i < kRows * (rank16 / 4); i += 256) {
+            const int j = i / (rank16 / 4), r = 4 * (i % (rank16 / 4));
+            uint4 h = make_uint4(0, 0, 0, 0);
+            if (j < tile.count) h = a.t[(place_of<kDirect>(tile, rows, j) * a.rpad + r) >> 2];
+            *reinterpret_cast<uint4*>(t + j * kTPitch + 2 * r) = h;
+        }
     }
     __syncthreads();
     uint16_t* stage = stages[wave];
@@ -744,7 +752,7 @@ int slices_of(int64_t C, int64_t want, int64_t steps_least) {
     const int64_t steps = (C + 127) / 128;
     int64_t s = want;
     if (s > steps / steps_least) s = steps / steps_least;
-    if (s > 32) s = 32;
+    if (s > 16) s = 16;
     return s < 1 ? 1 : (int)s;
 }
 
@@ -829,8 +837,8 @@ RequestAdaptersPlan request_adapters_plan(int64_t T, int64_t K, int64_t N, int64
     } else {
         // four workgroups a CU, all at once; the backward pass' two products take as long as each other
         const int64_t all = 1024 / p.live, of_x = backward && want_dadb ? (all * K + (K + N) / 2) / (K + N) : 0;
-        p.slices_x = slices_of(K, backward ? of_x : all, 4);
-        p.slices_dy = slices_of(N, all - of_x, 4);
+        p.slices_x = slices_of(K, backward ? of_x : all, backward ? 2 : 4);
+        p.slices_dy = slices_of(N, all - of_x, 2);
     }
     size_t at = 0;
     const auto take = [&](size_t bytes) {
