@@ -63,6 +63,45 @@ __device__ __forceinline__ Eight<k32> load_eight(const void* base, int i, int le
     return r;
 }
 
+// The same eight elements, from element `at` on of a matrix of `total` >= 8, of a row of any length, in two steps that hold no branch, so that many requests
+// are under way at once (with load_eight a wave at the end of a row waits for each): raw_eight asks for them, pulled back from the
+// matrix' end where they would leave it; true_eight shifts what came to its place and puts zeros behind the first `left`.
+template <bool k32>
+__device__ __forceinline__ Eight<k32> raw_eight(const void* matrix, int64_t at, int64_t total) {
+    return load_eight<k32, false, false>(static_cast<const char*>(matrix) + (at < total - 8 ? at : total - 8) * (k32 ? 4 : 2), 0, 8);
+}
+template <bool k32>
+__device__ __forceinline__ Eight<k32> true_eight(const Eight<k32>& q, int64_t at, int left, int64_t total) {
+    Eight<k32> r = q;
+    const int64_t past = at - (total - 8);
+    const int by = past <= 0 ? 0 : past < 8 ? (int)past : 8;
+    if (__any(by > 0 || left < 8)) {   // (a wave in the middle of a row has nothing to do)
+        uint32_t e[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if constexpr (k32) {
+                const uint4 v = q.q[j >> 2];
+                e[j] = (j & 3) == 0 ? v.x : (j & 3) == 1 ? v.y : (j & 3) == 2 ? v.z : v.w;
+            } else {
+                e[j] = unit_elem(q.q[0], j);
+            }
+        }
+#pragma unroll
+        for (int step = 1; step < 8; step *= 2)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) e[j] = by & step ? (j + step < 8 ? e[j + step] : 0u) : e[j];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = j < left && by < 8 ? e[j] : 0u;
+        if constexpr (k32) {
+            r.q[0] = make_uint4(e[0], e[1], e[2], e[3]);
+            r.q[1] = make_uint4(e[4], e[5], e[6], e[7]);
+        } else {
+            r.q[0] = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+        }
+    }
+    return r;
+}
+
 template <bool k32, bool kAligned = true>
 __device__ __forceinline__ void store_eight(void* base, int i, int left, const float (&x)[8]) {
     if (left >= 8) {

@@ -51,26 +51,33 @@ __device__ __forceinline__ void team_sum(float (&v)[kSums], float* slots) {
     }
 }
 
-// Eight elements of a row from i on, of which `left` are there; kWhole: all or none of them.
+// Eight elements of a row from i on, of which `left` are there, in two steps: asked for, then as they are.  kWhole: all or none of them are there.
 template <bool k32, bool kWhole>
-__device__ __forceinline__ Eight<k32> row_eight(const void* row, int i, int left) {
+__device__ __forceinline__ Eight<k32> row_request(const void* matrix, int64_t start, int i, int left, int64_t total) {
     if constexpr (kWhole) {
         Eight<k32> zero{};
-        return left > 0 ? load_eight<k32, false, false>(row, i, 8) : zero;
+        return left > 0 ? load_eight<k32, false, false>(static_cast<const char*>(matrix) + (start + i) * (k32 ? 4 : 2), 0, 8) : zero;
     } else {
-        return load_eight<k32, false, false>(row, i, left);
+        if (total < 8) return load_eight<k32, false, false>(static_cast<const char*>(matrix) + start * (k32 ? 4 : 2), i, left);   // the same for the launch
+        return raw_eight<k32>(matrix, start + i, total);
     }
+}
+template <bool k32, bool kWhole>
+__device__ __forceinline__ Eight<k32> row_values(const Eight<k32>& q, int64_t start, int i, int left, int64_t total) {
+    if (kWhole || total < 8) return q;
+    return true_eight<k32>(q, start + i, left, total);
 }
 
 // The same of weights, in fp32.
 template <bool kWhole>
-__device__ __forceinline__ void load_weights(const void* w, bool w32, int i, int left, float (&out)[8]) {
+__device__ __forceinline__ void load_weights(const void* w, bool w32, int i, int K, float (&out)[8]) {
+    const int left = K - i;
     if (w32) {
-        const Eight<true> q = row_eight<true, kWhole>(w, i, left);
+        const Eight<true> q = row_values<true, kWhole>(row_request<true, kWhole>(w, 0, i, left, K), 0, i, left, K);
 #pragma unroll
         for (int j = 0; j < 8; ++j) out[j] = q.get(j);
     } else {
-        const Eight<false> q = row_eight<false, kWhole>(w, i, left);
+        const Eight<false> q = row_values<false, kWhole>(row_request<false, kWhole>(w, 0, i, left, K), 0, i, left, K);
 #pragma unroll
         for (int j = 0; j < 8; ++j) out[j] = q.get(j);
     }
@@ -83,15 +90,25 @@ __global__ __launch_bounds__(kTeam < 4 ? 256 : 64 * kTeam) void layer_norm_kerne
     const int team = threadIdx.x / (64 * kTeam), at = threadIdx.x % (64 * kTeam), K = a.K;
     const int64_t row = (int64_t)blockIdx.x * kTeams + team;
     const bool live = row < a.T;   // (the others go through the barriers)
-    const int64_t start = (live ? row : 0) * K * (k32 ? 4 : 2);
-    const char* x = static_cast<const char*>(a.x) + start;
-    const char* residual = static_cast<const char*>(a.residual) + start;
-    char* y = static_cast<char*>(a.y) + start;
+    const int64_t start = (live ? row : 0) * K, total = a.T * K;
+    char* y = static_cast<char*>(a.y) + start * (k32 ? 4 : 2);
     float s[kUnits][8], sums[1] = {0.f};
+    Eight<k32> xq[kUnits], rq[kUnits];
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
         const int i = 8 * (at + 64 * kTeam * u), left = live ? K - i : 0;
-        const Eight<k32> q = row_eight<k32, kWhole>(x, i, left);
+        xq[u] = row_request<k32, kWhole>(a.x, start, i, left, total);
+    }
+    if (a.residual != nullptr)
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const int i = 8 * (at + 64 * kTeam * u), left = live ? K - i : 0;
+            rq[u] = row_request<k32, kWhole>(a.residual, start, i, left, total);
+        }
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+        const int i = 8 * (at + 64 * kTeam * u), left = live ? K - i : 0;
+        const Eight<k32> q = row_values<k32, kWhole>(xq[u], start, i, left, total);
 #pragma unroll
         for (int j = 0; j < 8; ++j) s[u][j] = q.get(j);
     }
@@ -99,14 +116,14 @@ __global__ __launch_bounds__(kTeam < 4 ? 256 : 64 * kTeam) void layer_norm_kerne
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
             const int i = 8 * (at + 64 * kTeam * u), left = live ? K - i : 0;
-            const Eight<k32> q = row_eight<k32, kWhole>(residual, i, left);
+            const Eight<k32> q = row_values<k32, kWhole>(rq[u], start, i, left, total);
             // the sum is rounded as it is stored, and the norm is of that: so is the gradient, which reads it back
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 s[u][j] += q.get(j);
                 if constexpr (!k32) s[u][j] = (float)(__bf16)s[u][j];
             }
-            if (left > 0) store_eight<k32, false>(static_cast<char*>(a.sum) + start, i, kWhole ? 8 : left, s[u]);
+            if (left > 0) store_eight<k32, false>(static_cast<char*>(a.sum) + start * (k32 ? 4 : 2), i, kWhole ? 8 : left, s[u]);
         }
     }
 #pragma unroll
@@ -137,8 +154,8 @@ __global__ __launch_bounds__(kTeam < 4 ? 256 : 64 * kTeam) void layer_norm_kerne
         const int i = 8 * (at + 64 * kTeam * u), left = K - i;
         if (left <= 0) break;
         float w[8], b[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        load_weights<kWhole>(a.weight, a.w32, i, left, w);
-        if (a.bias != nullptr) load_weights<kWhole>(a.bias, a.w32, i, left, b);
+        load_weights<kWhole>(a.weight, a.w32, i, K, w);
+        if (a.bias != nullptr) load_weights<kWhole>(a.bias, a.w32, i, K, b);
 #pragma unroll
         for (int j = 0; j < 8; ++j) w[j] = fmaf((s[u][j] - mean) * rstd, w[j], b[j]);
         store_eight<k32, false>(y, i, kWhole ? 8 : left, w);
@@ -146,7 +163,7 @@ __global__ __launch_bounds__(kTeam < 4 ? 256 : 64 * kTeam) void layer_norm_kerne
 }
 
 // kWeights: dw and db too, the workgroup's sums of them as part[0][blockIdx.x][K] and part[1][..]; a row's requests are then out while the one before is
-// worked on (kAhead), since a workgroup has its CU to itself.  lds: K floats where a workgroup has several teams.
+// worked on (kAhead), since a workgroup has its CU to itself.
 template <int kTeam, bool kWeights>
 constexpr int grad_waves() { return kWeights ? 8 : kTeam < 4 ? 4 : kTeam; }
 
@@ -155,7 +172,7 @@ __global__ __launch_bounds__((64 * grad_waves<kTeam, kWeights>())) void layer_no
     constexpr int kWaves = grad_waves<kTeam, kWeights>(), kTeams = kWaves / kTeam;
     constexpr bool kAhead = kWeights && kUnits <= 2;
     __shared__ float slots[2][kWaves * 2];
-    extern __shared__ float totals[];
+    __shared__ __align__(16) float totals[kTeams > 1 && kWeights ? 512 * kTeam * kUnits : 4];   // what the teams before have summed
     const int team = threadIdx.x / (64 * kTeam), at = threadIdx.x % (64 * kTeam), K = a.K;
     const bool want_dx = a.dx != nullptr, add = want_dx && a.dsum != nullptr;
     float dw[kWeights ? kUnits : 1][8] = {}, db[kWeights ? kUnits : 1][8] = {}, w[kUnits][8] = {};
@@ -163,23 +180,24 @@ __global__ __launch_bounds__((64 * grad_waves<kTeam, kWeights>())) void layer_no
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
             const int i = 8 * (at + 64 * kTeam * u);
-            load_weights<kWhole>(a.weight, a.w32, i, K - i, w[u]);
+            load_weights<kWhole>(a.weight, a.w32, i, K, w[u]);
         }
+    const int64_t total = a.T * K;
     struct Row {
         Eight<k32> x[kUnits], dy[kUnits], ds[kUnits];
         float mean, rstd;
     };
     const auto request = [&](Row& r, int64_t row) {
         const bool live = row < a.T;
-        const int64_t start = (live ? row : 0) * K * (k32 ? 4 : 2);
+        const int64_t start = (live ? row : 0) * K;
         r.mean = live ? a.mean[row] : 0.f;
         r.rstd = live ? a.rstd[row] : 0.f;
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
             const int i = 8 * (at + 64 * kTeam * u), left = live ? K - i : 0;
-            r.x[u] = row_eight<k32, kWhole>(static_cast<const char*>(a.x) + start, i, left);
-            r.dy[u] = row_eight<k32, kWhole>(static_cast<const char*>(a.dy) + start, i, left);
-            if (add) r.ds[u] = row_eight<k32, kWhole>(static_cast<const char*>(a.dsum) + start, i, left);
+            r.x[u] = row_request<k32, kWhole>(a.x, start, i, left, total);
+            r.dy[u] = row_request<k32, kWhole>(a.dy, start, i, left, total);
+            if (add) r.ds[u] = row_request<k32, kWhole>(a.dsum, start, i, left, total);
         }
     };
     const int64_t stride = (int64_t)gridDim.x * kTeams;
@@ -195,6 +213,16 @@ __global__ __launch_bounds__((64 * grad_waves<kTeam, kWeights>())) void layer_no
             if (row0 + stride < a.T) request(next, row + stride);
         } else {
             request(r, row);
+        }
+        if constexpr (!kWhole) {
+            const int64_t start = (live ? row : 0) * K;
+#pragma unroll
+            for (int u = 0; u < kUnits; ++u) {
+                const int i = 8 * (at + 64 * kTeam * u), left = live ? K - i : 0;
+                r.x[u] = row_values<k32, kWhole>(r.x[u], start, i, left, total);
+                r.dy[u] = row_values<k32, kWhole>(r.dy[u], start, i, left, total);
+                if (add) r.ds[u] = row_values<k32, kWhole>(r.ds[u], start, i, left, total);
+            }
         }
         float sums[2] = {0.f, 0.f};
 #pragma unroll
@@ -237,14 +265,20 @@ __global__ __launch_bounds__((64 * grad_waves<kTeam, kWeights>())) void layer_no
                 if (t == team) {
 #pragma unroll
                     for (int u = 0; u < kUnits; ++u) {
-                        const int i = 8 * (at + 64 * kTeam * u);
+                        const int i = 8 * (at + 64 * kTeam * u), left = K - i;
+                        float v[8];
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            if (i + (kWhole ? 0 : j) >= K) break;
-                            float s = which == 0 ? dw[u][j] : db[u][j];
-                            if (t > 0) s += totals[i + j];
-                            if (t < kTeams - 1) totals[i + j] = s;
-                            else part[i + j] = s;
+                        for (int j = 0; j < 8; ++j) v[j] = which == 0 ? dw[u][j] : db[u][j];
+                        if (t > 0) {   // (totals has whole vectors of room)
+                            const f32x4 lo = *reinterpret_cast<const f32x4*>(totals + i), hi = *reinterpret_cast<const f32x4*>(totals + i + 4);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) v[j] += j < 4 ? lo[j] : hi[j - 4];
+                        }
+                        if (t < kTeams - 1) {
+                            *reinterpret_cast<f32x4*>(totals + i) = f32x4{v[0], v[1], v[2], v[3]};
+                            *reinterpret_cast<f32x4*>(totals + i + 4) = f32x4{v[4], v[5], v[6], v[7]};
+                        } else if (left > 0) {
+                            store_eight<true, false>(part, i, kWhole ? 8 : left, v);
                         }
                     }
                 }
@@ -326,17 +360,16 @@ hipError_t launch_layer_norm(const LayerNormArgs& a, hipStream_t stream) {
 hipError_t launch_layer_norm_backward(const LayerNormGradArgs& a, void* dw, void* db, hipStream_t stream) {
     const bool weights = dw != nullptr || db != nullptr;
     const int64_t parts = layer_norm_parts(a.T, a.K);
-    const auto run = [&](auto kernel, int64_t groups, int threads, size_t lds) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3((unsigned)threads), lds, stream, a);
+    const auto run = [&](auto kernel, int64_t groups, int threads) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3((unsigned)threads), 0, stream, a);
     };
     if (a.T > 0 && weights)
         with_grad_team(a.K, [&](auto waves, auto units) {
             with_whole(a.K, [&](auto whole) {
                 constexpr int kTeam = waves, kUnits = units;
                 constexpr bool kWhole = decltype(whole)::value;
-                const size_t lds = kTeam < 8 ? (size_t)a.K * 4 : 0;
-                if (a.f32) run(layer_norm_backward_kernel<true, kTeam, kUnits, kWhole, true>, parts, 512, lds);
-                else run(layer_norm_backward_kernel<false, kTeam, kUnits, kWhole, true>, parts, 512, lds);
+                if (a.f32) run(layer_norm_backward_kernel<true, kTeam, kUnits, kWhole, true>, parts, 512);
+                else run(layer_norm_backward_kernel<false, kTeam, kUnits, kWhole, true>, parts, 512);
             });
         });
     else if (a.T > 0 && a.dx != nullptr)
@@ -344,8 +377,8 @@ hipError_t launch_layer_norm_backward(const LayerNormGradArgs& a, void* dw, void
             with_whole(a.K, [&](auto whole) {
                 constexpr int kTeam = waves, kUnits = units, kThreads = 64 * grad_waves<kTeam, false>(), kTeams = kThreads / 64 / kTeam;
                 constexpr bool kWhole = decltype(whole)::value;
-                if (a.f32) run(layer_norm_backward_kernel<true, kTeam, kUnits, kWhole, false>, (a.T + kTeams - 1) / kTeams, kThreads, 0);
-                else run(layer_norm_backward_kernel<false, kTeam, kUnits, kWhole, false>, (a.T + kTeams - 1) / kTeams, kThreads, 0);
+                if (a.f32) run(layer_norm_backward_kernel<true, kTeam, kUnits, kWhole, false>, (a.T + kTeams - 1) / kTeams, kThreads);
+                else run(layer_norm_backward_kernel<false, kTeam, kUnits, kWhole, false>, (a.T + kTeams - 1) / kTeams, kThreads);
             });
         });
     if (weights)

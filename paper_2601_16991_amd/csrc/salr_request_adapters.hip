@@ -494,7 +494,7 @@ __global__ __launch_bounds__(256, kMostR > 64 && kRows > 16 ? 1 : 4) void wide_k
         request_base(c0);
         if (rank > 0) request(c0, 0);
     }
-    if (a.slices > 0) {   // four lanes share a quad's slices, every fourth each, and are of one mind
+    if (kRows == 16 && a.slices > 0) {   // four lanes share a quad's slices, every fourth each, and are of one mind
         for (int i = threadIdx.x >> 2; i < kRows * (rank16 / 4); i += 64) {
             const int j = i / (rank16 / 4), r = 4 * (i % (rank16 / 4)), first = threadIdx.x & 3;
             f32x4 s = {0.f, 0.f, 0.f, 0.f};
@@ -514,7 +514,17 @@ __global__ __launch_bounds__(256, kMostR > 64 && kRows > 16 ? 1 : 4) void wide_k
         for (int i = threadIdx.x; i < kRows * (rank16 / 4); i += 256) {
             const int j = i / (rank16 / 4), r = 4 * (i % (rank16 / 4));
             uint4 h = make_uint4(0, 0, 0, 0);
-            if (j < tile.count) h = a.t[(place_of<kDirect>(tile, rows, j) * a.rpad + r) >> 2];
+            if (j < tile.count) {
+                const int64_t at = place_of<kDirect>(tile, rows, j) * a.rpad + r;
+                if (a.slices > 0) {
+                    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+                    for (int z = 0; z < a.slices; ++z) s += *reinterpret_cast<const f32x4*>(a.part + z * a.t_rows * a.rpad + at);
+                    h = two_halves(s);
+                } else {
+                    h = a.t[at >> 2];
+                }
+            }
             *reinterpret_cast<uint4*>(t + j * kTPitch + 2 * r) = h;
         }
     }
