@@ -557,7 +557,7 @@ salr_status_t salr_dropout(const void* x, const void* residual, int64_t count, s
  *
  *     mean = sum_k s[k] / K,   rstd = 1 / sqrt(sum_k (s[k] - mean)^2 / K + eps),   y[k] = (s[k] - mean) * rstd * weight[k] + bias[k]
  *
- *   x         in   [T, K] of `type`;  0 <= K <= 32768, T < 2^22 (else SHAPE)
+ *   x         in   [T, K] of `type`;  1 <= K <= 32768 where T > 0, T < 2^22 (else SHAPE)
  *   residual  in   [T, K] of `type`, or NULL
  *   weight    in   [K] of `weight_type`
  *   bias      in   [K] of `weight_type`, or NULL (zeros)
@@ -605,7 +605,7 @@ typedef struct {
 
 /*
  * salr_adapter_list_check -- whether the n records of a HOST array can be used; *max_rank gets the largest rank, which the calls want to know.  No
- * gradient may overlap another tensor of the list (not checked here).
+ * gradient may overlap another tensor of the list or of a call (not checked here).
  * Errors: INVALID_ARG (null where data is required, n or a rank negative, a pointer that is not 16-byte aligned), SHAPE (n > 4096),
  * UNSUPPORTED (a rank above 256).
  */
@@ -615,8 +615,9 @@ salr_status_t salr_adapter_list_check(const salr_adapter_t* adapters, int64_t n,
  * salr_adapters_add -- y[t] = base[t] + (x[t] A_i) B_i with i = ids[t]; a token with a negative id has no adapter: y[t] = base[t].
  * An id that is not below n gives NaN in its token's row.
  *
- *   list, n, max_rank  the records, on the device (8-byte aligned), their number (at least 1) and largest rank
- *   x          in   [T, K] bf16;  T < 2^28, K and N from 8 to 2^22 (else SHAPE)
+ *   list, n, max_rank  the records, on the device (8-byte aligned), their number (at least 1) and largest rank (ranks of a record above it are not
+ *                      looked at)
+ *   x          in   [T, K] bf16;  T < 2^28, T (max_rank + 15) < 2^34, K and N from 8 to 2^22 (else SHAPE)
  *   ids        in   [T] int32
  *   base       in   [T, N] bf16, the shared layer's output; NULL = zeros
  *   y          out  [T, N] bf16; may be base, overlaps x and base in no other way

@@ -63,13 +63,14 @@ bool overlaps(const void* a, size_t bytes, const void* b, size_t bytes_b) {
 }
 bool overlaps_in_part(const void* a, const void* b, size_t bytes) { return a != b && overlaps(a, bytes, b, bytes); }
 
-bool layer_norm_sizes(int64_t T, int64_t K) { return T <= salr::kLayerNormMostT && K <= salr::kLayerNormMostK; }
+bool layer_norm_sizes(int64_t T, int64_t K) { return T <= salr::kLayerNormMostT && K <= salr::kLayerNormMostK && (K > 0 || T == 0); }
 
 // Sizes of the calls on adapters of many requests.
 salr_status_t adapters_sizes(int64_t T, int64_t K, int64_t N, int64_t n, int64_t max_rank) {
     if (T < 0 || K < 0 || N < 0 || n < 1 || max_rank < 0 || max_rank > kMaxRank) return SALR_ERR_INVALID_ARG;
     const auto fits = [](int64_t columns) { return columns >= salr::kAdaptersLeastColumns && columns <= salr::kAdaptersMostColumns; };
     if (T > salr::kAdaptersMostT || !fits(K) || !fits(N) || n > salr::kAdaptersMostCount) return SALR_ERR_SHAPE;
+    if (T * (max_rank + 15) >= (int64_t)1 << 34) return SALR_ERR_SHAPE;   // (four of its values a thread)
     return SALR_OK;
 }
 
@@ -584,7 +585,7 @@ salr_status_t salr_layer_norm(const void* x, const void* residual, const void* w
                               salr_type_t weight_type, double eps, void* y, void* sum, float* mean, float* rstd, void* stream) {
     if (T < 0 || K < 0 || !is_type(type) || !is_type(weight_type) || !(eps >= 0.0 && eps <= std::numeric_limits<float>::max())) return SALR_ERR_INVALID_ARG;
     if (!layer_norm_sizes(T, K)) return SALR_ERR_SHAPE;
-    if (T == 0 || K == 0) return SALR_OK;
+    if (T == 0) return SALR_OK;
     const uintptr_t size = type == SALR_F32 ? 4 : 2, wsize = weight_type == SALR_F32 ? 4 : 2;
     const size_t bytes = (size_t)(T * K) * size, wbytes = (size_t)K * wsize, stats = (size_t)T * 4;
     if (!x || !weight || !y || (residual != nullptr) != (sum != nullptr)) return SALR_ERR_INVALID_ARG;

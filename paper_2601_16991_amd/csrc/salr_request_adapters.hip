@@ -86,6 +86,11 @@ __device__ __forceinline__ Tile find_tile(const Tokens& k, int self, int* rows) 
     return tile;
 }
 
+// (never more than the launch has room for, whatever the record says)
+__device__ __forceinline__ int rank_of(const salr_adapter_t& adapter, int rpad) {
+    return adapter.rank < rpad ? (int)adapter.rank : rpad;
+}
+
 // Row j's place in the sums of a tile.
 template <bool kDirect>
 __device__ __forceinline__ int64_t place_of(const Tile& tile, const int* rows, int j) {
@@ -262,7 +267,7 @@ __device__ __forceinline__ void narrow_tile(const NarrowArgs& a, const Tile& til
     const int64_t in_total = (int64_t)a.tokens.T * C;
     float* part = (second ? a.part[1] : a.part[0]) + (int64_t)z * a.t_rows * a.rpad;
     const salr_adapter_t& adapter = a.tokens.list[tile.group];
-    const int rank = (int)adapter.rank;
+    const int rank = rank_of(adapter, a.rpad);
     const uint16_t* factor = second ? adapter.b : adapter.a;
     const int64_t factor_total = (int64_t)rank * C;
     const int steps = (C + Lds::kCols - 1) / Lds::kCols;
@@ -445,7 +450,7 @@ __global__ __launch_bounds__(256, kMostR > 64 && kRows > 16 ? 1 : 4) void wide_k
         return;
     }
     const salr_adapter_t& adapter = a.tokens.list[tile.group];
-    const int rank = (int)adapter.rank, rank16 = (rank + 15) & ~15;
+    const int rank = rank_of(adapter, a.rpad), rank16 = (rank + 15) & ~15;
     const uint16_t* factor = kFactorA ? adapter.a : adapter.b;
     const int64_t factor_total = (int64_t)rank * C;
     uint4 q[kVectors];
@@ -635,7 +640,7 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, uint16_t* in_tile
     const salr_adapter_t& adapter = a.tokens.list[blockIdx.y];
     uint16_t* out = second ? adapter.db : adapter.da;
     if (out == nullptr) return;
-    const int rank = (int)adapter.rank, count = a.tokens.counts[blockIdx.y], start = a.tokens.starts[blockIdx.y];
+    const int rank = rank_of(adapter, a.rpad), count = a.tokens.counts[blockIdx.y], start = a.tokens.starts[blockIdx.y];
     const uint16_t* in = second ? a.in[1] : a.in[0];
     const uint4* s = (second ? a.s[1] : a.s[0]) + (int64_t)start * (a.rpad / 4);
     const int C = (int)(second ? a.C[1] : a.C[0]), c0 = kCols * ((int)blockIdx.x - (second ? a.blocks0 : 0));

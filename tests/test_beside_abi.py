@@ -57,9 +57,9 @@ def test_layer_norm_arguments(salr):
                 dict(eps=-1e-9), dict(eps=float("inf")), dict(eps=float("nan")), dict(x=at(0, 2)), dict(weight=at(2, 1)), dict(mean=at(6, 2)), dict(y=at(0, 4)),
                 dict(y=at(1, 400)), dict(y=at(5)), dict(sum=at(0, 396)), dict(y=at(2, 4)), dict(mean=at(7)), dict(mean=at(0)), dict(rstd=at(4, 64)), dict(rstd=at(3))):
         assert _norm(salr, **bad) == salr.SALR_ERR_INVALID_ARG, bad
-    for size in (dict(K=32769), dict(T=1 << 22)):
+    for size in (dict(K=32769), dict(T=1 << 22), dict(K=0)):
         assert _norm(salr, **size) == salr.SALR_ERR_SHAPE
-    assert _norm(salr, T=0, x=None) == salr.SALR_OK and _norm(salr, K=0, y=None) == salr.SALR_OK
+    assert _norm(salr, T=0, x=None) == salr.SALR_OK and _norm(salr, T=0, K=0, y=None) == salr.SALR_OK
 
 
 def _norm_grad(salr, T=8, K=100, **kw):
@@ -73,14 +73,14 @@ def test_layer_norm_backward_arguments(salr):
                 dict(dy=at(0, 2)), dict(dw=at(7, 2)), dict(dx=at(0, 4)), dict(dx=at(1, -4)), dict(dx=at(5, 400)), dict(dx=at(2)), dict(dw=at(8, 4)), dict(db=at(6, 4)),
                 dict(dw=at(2)), dict(db=at(3)), dict(dx=at(4))):
         assert _norm_grad(salr, **bad) == salr.SALR_ERR_INVALID_ARG, bad
-    for size in (dict(K=32769), dict(T=1 << 22)):
+    for size in (dict(K=32769), dict(T=1 << 22), dict(K=0)):
         assert _norm_grad(salr, **size) == salr.SALR_ERR_SHAPE
     need = salr.salr_layer_norm_backward_workspace_bytes(8, 100, True)
     assert need > 0 and salr.salr_layer_norm_backward_workspace_bytes(8, 100, False) == 0
     assert salr.salr_layer_norm_backward_workspace_bytes(8, 32769, True) == 0
     assert _norm_grad(salr, bytes=need - 1) == salr.SALR_ERR_CAPACITY
     assert _norm_grad(salr, dx=None, dw=None, db=None, dy=None) == salr.SALR_OK
-    assert _norm_grad(salr, T=0, dw=None, db=None, dy=None) == salr.SALR_OK and _norm_grad(salr, K=0, dy=None) == salr.SALR_OK
+    assert _norm_grad(salr, T=0, dw=None, db=None, dy=None) == salr.SALR_OK and _norm_grad(salr, T=0, K=0, dy=None) == salr.SALR_OK
 
 
 def test_adapter_list(salr):
@@ -116,7 +116,7 @@ def test_adapters_arguments(salr):
     for bad in sizes + (dict(list=None), dict(x=None), dict(ids=None), dict(dy=None), dict(ws=None), dict(list=at(0, 4)), dict(dy=at(3, 1)), dict(dx_base=at(4, 1)),
                         dict(dx=at(5, 1)), dict(dx=at(4, 2)), dict(dx=at(1)), dict(dx=at(3, -2)), dict(dx=at(2))):
         assert _grad(salr, **bad) == salr.SALR_ERR_INVALID_ARG, bad
-    for size in (dict(T=1 << 28), dict(K=(1 << 22) + 1), dict(N=(1 << 22) + 1), dict(n=4097), dict(K=7), dict(N=7), dict(K=0), dict(N=0)):
+    for size in (dict(T=1 << 28), dict(K=(1 << 22) + 1), dict(N=(1 << 22) + 1), dict(n=4097), dict(T=(1 << 28) - 1, rank=256), dict(K=7), dict(N=7), dict(K=0), dict(N=0)):
         assert _add(salr, **size) == salr.SALR_ERR_SHAPE and _grad(salr, **size) == salr.SALR_ERR_SHAPE, size
     for T in (8, 300):
         need = salr.salr_adapters_add_workspace_bytes(T, 64, 96, 3, 16)
