@@ -893,12 +893,12 @@ hipError_t launch_request_adapters_backward(const RequestAdaptersArgs& a, const 
         launch_narrow(a, p, a.want_dadb, true);
         const SumArgs s{{reinterpret_cast<const float*>(w + p.part_dy), reinterpret_cast<const float*>(w + p.part_x)}, {t_dy, t_x}, {p.slices_dy, p.slices_x}, a.T * p.rpad};
         hipLaunchKernelGGL(sum_slices_kernel, dim3((unsigned)((s.count / 4 + 255) / 256), a.want_dadb ? 2 : 1), dim3(256), 0, a.stream, s);
-        if (a.out != nullptr) launch_wide<true>(a, p, nullptr, t_dy, 0, a.K);
     }
-    if (a.want_dadb) {
+    if (a.want_dadb) {   // (before dx: it reads what the first products have read)
         if ((a.K + a.N) / 128 * a.n >= 512) launch_outer<128>(a, p, t_x, t_dy);
         else launch_outer<64>(a, p, t_x, t_dy);
     }
+    if (a.T > 0 && a.out != nullptr) launch_wide<true>(a, p, nullptr, t_dy, 0, a.K);
     return hipGetLastError();
 }
 
