@@ -617,7 +617,8 @@ salr_status_t salr_adapter_list_check(const salr_adapter_t* adapters, int64_t n,
  *
  *   list, n, max_rank  the records, on the device (8-byte aligned), their number (at least 1) and largest rank (ranks of a record above it are not
  *                      looked at)
- *   x          in   [T, K] bf16;  T < 2^28, T (max_rank + 15) < 2^34, K and N from 8 to 2^22 (else SHAPE)
+ *   x          in   [T, K] bf16;  T < 2^28, T (max_rank + 15) < 2^34, K and N from 8 to 2^22, (K + N) n <= 2^28
+ *                      (else SHAPE)
  *   ids        in   [T] int32
  *   base       in   [T, N] bf16, the shared layer's output; NULL = zeros
  *   y          out  [T, N] bf16; may be base, overlaps x and base in no other way

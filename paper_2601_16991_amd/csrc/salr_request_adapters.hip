@@ -420,19 +420,27 @@ struct WideArgs {
 // + 4 (j % 2) + m % 4): out is read and written in whole vectors.  An instruction takes 16 ranks: four of a lane with t's first half and the same four with its second.
 // kFactorA: the factor is A [C, r] (dx), else B [r, C] (y).
 // kRows: of a tile; of 64, two waves have one half each.
+template <int kRows, int kMostR, bool kFactorA>
+struct WideLds {
+    static constexpr int kTPitch = 2 * kMostR + 8, kPass = 32, kPitch = kFactorA ? kPass + 8 : 64 + 8, kOutPitch = 64 + 8;
+    static constexpr int kMB = kRows / 16 < 2 ? 1 : 2, kStage = (kFactorA ? 64 : kPass) * kPitch;   // kMB: blocks of rows of a wave
+    static_assert(16 * kMB * kOutPitch <= kStage, "out goes through the factor's place");
+    uint16_t t[kRows * kTPitch], stages[4][kStage];
+    int rows[kRows];
+};
+
 template <bool kDirect, int kRows, int kMostR, bool kFactorA, bool kWhole>
-__global__ __launch_bounds__(256, kMostR > 64 && kRows > 16 ? 1 : 4) void wide_kernel(WideArgs a) {
-    constexpr int kTPitch = 2 * kMostR + 8, kPass = 32, kVectors = kPass / 8, kPitch = kFactorA ? kPass + 8 : 64 + 8, kOutPitch = 64 + 8;
-    constexpr int kMB = kRows / 16 < 2 ? 1 : 2, kHalves = kRows / 16 / kMB, kStride = 256 / kHalves;   // blocks of rows of a wave, columns of a workgroup's step
-    __shared__ int rows[kRows];
-    __shared__ __align__(16) uint16_t t[kRows * kTPitch];
-    __shared__ __align__(16) uint16_t stages[4][(kFactorA ? 64 : kPass) * kPitch];
-    static_assert(16 * kMB * kOutPitch <= (kFactorA ? 64 : kPass) * kPitch, "out goes through the factor's place");
+__device__ __forceinline__ void wide_tile(const WideArgs& a, int block, WideLds<kRows, kMostR, kFactorA>& lds) {
+    typedef WideLds<kRows, kMostR, kFactorA> Lds;
+    constexpr int kTPitch = Lds::kTPitch, kPass = Lds::kPass, kVectors = kPass / 8, kPitch = Lds::kPitch, kOutPitch = Lds::kOutPitch;
+    constexpr int kMB = Lds::kMB, kHalves = kRows / 16 / kMB, kStride = 256 / kHalves;   // columns of a workgroup's step
+    int* rows = lds.rows;
+    uint16_t* t = lds.t;
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i16 = lane & 15, g = lane >> 4;
     const int C = (int)a.C, across = (C + a.per_group - 1) / a.per_group;
-    const Tile tile = find_tile<kDirect, kRows>(a.tokens, blockIdx.x / across, rows);
+    const Tile tile = find_tile<kDirect, kRows>(a.tokens, block / across, rows);
     if (tile.group < 0) return;
-    const int c_begin = (int)(blockIdx.x % across) * a.per_group, c_end = c_begin + a.per_group < C ? c_begin + a.per_group : C;
+    const int c_begin = block % across * a.per_group, c_end = c_begin + a.per_group < C ? c_begin + a.per_group : C;
     if (tile.group >= a.tokens.n) {   // no adapter: base as it is; an id that is none: NaN
         const bool none = tile.group == a.tokens.n;
         if (none && a.base == a.out) return;
@@ -534,7 +542,7 @@ __global__ __launch_bounds__(256, kMostR > 64 && kRows > 16 ? 1 : 4) void wide_k
         }
     }
     __syncthreads();
-    uint16_t* stage = stages[wave];
+    uint16_t* stage = lds.stages[wave];
     f32x4 acc[kMB][4];
     if (first_row >= tile.count) return;   // (no barrier follows)
     while (c0 < c_end) {
@@ -611,6 +619,12 @@ __global__ __launch_bounds__(256, kMostR > 64 && kRows > 16 ? 1 : 4) void wide_k
     }
 }
 
+template <bool kDirect, int kRows, int kMostR, bool kWhole>
+__global__ __launch_bounds__(256, kMostR > 64 && kRows > 16 ? 1 : 4) void wide_kernel(WideArgs a) {
+    __shared__ __align__(16) WideLds<kRows, kMostR, false> lds;
+    wide_tile<kDirect, kRows, kMostR, false, kWhole>(a, blockIdx.x, lds);
+}
+
 struct OuterArgs {
     Tokens tokens;
     const uint16_t* in[2];   // x (dA), dy (dB)
@@ -631,19 +645,19 @@ struct OuterLds {
 };
 
 template <int kRT, int kCols, bool kWhole, bool second>   // second: dB
-__device__ __forceinline__ void outer_tile(const OuterArgs& a, uint16_t* in_tile, uint16_t* s_tile) {
+__device__ __forceinline__ void outer_tile(const OuterArgs& a, int block, int group, uint16_t* in_tile, uint16_t* s_tile) {
     typedef OuterLds<kRT, kCols> Lds;
     constexpr int kBatch = Lds::kBatch, kTokens = Lds::kTokens, kPitch = Lds::kPitch, kSPitch = Lds::kSPitch;
     constexpr int kCT = kCols / 64, kX = kTokens * kCols / 8 / 256, kS = kTokens * 4 * kRT / 256, kAcross = kCols / 8;
     constexpr int kDeep = kRT < 4 ? 2 : 1;   // batches under way
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i16 = lane & 15, g = lane >> 4;
-    const salr_adapter_t& adapter = a.tokens.list[blockIdx.y];
+    const salr_adapter_t& adapter = a.tokens.list[group];
     uint16_t* out = second ? adapter.db : adapter.da;
     if (out == nullptr) return;
-    const int rank = rank_of(adapter, a.rpad), count = a.tokens.counts[blockIdx.y], start = a.tokens.starts[blockIdx.y];
+    const int rank = rank_of(adapter, a.rpad), count = a.tokens.counts[group], start = a.tokens.starts[group];
     const uint16_t* in = second ? a.in[1] : a.in[0];
     const uint4* s = (second ? a.s[1] : a.s[0]) + (int64_t)start * (a.rpad / 4);
-    const int C = (int)(second ? a.C[1] : a.C[0]), c0 = kCols * ((int)blockIdx.x - (second ? a.blocks0 : 0));
+    const int C = (int)(second ? a.C[1] : a.C[0]), c0 = kCols * (block - (second ? a.blocks0 : 0));
     const int64_t in_total = (int64_t)a.tokens.T * C;
     const int trow = threadIdx.x / kAcross, tvec = threadIdx.x % kAcross;
     for (int rb = 0; rb < rank; rb += 16 * kRT) {
@@ -749,11 +763,25 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, uint16_t* in_tile
     }
 }
 
-template <int kRT, int kCols, bool kWhole>
-__global__ __launch_bounds__(256, 2) void outer_kernel(OuterArgs a) {
-    __shared__ __align__(16) OuterLds<kRT, kCols> lds;
-    if ((int)blockIdx.x < a.blocks0) outer_tile<kRT, kCols, kWhole, false>(a, lds.in_tile, lds.s_tile);
-    else outer_tile<kRT, kCols, kWhole, true>(a, lds.in_tile, lds.s_tile);
+// The second half of the backward pass in one launch: the adapters' gradients, the longest first as far as their order has it, then dx.
+struct BackwardArgs {
+    OuterArgs outer;
+    WideArgs wide;
+    int across, outer_blocks;   // of a gradient pair, of all (0: not wanted)
+};
+template <int kRT, int kCols, int kMostR, bool kWhole>
+__global__ __launch_bounds__(256, kMostR > 64 ? 1 : 2) void backward_kernel(BackwardArgs a) {
+    __shared__ __align__(16) union Lds {
+        OuterLds<kRT, kCols> outer;
+        WideLds<64, kMostR, true> wide;
+    } lds;
+    if ((int)blockIdx.x >= a.outer_blocks) {
+        wide_tile<false, 64, kMostR, true, kWhole>(a.wide, (int)blockIdx.x - a.outer_blocks, lds.wide);
+    } else {
+        const int group = (int)blockIdx.x / a.across, block = (int)blockIdx.x % a.across;
+        if (block < a.outer.blocks0) outer_tile<kRT, kCols, kWhole, false>(a.outer, block, group, lds.outer.in_tile, lds.outer.s_tile);
+        else outer_tile<kRT, kCols, kWhole, true>(a.outer, block, group, lds.outer.in_tile, lds.outer.s_tile);
+    }
 }
 
 // ---- host
@@ -804,33 +832,42 @@ void launch_narrow(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p, b
     });
 }
 
-template <bool kFactorA>
-void launch_wide(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p, const float* part, const uint4* t, int slices, int64_t C) {
-    int64_t per_group = 256;   // as long as the chip has work for every place it has (six workgroups a CU, four of 64 tokens)
+// Columns of a workgroup of wide_tile, as long as the chip has work for every place it has (six workgroups a CU, four of 64 tokens).
+int per_group_of(const RequestAdaptersPlan& p, int64_t C) {
+    int64_t per_group = 256;
     while (per_group < C && p.live * ((C + 2 * per_group - 1) / (2 * per_group)) >= (p.direct ? 1536 : 1024)) per_group *= 2;
-    const WideArgs w{tokens_of(a, p), part, t, slices, p.t_rows, p.rpad, C, (int)per_group, a.base, a.out};
-    const dim3 grid((unsigned)(p.tiles * ((C + per_group - 1) / per_group)));
+    return (int)per_group;
+}
+
+void launch_forward_wide(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p) {
+    const int per_group = per_group_of(p, a.N);
+    const float* part = reinterpret_cast<const float*>(static_cast<char*>(a.workspace) + p.part_x);
+    const WideArgs w{tokens_of(a, p), part, nullptr, p.slices_x, p.t_rows, p.rpad, a.N, per_group, a.base, a.out};
+    const dim3 grid((unsigned)(p.tiles * ((a.N + per_group - 1) / per_group)));
     const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, a.stream, w); };
-    with_whole(C % 8 == 0, [&](auto whole) {
+    with_whole(a.N % 8 == 0, [&](auto whole) {
         constexpr bool kWhole = decltype(whole)::value;
-        if constexpr (!kFactorA)
-            if (p.direct) {
-                p.rpad <= 32 ? run(wide_kernel<true, 16, 32, false, kWhole>) : p.rpad <= 64 ? run(wide_kernel<true, 16, 64, false, kWhole>) : run(wide_kernel<true, 16, 256, false, kWhole>);
-                return;
-            }
-        p.rpad <= 32 ? run(wide_kernel<false, 64, 32, kFactorA, kWhole>) : p.rpad <= 64 ? run(wide_kernel<false, 64, 64, kFactorA, kWhole>) : run(wide_kernel<false, 64, 256, kFactorA, kWhole>);
+        if (p.direct) p.rpad <= 32 ? run(wide_kernel<true, 16, 32, kWhole>) : p.rpad <= 64 ? run(wide_kernel<true, 16, 64, kWhole>) : run(wide_kernel<true, 16, 256, kWhole>);
+        else p.rpad <= 32 ? run(wide_kernel<false, 64, 32, kWhole>) : p.rpad <= 64 ? run(wide_kernel<false, 64, 64, kWhole>) : run(wide_kernel<false, 64, 256, kWhole>);
     });
 }
 
 template <int kCols>
-void launch_outer(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p, const uint4* t_x, const uint4* t_dy) {
-    const int blocks0 = (int)((a.K + kCols - 1) / kCols), blocks1 = (int)((a.N + kCols - 1) / kCols);
-    const OuterArgs o{tokens_of(a, p), {a.x, a.dy}, {t_dy, t_x}, {a.K, a.N}, p.rpad, blocks0};
-    const dim3 grid((unsigned)(blocks0 + blocks1), (unsigned)a.n);
-    const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, a.stream, o); };
+void launch_backward(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p, const uint4* t_x, const uint4* t_dy) {
+    BackwardArgs b{};
+    const int blocks0 = (int)((a.K + kCols - 1) / kCols), blocks1 = (int)((a.N + kCols - 1) / kCols), per_group = per_group_of(p, a.K);
+    b.outer = OuterArgs{tokens_of(a, p), {a.x, a.dy}, {t_dy, t_x}, {a.K, a.N}, p.rpad, blocks0};
+    b.wide = WideArgs{tokens_of(a, p), nullptr, t_dy, 0, p.t_rows, p.rpad, a.K, per_group, a.base, a.out};
+    b.across = blocks0 + blocks1;
+    b.outer_blocks = a.want_dadb ? (int)(b.across * a.n) : 0;
+    const int64_t wide_blocks = a.T > 0 && a.out != nullptr ? p.tiles * ((a.K + per_group - 1) / per_group) : 0;
+    if (b.outer_blocks + wide_blocks == 0) return;
+    const dim3 grid((unsigned)(b.outer_blocks + wide_blocks));
+    const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, a.stream, b); };
     with_whole(a.K % 8 == 0 && a.N % 8 == 0, [&](auto whole) {
         constexpr bool kWhole = decltype(whole)::value;
-        p.rpad <= 16 ? run(outer_kernel<1, kCols, kWhole>) : p.rpad <= 32 ? run(outer_kernel<2, kCols, kWhole>) : run(outer_kernel<4, kCols, kWhole>);
+        if (p.rpad <= 32) p.rpad <= 16 ? run(backward_kernel<1, kCols, 32, kWhole>) : run(backward_kernel<2, kCols, 32, kWhole>);
+        else p.rpad <= 64 ? run(backward_kernel<4, kCols, 64, kWhole>) : run(backward_kernel<4, kCols, 256, kWhole>);
     });
 }
 
@@ -881,7 +918,7 @@ RequestAdaptersPlan request_adapters_plan(int64_t T, int64_t K, int64_t N, int64
 hipError_t launch_request_adapters(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p) {
     if (!p.direct) launch_order(a, p);
     launch_narrow(a, p, true, false);
-    launch_wide<false>(a, p, reinterpret_cast<const float*>(static_cast<char*>(a.workspace) + p.part_x), nullptr, p.slices_x, a.N);
+    launch_forward_wide(a, p);
     return hipGetLastError();
 }
 
@@ -894,11 +931,9 @@ hipError_t launch_request_adapters_backward(const RequestAdaptersArgs& a, const 
         const SumArgs s{{reinterpret_cast<const float*>(w + p.part_dy), reinterpret_cast<const float*>(w + p.part_x)}, {t_dy, t_x}, {p.slices_dy, p.slices_x}, a.T * p.rpad};
         hipLaunchKernelGGL(sum_slices_kernel, dim3((unsigned)((s.count / 4 + 255) / 256), a.want_dadb ? 2 : 1), dim3(256), 0, a.stream, s);
     }
-    if (a.want_dadb) {   // (before dx: it reads what the first products have read)
-        if ((a.K + a.N) / 128 * a.n >= 512) launch_outer<128>(a, p, t_x, t_dy);
-        else launch_outer<64>(a, p, t_x, t_dy);
-    }
-    if (a.T > 0 && a.out != nullptr) launch_wide<true>(a, p, nullptr, t_dy, 0, a.K);
+    // tiles of 128 columns where they are enough for the chip
+    if ((a.K + a.N) / 128 * a.n >= 512) launch_backward<128>(a, p, t_x, t_dy);
+    else launch_backward<64>(a, p, t_x, t_dy);
     return hipGetLastError();
 }
 
