@@ -59,13 +59,29 @@ struct Tile {
     int first;   // of an ordered launch: position of the first
 };
 
-// Tile `self` and, in rows[kRows] (LDS), its tokens, -1 behind the last.  Every thread calls it; ends with a barrier.
+// What is the same for the wave and does not change while a kernel runs comes through the scalar cache: a trip for a table's entry or an adapter's record
+// is what a workgroup's start consists of, and there it is half as long.
+template <typename T>
+__device__ __forceinline__ T scalar_load(const T* p) {
+    typedef const T __attribute__((address_space(4))) * Constant;
+    return *(Constant)(uintptr_t)p;
+}
+struct Adapter {
+    const uint16_t *a, *b;
+    int rank;   // (never more than the launch has room for, whatever the record says)
+};
+__device__ __forceinline__ Adapter adapter_of(const Tokens& k, int group, int rpad) {
+    const salr_adapter_t* record = k.list + group;
+    const int64_t rank = scalar_load(&record->rank);
+    return Adapter{scalar_load(&record->a), scalar_load(&record->b), rank < rpad ? (int)rank : rpad};
+}
+
+// Tile `self`; of a direct launch also its tokens in rows[kRows] (LDS, a barrier behind it).
 template <bool kDirect, int kRows>
 __device__ __forceinline__ Tile find_tile(const Tokens& k, int self, int* rows) {
-    const int lane = lane_id();
     Tile tile{-1, 0, 0};
     if constexpr (kDirect) {
-        const int group = lane < k.T ? group_of(k.ids[lane], k.n) : -2;
+        const int lane = lane_id(), group = lane < k.T ? group_of(k.ids[lane], k.n) : -2;
         const int mine = __builtin_amdgcn_readlane(group, self);
         const uint64_t same = __ballot(group == mine), below = same & (((uint64_t)1 << self) - 1);
         const int before = __popcll(below);
@@ -73,25 +89,20 @@ __device__ __forceinline__ Tile find_tile(const Tokens& k, int self, int* rows) 
         const int place = __popcll(same & (((uint64_t)1 << lane) - 1)) - before, left = __popcll(same) - before;
         tile.group = mine;
         tile.count = left < kRows ? left : kRows;
-        if (threadIdx.x < kRows) rows[threadIdx.x] = -1;
-        __syncthreads();
         if (threadIdx.x < kWave && group == mine && place >= 0 && place < kRows) rows[place] = lane;
+        __syncthreads();
     } else {
-        const int4 t = k.tiles[self];
-        tile = Tile{t.x, t.y, t.z};
-        if (tile.group < 0) return tile;
-        if (threadIdx.x < kRows) rows[threadIdx.x] = (int)threadIdx.x < tile.count ? k.order[tile.first + threadIdx.x] : -1;
+        const AlignedUint4 t = scalar_load(reinterpret_cast<const AlignedUint4*>(k.tiles + self));
+        tile = Tile{(int)t[0], (int)t[1], (int)t[2]};
     }
-    __syncthreads();
     return tile;
 }
 
-// (never more than the launch has room for, whatever the record says)
-__device__ __forceinline__ int rank_of(const salr_adapter_t& adapter, int rpad) {
-    return adapter.rank < rpad ? (int)adapter.rank : rpad;
+// Row j's token (j < count), and its place in the sums of a tile.
+template <bool kDirect>
+__device__ __forceinline__ int token_of(const Tokens& k, const Tile& tile, const int* rows, int j) {
+    return kDirect ? rows[j] : k.order[tile.first + j];
 }
-
-// Row j's place in the sums of a tile.
 template <bool kDirect>
 __device__ __forceinline__ int64_t place_of(const Tile& tile, const int* rows, int j) {
     return kDirect ? rows[j] : tile.first + j;
@@ -266,15 +277,15 @@ __device__ __forceinline__ void narrow_tile(const NarrowArgs& a, const Tile& til
     const int C = (int)(second ? a.C[1] : a.C[0]);
     const int64_t in_total = (int64_t)a.tokens.T * C;
     float* part = (second ? a.part[1] : a.part[0]) + (int64_t)z * a.t_rows * a.rpad;
-    const salr_adapter_t& adapter = a.tokens.list[tile.group];
-    const int rank = rank_of(adapter, a.rpad);
+    const Adapter adapter = adapter_of(a.tokens, tile.group, a.rpad);
+    const int rank = adapter.rank;
     const uint16_t* factor = second ? adapter.b : adapter.a;
     const int64_t factor_total = (int64_t)rank * C;
     const int steps = (C + Lds::kCols - 1) / Lds::kCols;
     const int vrow = threadIdx.x >> 4, vcol = 8 * (threadIdx.x & 15);
     int64_t row[kMB];   // (behind the last token the first one's: what comes of it is not stored)
 #pragma unroll
-    for (int i = 0; i < kMB; ++i) row[i] = (int64_t)lds.rows[16 * i + vrow < tile.count ? 16 * i + vrow : 0] * C;
+    for (int i = 0; i < kMB; ++i) row[i] = (int64_t)token_of<kDirect>(a.tokens, tile, lds.rows, 16 * i + vrow < tile.count ? 16 * i + vrow : 0) * C;
     for (int rb = 0; rb < rank; rb += 16 * kRT) {
         const int rts = (rank - rb + 15) / 16 < kRT ? (rank - rb + 15) / 16 : kRT;
         f32x4 acc[kRT] = {};
@@ -446,7 +457,7 @@ __device__ __forceinline__ void wide_tile(const WideArgs& a, int block, WideLds<
         if (none && a.base == a.out) return;
         const int width = (c_end - c_begin + 7) >> 3;
         for (int i = threadIdx.x; i < tile.count * width; i += 256) {
-            const int64_t at = (int64_t)rows[i / width] * C;
+            const int64_t at = (int64_t)token_of<kDirect>(a.tokens, tile, rows, i / width) * C;
             const int c = c_begin + 8 * (i % width), left = c_end - c;
             Eight<false> q{{make_uint4(0, 0, 0, 0)}};
             if (none && a.base != nullptr) q = load_eight<false, false, false>(a.base + at + c, 0, left);
@@ -457,8 +468,8 @@ __device__ __forceinline__ void wide_tile(const WideArgs& a, int block, WideLds<
         }
         return;
     }
-    const salr_adapter_t& adapter = a.tokens.list[tile.group];
-    const int rank = rank_of(adapter, a.rpad), rank16 = (rank + 15) & ~15;
+    const Adapter adapter = adapter_of(a.tokens, tile.group, a.rpad);
+    const int rank = adapter.rank, rank16 = (rank + 15) & ~15;
     const uint16_t* factor = kFactorA ? adapter.a : adapter.b;
     const int64_t factor_total = (int64_t)rank * C;
     uint4 q[kVectors];
@@ -495,7 +506,44 @@ __device__ __forceinline__ void wide_tile(const WideArgs& a, int block, WideLds<
     const int first_row = wave % kHalves * 16 * kMB, vrow = lane >> 3, vcol = 8 * (lane & 7);
     int64_t row[2 * kMB];   // of the vectors of out that this lane reads and writes, eight rows apart; behind the last token -1
 #pragma unroll
-    for (int i = 0; i < 2 * kMB; ++i) row[i] = rows[first_row + 8 * i + vrow] < 0 ? -1 : (int64_t)rows[first_row + 8 * i + vrow] * C;
+    for (int i = 0; i < 2 * kMB; ++i) {
+        const int j = first_row + 8 * i + vrow;
+        const int token = token_of<kDirect>(a.tokens, tile, rows, j < tile.count ? j : 0);
+        row[i] = j < tile.count ? (int64_t)token * C : -1;
+    }
+    // t's live rows; what the others hold comes to nothing that is stored
+    const int quads = rank16 / 4, items = tile.count * quads;
+    if (kRows == 16 && a.slices > 0) {   // four lanes share a quad's slices, every fourth each, and are of one mind
+        const int first = threadIdx.x & 3;
+        for (int i = threadIdx.x >> 2; i < items; i += 64) {
+            const int j = i / quads, r = 4 * (i % quads);
+            const float* from = a.part + place_of<kDirect>(tile, rows, j) * a.rpad + r;
+            f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+            for (int z = first; z < a.slices; z += 4) s += *reinterpret_cast<const f32x4*>(from + z * a.t_rows * a.rpad);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[e] += __shfl_xor(s[e], 1);
+                s[e] += __shfl_xor(s[e], 2);
+            }
+            if (first == 0) *reinterpret_cast<uint4*>(t + j * kTPitch + 2 * r) = two_halves(s);
+        }
+    } else {
+        for (int i = threadIdx.x; i < items; i += 256) {
+            const int j = i / quads, r = 4 * (i % quads);
+            const int64_t at = place_of<kDirect>(tile, rows, j) * a.rpad + r;
+            uint4 h;
+            if (a.slices > 0) {
+                f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+                for (int z = 0; z < a.slices; ++z) s += *reinterpret_cast<const f32x4*>(a.part + z * a.t_rows * a.rpad + at);
+                h = two_halves(s);
+            } else {
+                h = a.t[at >> 2];
+            }
+            *reinterpret_cast<uint4*>(t + j * kTPitch + 2 * r) = h;
+        }
+    }
     uint4 base[2 * kMB] = {};
     const auto request_base = [&](int c0) {   // (behind the last token any row: what comes of it is not stored)
         if (a.base == nullptr) return;
@@ -506,40 +554,6 @@ __device__ __forceinline__ void wide_tile(const WideArgs& a, int block, WideLds<
     if (c0 < c_end) {
         request_base(c0);
         if (rank > 0) request(c0, 0);
-    }
-    if (kRows == 16 && a.slices > 0) {   // four lanes share a quad's slices, every fourth each, and are of one mind
-        for (int i = threadIdx.x >> 2; i < kRows * (rank16 / 4); i += 64) {
-            const int j = i / (rank16 / 4), r = 4 * (i % (rank16 / 4)), first = threadIdx.x & 3;
-            f32x4 s = {0.f, 0.f, 0.f, 0.f};
-            if (j < tile.count) {
-                const float* from = a.part + place_of<kDirect>(tile, rows, j) * a.rpad + r;
-#pragma unroll 4
-                for (int z = first; z < a.slices; z += 4) s += *reinterpret_cast<const f32x4*>(from + z * a.t_rows * a.rpad);
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                s[e] += __shfl_xor(s[e], 1);
-                s[e] += __shfl_xor(s[e], 2);
-            }
-            if (first == 0) *reinterpret_cast<uint4*>(t + j * kTPitch + 2 * r) = two_halves(s);
-        }
-    } else {
-        for (int i = threadIdx.x; i < kRows * (rank16 / 4); i += 256) {
-            const int j = i / (rank16 / 4), r = 4 * (i % (rank16 / 4));
-            uint4 h = make_uint4(0, 0, 0, 0);
-            if (j < tile.count) {
-                const int64_t at = place_of<kDirect>(tile, rows, j) * a.rpad + r;
-                if (a.slices > 0) {
-                    f32x4 s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-                    for (int z = 0; z < a.slices; ++z) s += *reinterpret_cast<const f32x4*>(a.part + z * a.t_rows * a.rpad + at);
-                    h = two_halves(s);
-                } else {
-                    h = a.t[at >> 2];
-                }
-            }
-            *reinterpret_cast<uint4*>(t + j * kTPitch + 2 * r) = h;
-        }
     }
     __syncthreads();
     uint16_t* stage = lds.stages[wave];
@@ -651,10 +665,10 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, int block, int gr
     constexpr int kCT = kCols / 64, kX = kTokens * kCols / 8 / 256, kS = kTokens * 4 * kRT / 256, kAcross = kCols / 8;
     constexpr int kDeep = kRT < 4 ? 2 : 1;   // batches under way
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i16 = lane & 15, g = lane >> 4;
-    const salr_adapter_t& adapter = a.tokens.list[group];
-    uint16_t* out = second ? adapter.db : adapter.da;
+    const salr_adapter_t* record = a.tokens.list + group;
+    uint16_t* out = second ? scalar_load(&record->db) : scalar_load(&record->da);
     if (out == nullptr) return;
-    const int rank = rank_of(adapter, a.rpad), count = a.tokens.counts[group], start = a.tokens.starts[group];
+    const int rank = adapter_of(a.tokens, group, a.rpad).rank, count = scalar_load(a.tokens.counts + group), start = scalar_load(a.tokens.starts + group);
     const uint16_t* in = second ? a.in[1] : a.in[0];
     const uint4* s = (second ? a.s[1] : a.s[0]) + (int64_t)start * (a.rpad / 4);
     const int C = (int)(second ? a.C[1] : a.C[0]), c0 = kCols * (block - (second ? a.blocks0 : 0));
