@@ -4,8 +4,8 @@
 //   dx[t] = dx_base[t] + (dy[t] B_i^T) A_i^T,   dA_i = sum over i's tokens of x[t]^T (dy[t] B_i^T),   dB_i = sum of (x[t] A_i)^T dy[t]
 //
 // Tokens of one adapter are brought together into tiles, whose rows are read and written where they are: nothing is copied.
-//   up to kDirectTokens tokens   a workgroup is a token, finds its fellows among the ids by one comparison across the wave, and goes on if it
-//                                is the first of a tile of 16
+//   up to kDirectTokens tokens   a workgroup is a token, finds its fellows among the ids by comparisons across the wave, and goes on if
+//                                it is the first of a tile of 16
 //   more                         a launch in front orders the tokens by adapter (stable: sums over tokens have an order) and writes a table of tiles of 64
 // Then  narrow_kernel  t = in * factor (K or N columns down to r; fp32 sums over slices of the columns),
 //       wide_kernel    out = base + t * factor (r up to N or K columns),
@@ -37,7 +37,7 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-constexpr int kDirectTokens = 64;
+constexpr int kDirectTokens = 128;   // whole waves
 constexpr int kTileTokens = 64;   // of a launch that orders tokens
 
 struct Tokens {   // how a kernel finds its rows
@@ -81,15 +81,27 @@ template <bool kDirect, int kRows>
 __device__ __forceinline__ Tile find_tile(const Tokens& k, int self, int* rows) {
     Tile tile{-1, 0, 0};
     if constexpr (kDirect) {
-        const int lane = lane_id(), group = lane < k.T ? group_of(k.ids[lane], k.n) : -2;
-        const int mine = __builtin_amdgcn_readlane(group, self);
-        const uint64_t same = __ballot(group == mine), below = same & (((uint64_t)1 << self) - 1);
-        const int before = __popcll(below);
+        constexpr int kChunks = kDirectTokens / kWave;
+        const int lane = lane_id(), mine = group_of(scalar_load(k.ids + self), k.n);
+        bool same[kChunks];
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) same[c] = kWave * c + lane < k.T && group_of(k.ids[kWave * c + lane], k.n) == mine;
+        int before = 0, all = 0, place[kChunks];   // fellows before this one, all of them, and before each
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+            const uint64_t mask = __ballot(same[c]);
+            place[c] = all + __popcll(mask & (((uint64_t)1 << lane) - 1));
+            if (self >= kWave * (c + 1)) before += __popcll(mask);
+            else if (self >= kWave * c) before += __popcll(mask & (((uint64_t)1 << (self - kWave * c)) - 1));
+            all += __popcll(mask);
+        }
         if (before % kRows != 0) return tile;   // the same for the workgroup
-        const int place = __popcll(same & (((uint64_t)1 << lane) - 1)) - before, left = __popcll(same) - before;
         tile.group = mine;
-        tile.count = left < kRows ? left : kRows;
-        if (threadIdx.x < kWave && group == mine && place >= 0 && place < kRows) rows[place] = lane;
+        tile.count = all - before < kRows ? all - before : kRows;
+        if (threadIdx.x < kWave)
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c)
+                if (same[c] && place[c] >= before && place[c] < before + kRows) rows[place[c] - before] = kWave * c + lane;
         __syncthreads();
     } else {
         const AlignedUint4 t = scalar_load(reinterpret_cast<const AlignedUint4*>(k.tiles + self));

@@ -49,7 +49,7 @@ def _set(salr, s, train=False):
     return salr.AdapterSet(a, b, *([[torch.full_like(t, 9.0) for t in l] for l in (a, b)] if train else []))
 
 
-SIZES = [(1, 64, 96), (1, 4096, 4096), (2, 33, 8), (5, 8, 65), (3, 9, 11), (16, 512, 256), (17, 2720, 2731), (63, 100, 517), (64, 1030, 1024), (65, 64, 64), (130, 261, 300),
+SIZES = [(1, 64, 96), (1, 4096, 4096), (2, 33, 8), (5, 8, 65), (3, 9, 11), (16, 512, 256), (17, 2720, 2731), (63, 100, 517), (64, 1030, 1024), (65, 64, 64), (127, 48, 1000), (128, 300, 72), (129, 40, 520), (130, 261, 300),
          (300, 2720, 2731), (1000, 96, 4099), (700, 1600, 40)]
 
 
@@ -128,7 +128,7 @@ def test_adjoint(salr):
 
 def test_tokens_and_adapters_do_not_touch_each_other(salr):
     """NaN and infinities of one token, or of one adapter, stay with its own; an infinity in x is not NaN where the formula has none."""
-    for T in (40, 200):
+    for T in (40, 100, 200):
         s = _made(T, 96, 130, [5, 16, 20], "mixed", 2)
         s["ids"] = torch.arange(T, dtype=torch.int32) % 4 - 1
         x, ids, base, dy = _dev(s, "x", "ids", "base", "dy")
@@ -161,13 +161,14 @@ def test_tokens_and_adapters_do_not_touch_each_other(salr):
 
 def test_a_token_does_not_depend_on_the_others(salr):
     """The same sizes, other fellows: the same bits."""
-    s = _made(60, 500, 300, RANKS, "mixed", 6)
-    adapters = _set(salr, s)
-    x, ids, base = _dev(s, "x", "ids", "base")
-    one = adapters.add(x, ids, base)
-    turn = torch.randperm(60, generator=torch.Generator().manual_seed(1)).to(dev())
-    two = adapters.add(x[turn].contiguous(), ids[turn].contiguous(), base[turn].contiguous())
-    assert torch.equal(one[turn].view(torch.int16), two.view(torch.int16))
+    for T in (60, 120, 500):
+        s = _made(T, 500, 300, RANKS, "mixed", 6)
+        adapters = _set(salr, s)
+        x, ids, base = _dev(s, "x", "ids", "base")
+        one = adapters.add(x, ids, base)
+        turn = torch.randperm(T, generator=torch.Generator().manual_seed(1)).to(dev())
+        two = adapters.add(x[turn].contiguous(), ids[turn].contiguous(), base[turn].contiguous())
+        assert torch.equal(one[turn].view(torch.int16), two.view(torch.int16))
 
 
 def test_neighbours_stay(salr):
@@ -212,7 +213,7 @@ def test_no_tokens(salr):
     assert adapters.add(*_dev(s, "x", "ids", "base")).shape == (0, 96)
 
 
-@pytest.mark.parametrize("T", [20, 300])
+@pytest.mark.parametrize("T", [20, 110, 300])
 def test_captured(salr, T):
     """Ids and inputs change between the replays; what is left in the workspace does not matter."""
     s = _made(T, 416, 600, RANKS, "mixed", 7)
