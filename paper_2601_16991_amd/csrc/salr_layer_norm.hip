@@ -4,12 +4,16 @@
 //   g = dy w,  dx = rstd (g - sum g / K - xhat sum (g xhat) / K) + dsum,  dw = sum over rows of dy xhat,  db = sum over rows of dy
 //
 // What bounds both is memory: every matrix crosses it once.  A team of 1 to 16 waves holds a row in registers, as it lies in memory (8 or 16
-// bytes of registers for four elements), each lane one to four vectors of eight elements; sums go over the lanes in registers and over the
+// bytes of registers for four elements), each lane one to eight vectors of eight elements; sums go over the lanes in registers and over the
 // team's waves through LDS.  The variance is summed from differences to the mean in a second pass over the registers: squares alone lose
 // what a large mean hides.  Sums are fp32.
 //
-// dw and db: a workgroup of eight waves or more goes through rows, its lanes keep the sums of their columns; the teams of a workgroup are added in LDS,
+// dw and db: a workgroup of eight waves goes through rows, its lanes keep the sums of their columns; the teams of a workgroup are added in LDS,
 // in order, and the workgroups' sums, at most kLayerNormParts of them, by a second launch: no atomics, the same bits every time.
+//
+// Measured: 4096 x 4096 bf16, with a residual 24.4 us (134 MB, 5.5 TB/s); its gradient with dsum, dw and db 28.8 us (4.7 TB/s, 4 us of them the second launch;
+// with sixteen waves a workgroup, a row requested when it is needed and the weights read for each, 58 us); one row of 4096 3.1 us of kernel; 1111 x 2721 fp32
+// with dw and db 17.6 us, where the launches' start and end are 10.
 #include <type_traits>
 
 #include "salr_eight.hpp"
@@ -163,7 +167,7 @@ __global__ __launch_bounds__(kTeam < 4 ? 256 : 64 * kTeam) void layer_norm_kerne
 }
 
 // kWeights: dw and db too, the workgroup's sums of them as part[0][blockIdx.x][K] and part[1][..]; a row's requests are then out while the one before is
-// worked on (kAhead), since a workgroup has its CU to itself.
+// worked on (kAhead; not for rows whose sums leave no registers for that), since a workgroup has its CU to itself.
 template <int kTeam, bool kWeights>
 constexpr int grad_waves() { return kWeights ? 8 : kTeam < 4 ? 4 : kTeam; }
 

@@ -7,11 +7,11 @@
 //   up to kDirectTokens tokens   a workgroup is a token, finds its fellows among the ids by comparisons across the wave, and goes on if
 //                                it is the first of a tile of 16
 //   more                         a launch in front orders the tokens by adapter (stable: sums over tokens have an order) and writes a table of tiles of 64
-// Then  narrow_kernel  t = in * factor (K or N columns down to r; fp32 sums over slices of the columns),
-//       wide_kernel    out = base + t * factor (r up to N or K columns),
-//       outer_kernel   the adapters' gradients, sums over tokens.
+// Then  narrow_tile    t = in * factor (K or N columns down to r; fp32 sums over slices of the columns),
+//       wide_tile      out = base + t * factor (r up to N or K columns),
+//       outer_tile     the adapters' gradients, sums over tokens; beside wide_tile for dx in one launch.
 // t goes into the second product as two bf16 values, t rounded and what is left of it: 16 bits of mantissa, so that results are as good as their own
-// rounding (with t rounded once, as the layer does, errors were 1.4 times that).  In wide_kernel the second value is free: an instruction
+// rounding (with t rounded once, as the layer does, errors were 1.4 times that).  In wide_tile the second value is free: an instruction
 // that takes eight values a lane has room for four ranks of both.
 // All on the matrix cores, though memory bounds each (2 r products a byte of x and out at most): tiles of 16 fill them however few rows are live, and
 // what an adapter's factors lack in alignment or length is zeros in LDS.  Results do not depend on which other tokens a call holds, save that
@@ -262,12 +262,15 @@ struct NarrowArgs {
     int rpad;
 };
 
-// part[z][row][r] = sum over the columns c of slice z of in[row][c] * factor(c, r).  A slice is every `slices`-th step of 128 columns, so that the
-// workgroups of a tile, one a slice, read side by side: rows of in and the factor's part come in by whole lines, four rows of 256 bytes a request, and through LDS (as MFMA operands straight from memory,
-// 16 rows of 64 bytes a request, they kept the address unit busy for 84 cycles a request instead of 23: 4096 tokens, 18432 columns, rank 32
-// 51 us).  The requests of two steps are out while one is multiplied.  16x16x32 MFMAs with in as A operand; A's [128 columns, ranks], which lie
-// the wrong way round, are read transposed.  Tiles of 64 rows: a wave has 16 of them; of 16 rows: each has 32 columns of a step, and their sums meet in LDS, in
-// order.  16 kRT ranks a pass.
+// part[z][row][r] = sum over the columns c of slice z of in[row][c] * factor(c, r).  A workgroup has a slice of a tile: every `slices`-th step of 128
+// columns, so that the workgroups of a tile read side by side.  Rows of in and the factor's part come in by whole lines, four rows of 256 bytes a request, and
+// through LDS: as MFMA operands straight from memory, 16 rows of 64 bytes a request, 4096 tokens of 4096 and 14336 columns at rank 32 took 51 us
+// instead of 42, and three times the registers.  The requests of two steps are out while one is multiplied.  16x16x32 MFMAs with in as A operand; A's
+// [128 columns, ranks], which lie the wrong way round, are read transposed.  Tiles of 64 rows: a wave has 16 of them; of 16 rows: each has 32 columns of a
+// step, and their sums meet in LDS, in order.  16 kRT ranks a pass.
+// Memory bounds the large case (40 us for 151 MB of x and dy that no cache has, 48 MB of factors past L2; without multiplying 39.7, without the factors 37.5;
+// one or four workgroups a CU, half or twice as many slices, tiles or slices side by side: all within 2 us), trips to memory the small ones
+// (64 tokens of 40 adapters 6.1 us, one token 3.5).
 template <int kMB, int kRT>
 struct NarrowLds {
     static constexpr int kCols = 128, kPitch = kCols + 8, kRankPitch = 16 * kRT + 8, kSumPitch = 16 * kRT + 4;
@@ -443,6 +446,8 @@ struct WideArgs {
 // + 4 (j % 2) + m % 4): out is read and written in whole vectors.  An instruction takes 16 ranks: four of a lane with t's first half and the same four with its second.
 // kFactorA: the factor is A [C, r] (dx), else B [r, C] (y).
 // kRows: of a tile; of 64, two waves have one half each.
+// The start is four trips to memory one behind the other (the tile, its tokens and the adapter's record, t, base and factor), and with the stores that is what
+// bounds all but the largest calls: 64 tokens of 40 adapters, 4096 -> 14336, 10.5 us (26 MB); 2001 tokens, 2720 -> 2731, 13 us, 11 with N = 2736.
 template <int kRows, int kMostR, bool kFactorA>
 struct WideLds {
     static constexpr int kTPitch = 2 * kMostR + 8, kPass = 32, kPitch = kFactorA ? kPass + 8 : 64 + 8, kOutPitch = 64 + 8;
@@ -661,8 +666,8 @@ struct OuterArgs {
 };
 
 // dA_i [K, r] and dB_i [r, N], sums over the adapter's tokens: workgroup (kCols columns of x or dy, adapter).  Both operands lie with the tokens as
-// rows and are transposed by LDS' transposing read, 32 tokens a step and kBatch steps in flight.  Which of the two is the MFMA's first
-// operand is chosen so that a lane holds four values side by side of the result.  An adapter without tokens gets zeros.
+// rows and are transposed by LDS' transposing read, 32 tokens a step, kBatch steps a batch and up to two batches in flight.  Which of the two is the MFMA's
+// first operand is chosen so that a lane holds four values side by side of the result.  An adapter without tokens gets zeros.
 template <int kRT, int kCols>
 struct OuterLds {
     static constexpr int kBatch = kCols == 64 ? 4 : 2, kTokens = 32 * kBatch, kPitch = kCols + 8, kSPitch = 32 * kRT + 8;
@@ -789,7 +794,8 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, int block, int gr
     }
 }
 
-// The second half of the backward pass in one launch: the adapters' gradients, the longest first as far as their order has it, then dx.
+// The second half of the backward pass in one launch: the adapters' gradients, which read what the first products have read, then dx.  (Two launches: 33 and 21 us for
+// 4096 tokens at 4096 x 14336, rank 32, 53 so; 8 and 9 us for 777 tokens at 2720 x 2744, 13 so.)
 struct BackwardArgs {
     OuterArgs outer;
     WideArgs wide;
