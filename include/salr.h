@@ -617,8 +617,8 @@ salr_status_t salr_adapter_list_check(const salr_adapter_t* adapters, int64_t n,
  *
  *   list, n, max_rank  the records, on the device (8-byte aligned), their number (at least 1) and largest rank (ranks of a record above it are not
  *                      looked at)
- *   x          in   [T, K] bf16;  T < 2^28, T (max_rank + 15) < 2^34, K and N from 8 to 2^22, (K + N) n <= 2^28
- *                      (else SHAPE)
+ *   x          in   [T, K] bf16;  T < 2^28, T (max_rank + 15) < 2^34, K and N from 8 to 2^22, (K + N) (n + T / 1024)
+ *                      <= 2^29 (else SHAPE)
  *   ids        in   [T] int32
  *   base       in   [T, N] bf16, the shared layer's output; NULL = zeros
  *   y          out  [T, N] bf16; may be base, overlaps x and base in no other way
@@ -633,7 +633,9 @@ salr_status_t salr_adapter_list_check(const salr_adapter_t* adapters, int64_t n,
  *   dx_base    in   [T, K] bf16, the shared layer's dx; NULL = zeros
  *   dx         out  [T, K] bf16; may be dx_base; NULL = not computed.  NaN for a token whose id is not below n, which is in no adapter's gradient
  *   want_gradients  not 0: da and db of every record that has them are written; those of an adapter without a token as zeros
- *   workspace  --   salr_adapters_backward_workspace_bytes(T, K, N, n, max_rank, want_gradients) bytes, 256-byte aligned
+ *   workspace  --   salr_adapters_backward_workspace_bytes(T, K, N, n, max_rank, want_gradients) bytes, 256-byte aligned.  With gradients of
+ *                   more than 256 to 4096 tokens (from how many on follows from the sizes) it holds sums of chunks of them:
+ *                   8 (K + N) max_rank bytes for each chunk of as many
  *
  * bf16 in and out, fp32 sums; x A and dy B^T go into the second product as two bf16 values each (16 bits of mantissa).  Results are the same bit for bit
  * from call to call.  A token's infinity or NaN, or an adapter's, makes infinities or NaN of its own results only (and NaN of some that would be

@@ -71,7 +71,7 @@ salr_status_t adapters_sizes(int64_t T, int64_t K, int64_t N, int64_t n, int64_t
     const auto fits = [](int64_t columns) { return columns >= salr::kAdaptersLeastColumns && columns <= salr::kAdaptersMostColumns; };
     if (T > salr::kAdaptersMostT || !fits(K) || !fits(N) || n > salr::kAdaptersMostCount) return SALR_ERR_SHAPE;
     if (T * (max_rank + 15) >= (int64_t)1 << 34) return SALR_ERR_SHAPE;   // (four of its values a thread)
-    if ((K + N) * n > (int64_t)1 << 28) return SALR_ERR_SHAPE;            // (64 columns of an adapter a workgroup)
+    if ((K + N) * (n + T / 1024) > (int64_t)1 << 29) return SALR_ERR_SHAPE;   // (128 columns of a chunk of an adapter's tokens a workgroup)
     return SALR_OK;
 }
 

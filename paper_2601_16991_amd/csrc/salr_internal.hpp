@@ -923,7 +923,8 @@ struct RequestAdaptersPlan {
     int64_t t_rows;          // rows of the products with the first factor
     int rpad;                // their columns
     int slices_x, slices_dy; // slices of K and N that they are summed over
-    size_t order, starts, counts, table, part_x, part_dy, t_x, t_dy;   // offsets in the workspace
+    int chunk;               // backward: tokens of a chunk of the gradients' sums
+    size_t order, starts, counts, table, chunks, sums, part_x, part_dy, t_x, t_dy;   // offsets in the workspace
     size_t bytes;
 };
 RequestAdaptersPlan request_adapters_plan(int64_t T, int64_t K, int64_t N, int64_t n, int64_t max_rank, bool backward, bool want_dadb);

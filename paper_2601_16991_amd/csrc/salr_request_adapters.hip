@@ -193,7 +193,8 @@ __device__ __forceinline__ uint4 two_halves(f32x4 v) {
 // Group g, whose tokens start at place s, has the entries s / 64 + g and on of the table of tiles, up to the next group's, which are enough for its tiles
 // whatever s: so nobody has to know how many tiles the groups before have.  What is left over is marked as empty.
 constexpr int kOrderEach = 8;
-__global__ __launch_bounds__(1024) void order_tokens_kernel(const int32_t* ids, int T, int n, int32_t* order, int32_t* starts, int32_t* counts, int4* tiles) {
+__global__ __launch_bounds__(1024) void order_tokens_kernel(const int32_t* ids, int T, int n, int32_t* order, int32_t* starts, int32_t* counts, int4* tiles,
+                                                            int chunk, int4* chunks) {
     __shared__ uint32_t scratch[17];
     __shared__ int total[2][16];
     const int group = blockIdx.x, wave = threadIdx.x >> 6;
@@ -241,6 +242,14 @@ __global__ __launch_bounds__(1024) void order_tokens_kernel(const int32_t* ids, 
     for (int i = threadIdx.x; i < entries; i += 1024) {
         const int left = count - kTileTokens * i;
         tiles[entry + i] = make_int4(left > 0 ? group : -1, left < kTileTokens ? left : kTileTokens, at + kTileTokens * i, 0);
+    }
+    if (chunks != nullptr) {   // the table of chunks, likewise: an adapter's first entry is there even without a token, for its gradients' zeros
+        const int first = at / chunk + group, last = (at + count) / chunk + group;
+        for (int i = threadIdx.x; first + i <= last; i += 1024) {
+            const int left = count - chunk * i;
+            chunks[first + i] = make_int4(group < n && (i == 0 || left > 0) ? group : -1, at + chunk * i, left < 0 ? 0 : left < chunk ? left : chunk,
+                                          count > chunk ? 2 * (at / chunk) + i : -1);
+        }
     }
     if (count == 0) return;
     for (int64_t t0 = 0; t0 < T; t0 += 1024 * kOrderEach) {
@@ -662,30 +671,36 @@ struct OuterArgs {
     const uint4* s[2];       // dy B^T (dA), x A (dB): [T][rpad / 4] by position, as two_halves has them
     int64_t C[2];
     int rpad;
-    int blocks0;             // of kCols columns: of x
+    int blocks0;             // of kOuterCols columns: of x
+    const int4* chunks;      // adapter (-1: none), place of the first token, tokens, and where its sums go: -1 to the gradient, else one of
+    float* sums;             // [slots][K rpad + rpad N]
 };
+constexpr int kOuterCols = 128;
 
-// dA_i [K, r] and dB_i [r, N], sums over the adapter's tokens: workgroup (kCols columns of x or dy, adapter).  Both operands lie with the tokens as
-// rows and are transposed by LDS' transposing read, 32 tokens a step, kBatch steps a batch and up to two batches in flight.  Which of the two is the MFMA's
+// dA_i [K, r] and dB_i [r, N], sums over the adapter's tokens: workgroup (128 columns of x or dy, chunk of an adapter's tokens).  An adapter with more tokens than
+// a chunk has its sums joined by the launch behind, in order; a workgroup that went through 4096 tokens, 1.4 us for each 64, would be all there is to
+// wait for (one adapter of rank 64 at 4096 x 4096: 91 us).  Both operands lie with the tokens as rows and are transposed by LDS' transposing read, 32 tokens a step, kBatch steps a batch and up to two batches in flight.  Which of the two is the MFMA's
 // first operand is chosen so that a lane holds four values side by side of the result.  An adapter without tokens gets zeros.
-template <int kRT, int kCols>
+template <int kRT>
 struct OuterLds {
-    static constexpr int kBatch = kCols == 64 ? 4 : 2, kTokens = 32 * kBatch, kPitch = kCols + 8, kSPitch = 32 * kRT + 8;
+    static constexpr int kCols = kOuterCols, kBatch = 2, kTokens = 32 * kBatch, kPitch = kCols + 8, kSPitch = 32 * kRT + 8;
     uint16_t in_tile[kTokens * kPitch];
     uint16_t s_tile[kTokens * kSPitch];
 };
 
-template <int kRT, int kCols, bool kWhole, bool second>   // second: dB
-__device__ __forceinline__ void outer_tile(const OuterArgs& a, int block, int group, uint16_t* in_tile, uint16_t* s_tile) {
-    typedef OuterLds<kRT, kCols> Lds;
-    constexpr int kBatch = Lds::kBatch, kTokens = Lds::kTokens, kPitch = Lds::kPitch, kSPitch = Lds::kSPitch;
+template <int kRT, bool kWhole, bool second>   // second: dB
+__device__ __forceinline__ void outer_tile(const OuterArgs& a, int block, const AlignedUint4& chunk, uint16_t* in_tile, uint16_t* s_tile) {
+    typedef OuterLds<kRT> Lds;
+    constexpr int kCols = kOuterCols, kBatch = Lds::kBatch, kTokens = Lds::kTokens, kPitch = Lds::kPitch, kSPitch = Lds::kSPitch;
     constexpr int kCT = kCols / 64, kX = kTokens * kCols / 8 / 256, kS = kTokens * 4 * kRT / 256, kAcross = kCols / 8;
-    constexpr int kDeep = kRT < 4 ? 2 : 1;   // batches under way
+    // batches under way (two of rank 64 hold registers that a second workgroup would need: 4096 tokens at 4096 x 4096 39.5 us with one, 46.5 with two)
+    constexpr int kDeep = kRT < 4 ? 2 : 1;
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i16 = lane & 15, g = lane >> 4;
+    const int group = (int)chunk[0], start = (int)chunk[1], count = (int)chunk[2], slot = (int)chunk[3];
     const salr_adapter_t* record = a.tokens.list + group;
     uint16_t* out = second ? scalar_load(&record->db) : scalar_load(&record->da);
     if (out == nullptr) return;
-    const int rank = adapter_of(a.tokens, group, a.rpad).rank, count = scalar_load(a.tokens.counts + group), start = scalar_load(a.tokens.starts + group);
+    const int rank = adapter_of(a.tokens, group, a.rpad).rank;
     const uint16_t* in = second ? a.in[1] : a.in[0];
     const uint4* s = (second ? a.s[1] : a.s[0]) + (int64_t)start * (a.rpad / 4);
     const int C = (int)(second ? a.C[1] : a.C[0]), c0 = kCols * (block - (second ? a.blocks0 : 0));
@@ -779,6 +794,13 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, int block, int gr
                 const int r = rb + 16 * rt + (second ? i16 : 4 * g), c = c0 + 16 * (kCT * wave + ct) + (second ? 4 * g : i16);
                 if (r >= rank || c >= C) continue;
                 const int left = second ? C - c : rank - r;
+                if (slot >= 0) {   // [K][rpad], then [rpad][N]
+                    float* to = a.sums + (int64_t)slot * (a.C[0] + a.C[1]) * a.rpad + (second ? a.C[0] * a.rpad + (int64_t)r * C + c : (int64_t)c * a.rpad + r);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (i < left) to[i] = acc[ct][rt][i];
+                    continue;
+                }
                 uint16_t* to = second ? out + (int64_t)r * C + c : out + (int64_t)c * rank + r;
                 uint16_t e[4];
 #pragma unroll
@@ -799,20 +821,50 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, int block, int gr
 struct BackwardArgs {
     OuterArgs outer;
     WideArgs wide;
-    int across, outer_blocks;   // of a gradient pair, of all (0: not wanted)
+    int across, outer_blocks;   // of a chunk, of all (0: not wanted)
 };
-template <int kRT, int kCols, int kMostR, bool kWhole>
+template <int kRT, int kMostR, bool kWhole>
 __global__ __launch_bounds__(256, kMostR > 64 ? 1 : 2) void backward_kernel(BackwardArgs a) {
     __shared__ __align__(16) union Lds {
-        OuterLds<kRT, kCols> outer;
+        OuterLds<kRT> outer;
         WideLds<64, kMostR, true> wide;
     } lds;
     if ((int)blockIdx.x >= a.outer_blocks) {
         wide_tile<false, 64, kMostR, true, kWhole>(a.wide, (int)blockIdx.x - a.outer_blocks, lds.wide);
     } else {
-        const int group = (int)blockIdx.x / a.across, block = (int)blockIdx.x % a.across;
-        if (block < a.outer.blocks0) outer_tile<kRT, kCols, kWhole, false>(a.outer, block, group, lds.outer.in_tile, lds.outer.s_tile);
-        else outer_tile<kRT, kCols, kWhole, true>(a.outer, block, group, lds.outer.in_tile, lds.outer.s_tile);
+        const AlignedUint4 chunk = scalar_load(reinterpret_cast<const AlignedUint4*>(a.outer.chunks + (int)blockIdx.x / a.across));
+        const int block = (int)blockIdx.x % a.across;
+        if ((int)chunk[0] < 0) return;
+        if (block < a.outer.blocks0) outer_tile<kRT, kWhole, false>(a.outer, block, chunk, lds.outer.in_tile, lds.outer.s_tile);
+        else outer_tile<kRT, kWhole, true>(a.outer, block, chunk, lds.outer.in_tile, lds.outer.s_tile);
+    }
+}
+
+// The gradients of adapters of several chunks: workgroup (share of the values, adapter).
+struct JoinArgs {
+    Tokens tokens;
+    const float* sums;
+    int64_t K, N;
+    int rpad, chunk;
+};
+__global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
+    const int group = blockIdx.y, count = scalar_load(a.tokens.counts + group), start = scalar_load(a.tokens.starts + group);
+    if (count <= a.chunk) return;
+    const salr_adapter_t* record = a.tokens.list + group;
+    uint16_t *da = scalar_load(&record->da), *db = scalar_load(&record->db);
+    const int rank = adapter_of(a.tokens, group, a.rpad).rank, slots = (count + a.chunk - 1) / a.chunk;
+    const int64_t slot = (a.K + a.N) * a.rpad, of_a = a.K * rank, all = of_a + a.N * rank;
+    const float* sums = a.sums + 2 * (start / a.chunk) * slot;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const bool second = i >= of_a;
+        uint16_t* out = second ? db : da;
+        if (out == nullptr) continue;
+        const int64_t at = second ? i - of_a : i;
+        const float* from = sums + (second ? a.K * a.rpad + at : at / rank * a.rpad + at % rank);
+        float s = 0.f;
+#pragma unroll 8
+        for (int z = 0; z < slots; ++z) s += from[z * slot];
+        out[at] = f32_to_bf16_rne(s);
     }
 }
 
@@ -842,7 +894,7 @@ void launch_order(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p) {
     char* w = static_cast<char*>(a.workspace);
     hipLaunchKernelGGL(order_tokens_kernel, dim3((unsigned)a.n + 2), dim3(1024), 0, a.stream, a.ids, (int)a.T, (int)a.n,
                        reinterpret_cast<int32_t*>(w + p.order), reinterpret_cast<int32_t*>(w + p.starts), reinterpret_cast<int32_t*>(w + p.counts),
-                       reinterpret_cast<int4*>(w + p.table));
+                       reinterpret_cast<int4*>(w + p.table), p.chunk, p.chunk > 0 ? reinterpret_cast<int4*>(w + p.chunks) : nullptr);
 }
 
 template <typename Run>
@@ -884,23 +936,37 @@ void launch_forward_wide(const RequestAdaptersArgs& a, const RequestAdaptersPlan
     });
 }
 
-template <int kCols>
 void launch_backward(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p, const uint4* t_x, const uint4* t_dy) {
+    char* workspace = static_cast<char*>(a.workspace);
+    float* sums = reinterpret_cast<float*>(workspace + p.sums);
     BackwardArgs b{};
-    const int blocks0 = (int)((a.K + kCols - 1) / kCols), blocks1 = (int)((a.N + kCols - 1) / kCols), per_group = per_group_of(p, a.K);
-    b.outer = OuterArgs{tokens_of(a, p), {a.x, a.dy}, {t_dy, t_x}, {a.K, a.N}, p.rpad, blocks0};
+    const int blocks0 = (int)((a.K + kOuterCols - 1) / kOuterCols), blocks1 = (int)((a.N + kOuterCols - 1) / kOuterCols), per_group = per_group_of(p, a.K);
+    b.outer = OuterArgs{tokens_of(a, p), {a.x, a.dy}, {t_dy, t_x}, {a.K, a.N}, p.rpad, blocks0, reinterpret_cast<const int4*>(workspace + p.chunks), sums};
     b.wide = WideArgs{tokens_of(a, p), nullptr, t_dy, 0, p.t_rows, p.rpad, a.K, per_group, a.base, a.out};
     b.across = blocks0 + blocks1;
-    b.outer_blocks = a.want_dadb ? (int)(b.across * a.n) : 0;
+    b.outer_blocks = a.want_dadb ? (int)(b.across * (a.T / p.chunk + a.n)) : 0;
     const int64_t wide_blocks = a.T > 0 && a.out != nullptr ? p.tiles * ((a.K + per_group - 1) / per_group) : 0;
     if (b.outer_blocks + wide_blocks == 0) return;
     const dim3 grid((unsigned)(b.outer_blocks + wide_blocks));
     const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, a.stream, b); };
     with_whole(a.K % 8 == 0 && a.N % 8 == 0, [&](auto whole) {
         constexpr bool kWhole = decltype(whole)::value;
-        if (p.rpad <= 32) p.rpad <= 16 ? run(backward_kernel<1, kCols, 32, kWhole>) : run(backward_kernel<2, kCols, 32, kWhole>);
-        else p.rpad <= 64 ? run(backward_kernel<4, kCols, 64, kWhole>) : run(backward_kernel<4, kCols, 256, kWhole>);
+        if (p.rpad <= 32) p.rpad <= 16 ? run(backward_kernel<1, 32, kWhole>) : run(backward_kernel<2, 32, kWhole>);
+        else p.rpad <= 64 ? run(backward_kernel<4, 64, kWhole>) : run(backward_kernel<4, 256, kWhole>);
     });
+    if (a.want_dadb && a.T > p.chunk)
+        hipLaunchKernelGGL(join_kernel, dim3((unsigned)(a.n < 16 ? 2048 / a.n : 128), (unsigned)a.n), dim3(256), 0, a.stream, JoinArgs{tokens_of(a, p), sums, a.K, a.N, p.rpad, p.chunk});
+}
+
+// Tokens of a chunk of the gradients' sums.  Adapters enough for two workgroups a CU: 4096, since a chunk less costs a launch, and the sums a trip through memory
+// (4096 tokens of eight adapters, 4096 x 14336, rank 32: 97 us so, 112 with chunks of 1024).  Else as few as there are workgroups for, if the
+// batch were one adapter's: 4096 tokens of one adapter at 512 x 512 rank 16 43 us in one chunk, 13 so; at 4096 x 4096 rank 64 91 and 45.
+int chunk_of(int64_t T, int64_t K, int64_t N, int64_t n) {
+    const int64_t across = (K + N + kOuterCols - 1) / kOuterCols;
+    if (across * (n < T ? n : T) >= 512) return 4096;
+    int chunk = 1024;
+    while (chunk > 256 && across * (T / chunk) < 512) chunk /= 2;
+    return chunk;
 }
 
 }  // namespace
@@ -936,6 +1002,11 @@ RequestAdaptersPlan request_adapters_plan(int64_t T, int64_t K, int64_t N, int64
         p.counts = take((size_t)(n + 2) * 4);
         p.table = take((size_t)p.tiles * 16);
     }
+    if (backward) {
+        p.chunk = chunk_of(T, K, N, n);
+        p.chunks = take((size_t)(T / p.chunk + n + 2) * 16);
+        if (want_dadb && T > p.chunk) p.sums = take((size_t)(2 * (T / p.chunk) + 2) * (K + N) * p.rpad * 4);
+    }
     const size_t row = (size_t)T * p.rpad;
     if (!backward || want_dadb) p.part_x = take(row * 4 * p.slices_x);
     if (backward) {
@@ -963,9 +1034,7 @@ hipError_t launch_request_adapters_backward(const RequestAdaptersArgs& a, const 
         const SumArgs s{{reinterpret_cast<const float*>(w + p.part_dy), reinterpret_cast<const float*>(w + p.part_x)}, {t_dy, t_x}, {p.slices_dy, p.slices_x}, a.T * p.rpad};
         hipLaunchKernelGGL(sum_slices_kernel, dim3((unsigned)((s.count / 4 + 255) / 256), a.want_dadb ? 2 : 1), dim3(256), 0, a.stream, s);
     }
-    // tiles of 128 columns where they are enough for the chip
-    if ((a.K + a.N) / 128 * a.n >= 512) launch_backward<128>(a, p, t_x, t_dy);
-    else launch_backward<64>(a, p, t_x, t_dy);
+    launch_backward(a, p, t_x, t_dy);
     return hipGetLastError();
 }
 

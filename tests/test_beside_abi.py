@@ -116,7 +116,7 @@ def test_adapters_arguments(salr):
     for bad in sizes + (dict(list=None), dict(x=None), dict(ids=None), dict(dy=None), dict(ws=None), dict(list=at(0, 4)), dict(dy=at(3, 1)), dict(dx_base=at(4, 1)),
                         dict(dx=at(5, 1)), dict(dx=at(4, 2)), dict(dx=at(1)), dict(dx=at(3, -2)), dict(dx=at(2))):
         assert _grad(salr, **bad) == salr.SALR_ERR_INVALID_ARG, bad
-    for size in (dict(T=1 << 28), dict(K=(1 << 22) + 1), dict(N=(1 << 22) + 1), dict(n=4097), dict(K=1 << 21, N=1 << 21, n=65), dict(T=(1 << 28) - 1, rank=256), dict(K=7), dict(N=7), dict(K=0), dict(N=0)):
+    for size in (dict(T=1 << 28), dict(K=(1 << 22) + 1), dict(N=(1 << 22) + 1), dict(n=4097), dict(K=1 << 21, N=1 << 21, n=129), dict(T=(1 << 28) - 1, rank=256), dict(K=7), dict(N=7), dict(K=0), dict(N=0)):
         assert _add(salr, **size) == salr.SALR_ERR_SHAPE and _grad(salr, **size) == salr.SALR_ERR_SHAPE, size
     for T in (8, 300):
         need = salr.salr_adapters_add_workspace_bytes(T, 64, 96, 3, 16)

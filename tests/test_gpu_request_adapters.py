@@ -109,6 +109,22 @@ def test_backward(salr, T, K, N, kind):
     _backward(salr, s, with_base=False)
 
 
+@pytest.mark.parametrize("T,K,N,ranks", [(257, 64, 96, [16]), (1030, 40, 72, [13, 4]), (2100, 136, 60, [33]), (2600, 100, 4000, [8, 16, 5]), (5000, 264, 1160, [64, 1]), (9000, 72, 640, [4] * 100)])
+def test_many_tokens_of_one_adapter(salr, T, K, N, ranks):
+    """Gradients whose sums are joined: chunks that are full, all but empty, and an adapter beside them that has one."""
+    s = _made(T, K, N, ranks, "one", 11)
+    s["ids"][: T // 20] = 0
+    s["ids"][T // 3] = -1
+    _, dx, grads = _backward(salr, s)
+    _, dx2, again = _backward(salr, s)
+    assert torch.equal(dx, dx2) and all(torch.equal(p, q) for p, q in zip(grads, again))
+    x, dy, ids, dx_base = _dev(s, "x", "dy", "ids", "dx_base")
+    a, b = _dev(s, "a", "b")
+    only = [torch.empty_like(t) for t in b]
+    salr.AdapterSet(a, b, None, only).backward(dy, x, ids)
+    assert all(torch.equal(p, q) for p, q in zip(only, grads[len(a):]))
+
+
 def test_adjoint(salr):
     """(x A) B is linear in x, in A and in B: <dy, y> is <dx, x>, <dA, A> and <dB, B>, as differences along each of them would be."""
     s = _made(150, 320, 512, [16, 13, 64], "prompts", 8)
