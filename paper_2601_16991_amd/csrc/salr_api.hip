@@ -630,7 +630,7 @@ salr_status_t salr_layer_norm_backward(const void* dy, const void* x, const void
     if (overlaps_in_part(dx, dy, bytes) || overlaps_in_part(dx, x, bytes) || overlaps_in_part(dx, dsum, bytes) || overlaps(dx, bytes, weight, wbytes) ||
         overlaps(dx, bytes, mean, stats) || overlaps(dx, bytes, rstd, stats) || overlaps(dw, wbytes, db, wbytes))
         return SALR_ERR_INVALID_ARG;
-    for (const void* out : {dw, db})   // (written by a second launch: after weight, mean and rstd have been read, but dx is out by then)
+    for (const void* out : {dw, db})   // (written beside dx or after it)
         if (overlaps(out, wbytes, dx, bytes) || overlaps(out, wbytes, dy, bytes) || overlaps(out, wbytes, x, bytes) || overlaps(out, wbytes, dsum, bytes) ||
             overlaps(out, wbytes, weight, wbytes) || overlaps(out, wbytes, mean, stats) || overlaps(out, wbytes, rstd, stats))
             return SALR_ERR_INVALID_ARG;

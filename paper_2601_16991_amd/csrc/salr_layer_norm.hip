@@ -9,7 +9,8 @@
 // what a large mean hides.  Sums are fp32.
 //
 // dw and db: a workgroup of eight waves goes through rows, its lanes keep the sums of their columns; the teams of a workgroup are added in LDS,
-// in order, and the workgroups' sums, at most kLayerNormParts of them, by a second launch: no atomics, the same bits every time.
+// in order, and the workgroups' sums, at most kLayerNormParts of them, by a second launch: no atomics, the same bits every time.  Up to kLayerNormFewRows rows
+// workgroups of their own read x and dy again beside those that form dx: one launch.
 //
 // Measured: 4096 x 4096 bf16, with a residual 24.4 us (134 MB, 5.5 TB/s); its gradient with dsum, dw and db 28.8 us (4.7 TB/s, 4 us of them the second launch;
 // with sixteen waves a workgroup, a row requested when it is needed and the weights read for each, 58 us); one row of 4096 3.1 us of kernel; 1111 x 2721 fp32
@@ -172,7 +173,7 @@ template <int kTeam, bool kWeights>
 constexpr int grad_waves() { return kWeights ? 8 : kTeam < 4 ? 4 : kTeam; }
 
 template <bool k32, int kTeam, int kUnits, bool kWhole, bool kWeights>
-__global__ __launch_bounds__((64 * grad_waves<kTeam, kWeights>())) void layer_norm_backward_kernel(LayerNormGradArgs a) {
+__device__ __forceinline__ void backward_rows(const LayerNormGradArgs& a, int blocks) {
     constexpr int kWaves = grad_waves<kTeam, kWeights>(), kTeams = kWaves / kTeam;
     constexpr bool kAhead = kWeights && kUnits <= 2;
     __shared__ float slots[2][kWaves * 2];
@@ -204,7 +205,7 @@ __global__ __launch_bounds__((64 * grad_waves<kTeam, kWeights>())) void layer_no
             if (add) r.ds[u] = row_request<k32, kWhole>(a.dsum, start, i, left, total);
         }
     };
-    const int64_t stride = (int64_t)gridDim.x * kTeams;
+    const int64_t stride = (int64_t)blocks * kTeams;
     Row next;
     if constexpr (kAhead) request(next, (int64_t)blockIdx.x * kTeams + team);
     int parity = 0;
@@ -264,7 +265,7 @@ __global__ __launch_bounds__((64 * grad_waves<kTeam, kWeights>())) void layer_no
     if constexpr (kWeights) {
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
-            float* part = a.part + ((int64_t)which * gridDim.x + blockIdx.x) * K;
+            float* part = a.part + ((int64_t)which * blocks + blockIdx.x) * K;
             for (int t = 0; t < kTeams; ++t) {   // the teams one after the other
                 if (t == team) {
 #pragma unroll
@@ -290,6 +291,73 @@ __global__ __launch_bounds__((64 * grad_waves<kTeam, kWeights>())) void layer_no
             }
         }
     }
+}
+
+template <bool k32, int kTeam, int kUnits, bool kWhole, bool kWeights>
+__global__ __launch_bounds__((64 * grad_waves<kTeam, kWeights>())) void layer_norm_backward_kernel(LayerNormGradArgs a) {
+    backward_rows<k32, kTeam, kUnits, kWhole, kWeights>(a, (int)gridDim.x);
+}
+
+// dw and db of 64 columns by one workgroup that goes through all rows, eight lanes a row and four rows a lane at a time: for few rows, beside the workgroups
+// that form dx, instead of a launch behind them.  sums: 128 floats a wave.
+template <bool k32, bool kWhole>
+__device__ __forceinline__ void column_sums(const LayerNormGradArgs& a, int block, void* dw_out, void* db_out, float* sums) {
+    constexpr int kRows = 4;
+    const int K = a.K, c = 64 * block + 8 * (threadIdx.x & 7), left = K - c, waves = blockDim.x >> 6, wave = threadIdx.x >> 6, step = blockDim.x >> 3;
+    const int T = (int)a.T;
+    const int64_t total = a.T * K;
+    float dw[8] = {}, db[8] = {};
+    for (int t = threadIdx.x >> 3; t < T; t += kRows * step) {
+        Eight<k32> xq[kRows], dyq[kRows];
+        float mean[kRows], rstd[kRows];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {   // (rows behind the last: the last again, left out below)
+            const int64_t at = min(t + r * step, T - 1), start = at * K;
+            xq[r] = row_request<k32, kWhole>(a.x, start, c, left, total);
+            dyq[r] = row_request<k32, kWhole>(a.dy, start, c, left, total);
+            mean[r] = a.mean[at];
+            rstd[r] = a.rstd[at];
+        }
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            if (t + r * step >= T) break;
+            const int64_t start = (int64_t)(t + r * step) * K;
+            const Eight<k32> x = row_values<k32, kWhole>(xq[r], start, c, left, total), dy = row_values<k32, kWhole>(dyq[r], start, c, left, total);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                dw[j] = fmaf(dy.get(j), (x.get(j) - mean[r]) * rstd[r], dw[j]);
+                db[j] += dy.get(j);
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int apart = 8; apart < kWave; apart *= 2) {
+            dw[j] += __shfl_xor(dw[j], apart);
+            db[j] += __shfl_xor(db[j], apart);
+        }
+    if (lane_id() < 8)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            sums[128 * wave + 8 * lane_id() + j] = dw[j];
+            sums[128 * wave + 64 + 8 * lane_id() + j] = db[j];
+        }
+    __syncthreads();
+    const int at = 64 * block + (threadIdx.x & 63);
+    void* out = threadIdx.x < 64 ? dw_out : db_out;
+    if (threadIdx.x >= 128 || at >= K || out == nullptr) return;
+    float v = 0.f;
+    for (int w = 0; w < waves; ++w) v += sums[128 * w + threadIdx.x];
+    if (a.w32) static_cast<float*>(out)[at] = v;
+    else static_cast<uint16_t*>(out)[at] = f32_to_bf16_rne(v);
+}
+
+template <bool k32, int kTeam, int kUnits, bool kWhole>
+__global__ __launch_bounds__((64 * grad_waves<kTeam, false>())) void layer_norm_backward_few_kernel(LayerNormGradArgs a, int row_blocks, void* dw, void* db) {
+    __shared__ float sums[grad_waves<kTeam, false>() * 128];
+    if ((int)blockIdx.x < row_blocks) backward_rows<k32, kTeam, kUnits, kWhole, false>(a, row_blocks);
+    else column_sums<k32, kWhole>(a, (int)blockIdx.x - row_blocks, dw, db, sums);
 }
 
 // dw (y 0) and db (y 1) from the workgroups' sums, 64 columns a workgroup, every sixteenth part a wave.  parts 0: zeros.
@@ -367,6 +435,27 @@ hipError_t launch_layer_norm_backward(const LayerNormGradArgs& a, void* dw, void
     const auto run = [&](auto kernel, int64_t groups, int threads) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3((unsigned)threads), 0, stream, a);
     };
+    if (a.T > 0 && weights && a.T <= kLayerNormFewRows) {   // (leaves the workspace alone)
+        with_team(a.K, [&](auto waves, auto units) {
+            with_whole(a.K, [&](auto whole) {
+                constexpr int kTeam = waves, kUnits = units, kThreads = 64 * grad_waves<kTeam, false>(), kTeams = kThreads / 64 / kTeam;
+                constexpr bool kWhole = decltype(whole)::value;
+                const int rows = a.dx != nullptr ? (int)((a.T + kTeams - 1) / kTeams) : 0, columns = (a.K + 63) / 64;
+                const auto launch = [&](int row_blocks, int blocks) {
+                    const dim3 grid((unsigned)blocks), block(kThreads);
+                    if (a.f32) hipLaunchKernelGGL((layer_norm_backward_few_kernel<true, kTeam, kUnits, kWhole>), grid, block, 0, stream, a, row_blocks, dw, db);
+                    else hipLaunchKernelGGL((layer_norm_backward_few_kernel<false, kTeam, kUnits, kWhole>), grid, block, 0, stream, a, row_blocks, dw, db);
+                };
+                if (a.dx != nullptr && (a.dx == a.dy || a.dx == a.x)) {   // in place: the rows are written once the columns' workgroups have read them
+                    launch(0, columns);
+                    launch(rows, rows);
+                } else {
+                    launch(rows, rows + columns);
+                }
+            });
+        });
+        return hipGetLastError();
+    }
     if (a.T > 0 && weights)
         with_grad_team(a.K, [&](auto waves, auto units) {
             with_whole(a.K, [&](auto whole) {

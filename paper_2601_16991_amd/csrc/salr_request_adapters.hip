@@ -37,7 +37,9 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-constexpr int kDirectTokens = 128;   // whole waves
+// Whole waves.  128 tokens without an ordering launch against with one, 4096 x 14336 rank 16 of 32 adapters 18.8 us against 23.4, rank 64 of 64 adapters 44
+// against 68, rank 64 of one 23.8 against 25.8; 256 tokens 30.5 against 24.7 (32 adapters) and 30.8 against 25.8 (one of rank 64).
+constexpr int kDirectTokens = 128;
 constexpr int kTileTokens = 64;   // of a launch that orders tokens
 
 struct Tokens {   // how a kernel finds its rows
@@ -916,7 +918,8 @@ void launch_narrow(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p, b
     });
 }
 
-// Columns of a workgroup of wide_tile, as long as the chip has work for every place it has (six workgroups a CU, four of 64 tokens).
+// Columns of a workgroup of wide_tile: 256, and twice as many as long as the chip has work for every place it has (six workgroups a CU, four of 64 tokens).
+// 777 tokens, 2720 columns: 23 us in 1088 workgroups, 29 in 544 (and 26 in steps of 128 columns).
 int per_group_of(const RequestAdaptersPlan& p, int64_t C) {
     int64_t per_group = 256;
     while (per_group < C && p.live * ((C + 2 * per_group - 1) / (2 * per_group)) >= (p.direct ? 1536 : 1024)) per_group *= 2;

@@ -162,6 +162,26 @@ def test_in_place(salr):
         assert torch.equal(d[at], dx) and torch.equal(dw2, dw) and torch.equal(db2, db)
 
 
+@pytest.mark.parametrize("T,K", [(255, 264), (256, 1031), (257, 1031), (256, 16384)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_backward_about_few_rows(salr, T, K, dtype):
+    """The numbers of rows between which the sums of dw and db move into the launch that forms dx; dx apart, in dy's place and in x's."""
+    s = _inputs(T, K, dtype, torch.float32, 11)
+    x = s["x"].double()
+    mean = x.mean(1).float()
+    rstd = (x.var(1, unbiased=False) + 1e-5).rsqrt().float()
+    want, tol = ref.layer_norm_backward(s["dy"], s["x"], s["weight"], mean, rstd, s["dsum"])
+    ws = torch.empty(salr.salr_layer_norm_backward_workspace_bytes(T, K, True), dtype=torch.uint8, device=dev())
+    for at in (None, "dy", "x"):
+        d = {k: t.to(dev()) for k, t in s.items()}
+        dx = torch.empty_like(d["x"]) if at is None else d[at]
+        dw, db = torch.empty(K, device=dev()), torch.empty(K, device=dev())
+        salr.salr_layer_norm_backward(d["dy"], d["x"], d["weight"], mean.to(dev()), rstd.to(dev()), d["dsum"], dx, dw, db, ws)
+        ref.close(dx, want[0], tol[0], dtype)
+        ref.close(dw, want[1], tol[1], torch.float32)
+        ref.close(db, want[2], tol[2], torch.float32)
+
+
 @pytest.mark.parametrize("K", [9, 515, 4099])
 def test_neighbours_stay(salr, K):
     s = _inputs(5, K, torch.bfloat16, torch.float32)
