@@ -547,7 +547,7 @@ salr_status_t salr_grad_norm(const void* plan, int64_t chunks, salr_type_t grad_
  *                     they were at its capture: a program that replays a step changes *seed_device between the replays
  *   y            out  [count] of `type`; may be x or residual, else overlaps neither
  * Errors: INVALID_ARG (null where data is required, negative count, a type that is none, p outside [0, 1) or with c = 65536, a pointer that is
- * not aligned to its type, y overlapping x or residual in part), SHAPE (count > 2^42), HIP.
+ * not aligned to its type, y overlapping x or residual in part or seed_device), SHAPE (count > 2^42), HIP.
  */
 salr_status_t salr_dropout(const void* x, const void* residual, int64_t count, salr_type_t type, double p, int64_t seed, const int64_t* seed_device,
                            int64_t offset, void* y, void* stream);
@@ -581,7 +581,8 @@ salr_status_t salr_dropout(const void* x, const void* residual, int64_t count, s
  *   dw, db       out  [K] of `weight_type`, fp32 sums rounded once; NULL = not computed (a frozen norm).  T == 0 writes zeros
  *   workspace    --   salr_layer_norm_backward_workspace_bytes(T, K, dw or db wanted) bytes, 16-byte aligned; contents unspecified
  * Results are the same bit for bit from call to call.
- * Errors: as above, and CAPACITY.  The workspace query returns 0 for sizes the call would refuse.
+ * Errors: as above, INVALID_ARG also for a workspace that overlaps a tensor of the call, and CAPACITY.  The workspace query returns 0 for sizes the call
+ * would refuse.
  */
 salr_status_t salr_layer_norm(const void* x, const void* residual, const void* weight, const void* bias, int64_t T, int64_t K, salr_type_t type,
                               salr_type_t weight_type, double eps, void* y, void* sum, float* mean, float* rstd, void* stream);
@@ -641,7 +642,7 @@ salr_status_t salr_adapter_list_check(const salr_adapter_t* adapters, int64_t n,
  * from call to call.  A token's infinity or NaN, or an adapter's, makes infinities or NaN of its own results only (and NaN of some that would be
  * infinite: an infinite factor meets the second value, which may be zero).
  * Errors of both: INVALID_ARG (null where data is required, negative size, n < 1, max_rank outside [0, 256], a misaligned pointer (x, base, y, dy, dx_base,
- * dx: to 2 bytes; ids: to 4), an output that overlaps an input otherwise than told), SHAPE, CAPACITY, HIP.  The queries return 0 for sizes that are refused.
+ * dx: to 2 bytes; ids: to 4), an output that overlaps an input otherwise than told, a workspace that overlaps a tensor of the call or the list), SHAPE, CAPACITY, HIP.  The queries return 0 for sizes that are refused.
  */
 size_t salr_adapters_add_workspace_bytes(int64_t T, int64_t K, int64_t N, int64_t n, int64_t max_rank);
 salr_status_t salr_adapters_add(const salr_adapter_t* list, int64_t n, int64_t max_rank, const uint16_t* x, int64_t T, int64_t K, int64_t N,

@@ -576,7 +576,8 @@ salr_status_t salr_dropout(const void* x, const void* residual, int64_t count, s
     const uintptr_t size = type == SALR_F32 ? 4 : 2;
     if (!x || !y || misaligned(x, size) || misaligned(residual, size) || misaligned(y, size) || misaligned(seed_device, 8)) return SALR_ERR_INVALID_ARG;
     if (count > (int64_t)1 << 42) return SALR_ERR_SHAPE;
-    if (overlaps_in_part(x, y, (size_t)count * size) || overlaps_in_part(residual, y, (size_t)count * size)) return SALR_ERR_INVALID_ARG;
+    if (overlaps_in_part(x, y, (size_t)count * size) || overlaps_in_part(residual, y, (size_t)count * size) || overlaps(y, (size_t)count * size, seed_device, 8))
+        return SALR_ERR_INVALID_ARG;
     const salr::DropoutArgs args{x, residual, count, cut, seed, seed_device, offset, y, type == SALR_F32};
     const hipError_t e = salr::launch_dropout(args, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? SALR_OK : SALR_ERR_HIP;
@@ -637,6 +638,11 @@ salr_status_t salr_layer_norm_backward(const void* dy, const void* x, const void
     const size_t need = salr_layer_norm_backward_workspace_bytes(T, K, weights);
     if (workspace_bytes < need) return SALR_ERR_CAPACITY;
     if (need > 0 && !workspace) return SALR_ERR_INVALID_ARG;
+    for (const void* p : {dy, x, dsum, static_cast<const void*>(dx)})
+        if (overlaps(workspace, need, p, bytes)) return SALR_ERR_INVALID_ARG;
+    for (const void* p : {weight, static_cast<const void*>(dw), static_cast<const void*>(db)})
+        if (overlaps(workspace, need, p, wbytes)) return SALR_ERR_INVALID_ARG;
+    if (overlaps(workspace, need, mean, stats) || overlaps(workspace, need, rstd, stats)) return SALR_ERR_INVALID_ARG;
     const salr::LayerNormGradArgs args{dy, x, weight, mean, rstd, dsum, T, (int)K, dx, static_cast<float*>(workspace), type == SALR_F32, weight_type == SALR_F32};
     const hipError_t e = salr::launch_layer_norm_backward(args, dw, db, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? SALR_OK : SALR_ERR_HIP;
@@ -670,11 +676,14 @@ salr_status_t salr_adapters_add(const salr_adapter_t* list, int64_t n, int64_t m
     if (T == 0) return SALR_OK;
     if (!list || !x || !ids || !y) return SALR_ERR_INVALID_ARG;
     if (misaligned(list, 8) || misaligned(x, 2) || misaligned(ids, 4) || misaligned(base, 2) || misaligned(y, 2) || misaligned(workspace, 256)) return SALR_ERR_INVALID_ARG;
-    const size_t bytes = (size_t)(T * N) * 2;
-    if (overlaps_in_part(y, base, bytes) || overlaps(y, bytes, x, (size_t)(T * K) * 2) || overlaps(y, bytes, ids, (size_t)T * 4)) return SALR_ERR_INVALID_ARG;
+    const size_t bytes = (size_t)(T * N) * 2, in_bytes = (size_t)(T * K) * 2, ids_bytes = (size_t)T * 4, list_bytes = (size_t)n * sizeof(salr_adapter_t);
+    if (overlaps_in_part(y, base, bytes) || overlaps(y, bytes, x, in_bytes) || overlaps(y, bytes, ids, ids_bytes) || overlaps(y, bytes, list, list_bytes))
+        return SALR_ERR_INVALID_ARG;
     const salr::RequestAdaptersPlan plan = salr::request_adapters_plan(T, K, N, n, max_rank, false, false);
     if (workspace_bytes < plan.bytes) return SALR_ERR_CAPACITY;
-    if (!workspace) return SALR_ERR_INVALID_ARG;
+    if (!workspace || overlaps(workspace, plan.bytes, y, bytes) || overlaps(workspace, plan.bytes, base, bytes) || overlaps(workspace, plan.bytes, x, in_bytes) ||
+        overlaps(workspace, plan.bytes, ids, ids_bytes) || overlaps(workspace, plan.bytes, list, list_bytes))
+        return SALR_ERR_INVALID_ARG;
     const salr::RequestAdaptersArgs args{list, n, x, nullptr, T, K, N, ids, base, y, false, workspace, static_cast<hipStream_t>(stream)};
     const hipError_t e = salr::launch_request_adapters(args, plan);
     return e == hipSuccess ? SALR_OK : SALR_ERR_HIP;
@@ -695,13 +704,15 @@ salr_status_t salr_adapters_backward(const salr_adapter_t* list, int64_t n, int6
     if (misaligned(list, 8) || misaligned(x, 2) || misaligned(dy, 2) || misaligned(ids, 4) || misaligned(dx_base, 2) || misaligned(dx, 2) ||
         misaligned(workspace, 256))
         return SALR_ERR_INVALID_ARG;
-    const size_t bytes = (size_t)(T * K) * 2;
-    if (overlaps_in_part(dx, dx_base, bytes) || overlaps(dx, bytes, x, bytes) || overlaps(dx, bytes, dy, (size_t)(T * N) * 2) ||
-        overlaps(dx, bytes, ids, (size_t)T * 4))
+    const size_t bytes = (size_t)(T * K) * 2, in_bytes = (size_t)(T * N) * 2, ids_bytes = (size_t)T * 4, list_bytes = (size_t)n * sizeof(salr_adapter_t);
+    if (overlaps_in_part(dx, dx_base, bytes) || overlaps(dx, bytes, x, bytes) || overlaps(dx, bytes, dy, in_bytes) || overlaps(dx, bytes, ids, ids_bytes) ||
+        overlaps(dx, bytes, list, list_bytes))
         return SALR_ERR_INVALID_ARG;
     const salr::RequestAdaptersPlan plan = salr::request_adapters_plan(T, K, N, n, max_rank, true, want_gradients != 0);
     if (workspace_bytes < plan.bytes) return SALR_ERR_CAPACITY;
-    if (!workspace) return SALR_ERR_INVALID_ARG;
+    if (!workspace || overlaps(workspace, plan.bytes, dx, bytes) || overlaps(workspace, plan.bytes, dx_base, bytes) || overlaps(workspace, plan.bytes, x, bytes) ||
+        overlaps(workspace, plan.bytes, dy, in_bytes) || overlaps(workspace, plan.bytes, ids, ids_bytes) || overlaps(workspace, plan.bytes, list, list_bytes))
+        return SALR_ERR_INVALID_ARG;
     const salr::RequestAdaptersArgs args{list, n, x, dy, T, K, N, ids, dx_base, dx, want_gradients != 0, workspace, static_cast<hipStream_t>(stream)};
     const hipError_t e = salr::launch_request_adapters_backward(args, plan);
     return e == hipSuccess ? SALR_OK : SALR_ERR_HIP;

@@ -127,3 +127,15 @@ def test_adapters_arguments(salr):
     assert salr.salr_adapters_add_workspace_bytes(8, 64, 96, 0, 16) == 0 and salr.salr_adapters_backward_workspace_bytes(1 << 28, 64, 96, 1, 16, True) == 0
     assert _add(salr, T=0, x=None) == salr.SALR_OK
     assert _grad(salr, want=0, dx=None, dy=None) == salr.SALR_OK and _grad(salr, want=0, T=0, dy=None) == salr.SALR_OK
+
+
+def test_workspaces_and_inputs_that_share_memory(salr):
+    """A workspace over a tensor of the call, results over the list or the seed: refused."""
+    assert _dropout(salr, seed_device=at(3, 8)) == salr.SALR_ERR_INVALID_ARG
+    for i in range(9):
+        assert _norm_grad(salr, ws=at(i)) == salr.SALR_ERR_INVALID_ARG, i
+    for i in range(5):
+        assert _add(salr, ws=at(i)) == salr.SALR_ERR_INVALID_ARG, i
+    for i in range(6):
+        assert _grad(salr, ws=at(i)) == salr.SALR_ERR_INVALID_ARG, i
+    assert _add(salr, y=at(0, 48)) == salr.SALR_ERR_INVALID_ARG and _grad(salr, dx=at(0, 48)) == salr.SALR_ERR_INVALID_ARG
