@@ -92,7 +92,7 @@ __device__ __forceinline__ Tile find_tile(const Tokens& k, int self, int* rows) 
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) {
             const uint64_t mask = __ballot(same[c]);
-            place[c] = all + __popcll(mask & (((uint64_t)1 << lane) - 1));
+            place[c] = all + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));   // fellows on the lanes before this one
             if (self >= kWave * (c + 1)) before += __popcll(mask);
             else if (self >= kWave * c) before += __popcll(mask & (((uint64_t)1 << (self - kWave * c)) - 1));
             all += __popcll(mask);
@@ -129,18 +129,16 @@ __device__ __forceinline__ uint4 load16(const uint16_t* p) {
     return __builtin_bit_cast(uint4, *(Global)(uintptr_t)p);
 }
 
-// The eight values `by` places on, zeros behind the first `left` of them.
+// The eight values `by` places on, zeros behind the first `left` of them.  (In 32-bit words: a 64-bit shift whose amount was in the last vector register that its
+// kernel had gave other results here.)
 __device__ __forceinline__ uint4 from_place(uint4 q, int by, int left) {
-    uint64_t lo = q.x | (uint64_t)q.y << 32, hi = q.z | (uint64_t)q.w << 32;
-    const int bits = 16 * (by & 3);
-    lo = by & 4 ? hi : lo;
-    hi = by & 4 ? 0 : hi;
-    lo = lo >> bits | (hi << 1) << (63 - bits);
-    hi >>= bits;
-    const int a = left < 0 ? 0 : left < 4 ? left : 4, b = left < 4 ? 0 : left < 8 ? left - 4 : 4;
-    lo &= a == 4 ? ~(uint64_t)0 : ((uint64_t)1 << (16 * a)) - 1;
-    hi &= b == 4 ? ~(uint64_t)0 : ((uint64_t)1 << (16 * b)) - 1;
-    return make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
+    if (!__any(by > 0 || left < 8)) return q;   // (a wave in the middle of a row has nothing to do)
+    const auto choose = [](bool there, uint32_t a, uint32_t b) { return there ? a : b; };
+    uint32_t a = choose(by & 4, q.z, q.x), b = choose(by & 4, q.w, q.y), c = choose(by & 4, 0, q.z), d = choose(by & 4, 0, q.w);
+    a = choose(by & 2, b, a), b = choose(by & 2, c, b), c = choose(by & 2, d, c), d = choose(by & 2, 0, d);
+    a = choose(by & 1, a >> 16 | b << 16, a), b = choose(by & 1, b >> 16 | c << 16, b), c = choose(by & 1, c >> 16 | d << 16, c), d = choose(by & 1, d >> 16, d);
+    const auto cut = [&](uint32_t v, int from) { return left >= from + 2 ? v : left > from ? v & 0xFFFFu : 0u; };
+    return make_uint4(cut(a, 0), cut(b, 2), cut(c, 4), cut(d, 6));
 }
 
 // Columns c .. c + 7 of the row of C >= 8 that starts at element `start` of a matrix of `total`, in two steps, so that nothing waits for a request until it

@@ -81,6 +81,17 @@ def test_ranks_and_counts(salr, ranks, T):
     _backward(salr, s)
 
 
+@pytest.mark.parametrize("ranks", [[16], [13, 5], [32], [31, 20], [64], [61, 4], [128, 9]])
+@pytest.mark.parametrize("T,K,N", [(1, 1031, 96), (7, 517, 331), (100, 264, 1031), (150, 517, 331), (150, 1031, 96), (150, 1024, 331)])
+def test_lengths_and_ranks(salr, T, K, N, ranks):
+    """Every form of the products (how many tokens, the largest rank of the set) with lengths and ranks of whole vectors and of others."""
+    s = _made(T, K, N, ranks, "prompts", 14)
+    s["ids"][0] = 0
+    want, tol = ref.adapters(s["x"], s["ids"], s["a"], s["b"], s["base"])
+    ref.close(_set(salr, s).add(*_dev(s, "x", "ids", "base")), want, tol, torch.bfloat16)
+    _backward(salr, s)
+
+
 def _backward(salr, s, with_base=True):
     x, dy, ids, dx_base = _dev(s, "x", "dy", "ids", "dx_base")
     adapters = _set(salr, s, train=True)
