@@ -6,6 +6,7 @@
 // Tokens of one adapter are brought together into tiles, whose rows are read and written where they are: nothing is copied.
 //   up to kDirectTokens tokens   a workgroup is a token, finds its fellows among the ids by comparisons across the wave, and goes on if
 //                                it is the first of a tile of 16
+//   few of them                  see few_tokens_kernel: all of it in one launch
 //   more                         a launch in front orders the tokens by adapter (stable: sums over tokens have an order) and writes a table of tiles of 64
 // Then  narrow_tile    t = in * factor (K or N columns down to r; fp32 sums over slices of the columns),
 //       wide_tile      out = base + t * factor (r up to N or K columns),
@@ -1019,7 +1020,124 @@ RequestAdaptersPlan request_adapters_plan(int64_t T, int64_t K, int64_t N, int64
     return p;
 }
 
+// Few tokens in one launch: a workgroup is a token and 512 columns of its output, and forms all of the token's t for them.  What memory brings twice that way costs less
+// than a second launch, as long as it is not much.  Threads are vectors of eight ranks, then columns of x: A comes in as it lies; t is fp32 throughout.  The
+// second product's operands are asked for before the first one's sums go round.
+struct FewArgs {
+    Tokens tokens;
+    const uint16_t *x, *base;   // base may be out, or null (zeros)
+    uint16_t* out;
+    int K, N, rpad, pieces;
+};
+constexpr int kFewColumns = 512, kFewRank = 64;
+template <int kRT, bool kWhole>
+__global__ __launch_bounds__(1024) void few_tokens_kernel(FewArgs a) {
+    constexpr int kWaves = 16, kDeep = 8;
+    __shared__ float t_sums[kWaves][16 * kRT];
+    __shared__ f32x4 out_sums[kWaves][kFewColumns / 4];
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int token = blockIdx.x / a.pieces, piece = blockIdx.x % a.pieces * kFewColumns, column = piece + (int)threadIdx.x;
+    const bool writes = threadIdx.x < kFewColumns && column < a.N;
+    const int64_t place = (int64_t)token * a.N + column;
+    uint32_t before = 0;
+    if (writes && a.base != nullptr) before = a.base[place];
+    const int group = group_of(scalar_load(a.tokens.ids + token), a.tokens.n);
+    Adapter adapter{nullptr, nullptr, 0};
+    if (group < a.tokens.n) adapter = adapter_of(a.tokens, group, a.rpad);
+    const int rank = adapter.rank;
+    float y = 0.f;
+    if (rank > 0) {   // the same for the workgroup
+        uint4 b[kRT];
+        const int64_t b_total = (int64_t)rank * a.N, a_total = (int64_t)rank * a.K;
+#pragma unroll
+        for (int i = 0; i < kRT; ++i) {
+            const int r = wave + kWaves * i;
+            b[i] = raw_eight<kWhole>(adapter.b, (int64_t)(r < rank ? r : rank - 1) * a.N, piece + 8 * lane, a.N, b_total);
+        }
+        const int vectors = (rank + 7) / 8, shift = vectors <= 1 ? 0 : 32 - __builtin_clz(vectors - 1);   // a row's, and of how many threads
+        const int v = threadIdx.x & ((1 << shift) - 1), step = 1024 >> shift;
+        const uint16_t* x = a.x + (int64_t)token * a.K;
+        float acc[8] = {};
+        for (int c = threadIdx.x >> shift; c < a.K; c += kDeep * step) {
+            uint4 q[kDeep];
+            uint16_t xs[kDeep];
+#pragma unroll
+            for (int i = 0; i < kDeep; ++i) {   // (behind the last column that one again, left out below)
+                const int at = c + i * step < a.K ? c + i * step : a.K - 1;
+                q[i] = raw_ranks(adapter.a, at, 8 * v, rank, a_total);
+                xs[i] = x[at];
+            }
+#pragma unroll
+            for (int i = 0; i < kDeep; ++i) {
+                if (c + i * step >= a.K) break;
+                const uint4 f = true_ranks(q[i], c + i * step, 8 * v, rank, a_total);
+                const float xv = bf16_bits_to_f32(xs[i]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[j] = fmaf(xv, bf16_bits_to_f32(unit_elem(f, j)), acc[j]);
+            }
+        }
+        // sums over the lanes with the same v: three exchanges halve what a lane has, until it is one rank
+        float four[4], two[2];
+        const bool h5 = lane & 32, h4 = lane & 16, h3 = lane & 8;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) four[j] = (h5 ? acc[j + 4] : acc[j]) + __shfl_xor(h5 ? acc[j] : acc[j + 4], 32);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) two[j] = (h4 ? four[j + 2] : four[j]) + __shfl_xor(h4 ? four[j] : four[j + 2], 16);
+        float one = (h3 ? two[1] : two[0]) + __shfl_xor(h3 ? two[0] : two[1], 8);
+        for (int apart = 1 << shift; apart < 8; apart *= 2) one += __shfl_xor(one, apart);
+        if ((lane & 7) < (1 << shift) && v < vectors) t_sums[wave][8 * v + 4 * h5 + 2 * h4 + h3] = one;
+        __syncthreads();
+        // a wave has every sixteenth rank: sixteen lanes add up the waves' sums of each
+        float t = 0.f;
+        const int mine = wave + kWaves * (lane >> 4);
+        if (mine < rank) t = t_sums[lane & 15][mine];
+#pragma unroll
+        for (int apart = 1; apart < 16; apart *= 2) t += __shfl_xor(t, apart);
+        f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < kRT; ++i) {
+            const int r = wave + kWaves * i;
+            if (r >= rank) break;
+            const float ti = __shfl(t, 16 * i);
+            const uint4 f = true_eight<kWhole>(b[i], (int64_t)r * a.N, piece + 8 * lane, a.N, b_total);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                lo[j] = fmaf(ti, bf16_bits_to_f32(unit_elem(f, j)), lo[j]);
+                hi[j] = fmaf(ti, bf16_bits_to_f32(unit_elem(f, j + 4)), hi[j]);
+            }
+        }
+        out_sums[wave][2 * lane] = lo;
+        out_sums[wave][2 * lane + 1] = hi;
+        __syncthreads();
+        if (threadIdx.x < kFewColumns)
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) y += reinterpret_cast<const float*>(out_sums[w])[threadIdx.x];
+    }
+    if (writes) a.out[place] = group > a.tokens.n ? 0x7FC0 : rank > 0 ? f32_to_bf16_rne(bf16_bits_to_f32(before) + y) : before;
+}
+
+// When that is faster than two launches.  One token, 4096 x 4096 rank 16 6.6 us against 8.2 (kernels alone; a call 4.9 to 6.5 against 8.25), 2048 x 8192 rank 32
+// 7.3 against 8.8, 1024 x 4096 rank 64 7.0 against 9.8; sixteen tokens 512 x 512 rank 16 6.4 against 8.2.  Outside: one token, 4096 x 14336 rank 16 (28
+// workgroups) 8.0 against 8.3, 14336 x 4096 10.8 against 9.6, 4096 x 4096 rank 64 12.3 against 10.2; four tokens 4096 x 4096 rank 16 8.5 against 8.3.
+bool few_tokens(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p) {
+    const int64_t pieces = (a.N + kFewColumns - 1) / kFewColumns;
+    return p.rpad <= kFewRank && a.K * p.rpad <= 65536 && a.T * pieces <= 16;
+}
+void launch_few_tokens(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p) {
+    const int pieces = (int)((a.N + kFewColumns - 1) / kFewColumns);
+    const FewArgs f{tokens_of(a, p), a.x, a.base, a.out, (int)a.K, (int)a.N, p.rpad, pieces};
+    const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)(a.T * pieces)), dim3(1024), 0, a.stream, f); };
+    with_whole(a.N % 8 == 0, [&](auto whole) {
+        constexpr bool kWhole = decltype(whole)::value;
+        p.rpad <= 16 ? run(few_tokens_kernel<1, kWhole>) : p.rpad <= 32 ? run(few_tokens_kernel<2, kWhole>) : run(few_tokens_kernel<4, kWhole>);
+    });
+}
+
 hipError_t launch_request_adapters(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p) {
+    if (few_tokens(a, p)) {   // (leaves the workspace alone)
+        launch_few_tokens(a, p);
+        return hipGetLastError();
+    }
     if (!p.direct) launch_order(a, p);
     launch_narrow(a, p, true, false);
     launch_forward_wide(a, p);
