@@ -172,9 +172,9 @@ __global__ __launch_bounds__(kTeam < 4 ? 256 : 64 * kTeam) void layer_norm_kerne
 template <int kTeam, bool kWeights>
 constexpr int grad_waves() { return kWeights ? 8 : kTeam < 4 ? 4 : kTeam; }
 
-template <bool k32, int kTeam, int kUnits, bool kWhole, bool kWeights>
+template <bool k32, int kTeam, int kUnits, bool kWhole, bool kWeights, int kWaves>
 __device__ __forceinline__ void backward_rows(const LayerNormGradArgs& a, int blocks) {
-    constexpr int kWaves = grad_waves<kTeam, kWeights>(), kTeams = kWaves / kTeam;
+    constexpr int kTeams = kWaves / kTeam;
     constexpr bool kAhead = kWeights && kUnits <= 2;
     __shared__ float slots[2][kWaves * 2];
     __shared__ __align__(16) float totals[kTeams > 1 && kWeights ? 512 * kTeam * kUnits : 4];   // what the teams before have summed
@@ -295,7 +295,7 @@ __device__ __forceinline__ void backward_rows(const LayerNormGradArgs& a, int bl
 
 template <bool k32, int kTeam, int kUnits, bool kWhole, bool kWeights>
 __global__ __launch_bounds__((64 * grad_waves<kTeam, kWeights>())) void layer_norm_backward_kernel(LayerNormGradArgs a) {
-    backward_rows<k32, kTeam, kUnits, kWhole, kWeights>(a, (int)gridDim.x);
+    backward_rows<k32, kTeam, kUnits, kWhole, kWeights, grad_waves<kTeam, kWeights>()>(a, (int)gridDim.x);
 }
 
 // dw and db of 64 columns by one workgroup that goes through all rows, eight lanes a row and four rows a lane at a time: for few rows, beside the workgroups
@@ -353,10 +353,12 @@ __device__ __forceinline__ void column_sums(const LayerNormGradArgs& a, int bloc
     else static_cast<uint16_t*>(out)[at] = f32_to_bf16_rne(v);
 }
 
+template <int kTeam>
+constexpr int few_waves() { return kTeam < 8 ? 8 : kTeam; }
 template <bool k32, int kTeam, int kUnits, bool kWhole>
-__global__ __launch_bounds__((64 * grad_waves<kTeam, false>())) void layer_norm_backward_few_kernel(LayerNormGradArgs a, int row_blocks, void* dw, void* db) {
-    __shared__ float sums[grad_waves<kTeam, false>() * 128];
-    if ((int)blockIdx.x < row_blocks) backward_rows<k32, kTeam, kUnits, kWhole, false>(a, row_blocks);
+__global__ __launch_bounds__(64 * few_waves<kTeam>()) void layer_norm_backward_few_kernel(LayerNormGradArgs a, int row_blocks, void* dw, void* db) {
+    __shared__ float sums[few_waves<kTeam>() * 128];
+    if ((int)blockIdx.x < row_blocks) backward_rows<k32, kTeam, kUnits, kWhole, false, few_waves<kTeam>()>(a, row_blocks);
     else column_sums<k32, kWhole>(a, (int)blockIdx.x - row_blocks, dw, db, sums);
 }
 
@@ -438,7 +440,7 @@ hipError_t launch_layer_norm_backward(const LayerNormGradArgs& a, void* dw, void
     if (a.T > 0 && weights && a.T <= kLayerNormFewRows) {   // (leaves the workspace alone)
         with_team(a.K, [&](auto waves, auto units) {
             with_whole(a.K, [&](auto whole) {
-                constexpr int kTeam = waves, kUnits = units, kThreads = 64 * grad_waves<kTeam, false>(), kTeams = kThreads / 64 / kTeam;
+                constexpr int kTeam = waves, kUnits = units, kThreads = 64 * few_waves<kTeam>(), kTeams = few_waves<kTeam>() / kTeam;
                 constexpr bool kWhole = decltype(whole)::value;
                 const int rows = a.dx != nullptr ? (int)((a.T + kTeams - 1) / kTeams) : 0, columns = (a.K + 63) / 64;
                 const auto launch = [&](int row_blocks, int blocks) {

@@ -162,7 +162,7 @@ def test_in_place(salr):
         assert torch.equal(d[at], dx) and torch.equal(dw2, dw) and torch.equal(db2, db)
 
 
-@pytest.mark.parametrize("T,K", [(255, 264), (256, 1031), (257, 1031), (256, 16384)])
+@pytest.mark.parametrize("T,K", [(255, 264), (256, 1031), (257, 1031), (256, 16384), (511, 515), (512, 4096), (513, 4096), (40, 32768)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_backward_about_few_rows(salr, T, K, dtype):
     """The numbers of rows between which the sums of dw and db move into the launch that forms dx; dx apart, in dy's place and in x's."""
