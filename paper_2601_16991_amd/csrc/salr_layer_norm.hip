@@ -385,13 +385,18 @@ __global__ __launch_bounds__(1024) void layer_norm_parts_kernel(const float* par
 
 // The team for rows of K: as few waves as hold a row with two vectors a lane.
 template <typename Run>
-void with_team(int64_t K, Run run) {
+void with_team_to_8192(int64_t K, Run run) {
     using std::integral_constant;
     if (K <= 512) run(integral_constant<int, 1>(), integral_constant<int, 1>());
     else if (K <= 1024) run(integral_constant<int, 1>(), integral_constant<int, 2>());
     else if (K <= 2048) run(integral_constant<int, 2>(), integral_constant<int, 2>());
     else if (K <= 4096) run(integral_constant<int, 4>(), integral_constant<int, 2>());
-    else if (K <= 8192) run(integral_constant<int, 8>(), integral_constant<int, 2>());
+    else run(integral_constant<int, 8>(), integral_constant<int, 2>());
+}
+template <typename Run>
+void with_team(int64_t K, Run run) {
+    using std::integral_constant;
+    if (K <= 8192) with_team_to_8192(K, run);
     else if (K <= 16384) run(integral_constant<int, 16>(), integral_constant<int, 2>());
     else run(integral_constant<int, 16>(), integral_constant<int, 4>());
 }
@@ -400,7 +405,7 @@ void with_team(int64_t K, Run run) {
 template <typename Run>
 void with_grad_team(int64_t K, Run run) {
     using std::integral_constant;
-    if (K <= 8192) with_team(K, run);
+    if (K <= 8192) with_team_to_8192(K, run);
     else if (K <= 16384) run(integral_constant<int, 8>(), integral_constant<int, 4>());
     else run(integral_constant<int, 8>(), integral_constant<int, 8>());
 }
