@@ -610,7 +610,9 @@ salr_status_t salr_layer_norm(const void* x, const void* residual, const void* w
 
 size_t salr_layer_norm_backward_workspace_bytes(int64_t T, int64_t K, int want_weights) {
     if (T <= 0 || K <= 0 || !layer_norm_sizes(T, K) || !want_weights) return 0;
-    return (size_t)(salr::layer_norm_parts(T, K) * K) * 2 * sizeof(float);
+    // (one launch keeps no sums; a workgroup's place is asked for all the same, so that a call for dw or db always names a workspace)
+    const int64_t parts = T <= salr::kLayerNormFewRows ? 1 : salr::layer_norm_parts(T, K);
+    return (size_t)(parts * K) * 2 * sizeof(float);
 }
 
 salr_status_t salr_layer_norm_backward(const void* dy, const void* x, const void* weight, const float* mean, const float* rstd, const void* dsum, int64_t T,

@@ -94,3 +94,16 @@ def test_neighbours_stay(salr, K):
     assert all(torch.equal(p, q) for p, q in zip((dx, dw, db), want))
     assert bool((buf[:5] == 3).all()) and bool((buf[5 + T * K:] == 3).all())
     assert bool((sums[:3] == 3).all()) and bool((sums[3 + K:20 + K] == 3).all()) and bool((sums[20 + 2 * K:] == 3).all())
+
+
+@pytest.mark.parametrize("T,K", [(1, 5), (300, 1031), (512, 4096), (130, 32768)])
+def test_one_launch_leaves_its_workspace_alone(salr, T, K):
+    gen = torch.Generator().manual_seed(T + K)
+    dy, x = (torch.randn(T, K, generator=gen).to(dev()) for _ in range(2))
+    w = torch.ones(K, device=dev())
+    _, _, mean, rstd = salr.layer_norm(x, w)
+    want = salr.layer_norm_backward(dy, x, w, mean, rstd, need_dw=True, need_db=True)
+    need = salr.salr_layer_norm_backward_workspace_bytes(T, K, True)
+    ws = torch.full((need + 64,), 255, dtype=torch.uint8, device=dev())
+    got = salr.layer_norm_backward(dy, x, w, mean, rstd, need_dw=True, need_db=True, workspace=ws[:need])
+    assert all(torch.equal(p, q) for p, q in zip(got, want)) and bool((ws == 255).all())
