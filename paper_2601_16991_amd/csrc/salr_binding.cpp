@@ -701,6 +701,12 @@ const at::Tensor& alike(PyObject* o, const at::Tensor& like, const char* name) {
 }
 void* address(const at::Tensor& t) { return t.defined() && t.numel() > 0 ? t.data_ptr() : nullptr; }
 
+// A caller's tensors that a call has written: autograd sees by their versions that what it saved of them is another value now.
+void written(std::initializer_list<const at::Tensor*> tensors) {
+    for (const at::Tensor* t : tensors)
+        if (t->defined() && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+}
+
 const at::Tensor& given_float(PyObject* o, const char* name) {
     const at::Tensor& t = tensor_of(o, name);
     if (!t.defined()) fail(PyExc_TypeError, "%s must be a tensor", name);
@@ -748,6 +754,7 @@ PyObject* py_dropout(PyObject*, PyObject* const* v, Py_ssize_t n) {
         st = salr_dropout(address(x), address(residual), x.numel(), type, p, seed, seed_device, offset, address(y), stream);
     }
     check(st, "salr_dropout");
+    if (v[5] != Py_None) written({&y});
     return result(v[5], std::move(y));
     SALR_CATCH
 }
@@ -787,7 +794,8 @@ PyObject* py_layer_norm(PyObject*, PyObject* const* v, Py_ssize_t n) {
     const OnDevice on(x.device());
     at::Tensor y, sum, mean, rstd;
     float *mp, *rp;
-    if (PyObject_IsTrue(v[10]) == 1) {
+    const bool made = PyObject_IsTrue(v[10]) == 1;
+    if (made) {
         y = empty_on({T, K}, x.scalar_type(), x);
         if (residual.defined()) sum = empty_on({T, K}, x.scalar_type(), x);
         mean = empty_on({T}, at::kFloat, x);
@@ -808,6 +816,7 @@ PyObject* py_layer_norm(PyObject*, PyObject* const* v, Py_ssize_t n) {
         st = salr_layer_norm(address(x), address(residual), address(weight), address(bias), T, K, type, wtype, eps, address(y), address(sum), mp, rp, stream);
     }
     check(st, "salr_layer_norm");
+    if (!made) written({&y, &sum, &tensor_of(v[7], "mean"), &tensor_of(v[8], "rstd")});
     return tuple_of({&y, &sum, &mean, &rstd});
     SALR_CATCH
 }
@@ -841,6 +850,8 @@ PyObject* py_layer_norm_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
                                       address(db), ws.ptr, ws.bytes, stream);
     }
     check(st, "salr_layer_norm_backward");
+    for (const auto& [given, out] : {std::pair<PyObject*, const at::Tensor*>{v[6], &dx}, {v[7], &dw}, {v[8], &db}})
+        if (given != Py_True) written({out});
     return tuple_of({&dx, &dw, &db});
     SALR_CATCH
 }
@@ -953,6 +964,7 @@ PyObject* py_adapters_add(PyObject*, PyObject* const* v, Py_ssize_t n) {
                                static_cast<uint16_t*>(address(base)), static_cast<uint16_t*>(address(y)), ws.ptr, ws.bytes, stream);
     }
     check(st, "salr_adapters_add");
+    if (v[9] != Py_None) written({&y});
     return result(v[9], std::move(y));
     SALR_CATCH
 }
@@ -985,6 +997,7 @@ PyObject* py_adapters_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
     }
     check(st, "salr_adapters_backward");
     if (gradients) c.held.changed();
+    if (v[10] != Py_True) written({&dx});
     if (!dx.defined()) Py_RETURN_NONE;
     return THPVariable_Wrap(std::move(dx));
     SALR_CATCH
