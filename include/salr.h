@@ -616,8 +616,8 @@ salr_status_t salr_adapter_list_check(const salr_adapter_t* adapters, int64_t n,
  * salr_adapters_add -- y[t] = base[t] + (x[t] A_i) B_i with i = ids[t]; a token with a negative id has no adapter: y[t] = base[t].
  * An id that is not below n gives NaN in its token's row.
  *
- *   list, n, max_rank  the records, on the device (8-byte aligned), their number (at least 1) and largest rank (ranks of a record above it are not
- *                      looked at)
+ *   list, n, max_rank  the records, on the device (8-byte aligned), their number (at least 1) and largest rank (of a record with more, only so many
+ *                      columns of a and rows of b are looked at, and as many of da and db written)
  *   x          in   [T, K] bf16;  T < 2^28, T (max_rank + 15) < 2^34, K and N from 8 to 2^22, (K + N) (n + T / 1024)
  *                      <= 2^29 (else SHAPE)
  *   ids        in   [T] int32

@@ -925,7 +925,7 @@ struct RequestAdaptersPlan {
     int64_t rows, tiles;     // tokens of a tile, tiles of the launches
     int64_t live;            // of which so many are expected to hold tokens
     int64_t t_rows;          // rows of the products with the first factor
-    int rpad;                // their columns
+    int max_rank, rpad;      // ranks that a call looks at; columns of t
     int slices_x, slices_dy; // slices of K and N that they are summed over
     int chunk;               // backward: tokens of a chunk of the gradients' sums
     size_t order, starts, counts, table, chunks, sums, part_x, part_dy, t_x, t_dy;   // offsets in the workspace

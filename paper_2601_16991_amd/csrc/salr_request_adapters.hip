@@ -71,12 +71,12 @@ __device__ __forceinline__ T scalar_load(const T* p) {
 }
 struct Adapter {
     const uint16_t *a, *b;
-    int rank;   // (never more than the launch has room for, whatever the record says)
+    int rank, pitch;   // never more ranks than the call names, whatever the record says; elements of a row of A: the record's
 };
-__device__ __forceinline__ Adapter adapter_of(const Tokens& k, int group, int rpad) {
+__device__ __forceinline__ Adapter adapter_of(const Tokens& k, int group, int max_rank) {
     const salr_adapter_t* record = k.list + group;
     const int64_t rank = scalar_load(&record->rank);
-    return Adapter{scalar_load(&record->a), scalar_load(&record->b), rank < rpad ? (int)rank : rpad};
+    return Adapter{scalar_load(&record->a), scalar_load(&record->b), rank < max_rank ? (int)rank : max_rank, (int)rank};
 }
 
 // Tile `self`; of a direct launch also its tokens in rows[kRows] (LDS, a barrier behind it).
@@ -164,14 +164,14 @@ __device__ __forceinline__ uint4 true_eight(uint4 q, int64_t start, int c, int C
     }
 }
 
-// Ranks r .. r + 7 of a row of a factor A [C, rank], likewise; behind the last rank whatever comes, but nothing from behind the matrix.
-__device__ __forceinline__ uint4 raw_ranks(const uint16_t* m, int64_t row, int r, int rank, int64_t total) {
-    const int64_t at = row * rank + r;
+// Ranks r .. r + 7 of a row of a factor A [C, pitch], likewise; behind the last rank whatever comes, but nothing from behind the matrix.
+__device__ __forceinline__ uint4 raw_ranks(const uint16_t* m, int64_t row, int r, int pitch, int64_t total) {
+    const int64_t at = row * pitch + r;
     return load16(m + (at < total - 8 ? at : total - 8));
 }
-__device__ __forceinline__ uint4 true_ranks(uint4 q, int64_t row, int r, int rank, int64_t total) {
-    if ((rank & 7) == 0) return q;   // (whole vectors are pulled back only where r >= rank)
-    const int64_t past = row * rank + r - (total - 8);
+__device__ __forceinline__ uint4 true_ranks(uint4 q, int64_t row, int r, int pitch, int64_t total) {
+    if ((pitch & 7) == 0) return q;   // (whole vectors are pulled back only where r >= pitch)
+    const int64_t past = row * pitch + r - (total - 8);
     return from_place(q, past > 0 ? past < 8 ? (int)past : 7 : 0, 8);
 }
 
@@ -269,7 +269,7 @@ struct NarrowArgs {
     float* part[2];           // [slices][t_rows][rpad]
     int slices[2];
     int64_t t_rows;
-    int rpad;
+    int rpad, max_rank;
 };
 
 // part[z][row][r] = sum over the columns c of slice z of in[row][c] * factor(c, r).  A workgroup has a slice of a tile: every `slices`-th step of 128
@@ -302,10 +302,10 @@ __device__ __forceinline__ void narrow_tile(const NarrowArgs& a, const Tile& til
     const int C = (int)(second ? a.C[1] : a.C[0]);
     const int64_t in_total = (int64_t)a.tokens.T * C;
     float* part = (second ? a.part[1] : a.part[0]) + (int64_t)z * a.t_rows * a.rpad;
-    const Adapter adapter = adapter_of(a.tokens, tile.group, a.rpad);
-    const int rank = adapter.rank;
+    const Adapter adapter = adapter_of(a.tokens, tile.group, a.max_rank);
+    const int rank = adapter.rank, pitch = adapter.pitch;
     const uint16_t* factor = second ? adapter.b : adapter.a;
-    const int64_t factor_total = (int64_t)rank * C;
+    const int64_t factor_total = (int64_t)(second ? rank : pitch) * C;
     const int steps = (C + Lds::kCols - 1) / Lds::kCols;
     const int vrow = threadIdx.x >> 4, vcol = 8 * (threadIdx.x & 15);
     int64_t row[kMB];   // (behind the last token the first one's: what comes of it is not stored)
@@ -328,7 +328,7 @@ __device__ __forceinline__ void narrow_tile(const NarrowArgs& a, const Tile& til
                     q.f[i] = raw_eight<kWhole>(factor, (int64_t)(r < rank ? r : rank - 1) * C, c + vcol, C, factor_total);
                 } else {                  // vector v of [128][16 kRT]
                     const int v = threadIdx.x + 256 * i, k = c + v / (2 * kRT);
-                    q.f[i] = raw_ranks(factor, k < C ? k : C - 1, rb + 8 * (v % (2 * kRT)), rank, factor_total);
+                    q.f[i] = raw_ranks(factor, k < C ? k : C - 1, rb + 8 * (v % (2 * kRT)), pitch, factor_total);
                 }
             }
         };
@@ -345,7 +345,7 @@ __device__ __forceinline__ void narrow_tile(const NarrowArgs& a, const Tile& til
                         true_eight<kWhole>(q.f[i], (int64_t)(r < rank ? r : rank - 1) * C, c + vcol, C, factor_total);
                 } else {
                     const int v = threadIdx.x + 256 * i, k = c + v / (2 * kRT);
-                    const uint4 f = true_ranks(q.f[i], k < C ? k : C - 1, rb + 8 * (v % (2 * kRT)), rank, factor_total);
+                    const uint4 f = true_ranks(q.f[i], k < C ? k : C - 1, rb + 8 * (v % (2 * kRT)), pitch, factor_total);
                     *reinterpret_cast<uint4*>(lds.factor + v / (2 * kRT) * kRankPitch + 8 * (v % (2 * kRT))) = k < C ? f : make_uint4(0, 0, 0, 0);
                 }
             }
@@ -442,7 +442,7 @@ struct WideArgs {
     const uint4* t;         // [t_rows][rpad / 4], as two_halves has them
     int slices;
     int64_t t_rows;
-    int rpad;
+    int rpad, max_rank;
     int64_t C;              // columns of out
     int per_group;          // of a workgroup, whole steps of its waves
     const uint16_t* base;   // may be out, or null (zeros)
@@ -495,10 +495,10 @@ __device__ __forceinline__ void wide_tile(const WideArgs& a, int block, WideLds<
         }
         return;
     }
-    const Adapter adapter = adapter_of(a.tokens, tile.group, a.rpad);
-    const int rank = adapter.rank, rank16 = (rank + 15) & ~15;
+    const Adapter adapter = adapter_of(a.tokens, tile.group, a.max_rank);
+    const int rank = adapter.rank, rank16 = (rank + 15) & ~15, pitch = adapter.pitch;
     const uint16_t* factor = kFactorA ? adapter.a : adapter.b;
-    const int64_t factor_total = (int64_t)rank * C;
+    const int64_t factor_total = (int64_t)(kFactorA ? pitch : rank) * C;
     uint4 q[kVectors];
     const auto request = [&](int c0, int rb) {   // the factor's part for 64 columns and kPass ranks
 #pragma unroll
@@ -506,7 +506,7 @@ __device__ __forceinline__ void wide_tile(const WideArgs& a, int block, WideLds<
             if (!kFactorA && rb + 8 * v >= rank16) continue;   // the same for the workgroup
             if constexpr (kFactorA) {   // vectors of [64 columns][kPass ranks]
                 const int i = lane + 64 * v, k = c0 + i / kVectors;
-                q[v] = raw_ranks(factor, k < C ? k : C - 1, rb + 8 * (i % kVectors), rank, factor_total);
+                q[v] = raw_ranks(factor, k < C ? k : C - 1, rb + 8 * (i % kVectors), pitch, factor_total);
             } else {                    // vectors of [kPass ranks][64 columns]
                 const int r = rb + 8 * v + (lane >> 3);
                 q[v] = raw_eight<kWhole>(factor, (int64_t)(r < rank ? r : rank - 1) * C, c0 + 8 * (lane & 7), C, factor_total);
@@ -519,7 +519,7 @@ __device__ __forceinline__ void wide_tile(const WideArgs& a, int block, WideLds<
             const int i = lane + 64 * v;
             if constexpr (kFactorA) {
                 const int k = c0 + i / kVectors, r = rb + 8 * (i % kVectors);
-                const uint4 f = true_ranks(q[v], k < C ? k : C - 1, r, rank, factor_total);
+                const uint4 f = true_ranks(q[v], k < C ? k : C - 1, r, pitch, factor_total);
                 *reinterpret_cast<uint4*>(stage + i / kVectors * kPitch + 8 * (i % kVectors)) = rank - r >= 8 ? f : from_place(f, 0, rank - r);
             } else {
                 const int r = rb + 8 * v + (lane >> 3);
@@ -671,7 +671,7 @@ struct OuterArgs {
     const uint16_t* in[2];   // x (dA), dy (dB)
     const uint4* s[2];       // dy B^T (dA), x A (dB): [T][rpad / 4] by position, as two_halves has them
     int64_t C[2];
-    int rpad;
+    int rpad, max_rank;
     int blocks0;             // of kOuterCols columns: of x
     const int4* chunks;      // adapter (-1: none), place of the first token, tokens, and where its sums go: -1 to the gradient, else one of
     float* sums;             // [slots][K rpad + rpad N]
@@ -701,7 +701,8 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, int block, const 
     const salr_adapter_t* record = a.tokens.list + group;
     uint16_t* out = second ? scalar_load(&record->db) : scalar_load(&record->da);
     if (out == nullptr) return;
-    const int rank = adapter_of(a.tokens, group, a.rpad).rank;
+    const Adapter adapter = adapter_of(a.tokens, group, a.max_rank);
+    const int rank = adapter.rank;
     const uint16_t* in = second ? a.in[1] : a.in[0];
     const uint4* s = (second ? a.s[1] : a.s[0]) + (int64_t)start * (a.rpad / 4);
     const int C = (int)(second ? a.C[1] : a.C[0]), c0 = kCols * (block - (second ? a.blocks0 : 0));
@@ -802,7 +803,7 @@ __device__ __forceinline__ void outer_tile(const OuterArgs& a, int block, const 
                         if (i < left) to[i] = acc[ct][rt][i];
                     continue;
                 }
-                uint16_t* to = second ? out + (int64_t)r * C + c : out + (int64_t)c * rank + r;
+                uint16_t* to = second ? out + (int64_t)r * C + c : out + (int64_t)c * adapter.pitch + r;
                 uint16_t e[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) e[i] = f32_to_bf16_rne(acc[ct][rt][i]);
@@ -846,14 +847,15 @@ struct JoinArgs {
     Tokens tokens;
     const float* sums;
     int64_t K, N;
-    int rpad, chunk;
+    int rpad, max_rank, chunk;
 };
 __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
     const int group = blockIdx.y, count = scalar_load(a.tokens.counts + group), start = scalar_load(a.tokens.starts + group);
     if (count <= a.chunk) return;
     const salr_adapter_t* record = a.tokens.list + group;
     uint16_t *da = scalar_load(&record->da), *db = scalar_load(&record->db);
-    const int rank = adapter_of(a.tokens, group, a.rpad).rank, slots = (count + a.chunk - 1) / a.chunk;
+    const Adapter adapter = adapter_of(a.tokens, group, a.max_rank);
+    const int rank = adapter.rank, slots = (count + a.chunk - 1) / a.chunk;
     const int64_t slot = (a.K + a.N) * a.rpad, of_a = a.K * rank, all = of_a + a.N * rank;
     const float* sums = a.sums + 2 * (start / a.chunk) * slot;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
@@ -865,7 +867,7 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
         float s = 0.f;
 #pragma unroll 8
         for (int z = 0; z < slots; ++z) s += from[z * slot];
-        out[at] = f32_to_bf16_rne(s);
+        out[second ? at : at / rank * adapter.pitch + at % rank] = f32_to_bf16_rne(s);
     }
 }
 
@@ -907,7 +909,7 @@ void with_whole(bool whole, Run run) {   // rows of whole vectors
 void launch_narrow(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p, bool x_too, bool dy_too) {
     char* w = static_cast<char*>(a.workspace);
     NarrowArgs n{tokens_of(a, p), {a.x, a.dy}, {a.K, a.N}, {reinterpret_cast<float*>(w + p.part_x), reinterpret_cast<float*>(w + p.part_dy)},
-                 {x_too ? p.slices_x : 0, dy_too ? p.slices_dy : 0}, p.t_rows, p.rpad};
+                 {x_too ? p.slices_x : 0, dy_too ? p.slices_dy : 0}, p.t_rows, p.rpad, p.max_rank};
     const dim3 grid((unsigned)(p.tiles * (n.slices[0] + n.slices[1])));
     const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, a.stream, n); };
     with_whole((!x_too || a.K % 8 == 0) && (!dy_too || a.N % 8 == 0), [&](auto whole) {
@@ -928,7 +930,7 @@ int per_group_of(const RequestAdaptersPlan& p, int64_t C) {
 void launch_forward_wide(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p) {
     const int per_group = per_group_of(p, a.N);
     const float* part = reinterpret_cast<const float*>(static_cast<char*>(a.workspace) + p.part_x);
-    const WideArgs w{tokens_of(a, p), part, nullptr, p.slices_x, p.t_rows, p.rpad, a.N, per_group, a.base, a.out};
+    const WideArgs w{tokens_of(a, p), part, nullptr, p.slices_x, p.t_rows, p.rpad, p.max_rank, a.N, per_group, a.base, a.out};
     const dim3 grid((unsigned)(p.tiles * ((a.N + per_group - 1) / per_group)));
     const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, a.stream, w); };
     with_whole(a.N % 8 == 0, [&](auto whole) {
@@ -943,8 +945,8 @@ void launch_backward(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p,
     float* sums = reinterpret_cast<float*>(workspace + p.sums);
     BackwardArgs b{};
     const int blocks0 = (int)((a.K + kOuterCols - 1) / kOuterCols), blocks1 = (int)((a.N + kOuterCols - 1) / kOuterCols), per_group = per_group_of(p, a.K);
-    b.outer = OuterArgs{tokens_of(a, p), {a.x, a.dy}, {t_dy, t_x}, {a.K, a.N}, p.rpad, blocks0, reinterpret_cast<const int4*>(workspace + p.chunks), sums};
-    b.wide = WideArgs{tokens_of(a, p), nullptr, t_dy, 0, p.t_rows, p.rpad, a.K, per_group, a.base, a.out};
+    b.outer = OuterArgs{tokens_of(a, p), {a.x, a.dy}, {t_dy, t_x}, {a.K, a.N}, p.rpad, p.max_rank, blocks0, reinterpret_cast<const int4*>(workspace + p.chunks), sums};
+    b.wide = WideArgs{tokens_of(a, p), nullptr, t_dy, 0, p.t_rows, p.rpad, p.max_rank, a.K, per_group, a.base, a.out};
     b.across = blocks0 + blocks1;
     b.outer_blocks = a.want_dadb ? (int)(b.across * (a.T / p.chunk + a.n)) : 0;
     const int64_t wide_blocks = a.T > 0 && a.out != nullptr ? p.tiles * ((a.K + per_group - 1) / per_group) : 0;
@@ -957,7 +959,7 @@ void launch_backward(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p,
         else p.rpad <= 64 ? run(backward_kernel<4, 64, kWhole>) : run(backward_kernel<4, 256, kWhole>);
     });
     if (a.want_dadb && a.T > p.chunk)
-        hipLaunchKernelGGL(join_kernel, dim3((unsigned)(a.n < 16 ? 2048 / a.n : 128), (unsigned)a.n), dim3(256), 0, a.stream, JoinArgs{tokens_of(a, p), sums, a.K, a.N, p.rpad, p.chunk});
+        hipLaunchKernelGGL(join_kernel, dim3((unsigned)(a.n < 16 ? 2048 / a.n : 128), (unsigned)a.n), dim3(256), 0, a.stream, JoinArgs{tokens_of(a, p), sums, a.K, a.N, p.rpad, p.max_rank, p.chunk});
 }
 
 // Tokens of a chunk of the gradients' sums.  Adapters enough for two workgroups a CU: 4096, since a chunk less costs a launch, and the sums a trip through memory
@@ -980,6 +982,7 @@ RequestAdaptersPlan request_adapters_plan(int64_t T, int64_t K, int64_t N, int64
     const int64_t groups = n + 2 < T ? n + 2 : T;   // that hold a token
     p.tiles = p.direct ? T : T / kTileTokens + n + 2;
     p.t_rows = T;
+    p.max_rank = (int)max_rank;
     p.rpad = (int)((max_rank + 15) / 16 * 16);
     if (p.rpad == 0) p.rpad = 16;
     p.live = p.direct ? (n < T ? n : T) : (T + kTileTokens - 1) / kTileTokens + groups / 2;   // tiles to expect
@@ -1027,7 +1030,7 @@ struct FewArgs {
     Tokens tokens;
     const uint16_t *x, *base;   // base may be out, or null (zeros)
     uint16_t* out;
-    int K, N, rpad, pieces;
+    int K, N, max_rank, pieces;
 };
 constexpr int kFewColumns = 512, kFewRank = 64;
 template <int kRT, bool kWhole>
@@ -1042,13 +1045,13 @@ __global__ __launch_bounds__(1024) void few_tokens_kernel(FewArgs a) {
     uint32_t before = 0;
     if (writes && a.base != nullptr) before = a.base[place];
     const int group = group_of(scalar_load(a.tokens.ids + token), a.tokens.n);
-    Adapter adapter{nullptr, nullptr, 0};
-    if (group < a.tokens.n) adapter = adapter_of(a.tokens, group, a.rpad);
+    Adapter adapter{nullptr, nullptr, 0, 0};
+    if (group < a.tokens.n) adapter = adapter_of(a.tokens, group, a.max_rank);
     const int rank = adapter.rank;
     float y = 0.f;
     if (rank > 0) {   // the same for the workgroup
         uint4 b[kRT];
-        const int64_t b_total = (int64_t)rank * a.N, a_total = (int64_t)rank * a.K;
+        const int64_t b_total = (int64_t)rank * a.N, a_total = (int64_t)adapter.pitch * a.K;
 #pragma unroll
         for (int i = 0; i < kRT; ++i) {
             const int r = wave + kWaves * i;
@@ -1064,13 +1067,13 @@ __global__ __launch_bounds__(1024) void few_tokens_kernel(FewArgs a) {
 #pragma unroll
             for (int i = 0; i < kDeep; ++i) {   // (behind the last column that one again, left out below)
                 const int at = c + i * step < a.K ? c + i * step : a.K - 1;
-                q[i] = raw_ranks(adapter.a, at, 8 * v, rank, a_total);
+                q[i] = raw_ranks(adapter.a, at, 8 * v, adapter.pitch, a_total);
                 xs[i] = x[at];
             }
 #pragma unroll
             for (int i = 0; i < kDeep; ++i) {
                 if (c + i * step >= a.K) break;
-                const uint4 f = true_ranks(q[i], c + i * step, 8 * v, rank, a_total);
+                const uint4 f = true_ranks(q[i], c + i * step, 8 * v, adapter.pitch, a_total);
                 const float xv = bf16_bits_to_f32(xs[i]);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) acc[j] = fmaf(xv, bf16_bits_to_f32(unit_elem(f, j)), acc[j]);
@@ -1125,7 +1128,7 @@ bool few_tokens(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p) {
 }
 void launch_few_tokens(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p) {
     const int pieces = (int)((a.N + kFewColumns - 1) / kFewColumns);
-    const FewArgs f{tokens_of(a, p), a.x, a.base, a.out, (int)a.K, (int)a.N, p.rpad, pieces};
+    const FewArgs f{tokens_of(a, p), a.x, a.base, a.out, (int)a.K, (int)a.N, p.max_rank, pieces};
     const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)(a.T * pieces)), dim3(1024), 0, a.stream, f); };
     with_whole(a.N % 8 == 0, [&](auto whole) {
         constexpr bool kWhole = decltype(whole)::value;
