@@ -606,7 +606,8 @@ typedef struct {
 
 /*
  * salr_adapter_list_check -- whether the n records of a HOST array can be used; *max_rank gets the largest rank, which the calls want to know.  No
- * gradient may overlap another tensor of the list or of a call (not checked here).
+ * gradient may overlap another tensor of the list or of a call, and no output or workspace of a call a tensor of the list (not checked, here or there: the
+ * records lie on the device by then).
  * Errors: INVALID_ARG (null where data is required, n or a rank negative, a pointer that is not 16-byte aligned), SHAPE (n > 4096),
  * UNSUPPORTED (a rank above 256).
  */
@@ -623,7 +624,8 @@ salr_status_t salr_adapter_list_check(const salr_adapter_t* adapters, int64_t n,
  *   ids        in   [T] int32
  *   base       in   [T, N] bf16, the shared layer's output; NULL = zeros
  *   y          out  [T, N] bf16; may be base, overlaps x and base in no other way
- *   workspace  --   salr_adapters_add_workspace_bytes(T, K, N, n, max_rank) bytes, 256-byte aligned; contents unspecified
+ *   workspace  --   salr_adapters_add_workspace_bytes(T, K, N, n, max_rank) bytes, 256-byte aligned; contents unspecified.  (More tokens can need
+ *                   less: a workspace for several T has the largest of their sizes)
  *
  * salr_adapters_backward -- the adjoint:
  *
@@ -638,7 +640,8 @@ salr_status_t salr_adapter_list_check(const salr_adapter_t* adapters, int64_t n,
  *                   more than 256 to 4096 tokens (from how many on follows from the sizes) it holds sums of chunks of them:
  *                   8 (K + N) max_rank bytes for each chunk of as many
  *
- * bf16 in and out, fp32 sums; x A and dy B^T go into the second product as two bf16 values each (16 bits of mantissa).  Results are the same bit for bit
+ * bf16 in and out, fp32 sums; x A and dy B^T go into the second product as two bf16 values each (16 bits of mantissa; x A of one or a few tokens, up to 2^16 values
+ * of an A, as it is in fp32).  Results are the same bit for bit
  * from call to call.  A token's infinity or NaN, or an adapter's, makes infinities or NaN of its own results only (and NaN of some that would be
  * infinite: an infinite factor meets the second value, which may be zero).
  * Errors of both: INVALID_ARG (null where data is required, negative size, n < 1, max_rank outside [0, 256], a misaligned pointer (x, base, y, dy, dx_base,

@@ -856,11 +856,15 @@ class AdapterSet:
 
         y[t] = base[t] + (x[t] A_i) B_i,  i = ids[t]
 
+    Every call looks at all tensors of the set on the host, and beyond 128 tokens at all ids once for each adapter on the GPU.  Up to 64 adapters that takes no time
+    that was seen (one token, 1024 x 1024, rank 16: 4.3 us, 6.0 with 512 adapters, 34 with 4096), so a set is for adapters that are in use; another adapter is
+    another set.
+
     The set is laid out and copied to the GPU when the object is made.  The tensors keep their memory: a call raises ValueError where one has other
     memory than it had then; values may change (an optimiser's copies).  An id that is not below the number of adapters gives NaN in its token's row.
 
     da, db   bf16 tensors of the shapes of a and b (or None for a pair that is frozen) that ``backward`` writes, as ``AdamW`` reads gradients where
-             they are.  None of them may share memory with another tensor of the set.
+             they are.  None of them may share memory with another tensor of the set, which is checked, or of a call, which is not.
     """
 
     def __init__(self, a: Sequence[torch.Tensor], b: Sequence[torch.Tensor], da: Optional[Sequence[Optional[torch.Tensor]]] = None,
@@ -873,11 +877,11 @@ class AdapterSet:
         self._add, self._backward = _native().adapters_add, _native().adapters_backward
 
     def workspace_bytes(self, T: int) -> int:
-        """Of a workspace for ``add`` on T tokens."""
+        """Of a workspace for ``add`` on T tokens (more tokens can need less: take the largest of those that will come)."""
         return salr_adapters_add_workspace_bytes(T, self.K, self.N, self.n, self.max_rank)
 
     def backward_workspace_bytes(self, T: int) -> int:
-        """Of a workspace for ``backward`` on T tokens."""
+        """Of a workspace for ``backward`` on T tokens (likewise)."""
         return salr_adapters_backward_workspace_bytes(T, self.K, self.N, self.n, self.max_rank, True)
 
     def add(self, x: torch.Tensor, ids: torch.Tensor, base: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,

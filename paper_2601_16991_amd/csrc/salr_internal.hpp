@@ -883,7 +883,8 @@ constexpr int64_t kLayerNormMostK = 32768;         // a row is held in the regis
 constexpr int64_t kLayerNormMostT = (1 << 22) - 1; // workgroups of up to 1024 threads, fewer than 2^32 of them in a launch
 // Rows up to which dw and db are summed beside dx instead of behind it: 1 x 512 3.4 us of kernels against 5.9, 64 x 4096 4.1 against 7.6, 256 x 512 4.5
 // against 7.3, 512 x 4096 7.9 against 13.0, 512 x 768 fp32 5.8 against 9.9; 1024 x 4096 12.4 against 16.0, but 1024 x 768 fp32 10.6 against 9.6 and 2048 x 4096
-// 20.9 against 18.9.  (Workgroups of 4 or 16 waves: 512 x 4096 8.1 and 7.3, 256 x 4096 5.3 and 5.8.)
+// 20.9 against 18.9.  So wide rows go on gaining up to some 1500 of them and narrow ones do not (a workgroup has 64 columns, and more of them share the rows): a
+// limit in rows alone is where no size that was measured loses.  (Workgroups of 4 or 16 waves: 512 x 4096 8.1 and 7.3, 256 x 4096 5.3 and 5.8.)
 constexpr int64_t kLayerNormFewRows = 512;
 constexpr int64_t kLayerNormParts = 256;           // workgroups that sum dw and db: one a CU
 struct LayerNormArgs {

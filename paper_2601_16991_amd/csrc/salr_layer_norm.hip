@@ -11,10 +11,14 @@
 // dw and db: a workgroup of eight waves goes through rows, its lanes keep the sums of their columns; the teams of a workgroup are added in LDS,
 // in order, and the workgroups' sums, at most kLayerNormParts of them, by a second launch: no atomics, the same bits every time.  Up to kLayerNormFewRows rows
 // workgroups of their own read x and dy again beside those that form dx: one launch.
+// Wide rows: above 16384 columns no form of the gradient has registers for what a lane holds, and above 8192 the one with dw and db has not.
+// What does not fit goes to scratch memory and back (the compiler's report, in registers a lane: with dw and db 10 to 84 up to 16384 columns, 366 and 430 for rows of
+// odd lengths, 682 to 1870 above; dx alone above 16384 107 to 198, 476 and 676 for odd ones).
 //
 // Measured: 4096 x 4096 bf16, with a residual 24.4 us (134 MB, 5.5 TB/s); its gradient with dsum, dw and db 28.8 us (4.7 TB/s, 4 us of them the second launch;
 // with sixteen waves a workgroup, a row requested when it is needed and the weights read for each, 58 us); one row of 4096 3.1 us of kernel; 1111 x 2721 fp32
-// with dw and db 17.6 us, where the launches' start and end are 10.
+// with dw and db 17.6 us, where the launches' start and end are 10.  Wide rows, bf16, with dw and db and dx alone: 1024 x 14336 37.5 and 23.8 us, 4096 x 14336 93
+// and 77 (254 and 114 at 14335), 4096 x 28672 1250 and 459 (1365 and 806 at 28671; its bytes take 135).
 #include <type_traits>
 
 #include "salr_eight.hpp"
@@ -401,7 +405,8 @@ void with_team(int64_t K, Run run) {
     else run(integral_constant<int, 16>(), integral_constant<int, 4>());
 }
 
-// The team that sums dw and db too: eight waves at most, whose lanes have 256 registers each for their columns' sums.
+// The team that sums dw and db too: eight waves at most, whose lanes have 256 registers each.  Enough for dw, db, the weights and a row up to two vectors a lane, not
+// for four or eight (see above): those are for being there at all.
 template <typename Run>
 void with_grad_team(int64_t K, Run run) {
     using std::integral_constant;

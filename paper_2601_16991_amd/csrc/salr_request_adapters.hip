@@ -13,10 +13,10 @@
 //       outer_tile     the adapters' gradients, sums over tokens; beside wide_tile for dx in one launch.
 // t goes into the second product as two bf16 values, t rounded and what is left of it: 16 bits of mantissa, so that results are as good as their own
 // rounding (with t rounded once, as the layer does, errors were 1.4 times that).  In wide_tile the second value is free: an instruction
-// that takes eight values a lane has room for four ranks of both.
-// All on the matrix cores, though memory bounds each (2 r products a byte of x and out at most): tiles of 16 fill them however few rows are live, and
+// that takes eight values a lane has room for four ranks of both.  (few_tokens_kernel keeps t in fp32, on the vector units.)
+// All others on the matrix cores, though memory bounds each (2 r products a byte of x and out at most): tiles of 16 fill them however few rows are live, and
 // what an adapter's factors lack in alignment or length is zeros in LDS.  Results do not depend on which other tokens a call holds, save that
-// the number of slices follows from its sizes.
+// which of these forms it takes, and the number of slices, follow from its sizes.
 #include <type_traits>
 
 #include "salr_adapter_t.hpp"
@@ -130,8 +130,8 @@ __device__ __forceinline__ uint4 load16(const uint16_t* p) {
     return __builtin_bit_cast(uint4, *(Global)(uintptr_t)p);
 }
 
-// The eight values `by` places on, zeros behind the first `left` of them.  (In 32-bit words: a 64-bit shift whose amount was in the last vector register that its
-// kernel had gave other results here.)
+// The eight values `by` places on, zeros behind the first `left` of them.  (In 32-bit words: with 64-bit shifts one wave of a kernel that was
+// being written here had NaN for its values.  Why was not shown; what was seen is that the shift's amount lay in the last vector register of that kernel.)
 __device__ __forceinline__ uint4 from_place(uint4 q, int by, int left) {
     if (!__any(by > 0 || left < 8)) return q;   // (a wave in the middle of a row has nothing to do)
     const auto choose = [](bool there, uint32_t a, uint32_t b) { return there ? a : b; };
@@ -457,7 +457,8 @@ struct WideArgs {
 // kFactorA: the factor is A [C, r] (dx), else B [r, C] (y).
 // kRows: of a tile; of 64, two waves have one half each.
 // The start is four trips to memory one behind the other (the tile, its tokens and the adapter's record, t, base and factor), and with the stores that is what
-// bounds all but the largest calls: 64 tokens of 40 adapters, 4096 -> 14336, 10.5 us (26 MB); 2001 tokens, 2720 -> 2731, 13 us, 11 with N = 2736.
+// bounds all but the largest calls: 64 tokens of 40 adapters, 4096 -> 14336, 10.5 us (26 MB); 2001 tokens, 2720 -> 2731, 13 us, 11 with N = 2736.  Three of
+// them follow from each other; base and factor are only asked for behind the sum of t, on which they do not depend.
 template <int kRows, int kMostR, bool kFactorA>
 struct WideLds {
     static constexpr int kTPitch = 2 * kMostR + 8, kPass = 32, kPitch = kFactorA ? kPass + 8 : 64 + 8, kOutPitch = 64 + 8;
@@ -919,7 +920,8 @@ void launch_narrow(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p, b
     });
 }
 
-// Columns of a workgroup of wide_tile: 256, and twice as many as long as the chip has work for every place it has (six workgroups a CU, four of 64 tokens).
+// Columns of a workgroup of wide_tile: 256, and twice as many as long as the chip has work for every place it has (six workgroups a CU, four of 64 tokens; ranks
+// above 64, whose t takes 66 KB of LDS however many they are, leave place for one, which the rule does not know).
 // 777 tokens, 2720 columns: 23 us in 1088 workgroups, 29 in 544 (and 26 in steps of 128 columns).
 int per_group_of(const RequestAdaptersPlan& p, int64_t C) {
     int64_t per_group = 256;
@@ -1119,9 +1121,11 @@ __global__ __launch_bounds__(1024) void few_tokens_kernel(FewArgs a) {
     if (writes) a.out[place] = group > a.tokens.n ? 0x7FC0 : rank > 0 ? f32_to_bf16_rne(bf16_bits_to_f32(before) + y) : before;
 }
 
-// When that is faster than two launches.  One token, 4096 x 4096 rank 16 6.6 us against 8.2 (kernels alone; a call 4.9 to 6.5 against 8.25), 2048 x 8192 rank 32
+// Where that is faster than two launches.  One token, 4096 x 4096 rank 16 6.6 us against 8.2 (kernels alone; a call 4.9 to 6.5 against 8.25), 2048 x 8192 rank 32
 // 7.3 against 8.8, 1024 x 4096 rank 64 7.0 against 9.8; sixteen tokens 512 x 512 rank 16 6.4 against 8.2.  Outside: one token, 4096 x 14336 rank 16 (28
 // workgroups) 8.0 against 8.3, 14336 x 4096 10.8 against 9.6, 4096 x 4096 rank 64 12.3 against 10.2; four tokens 4096 x 4096 rank 16 8.5 against 8.3.
+// The limit of A is on the safe side: in calls of one token one launch took 5.8 us against 8.3 at 80 K values of it (5120 x 4096 rank 16), 6.4 to 7.0 against 8.6 to 9.5 at 128 K
+// (8192 x 4096 rank 16, 4096 x 4096 rank 32, 2048 x 4096 rank 64), 7.9 against 9.2 at 192 K (12288 x 4096 rank 16) and 9.0 against 9.4 at 224 K.
 bool few_tokens(const RequestAdaptersArgs& a, const RequestAdaptersPlan& p) {
     const int64_t pieces = (a.N + kFewColumns - 1) / kFewColumns;
     return p.rpad <= kFewRank && a.K * p.rpad <= 65536 && a.T * pieces <= 16;
