@@ -565,7 +565,8 @@ salr_status_t salr_dropout(const void* x, const void* residual, int64_t count, s
  *   sum       out  [T, K] of `type`: s, what the next residual and the backward pass take; may be x or residual, not y.  NULL iff residual is
  *   mean      out  [T] fp32, or NULL
  *   rstd      out  [T] fp32, or NULL
- * Sums are fp32, squares are of differences to the mean.  A row with an infinity or NaN gives NaN, other rows are not touched by it.
+ * Sums are fp32, squares are of differences to the mean (whose sum is infinite from deviations of some 1e19 on: rstd is 0 then).  A row with an infinity or NaN gives
+ * NaN, other rows are not touched by it.
  * Errors: INVALID_ARG (null where data is required, negative size, a type that is none, eps negative or not finite, a pointer that is not
  * aligned to its type, sum without residual or the other way round, an output that overlaps an input in part or another output), SHAPE, HIP.
  *
